@@ -38,6 +38,12 @@ class Sweep(C.Structure):
                 ("step", C.c_int64 * MAX_RANK)]
 
 
+class Checkpoint8(C.Structure):
+    """``hpacml8_checkpoint``"""
+    _fields_ = [("codes", C.c_void_p), ("exps", C.c_void_p), ("rows", C.c_int64), ("ld_codes", C.c_int64),
+                ("ld_exps", C.c_int64), ("width", C.c_int32), ("act", C.c_int32)]
+
+
 class Layer(C.Structure):
     _fields_ = [("kind", C.c_int32), ("out_channels", C.c_int32), ("kernel", C.c_int32 * 2),
                 ("stride", C.c_int32 * 2), ("padding", C.c_int32), ("pad_mode", C.c_int32), ("act", C.c_int32)]
@@ -82,6 +88,24 @@ SIGNATURES = {
     "hpacml_region_destroy": (None, [C.c_void_p]),
 }
 
+# every symbol of include/hpacml8.h (dense layers in 8 bits)
+BLOCK8, MAX_WIDTH8 = 32, 16384
+SIGNATURES8 = {
+    "hpacml8_linear_create": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, _P(C.c_void_p)]),
+    "hpacml8_linear_destroy": (None, [C.c_void_p]),
+    "hpacml8_linear_scratch": (C.c_int, [C.c_void_p, C.c_int64, _P(C.c_size_t)]),
+    "hpacml8_linear_run": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
+                                     C.c_int64, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hpacml8_checkpoint_save": (C.c_int, [_P(Checkpoint8), C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int32,
+                                          C.c_int64, C.c_void_p]),
+    "hpacml8_checkpoint_load": (C.c_int, [_P(Checkpoint8), C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]),
+    "hpacml8_backward_scratch": (C.c_int, [_P(Checkpoint8), C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32,
+                                           C.c_int32, _P(C.c_size_t)]),
+    "hpacml8_backward": (C.c_int, [_P(Checkpoint8), C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
+                                   C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                                   C.c_size_t, C.c_void_p]),
+}
+
 _lib = None
 
 
@@ -93,7 +117,7 @@ def lib():
             raise RuntimeError("libhpacml.so is not built: run `python -m paper_2407_18352_amd.build` "
                                "(or __graft_entry__.build())")
         L = C.CDLL(LIB_PATH)
-        for name, (res, args) in SIGNATURES.items():
+        for name, (res, args) in list(SIGNATURES.items()) + list(SIGNATURES8.items()):
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args

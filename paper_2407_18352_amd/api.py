@@ -338,3 +338,160 @@ class Region:
             self.close()
         except Exception:
             pass
+
+
+# ---- dense layers in 8 bits (include/hpacml8.h) -----------------------------
+
+def _matrix(t, what, rows=None, width=None, dtypes=None):
+    """(pointer, ABI type, row pitch) of a device matrix with contiguous rows."""
+    import torch
+    kinds = {torch.float32: _abi.F32, torch.bfloat16: _abi.BF16}
+    if not t.is_cuda or t.dtype not in kinds or (dtypes is not None and kinds[t.dtype] not in dtypes):
+        raise TypeError("%s must be a %s device tensor" % (what, "float32" if dtypes == (_abi.F32,) else
+                                                           "float32 or bfloat16" if dtypes is None else "bfloat16"))
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (width is not None and shape[1] != width):
+        raise ValueError("%s: shape %s, expected %s x %s" % (what, tuple(shape), "rows" if rows is None else rows,
+                                                             "width" if width is None else width))
+    if shape[1] > 1 and shape[0] > 0 and stride[1] != 1:
+        raise ValueError("%s: the values of a row must be contiguous" % what)
+    return t.data_ptr(), kinds[t.dtype], stride[0] if shape[0] > 1 else max(shape[1], 1)
+
+
+def _scratch8(scratch, need):
+    """(pointer, bytes) of the caller's scratch tensor, or of one from torch's allocator (kept by the caller of this)."""
+    import torch
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+    elif not scratch.is_cuda or not scratch.is_contiguous():
+        raise TypeError("scratch must be a contiguous device tensor")
+    return scratch, scratch.data_ptr(), scratch.numel() * scratch.element_size()
+
+
+def _own_scratch8(scratch, need, stream):
+    """Scratch for a call that was given none: only on torch's current stream, whose order the allocator follows."""
+    if scratch is None and stream is not None:
+        raise ValueError("a call on a stream of its own needs scratch memory")
+    return _scratch8(scratch, need())
+
+
+class Linear8:
+    """A dense layer's weights in 8-bit integers with a scale per output
+    (``hpacml8_linear_create``): ``W`` [out][in] and ``b`` [out] or None,
+    float32 (numpy, or torch on the CPU or the device), copied."""
+
+    def __init__(self, W, b=None):
+        import numpy as np
+        import torch
+        W = torch.as_tensor(np.asarray(W) if not isinstance(W, torch.Tensor) else W)
+        if W.dim() != 2 or W.numel() == 0:
+            raise ValueError("W: shape %s, expected out x in" % (tuple(W.shape),))
+        W = W.detach().to(torch.float32).contiguous()
+        if b is not None:
+            b = torch.as_tensor(np.asarray(b) if not isinstance(b, torch.Tensor) else b).detach().to(torch.float32).contiguous()
+            if tuple(b.shape) != (W.shape[0],):
+                raise ValueError("b: shape %s, expected %d" % (tuple(b.shape), W.shape[0]))
+        self.n_out, self.n_in = int(W.shape[0]), int(W.shape[1])
+        h = C.c_void_p()
+        check(lib().hpacml8_linear_create(self.n_in, self.n_out, W.data_ptr(), None if b is None else b.data_ptr(),
+                                          C.byref(h)), "hpacml8_linear_create")
+        self.handle = h
+
+    def scratch_bytes(self, n_rows: int) -> int:
+        n = C.c_size_t()
+        check(lib().hpacml8_linear_scratch(self.handle, int(n_rows), C.byref(n)), "hpacml8_linear_scratch")
+        return n.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().hpacml8_linear_destroy(self.handle)
+            self.handle = None
+
+    __del__ = Model.__del__
+
+
+def linear8(layer: Linear8, x, y, act: int = _abi.ACT_IDENTITY, scratch=None, stream=None) -> None:
+    """``hpacml8_linear_run``: ``y`` [n][out] = act(``x`` [n][in] W^T + b) with
+    8-bit products; float32 or bfloat16 device tensors, rows may lie inside
+    wider ones.  ``scratch``: at least ``layer.scratch_bytes(n)`` bytes (None:
+    from torch's allocator, on its current stream)."""
+    px, tx, ldx = _matrix(x, "x", width=layer.n_in)
+    n = x.shape[0]
+    py, ty, ldy = _matrix(y, "y", rows=n, width=layer.n_out)
+    keep, ps, bytes_ = _own_scratch8(scratch, lambda: layer.scratch_bytes(n), stream)
+    check(lib().hpacml8_linear_run(layer.handle, px, tx, ldx, n, py, ty, ldy, act, ps, bytes_, _stream(stream)),
+          "hpacml8_linear_run")
+
+
+class Checkpoint8:
+    """Buffers of an activation [rows][width] kept in 8 bits (``hpacml8_checkpoint``);
+    ``act``: what the activation is the output of (ACT_RELU or ACT_IDENTITY).
+    ``codes`` and ``exps`` may be given (uint8 device tensors of ``rows`` rows)."""
+
+    def __init__(self, rows: int, width: int, act: int, codes=None, exps=None):
+        import torch
+        blocks = -(-int(width) // _abi.BLOCK8)
+        if codes is None:
+            codes = torch.empty((rows, blocks * _abi.BLOCK8), dtype=torch.uint8, device="cuda")
+        if exps is None:
+            exps = torch.empty((rows, blocks), dtype=torch.uint8, device="cuda")
+        for t, what, least in ((codes, "codes", blocks * _abi.BLOCK8), (exps, "exps", blocks)):
+            if t.dtype != torch.uint8 or not t.is_cuda:
+                raise TypeError("%s must be a uint8 device tensor" % what)
+            if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError("%s: shape %s, expected %d x at least %d, rows contiguous" % (what, tuple(t.shape), rows, least))
+        self.rows, self.width, self.act, self.codes, self.exps = int(rows), int(width), int(act), codes, exps
+        c = _abi.Checkpoint8()
+        c.codes, c.exps = codes.data_ptr(), exps.data_ptr()
+        c.rows, c.width, c.act = self.rows, self.width, self.act
+        c.ld_codes = codes.stride(0) if rows > 1 else blocks * _abi.BLOCK8
+        c.ld_exps = exps.stride(0) if rows > 1 else blocks
+        self.desc = c
+
+
+def checkpoint8_save(kept: Checkpoint8, z, a=None, stream=None) -> None:
+    """``hpacml8_checkpoint_save``: keeps act(``z``), and writes it to ``a`` as
+    well (which may be ``z``)."""
+    pz, tz, ldz = _matrix(z, "z", kept.rows, kept.width)
+    pa, ta, lda = (None, 0, 0) if a is None else _matrix(a, "a", kept.rows, kept.width)
+    check(lib().hpacml8_checkpoint_save(C.byref(kept.desc), pz, tz, ldz, pa, ta, lda, _stream(stream)),
+          "hpacml8_checkpoint_save")
+
+
+def checkpoint8_load(kept: Checkpoint8, a, stream=None) -> None:
+    """``hpacml8_checkpoint_load``: what ``kept`` stands for."""
+    pa, ta, lda = _matrix(a, "a", kept.rows, kept.width)
+    check(lib().hpacml8_checkpoint_load(C.byref(kept.desc), pa, ta, lda, _stream(stream)), "hpacml8_checkpoint_load")
+
+
+def backward8_scratch_bytes(kept: Checkpoint8, dy, W=None, dw: bool = True) -> int:
+    """Bytes of scratch ``backward8`` needs (``W``: given when dx is wanted)."""
+    _, t, ld = _matrix(dy, "dy", rows=kept.rows)
+    n = C.c_size_t()
+    check(lib().hpacml8_backward_scratch(C.byref(kept.desc), dy.data_ptr(), t, ld, dy.shape[1], 1 if dw else 0,
+                                         0 if W is None else 1, C.byref(n)), "hpacml8_backward_scratch")
+    return n.value
+
+
+def backward8(kept: Checkpoint8, dy, dw=None, db=None, W=None, dx=None, accumulate: bool = False, scratch=None,
+              stream=None) -> None:
+    """``hpacml8_backward``: the gradients of a linear layer whose input is
+    ``kept``, from ``dy`` [n][out] (float32 or bfloat16): ``dw`` [out][in] and
+    ``db`` [out] in float32, ``dx`` [n][in] in dy's type from ``W`` [out][in]
+    (dy's type).  Gradients not given are not computed."""
+    py, ty, ldy = _matrix(dy, "dy", rows=kept.rows)
+    n_out = dy.shape[1]
+    pw = lddw = pb = pW = ldW = px = ldx = None
+    if dw is not None:
+        pw, _, lddw = _matrix(dw, "dw", n_out, kept.width, (_abi.F32,))
+    if db is not None:
+        pb, _, _ = _matrix(db.unsqueeze(0), "db", 1, n_out, (_abi.F32,))
+    if dx is not None:
+        if W is None:
+            raise ValueError("dx needs W")
+        pW, _, ldW = _matrix(W, "W", n_out, kept.width, (ty,))
+        px, _, ldx = _matrix(dx, "dx", kept.rows, kept.width, (ty,))
+    keep, ps, bytes_ = _own_scratch8(scratch, lambda: backward8_scratch_bytes(
+        kept, dy, W if dx is not None else None, dw is not None or db is not None), stream)
+    check(lib().hpacml8_backward(C.byref(kept.desc), py, ty, ldy, n_out, pW, ldW or 0, pw, lddw or 0, pb, px, ldx or 0,
+                                 1 if accumulate else 0, ps, bytes_, _stream(stream)), "hpacml8_backward")

@@ -1,0 +1,131 @@
+// Dense layers in 8 bits: launchers, and the device arithmetic they share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "hpacml8.h"
+
+namespace hpacml {
+
+// Row pitch of int8 codes and of bf16 planes laid out for the products: whole
+// slabs of 128 bytes, so that a product's loop over k has no remainder.
+constexpr int kSlabBytes = 128;
+constexpr int64_t slab_pitch8(int64_t k) { return (k + 127) / 128 * 128; }
+constexpr int64_t slab_pitch16(int64_t k) { return (k + 63) / 64 * 64; }
+
+// codes [rows][pitch] and scales [rows] of x [rows][width]; columns from
+// width to pitch are written as 0.
+hipError_t launch_codes_by_row(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t width, int8_t *codes,
+                               int64_t pitch, float *scales, hipStream_t stream);
+
+// y = act(s_i t_j sum_k q_ik w_jk + b_j)
+struct Linear8Args {
+    const int8_t *q;      // [rows][pitch]
+    const float *s;       // [rows]
+    const int8_t *w;      // [n_out][pitch]
+    const float *t;       // [n_out]
+    const float *b;       // [n_out] or NULL
+    void *y;
+    int64_t rows, pitch, ldy;
+    int32_t n_out, relu;
+};
+hipError_t launch_linear8(const Linear8Args &a, int32_t y_dtype, hipStream_t stream);
+
+hipError_t launch_checkpoint_save(const hpacml8_checkpoint &c, const void *z, int32_t z_dtype, int64_t ldz, void *a,
+                                  int32_t a_dtype, int64_t lda, hipStream_t stream);
+hipError_t launch_checkpoint_load(const hpacml8_checkpoint &c, void *a, int32_t a_dtype, int64_t lda,
+                                  hipStream_t stream);
+
+// The backward pass.  Everything it puts into scratch, as byte offsets.
+struct Backward8Plan {
+    int32_t planes;       // bf16 terms of an operand: 1 (bf16) or 3 (fp32)
+    bool direct;          // dy is read in place
+    int64_t pitch;        // of dy's planes and W's transposed planes (elements)
+    int32_t splits;       // parts of the rows that sum into dw apart
+    int64_t rows_per_split;
+    size_t off_dy, off_wt, off_dw, off_db, bytes;
+};
+Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_t dtype, int64_t lddy, int32_t n_out,
+                             bool want_dw, bool want_dx);
+struct Backward8Args {
+    hpacml8_checkpoint c;
+    const void *dy;
+    int32_t dtype;
+    int64_t lddy;
+    int32_t n_out;
+    const void *W;
+    int64_t ldw;
+    float *dw;
+    int64_t lddw;
+    float *db;
+    void *dx;
+    int64_t lddx;
+    int32_t accumulate;
+    char *scratch;
+};
+hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipStream_t stream);
+
+// ---- device arithmetic --------------------------------------------------------
+
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ float bf16_bits_value(uint32_t h) { return __builtin_bit_cast(float, h << 16); }
+// nearest even; a NaN stays one
+__device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+__device__ __forceinline__ float load_value(const float *p) { return *p; }
+__device__ __forceinline__ float load_value(const uint16_t *p) { return bf16_bits_value(*p); }
+__device__ __forceinline__ void store_value(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store_value(uint16_t *p, float v) { *p = bf16_bits(v); }
+
+// max(x, 0) that keeps a NaN
+__device__ __forceinline__ float relu_keep_nan(float x) { return x < 0.f ? 0.f : x; }
+
+// The exponent byte of a block whose largest magnitude has these bits, and
+// the factor 2^-e that turns its values into codes.  amax in [2^(E-127),
+// 2^(E-126)) for exponent field E, so e + 127 = E - 7 (codes to 255) or
+// E - 6 (codes to 127); not below 1 (e = -126).
+__device__ __forceinline__ uint32_t block_exp(uint32_t amax_bits, bool relu) {
+    const uint32_t field = amax_bits >> 23, less = relu ? 7u : 6u;
+    return field == 255u ? 255u : field > less ? field - less : 1u;
+}
+__device__ __forceinline__ float block_factor(uint32_t byte) {
+    return byte == 255u ? 1.f : __builtin_bit_cast(float, (254u - byte) << 23);
+}
+// 2^e of an exponent byte (infinite for 255)
+__device__ __forceinline__ float block_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+template <bool RELU>
+__device__ __forceinline__ uint32_t block_code(float a, float factor) {
+    const float r = rintf(a * factor);
+    if (RELU)
+        return a > 0.f ? (uint32_t)fminf(fmaxf(r, 1.f), 255.f) : 0u;
+    return (uint32_t)((int32_t)fminf(fmaxf(r, -127.f), 127.f) + 128);
+}
+// exact in bf16 (8 significant bits)
+template <bool RELU>
+__device__ __forceinline__ float block_value(uint32_t code, float scale) {
+    return RELU ? (float)code * scale : ((float)code - 128.f) * scale;
+}
+
+// x as the exact sum of three bf16 terms, each the nearest to what is left
+// (a term that would round up to infinity is cut instead; infinities and
+// NaNs are the first term alone).
+__device__ __forceinline__ void split3(float x, uint16_t out[3]) {
+    uint16_t hi = bf16_bits(x);
+    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
+    const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
+    if (finite && (hi & 0x7F80u) == 0x7F80u)
+        hi = (uint16_t)(bits >> 16);
+    const float r = x - bf16_bits_value(hi);
+    const uint16_t mid = bf16_bits(r);
+    out[0] = hi;
+    out[1] = finite ? mid : (uint16_t)0;
+    out[2] = finite ? bf16_bits(r - bf16_bits_value(mid)) : (uint16_t)0;
+}
+
+}  // namespace hpacml

@@ -1,0 +1,77 @@
+"""Host-side checks of the 8-bit dense layers (no GPU needed): the library
+exports every symbol hpacml8.h declares, the binding's structure matches the
+header's, and bad descriptions are refused before any device work."""
+import ctypes as C
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2407_18352_amd import _abi
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "hpacml8.h")
+FAKE = 0x10000000   # never dereferenced
+
+
+def test_library_exports_every_declared_symbol():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(hpacml8_[a-z_]+)\s*\(", text))
+    assert names == set(_abi.SIGNATURES8)
+    out = subprocess.run(["nm", "-D", "--defined-only", _abi.LIB_PATH], capture_output=True, text=True).stdout
+    assert set(re.findall(r"\b(hpacml8_\w+)\b", out)) == names
+
+
+def test_header_compiles_as_c_and_structures_agree(tmp_path):
+    src = tmp_path / "t.c"
+    src.write_text('#include <stdio.h>\n#include "hpacml8.h"\nint main(void) { printf("%zu %zu %d %d", sizeof(hpacml8_checkpoint), '
+                   "offsetof(hpacml8_checkpoint, act), HPACML8_BLOCK, HPACML8_MAX_WIDTH); return 0; }")
+    exe = tmp_path / "t"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [C.sizeof(_abi.Checkpoint8), _abi.Checkpoint8.act.offset, _abi.BLOCK8, _abi.MAX_WIDTH8]
+
+
+def _kept(**more):
+    c = _abi.Checkpoint8()
+    c.codes, c.exps, c.rows, c.ld_codes, c.ld_exps, c.width, c.act = FAKE, FAKE, 10, 64, 2, 40, _abi.ACT_RELU
+    for k, v in more.items():
+        setattr(c, k, v)
+    return c
+
+
+@pytest.mark.parametrize("more, status", [
+    ({}, _abi.OK), (dict(rows=0), _abi.OK), (dict(rows=-1), _abi.E_INVAL), (dict(width=0), _abi.E_INVAL),
+    (dict(act=2), _abi.E_INVAL), (dict(ld_codes=63), _abi.E_INVAL), (dict(ld_codes=80), _abi.E_INVAL),
+    (dict(ld_codes=32), _abi.E_INVAL), (dict(ld_exps=1), _abi.E_INVAL), (dict(rows=1 << 40), _abi.E_UNSUPPORTED),
+    (dict(width=_abi.MAX_WIDTH8 + 1, ld_codes=1 << 16, ld_exps=1 << 16), _abi.E_UNSUPPORTED),
+])
+def test_checkpoint_descriptions(more, status):
+    n = C.c_size_t()
+    assert _abi.lib().hpacml8_backward_scratch(_kept(**more), FAKE, _abi.BF16, 8, 8, 1, 1, C.byref(n)) == status
+
+
+@pytest.mark.parametrize("kind, lddy, n_out, status", [
+    (_abi.F32, 8, 8, _abi.OK), (2, 8, 8, _abi.E_INVAL), (_abi.F32, 7, 8, _abi.E_INVAL), (_abi.F32, 8, 0, _abi.E_INVAL),
+    (_abi.F32, 1 << 20, 1 << 20, _abi.E_UNSUPPORTED),
+])
+def test_backward_descriptions(kind, lddy, n_out, status):
+    n = C.c_size_t()
+    assert _abi.lib().hpacml8_backward_scratch(_kept(), FAKE, kind, lddy, n_out, 1, 1, C.byref(n)) == status
+
+
+def test_null_arguments():
+    L = _abi.lib()
+    n, h = C.c_size_t(), C.c_void_p()
+    assert L.hpacml8_backward_scratch(None, FAKE, 0, 8, 8, 1, 1, C.byref(n)) == _abi.E_INVAL
+    assert L.hpacml8_backward_scratch(_kept(), FAKE, 0, 8, 8, 1, 1, None) == _abi.E_INVAL
+    assert L.hpacml8_linear_create(4, 4, None, None, C.byref(h)) == _abi.E_INVAL and not h.value
+    assert L.hpacml8_linear_create(0, 4, FAKE, None, C.byref(h)) == _abi.E_INVAL and not h.value
+    assert L.hpacml8_linear_create(4, _abi.MAX_WIDTH8 + 1, FAKE, None, C.byref(h)) == _abi.E_UNSUPPORTED and not h.value
+    assert L.hpacml8_linear_create(4, 4, FAKE, None, None) == _abi.E_INVAL
+    assert L.hpacml8_linear_scratch(None, 4, C.byref(n)) == _abi.E_INVAL
+    assert L.hpacml8_linear_run(None, FAKE, 0, 4, 1, FAKE, 0, 4, 0, FAKE, 0, None) == _abi.E_INVAL
+    assert L.hpacml8_checkpoint_save(None, FAKE, 0, 40, None, 0, 0, None) == _abi.E_INVAL
+    assert L.hpacml8_checkpoint_load(None, FAKE, 0, 40, None) == _abi.E_INVAL
+    L.hpacml8_linear_destroy(None)
