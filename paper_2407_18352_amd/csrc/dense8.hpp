@@ -77,6 +77,13 @@ __device__ __forceinline__ float bf16_bits_value(uint32_t h) { return __builtin_
 // nearest even; a NaN stays one
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
+// two of them in one word, the first in the low half (one instruction)
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
 __device__ __forceinline__ float load_value(const float *p) { return *p; }
 __device__ __forceinline__ float load_value(const uint16_t *p) { return bf16_bits_value(*p); }
 __device__ __forceinline__ void store_value(float *p, float v) { *p = v; }

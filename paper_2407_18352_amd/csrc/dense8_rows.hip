@@ -1,5 +1,10 @@
 // Row-wise kernels of the 8-bit dense layers: codes and scales of a row, and
 // activations put away in 8 bits and brought back.  All are bound by memory.
+//
+// A lane takes eight consecutive values at a time: 16 bytes of bf16 or 32 of
+// fp32, from any address (the hardware loads and stores 16 bytes at an
+// element's alignment), and 8 bytes of codes.  Only the chunk that crosses a
+// row's end goes value by value.
 #include "dense8.hpp"
 
 namespace hpacml {
@@ -7,108 +12,248 @@ namespace hpacml {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kMaxBlocks = 1 << 16;   // the kernels loop beyond them
+constexpr int kMaxBlocks = 1 << 14;   // the kernels loop beyond them
+constexpr int kChunk = 8;
 
-dim3 blocks_for(int64_t items, int64_t per_block) {
-    const int64_t n = (items + per_block - 1) / per_block;
-    return dim3((uint32_t)(n < kMaxBlocks ? n : kMaxBlocks));
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+
+// chunk at `p`, of which the first n values exist (the others become 0)
+__device__ __forceinline__ void load_chunk(const float *p, int n, float (&v)[kChunk]) {
+    if (n >= kChunk) {
+        const f32x4 a = ((const f32x4_any *)p)[0], b = ((const f32x4_any *)p)[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = a[e];
+            v[4 + e] = b[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e)
+            v[e] = e < n ? p[e] : 0.f;
+    }
+}
+__device__ __forceinline__ void load_chunk(const uint16_t *p, int n, float (&v)[kChunk]) {
+    if (n >= kChunk) {
+        const u32x4 a = *(const u32x4_any *)p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __builtin_bit_cast(float, a[e] << 16);
+            v[2 * e + 1] = __builtin_bit_cast(float, a[e] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e)
+            v[e] = e < n ? bf16_bits_value(p[e]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store_chunk(float *p, int n, const float (&v)[kChunk]) {
+    if (n >= kChunk) {
+        ((f32x4_any *)p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+        ((f32x4_any *)p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e)
+            if (e < n)
+                p[e] = v[e];
+    }
+}
+__device__ __forceinline__ void store_chunk(uint16_t *p, int n, const float (&v)[kChunk]) {
+    if (n >= kChunk) {
+        u32x4 a;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            a[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+        *(u32x4_any *)p = a;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e)
+            if (e < n)
+                p[e] = bf16_bits(v[e]);
+    }
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t v, int lanes) {
-    for (int d = lanes / 2; d > 0; d /= 2)
+// largest magnitude as bits: an infinity is above every number, a NaN above it
+__device__ __forceinline__ uint32_t top_bits(const float (&v)[kChunk]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < kChunk; ++e)
+        m = max(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7FFFFFFFu);
+    return m;
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d /= 2)
         v = max(v, (uint32_t)__shfl_xor((int)v, d));
     return v;
 }
 
-// One wave per row: the largest magnitude (as bits, so that an infinity or a
-// NaN is the largest), then the codes.
-template <typename T>
+// LANES lanes per row, HELD chunks of each lane in registers: rows up to
+// LANES * HELD chunks are read once, longer ones a second time (from the
+// caches) for their codes.
+template <typename T, int LANES, int HELD>
 __global__ void __launch_bounds__(kThreads) codes_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows,
                                                          int32_t width, int8_t *__restrict__ codes, int64_t pitch,
                                                          float *__restrict__ scales) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t r = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); r < rows;
-         r += (int64_t)gridDim.x * (kThreads / 64)) {
+    constexpr int kRows = kThreads / LANES;
+    const int lane = threadIdx.x % LANES, chunks = (int)(pitch / kChunk);
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; r < rows; r += (int64_t)gridDim.x * kRows) {
         const T *row = x + r * ldx;
+        float v[HELD][kChunk];
         uint32_t top = 0;
-        for (int k = lane; k < width; k += 64)
-            top = max(top, __builtin_bit_cast(uint32_t, load_value(row + k)) & 0x7FFFFFFFu);
-        top = wave_max(top, 64);
+        for (int c = lane; c < chunks; c += LANES * HELD) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                const int k = (c + h * LANES) * kChunk;
+                load_chunk(row + k, width - k, v[h]);
+            }
+#pragma unroll
+            for (int h = 0; h < HELD; ++h)
+                top = max(top, top_bits(v[h]));
+        }
+        top = lanes_max<LANES>(top);
         const float amax = __builtin_bit_cast(float, top);
         const bool finite = top < 0x7F800000u, live = finite && amax >= 0x1p-119f;
         const float inv = live ? 127.f / amax : 0.f;
         if (lane == 0)
             scales[r] = !finite ? __builtin_nanf("") : live ? amax / 127.f : 0.f;
-        for (int k = lane; k < pitch; k += 64)
-            codes[r * pitch + k] = k < width && live ? (int8_t)rintf(load_value(row + k) * inv) : (int8_t)0;
+        for (int c = lane; c < chunks; c += LANES * HELD) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                const int at = c + h * LANES;
+                if (at >= chunks)
+                    break;
+                if (chunks > LANES * HELD)
+                    load_chunk(row + at * kChunk, width - at * kChunk, v[h]);
+                uint32_t q[2] = {0, 0};
+                if (live) {   // rows that count as zeros, or are not finite: codes 0
+#pragma unroll
+                    for (int e = 0; e < kChunk; ++e)
+                        q[e / 4] |= ((uint32_t)(int32_t)rintf(v[h][e] * inv) & 0xFFu) << (8 * (e % 4));
+                }
+                *(uint2 *)(codes + r * pitch + at * kChunk) = uint2{q[0], q[1]};
+            }
+        }
     }
 }
 
-// 32 lanes per block of channels.
+// A block of threads covers `cols` chunks (a power of two, at least the four
+// of a block of channels) of kThreads / cols rows.
 template <typename Z, typename A, bool RELU>
-__global__ void __launch_bounds__(kThreads) save_kernel(hpacml8_checkpoint c, const Z *__restrict__ z, int64_t ldz,
-                                                        A *a, int64_t lda) {
-    const int64_t blocks = (c.width + 31) / 32;
-    for (int64_t id = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); id < c.rows * blocks;
-         id += (int64_t)gridDim.x * (kThreads / 32)) {
-        const int64_t r = id / blocks, blk = id - r * blocks;
-        const int k = (int)blk * 32 + (threadIdx.x & 31);
-        float v = 0.f;
-        if (k < c.width) {
-            v = load_value(z + r * ldz + k);
-            if (RELU)
-                v = relu_keep_nan(v);
+__global__ void __launch_bounds__(kThreads) save_kernel(hpacml8_checkpoint c, const Z *z, int64_t ldz,
+                                                        A *a, int64_t lda, int cols_log) {
+    const int col = threadIdx.x & ((1 << cols_log) - 1), per = kThreads >> cols_log;
+    const int chunks = (c.width + 31) / 32 * 4;
+    for (int64_t r = (int64_t)blockIdx.x * per + (threadIdx.x >> cols_log); r < c.rows; r += (int64_t)gridDim.x * per)
+        for (int at = col; at < chunks; at += 1 << cols_log) {
+            const int k = at * kChunk, n = c.width - k;
+            float v[kChunk];
+            load_chunk(z + r * ldz + k, n, v);
+            if (RELU) {
+#pragma unroll
+                for (int e = 0; e < kChunk; ++e)
+                    v[e] = relu_keep_nan(v[e]);
+            }
+            const uint32_t byte = block_exp(lanes_max<4>(top_bits(v)), RELU);
+            const float f = block_factor(byte);
+            uint32_t q[2] = {0, 0};
+#pragma unroll
+            for (int e = 0; e < kChunk; ++e)
+                q[e / 4] |= block_code<RELU>(v[e], f) << (8 * (e % 4));
+            *(uint2 *)((uint8_t *)c.codes + r * c.ld_codes + k) = uint2{q[0], q[1]};
+            if ((at & 3) == 0)
+                ((uint8_t *)c.exps)[r * c.ld_exps + at / 4] = (uint8_t)byte;
+            if (a)
+                store_chunk(a + r * lda + k, n, v);
         }
-        const uint32_t e = block_exp(wave_max(__builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu, 32), RELU);
-        ((uint8_t *)c.codes)[r * c.ld_codes + k] = (uint8_t)block_code<RELU>(v, block_factor(e));
-        if ((threadIdx.x & 31) == 0)
-            ((uint8_t *)c.exps)[r * c.ld_exps + blk] = (uint8_t)e;
-        if (a && k < c.width)
-            store_value(a + r * lda + k, v);
-    }
 }
 
 template <typename A, bool RELU>
-__global__ void __launch_bounds__(kThreads) load_kernel(hpacml8_checkpoint c, A *__restrict__ a, int64_t lda) {
-    for (int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x; id < c.rows * c.width;
-         id += (int64_t)gridDim.x * kThreads) {
-        const int64_t r = id / c.width, k = id - r * c.width;
-        const float s = block_scale(((const uint8_t *)c.exps)[r * c.ld_exps + k / 32]);
-        store_value(a + r * lda + k, block_value<RELU>(((const uint8_t *)c.codes)[r * c.ld_codes + k], s));
-    }
+__global__ void __launch_bounds__(kThreads) load_kernel(hpacml8_checkpoint c, A *__restrict__ a, int64_t lda,
+                                                        int cols_log) {
+    const int col = threadIdx.x & ((1 << cols_log) - 1), per = kThreads >> cols_log;
+    const int chunks = (c.width + kChunk - 1) / kChunk;
+    for (int64_t r = (int64_t)blockIdx.x * per + (threadIdx.x >> cols_log); r < c.rows; r += (int64_t)gridDim.x * per)
+        for (int at = col; at < chunks; at += 1 << cols_log) {
+            const int k = at * kChunk;
+            const uint2 q = *(const uint2 *)((const uint8_t *)c.codes + r * c.ld_codes + k);
+            const float s = block_scale(((const uint8_t *)c.exps)[r * c.ld_exps + at / 4]);
+            float v[kChunk];
+#pragma unroll
+            for (int e = 0; e < kChunk; ++e)
+                v[e] = block_value<RELU>(((e < 4 ? q.x : q.y) >> (8 * (e % 4))) & 0xFFu, s);
+            store_chunk(a + r * lda + k, c.width - k, v);
+        }
+}
+
+dim3 blocks_for(int64_t rows, int64_t per_block) {
+    const int64_t n = (rows + per_block - 1) / per_block;
+    return dim3((uint32_t)(n < kMaxBlocks ? n : kMaxBlocks));
+}
+
+template <typename T, int LANES, int HELD>
+void codes_as(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *codes, int64_t pitch, float *scales,
+              hipStream_t stream) {
+    codes_kernel<T, LANES, HELD><<<blocks_for(rows, kThreads / LANES), kThreads, 0, stream>>>((const T *)x, ldx, rows,
+                                                                                             width, codes, pitch, scales);
+}
+
+template <typename T>
+void codes_of(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *codes, int64_t pitch, float *scales,
+              hipStream_t st) {
+    const int64_t chunks = pitch / kChunk;   // a multiple of 16
+    if (chunks <= 16)
+        codes_as<T, 16, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+    else if (chunks <= 32)
+        codes_as<T, 32, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+    else if (chunks <= 64)
+        codes_as<T, 64, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+    else if (chunks <= 128)
+        codes_as<T, 64, 2>(x, ldx, rows, width, codes, pitch, scales, st);
+    else if (chunks <= 256)
+        codes_as<T, 64, 4>(x, ldx, rows, width, codes, pitch, scales, st);
+    else
+        codes_as<T, 64, 8>(x, ldx, rows, width, codes, pitch, scales, st);
+}
+
+// log2 of the chunks a row of a block of threads covers: 4 .. 256
+int cols_log(int chunks) {
+    int l = 2;
+    while ((1 << l) < chunks && (1 << l) < kThreads)
+        ++l;
+    return l;
+}
+
+template <typename Z, typename A>
+void save_as(const hpacml8_checkpoint &c, const void *z, int64_t ldz, void *a, int64_t lda, hipStream_t stream) {
+    const int l = cols_log((c.width + 31) / 32 * 4);
+    const dim3 grid = blocks_for(c.rows, kThreads >> l);
+    if (c.act == HPACML_ACT_RELU)
+        save_kernel<Z, A, true><<<grid, kThreads, 0, stream>>>(c, (const Z *)z, ldz, (A *)a, lda, l);
+    else
+        save_kernel<Z, A, false><<<grid, kThreads, 0, stream>>>(c, (const Z *)z, ldz, (A *)a, lda, l);
+}
+template <typename A>
+void load_as(const hpacml8_checkpoint &c, void *a, int64_t lda, hipStream_t stream) {
+    const int l = cols_log((c.width + kChunk - 1) / kChunk);
+    const dim3 grid = blocks_for(c.rows, kThreads >> l);
+    if (c.act == HPACML_ACT_RELU)
+        load_kernel<A, true><<<grid, kThreads, 0, stream>>>(c, (A *)a, lda, l);
+    else
+        load_kernel<A, false><<<grid, kThreads, 0, stream>>>(c, (A *)a, lda, l);
 }
 
 }  // namespace
 
 hipError_t launch_codes_by_row(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t width, int8_t *codes,
                                int64_t pitch, float *scales, hipStream_t stream) {
-    const dim3 grid = blocks_for(rows, kThreads / 64);
     if (dtype == HPACML_F32)
-        codes_kernel<float><<<grid, kThreads, 0, stream>>>((const float *)x, ldx, rows, width, codes, pitch, scales);
+        codes_of<float>(x, ldx, rows, width, codes, pitch, scales, stream);
     else
-        codes_kernel<uint16_t><<<grid, kThreads, 0, stream>>>((const uint16_t *)x, ldx, rows, width, codes, pitch,
-                                                              scales);
+        codes_of<uint16_t>(x, ldx, rows, width, codes, pitch, scales, stream);
     return hipGetLastError();
 }
-
-namespace {
-template <typename Z, typename A>
-void save_as(const hpacml8_checkpoint &c, const void *z, int64_t ldz, void *a, int64_t lda, hipStream_t stream) {
-    const dim3 grid = blocks_for(c.rows * ((c.width + 31) / 32), kThreads / 32);
-    if (c.act == HPACML_ACT_RELU)
-        save_kernel<Z, A, true><<<grid, kThreads, 0, stream>>>(c, (const Z *)z, ldz, (A *)a, lda);
-    else
-        save_kernel<Z, A, false><<<grid, kThreads, 0, stream>>>(c, (const Z *)z, ldz, (A *)a, lda);
-}
-template <typename A>
-void load_as(const hpacml8_checkpoint &c, void *a, int64_t lda, hipStream_t stream) {
-    const dim3 grid = blocks_for(c.rows * c.width, kThreads);
-    if (c.act == HPACML_ACT_RELU)
-        load_kernel<A, true><<<grid, kThreads, 0, stream>>>(c, (A *)a, lda);
-    else
-        load_kernel<A, false><<<grid, kThreads, 0, stream>>>(c, (A *)a, lda);
-}
-}  // namespace
 
 hipError_t launch_checkpoint_save(const hpacml8_checkpoint &c, const void *z, int32_t z_dtype, int64_t ldz, void *a,
                                   int32_t a_dtype, int64_t lda, hipStream_t stream) {

@@ -1,70 +1,98 @@
 // y = act(s_i t_j sum_k q_ik w_jk + b_j): int8 codes on v_mfma_i32_16x16x64_i8,
 // exact 32-bit sums, fp32 epilogue.
-#include "dense8.hpp"
+#include "dense8_nt.hpp"
 
 namespace hpacml {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 64;                    // rows and outputs of a block
-constexpr int64_t kMaxBlocks = 1 << 20;       // the kernel loops beyond them
-constexpr int kPitch = kSlabBytes + 16;      // of an LDS row
+__device__ __forceinline__ void store4(float *p, const float (&v)[4], int n, bool whole) {
+    if (whole)
+        *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
+    else
+        for (int e = 0; e < 4; ++e)
+            if (e < n)
+                p[e] = v[e];
+}
+__device__ __forceinline__ void store4(uint16_t *p, const float (&v)[4], int n, bool whole) {
+    if (whole) {
+        uint2 u;
+        u.x = bf16_bits(v[0]) | (uint32_t)bf16_bits(v[1]) << 16;
+        u.y = bf16_bits(v[2]) | (uint32_t)bf16_bits(v[3]) << 16;
+        *(uint2 *)p = u;
+    } else {
+        for (int e = 0; e < 4; ++e)
+            if (e < n)
+                p[e] = bf16_bits(v[e]);
+    }
+}
+
+template <typename Y, int WA, int WB, int NA, int NB>
+__global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, uint32_t out_tiles, uint32_t point_tiles) {
+    typedef nt::Tile<nt::I8, WA, WB, NA, NB> T;
+    __shared__ __align__(1024) char lds[2 * T::kBuf];
+    const nt::TileAt at = nt::tile_at(blockIdx.x, gridDim.x, out_tiles, point_tiles);
+    const int64_t a0 = at.out * T::kA, b0 = at.point * T::kB;
+    i32x4 acc[NA][NB] = {};
+    T t;
+    t.template run<false>({(const char *)p.w, p.n_out, p.pitch, p.pitch, 0}, {(const char *)p.q, p.rows, p.pitch, p.pitch, 0},
+                          a0, b0, 1, lds, acc);
+    // four outputs of a point at once where every row keeps their alignment
+    const bool wide = ((uintptr_t)p.y & (4 * sizeof(Y) - 1)) == 0 && (p.ldy & 3) == 0;
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+        const int n = (int)a0 + t.out_of(a);
+        float sc[4], bias[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int j = min(n + e, p.n_out - 1);
+            sc[e] = p.t[j];
+            bias[e] = p.b ? p.b[j] : 0.f;
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int64_t r = b0 + t.point_of(b);
+            if (r >= p.rows || n >= p.n_out)
+                continue;
+            const float s = p.s[r];
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = (float)acc[a][b][e] * s * sc[e] + bias[e];
+                if (p.relu)
+                    v[e] = relu_keep_nan(v[e]);
+            }
+            store4((Y *)p.y + r * p.ldy + n, v, p.n_out - n, wide && n + 4 <= p.n_out);
+        }
+    }
+}
+
+template <typename Y, int WA, int WB, int NA, int NB>
+void launch_tile(const Linear8Args &a, hipStream_t stream) {
+    typedef nt::Tile<nt::I8, WA, WB, NA, NB> T;
+    const uint32_t out_tiles = (uint32_t)((a.n_out + T::kA - 1) / T::kA), point_tiles = (uint32_t)((a.rows + T::kB - 1) / T::kB);
+    linear8_kernel<Y, WA, WB, NA, NB><<<dim3(out_tiles * point_tiles), T::kThreads, 0, stream>>>(a, out_tiles, point_tiles);
+}
 
 template <typename Y>
-__global__ void __launch_bounds__(kThreads) linear8_kernel(Linear8Args p, int64_t tiles, int32_t col_tiles) {
-    __shared__ __align__(16) int8_t qs[kTile][kPitch], ws[kTile][kPitch];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wr = (wave & 1) * 32, wc = (wave >> 1) * 32;
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t r0 = tile / col_tiles * kTile;
-        const int c0 = (int)(tile % col_tiles) * kTile;
-        i32x4 acc[2][2] = {};
-        for (int64_t k = 0; k < p.pitch; k += kSlabBytes) {
-            for (int i = tid; i < kTile * 8; i += kThreads) {
-                const int row = i >> 3, chunk = (i & 7) * 16;
-                const int64_t r = min(r0 + row, p.rows - 1);
-                const int64_t n = min(c0 + row, p.n_out - 1);
-                *(i32x4 *)&qs[row][chunk] = *(const i32x4 *)(p.q + r * p.pitch + k + chunk);
-                *(i32x4 *)&ws[row][chunk] = *(const i32x4 *)(p.w + n * p.pitch + k + chunk);
-            }
-            __syncthreads();
-            for (int s = 0; s < 2; ++s) {
-                i32x4 a[2], b[2];
-                for (int t = 0; t < 2; ++t) {
-                    a[t] = *(const i32x4 *)&qs[wr + t * 16 + (lane & 15)][s * 64 + (lane >> 4) * 16];
-                    b[t] = *(const i32x4 *)&ws[wc + t * 16 + (lane & 15)][s * 64 + (lane >> 4) * 16];
-                }
-                for (int t = 0; t < 2; ++t)
-                    for (int u = 0; u < 2; ++u)
-                        acc[t][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t], b[u], acc[t][u], 0, 0, 0);
-            }
-            __syncthreads();
-        }
-        for (int t = 0; t < 2; ++t)
-            for (int u = 0; u < 2; ++u)
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t r = r0 + wr + t * 16 + (lane >> 4) * 4 + e;
-                    const int n = c0 + wc + u * 16 + (lane & 15);
-                    if (r < p.rows && n < p.n_out) {
-                        float v = (float)acc[t][u][e] * p.s[r] * p.t[n];
-                        if (p.b)
-                            v += p.b[n];
-                        store_value((Y *)p.y + r * p.ldy + n, p.relu ? relu_keep_nan(v) : v);
-                    }
-                }
-    }
+void launch_as(const Linear8Args &a, hipStream_t stream) {
+    const int64_t big = ((a.n_out + 255) / 256) * ((a.rows + 255) / 256);
+    const int64_t mid = ((a.n_out + 127) / 128) * ((a.rows + 127) / 128);
+    if (big >= 512 && a.pitch >= 2048)
+        launch_tile<Y, 4, 2, 4, 8>(a, stream);
+    else if (mid >= 256 && a.n_out > 64)
+        launch_tile<Y, 2, 2, 4, 4>(a, stream);
+    else
+        launch_tile<Y, 2, 2, 2, 2>(a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_linear8(const Linear8Args &a, int32_t y_dtype, hipStream_t stream) {
-    const int32_t col_tiles = (a.n_out + kTile - 1) / kTile;
-    const int64_t tiles = (a.rows + kTile - 1) / kTile * col_tiles;
-    const dim3 grid((uint32_t)(tiles < kMaxBlocks ? tiles : kMaxBlocks));
     if (y_dtype == HPACML_F32)
-        linear8_kernel<float><<<grid, kThreads, 0, stream>>>(a, tiles, col_tiles);
+        launch_as<float>(a, stream);
     else
-        linear8_kernel<uint16_t><<<grid, kThreads, 0, stream>>>(a, tiles, col_tiles);
+        launch_as<uint16_t>(a, stream);
     return hipGetLastError();
 }
 
