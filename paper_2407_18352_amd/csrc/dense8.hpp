@@ -42,6 +42,7 @@ struct Backward8Plan {
     int32_t planes;       // bf16 terms of an operand: 1 (bf16) or 3 (fp32)
     bool direct;          // dy is read in place
     int64_t pitch;        // of dy's planes and W's transposed planes (elements)
+    int32_t tile;         // of dw
     int32_t splits;       // parts of the rows that sum into dw apart
     int64_t rows_per_split;
     size_t off_dy, off_wt, off_dw, off_db, bytes;
@@ -88,6 +89,29 @@ __device__ __forceinline__ float load_value(const float *p) { return *p; }
 __device__ __forceinline__ float load_value(const uint16_t *p) { return bf16_bits_value(*p); }
 __device__ __forceinline__ void store_value(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_value(uint16_t *p, float v) { *p = bf16_bits(v); }
+
+// Up to n of four values at p: in one store where `whole` says that all four
+// exist and p is aligned to them.
+__device__ __forceinline__ void store_four(float *p, const float (&v)[4], int n, bool whole) {
+    if (whole) {
+        *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n)
+                p[e] = v[e];
+    }
+}
+__device__ __forceinline__ void store_four(uint16_t *p, const float (&v)[4], int n, bool whole) {
+    if (whole) {
+        *(uint2 *)p = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n)
+                p[e] = bf16_bits(v[e]);
+    }
+}
 
 // max(x, 0) that keeps a NaN
 __device__ __forceinline__ float relu_keep_nan(float x) { return x < 0.f ? 0.f : x; }

@@ -161,6 +161,13 @@ struct Tile {
     __device__ __forceinline__ int point_of(int u) const { return (wave % WB * NB + u) * 16 + (lane & 15); }
 };
 
+// Rows of one launch: a launch of more than 2^22 blocks is split (a grid holds
+// fewer than 2^32 threads).
+inline int64_t rows_per_launch(uint32_t out_tiles, int64_t tile) {
+    const int64_t point_tiles = (int64_t)(1 << 22) / out_tiles;
+    return (point_tiles < 1 ? 1 : point_tiles) * tile;
+}
+
 // Block id -> tile.  Blocks go to the eight XCDs in turn; each XCD takes a
 // contiguous run of tiles, so that what its blocks share meets in its L2, and
 // a run goes through groups of `kGroup` point tiles by all output tiles.

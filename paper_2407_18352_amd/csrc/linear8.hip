@@ -6,27 +6,6 @@ namespace hpacml {
 
 namespace {
 
-__device__ __forceinline__ void store4(float *p, const float (&v)[4], int n, bool whole) {
-    if (whole)
-        *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
-    else
-        for (int e = 0; e < 4; ++e)
-            if (e < n)
-                p[e] = v[e];
-}
-__device__ __forceinline__ void store4(uint16_t *p, const float (&v)[4], int n, bool whole) {
-    if (whole) {
-        uint2 u;
-        u.x = bf16_bits(v[0]) | (uint32_t)bf16_bits(v[1]) << 16;
-        u.y = bf16_bits(v[2]) | (uint32_t)bf16_bits(v[3]) << 16;
-        *(uint2 *)p = u;
-    } else {
-        for (int e = 0; e < 4; ++e)
-            if (e < n)
-                p[e] = bf16_bits(v[e]);
-    }
-}
-
 template <typename Y, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, uint32_t out_tiles, uint32_t point_tiles) {
     typedef nt::Tile<nt::I8, WA, WB, NA, NB> T;
@@ -62,7 +41,7 @@ __global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, ui
                 if (p.relu)
                     v[e] = relu_keep_nan(v[e]);
             }
-            store4((Y *)p.y + r * p.ldy + n, v, p.n_out - n, wide && n + 4 <= p.n_out);
+            store_four((Y *)p.y + r * p.ldy + n, v, p.n_out - n, wide && n + 4 <= p.n_out);
         }
     }
 }
@@ -70,8 +49,17 @@ __global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, ui
 template <typename Y, int WA, int WB, int NA, int NB>
 void launch_tile(const Linear8Args &a, hipStream_t stream) {
     typedef nt::Tile<nt::I8, WA, WB, NA, NB> T;
-    const uint32_t out_tiles = (uint32_t)((a.n_out + T::kA - 1) / T::kA), point_tiles = (uint32_t)((a.rows + T::kB - 1) / T::kB);
-    linear8_kernel<Y, WA, WB, NA, NB><<<dim3(out_tiles * point_tiles), T::kThreads, 0, stream>>>(a, out_tiles, point_tiles);
+    const uint32_t out_tiles = (uint32_t)((a.n_out + T::kA - 1) / T::kA);
+    const int64_t step = nt::rows_per_launch(out_tiles, T::kB);
+    for (int64_t r = 0; r < a.rows; r += step) {
+        Linear8Args p = a;
+        p.rows = a.rows - r < step ? a.rows - r : step;
+        p.q += r * a.pitch;
+        p.s += r;
+        p.y = (Y *)a.y + r * a.ldy;
+        const uint32_t point_tiles = (uint32_t)((p.rows + T::kB - 1) / T::kB);
+        linear8_kernel<Y, WA, WB, NA, NB><<<dim3(out_tiles * point_tiles), T::kThreads, 0, stream>>>(p, out_tiles, point_tiles);
+    }
 }
 
 template <typename Y>
