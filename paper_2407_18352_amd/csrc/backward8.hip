@@ -64,7 +64,7 @@ struct DxArgs {
 template <typename X, bool EDGE, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB) dx_kernel(DxArgs p) {
     typedef nt::Tile<nt::Bf16, WA, WB, NA, NB> T;
-    __shared__ __align__(1024) char lds[2 * T::kBuf];
+    __shared__ __align__(1024) char lds[T::kLds];
     const nt::TileAt at = nt::tile_at(blockIdx.x, gridDim.x, p.in_tiles, p.point_tiles);
     const int64_t a0 = at.out * T::kA, b0 = at.point * T::kB;
     f32x4 acc[NA][NB] = {};
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
             load_x(1);
     }
     for (int s = 0; s < total; ++s) {
-        nt::wait_loads();
+        nt::wait_loads<0>();
         nt::barrier();
         const char *buf = lds + (s & 1) * T::kBuf;
         if (s + 1 < total) {

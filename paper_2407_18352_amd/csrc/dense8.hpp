@@ -9,10 +9,10 @@
 namespace hpacml {
 
 // Row pitch of int8 codes and of bf16 planes laid out for the products: whole
-// slabs of 128 bytes, so that a product's loop over k has no remainder.
-constexpr int kSlabBytes = 128;
-constexpr int64_t slab_pitch8(int64_t k) { return (k + 127) / 128 * 128; }
-constexpr int64_t slab_pitch16(int64_t k) { return (k + 63) / 64 * 64; }
+// slabs of 64 bytes, so that a product's loop over k has no remainder.
+constexpr int kSlabBytes = 64;
+constexpr int64_t slab_pitch8(int64_t k) { return (k + 63) / 64 * 64; }
+constexpr int64_t slab_pitch16(int64_t k) { return (k + 31) / 32 * 32; }
 
 // codes [rows][pitch] and scales [rows] of x [rows][width]; columns from
 // width to pitch are written as 0.
@@ -24,8 +24,8 @@ struct Linear8Args {
     const int8_t *q;      // [rows][pitch]
     const float *s;       // [rows]
     const int8_t *w;      // [n_out][pitch]
-    const float *t;       // [n_out]
-    const float *b;       // [n_out] or NULL
+    const float *t;       // [n_out], to a multiple of four
+    const float *b;       // the same; zeros without a bias
     void *y;
     int64_t rows, pitch, ldy;
     int32_t n_out, relu;

@@ -12,7 +12,7 @@ struct hpacml8_linear_s {
     int device = 0;
     int32_t n_in = 0, n_out = 0;
     int64_t pitch = 0;
-    char *buf = nullptr;      // codes [n_out][pitch], scales [n_out], biases [n_out]
+    char *buf = nullptr;      // codes [n_out][pitch], then scales and biases, each to a multiple of four
     int8_t *w = nullptr;
     float *t = nullptr, *b = nullptr;
 };
@@ -139,20 +139,22 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
     l->n_out = n_out;
     l->pitch = slab_pitch8(n_in);
     float *staged = nullptr;
-    const size_t codes = (size_t)n_out * l->pitch, wbytes = (size_t)n_out * n_in * 4;
+    const size_t codes = (size_t)n_out * l->pitch, wbytes = (size_t)n_out * n_in * 4, outs = ((size_t)n_out + 3) / 4 * 4;
     hipError_t e = hipGetDevice(&l->device);
     if (e == hipSuccess)
         e = hipDeviceSynchronize();
     if (e == hipSuccess)
-        e = hipMalloc((void **)&l->buf, codes + (size_t)n_out * 8);
+        e = hipMalloc((void **)&l->buf, codes + outs * 8);
     if (e == hipSuccess)
         e = hipMalloc((void **)&staged, wbytes);
     if (e == hipSuccess) {
         l->w = (int8_t *)l->buf;
         l->t = (float *)(l->buf + codes);
-        l->b = b ? l->t + n_out : nullptr;
-        e = hipMemcpy(staged, W, wbytes, hipMemcpyDefault);
+        l->b = l->t + outs;
+        e = hipMemset(l->t, 0, outs * 8);
     }
+    if (e == hipSuccess)
+        e = hipMemcpy(staged, W, wbytes, hipMemcpyDefault);
     if (e == hipSuccess && b)
         e = hipMemcpy(l->b, b, (size_t)n_out * 4, hipMemcpyDefault);
     if (e == hipSuccess)

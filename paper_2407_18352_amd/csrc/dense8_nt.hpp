@@ -1,21 +1,24 @@
 // The product both operands of which lie along k: C[a][b] = sum_k A[a][k] B[b][k],
 // int8 codes with 32-bit sums or bf16 with fp32 sums.
 //
-// A block computes a tile of C.  The operands pass through LDS in slabs of 128
-// bytes of k (128 codes, 64 bf16), double-buffered: while the block works on a
-// slab, direct global-to-LDS loads bring the next.  A row of a slab is eight
-// 16-byte chunks, chunk c stored at c ^ swizzle(row), so that the 16 rows a
-// matrix instruction reads at one chunk fall on different banks; the direct
-// loads can't permute what they write, so each lane fetches the chunk that
-// belongs where its bytes land.  A holds the outputs and B the points: a lane
-// of the matrix instruction's result then has four consecutive outputs of one
-// point, which is what a row-major store wants.
+// A block computes a tile of C.  The operands pass through LDS in slabs of 64
+// bytes of k (64 codes, 32 bf16: one matrix instruction's depth), a ring of
+// kRing of them filled by direct global-to-LDS loads.  While the matrix cores
+// work on slab s from registers, a wave reads slab s + 1's fragments from LDS
+// and the loads of slabs up to s + kRing are under way; what a slab's loads
+// have to wait for in the memory system is covered by the slabs before it.
+// One barrier per slab publishes slab s + 1 (its loads have been waited for)
+// and frees slab s (its fragments are in registers).
+//
+// A row of a slab is four 16-byte chunks, chunk c stored at c ^ swizzle(row),
+// so that the 16 rows a matrix instruction reads at one chunk fall on different
+// banks; the direct loads can't permute what they write, so each lane fetches
+// the chunk that belongs where its bytes land.  A holds the outputs and B the
+// points: a lane of the matrix instruction's result then has four consecutive
+// outputs of one point, which is what a row-major store wants.
 //
 // The direct loads are inline assembly: seeing them, the compiler would make
-// every LDS read wait for all of them.  Their completion is waited for by
-// hand (all of them, once per slab) before the barrier that publishes a slab.
-// That one barrier per slab also keeps the next loads off the buffer until
-// every wave has its fragments of it in registers.
+// every LDS read wait for all of them.  Their completion is waited for by hand.
 #pragma once
 
 #include "dense8.hpp"
@@ -46,13 +49,19 @@ __device__ __forceinline__ void load_to_lds(const void *g, uint32_t lds) {
                  : "v"(g), "s"(lds)
                  : "memory");
 }
-// this wave's loads have arrived and its LDS reads are in registers
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0070); }
+// at most N of this wave's vector-memory loads are still under way, and its
+// LDS reads are in registers
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_sched_barrier(0);   // the matrix instructions written before it stay before it
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+}
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_offset(const void *p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
 }
-__device__ __forceinline__ int swizzle(int row) { return row & 7; }
+__device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
 
 // what a load beyond an operand's width reads
 __device__ __align__(16) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
@@ -67,14 +76,16 @@ struct Operand {
 // Blocks of WA x WB waves, each NA x NB tiles of 16 x 16.
 template <typename Mma, int WA, int WB, int NA, int NB>
 struct Tile {
-    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves;
+    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRing = 4;
     static constexpr int kA = 16 * NA * WA, kB = 16 * NB * WB;
-    static constexpr int kBuf = (kA + kB) * kSlabBytes;
-    static constexpr int kLoadsA = kA / (8 * kWaves), kLoadsB = kB / (8 * kWaves);
-    static_assert(kLoadsA * 8 * kWaves == kA && kLoadsB * 8 * kWaves == kB, "whole loads per wave");
+    static constexpr int kBuf = (kA + kB) * kSlabBytes, kLds = kRing * kBuf;
+    static constexpr int kLoadsA = kA / (16 * kWaves), kLoadsB = kB / (16 * kWaves), kLoads = kLoadsA + kLoadsB;
+    static_assert(kLoadsA * 16 * kWaves == kA && kLoadsB * 16 * kWaves == kB, "whole loads per wave");
     typedef typename Mma::Acc Acc;
+    struct Frags {
+        u32x4 a[NA], b[NB];
+    };
 
-    const char *pa[kLoadsA], *pb[kLoadsB];
     int wave, lane;
 
     // acc[a][b]: outputs a0 + 16 (WA-wave * NA + a) + 4 (lane / 16) + e of
@@ -87,39 +98,36 @@ struct Tile {
                                         Acc (&acc)[NA][NB]) {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int row8 = lane >> 3, chunk = (lane & 7) ^ swizzle(row8);   // swizzle(row) depends on row % 8 alone
+        const int row16 = lane >> 2, chunk = (lane & 3) ^ swizzle(row16);   // swizzle(row) depends on row % 16 alone
         int64_t oa[kLoadsA], ob[kLoadsB];
 #pragma unroll
         for (int i = 0; i < kLoadsA; ++i)
-            oa[i] = min(a0 + (i * kWaves + wave) * 8 + row8, A.rows - 1) * A.pitch + chunk * 16;
+            oa[i] = min(a0 + (i * kWaves + wave) * 16 + row16, A.rows - 1) * A.pitch + chunk * 16;
 #pragma unroll
         for (int i = 0; i < kLoadsB; ++i)
-            ob[i] = min(b0 + (i * kWaves + wave) * 8 + row8, B.rows - 1) * B.pitch + chunk * 16;
-        const uint32_t base = lds_offset(lds);
+            ob[i] = min(b0 + (i * kWaves + wave) * 16 + row16, B.rows - 1) * B.pitch + chunk * 16;
+        const uint32_t base = lds_offset(lds) + wave * 1024;
         const int wa = wave / WB, wb = wave % WB;
-        const int fr = (lane & 15) * kSlabBytes, sw = swizzle(lane & 7), grp = lane >> 4;
+        const int fr = (lane & 15) * kSlabBytes + ((lane >> 4) ^ swizzle(lane & 15)) * 16;
         const char *fa = lds + wa * NA * 16 * kSlabBytes + fr, *fb = lds + (kA + wb * NB * 16) * kSlabBytes + fr;
 
         const int slabs = (int)((max(A.width, B.width) + kSlabBytes - 1) / kSlabBytes);
-        int rank = terms - 1, term = 0, slab = 0;   // what is loaded next
+        const int total = slabs * (terms * (terms + 1) / 2);
+        int rank = terms - 1, term = 0, slab = 0, loaded = 0;   // what is loaded next
         const char *ga = A.base + term * A.plane, *gb = B.base + (rank - term) * B.plane;
-        auto load = [&](int buf) {
-            const uint32_t to = base + buf * kBuf + wave * 1024;
+        // one of the direct loads of the slab loaded next
+        auto load_part = [&](int i) {
+            const uint32_t to = base + (loaded & (kRing - 1)) * kBuf;
             const int64_t k = (int64_t)slab * kSlabBytes;
-#pragma unroll
-            for (int i = 0; i < kLoadsA; ++i) {
-                const void *g = ga + oa[i] + k;
-                if (EDGE && k + chunk * 16 >= A.width)
-                    g = zero_chunk;
-                load_to_lds(g, to + i * kWaves * 1024);
-            }
-#pragma unroll
-            for (int i = 0; i < kLoadsB; ++i) {
-                const void *g = gb + ob[i] + k;
-                if (EDGE && k + chunk * 16 >= B.width)
-                    g = zero_chunk;
-                load_to_lds(g, to + (kA * kSlabBytes) + i * kWaves * 1024);
-            }
+            const bool of_a = i < kLoadsA;
+            const int n = of_a ? i : i - kLoadsA;
+            const void *g = of_a ? ga + oa[of_a ? n : 0] + k : gb + ob[of_a ? 0 : n] + k;
+            if (EDGE && k + chunk * 16 >= (of_a ? A.width : B.width))
+                g = zero_chunk;
+            load_to_lds(g, to + (of_a ? 0 : kA * kSlabBytes) + n * kWaves * 1024);
+        };
+        auto load_done = [&]() {
+            ++loaded;
             if (++slab == slabs) {
                 slab = 0;
                 if (++term > rank) {
@@ -130,30 +138,86 @@ struct Tile {
                 gb = B.base + (rank - term) * B.plane;
             }
         };
-        const int total = slabs * (terms * (terms + 1) / 2);
-        load(0);
-        for (int s = 0; s < total; ++s) {
-            wait_loads();
+        auto load = [&]() {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                load_part(i);
+            load_done();
+        };
+        auto read_part = [&](int at, int i, Frags &f) {
+            if (i < NA)
+                f.a[i < NA ? i : 0] = *(const u32x4 *)(fa + at + i * 16 * kSlabBytes);
+            else
+                f.b[i < NA ? 0 : i - NA] = *(const u32x4 *)(fb + at + (i - NA) * 16 * kSlabBytes);
+        };
+        auto read = [&](int s, Frags &f) {
+#pragma unroll
+            for (int i = 0; i < NA + NB; ++i)
+                read_part((s & (kRing - 1)) * kBuf, i, f);
+        };
+        auto multiply = [&](const Frags &f, int i) {
+            acc[i % NA][i / NA] = Mma::mul(f.a[i % NA], f.b[i / NA], acc[i % NA][i / NA]);
+        };
+        // Slab s from `now`, slab s + 1 to `next`, slab s + kRing to where
+        // slab s was.  Slab s + 1's loads have kRing - 2 slabs behind them
+        // that may still be under way.  The LDS reads and loads go out evenly
+        // between the matrix instructions: issued in one block they would
+        // hold up the waves, all of which come from the barrier together.
+        auto step = [&](int s, const Frags &now, Frags &next) {
+            constexpr int kOps = NA + NB + kLoads, kMul = NA * NB;
+            wait_loads<(kRing - 2) * kLoads>();
             barrier();
-            const int cur = (s & 1) * kBuf;
-            if (s + 1 < total)
-                load((s + 1) & 1);
+            const int at = ((s + 1) & (kRing - 1)) * kBuf;
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                const int at = cur + (((ks * 4 + grp) ^ sw) * 16);
-                u32x4 a[NA], b[NB];
+            for (int i = 0, op = 0; i < kMul; ++i) {
+                multiply(now, i);
 #pragma unroll
-                for (int t = 0; t < NA; ++t)
-                    a[t] = *(const u32x4 *)(fa + at + t * 16 * kSlabBytes);
-#pragma unroll
-                for (int t = 0; t < NB; ++t)
-                    b[t] = *(const u32x4 *)(fb + at + t * 16 * kSlabBytes);
-#pragma unroll
-                for (int u = 0; u < NB; ++u)
-#pragma unroll
-                    for (int t = 0; t < NA; ++t)
-                        acc[t][u] = Mma::mul(a[t], b[u], acc[t][u]);
+                for (; op < kOps * (i + 1) / kMul; ++op) {
+                    if (op < NA + NB)
+                        read_part(at, op, next);
+                    else
+                        load_part(op - NA - NB);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
+            load_done();
+        };
+        // the same near the end, where no more loads follow
+        auto last_step = [&](int s, const Frags &now, Frags &next) {
+            wait_loads<0>();
+            if (s + 1 < total) {
+                barrier();
+                read(s + 1, next);
+            }
+#pragma unroll
+            for (int i = 0; i < NA * NB; ++i)
+                multiply(now, i);
+        };
+        Frags f0, f1;
+#pragma unroll
+        for (int i = 0; i < kRing; ++i)
+            if (i < total)
+                load();
+        if (total >= kRing)
+            wait_loads<(kRing - 1) * kLoads>();
+        else
+            wait_loads<0>();
+        barrier();
+        read(0, f0);
+        int s = 0;
+        for (; s + 1 + kRing < total; s += 2) {
+            step(s, f0, f1);
+            step(s + 1, f1, f0);
+        }
+        if (s + kRing < total) {
+            step(s, f0, f1);
+            ++s;
+            f0 = f1;
+        }
+        for (; s < total; s += 2) {
+            last_step(s, f0, f1);
+            if (s + 1 < total)
+                last_step(s + 1, f1, f0);
         }
     }
     // first output and point of this lane's acc[t][u]

@@ -202,8 +202,10 @@ void codes_as(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *c
 template <typename T>
 void codes_of(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *codes, int64_t pitch, float *scales,
               hipStream_t st) {
-    const int64_t chunks = pitch / kChunk;   // a multiple of 16
-    if (chunks <= 16)
+    const int64_t chunks = pitch / kChunk;   // a multiple of 8
+    if (chunks <= 8)
+        codes_as<T, 8, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+    else if (chunks <= 16)
         codes_as<T, 16, 1>(x, ldx, rows, width, codes, pitch, scales, st);
     else if (chunks <= 32)
         codes_as<T, 32, 1>(x, ldx, rows, width, codes, pitch, scales, st);

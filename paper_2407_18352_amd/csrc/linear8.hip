@@ -9,39 +9,37 @@ namespace {
 template <typename Y, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, uint32_t out_tiles, uint32_t point_tiles) {
     typedef nt::Tile<nt::I8, WA, WB, NA, NB> T;
-    __shared__ __align__(1024) char lds[2 * T::kBuf];
+    __shared__ __align__(1024) char lds[T::kLds];
     const nt::TileAt at = nt::tile_at(blockIdx.x, gridDim.x, out_tiles, point_tiles);
     const int64_t a0 = at.out * T::kA, b0 = at.point * T::kB;
     i32x4 acc[NA][NB] = {};
     T t;
     t.template run<false>({(const char *)p.w, p.n_out, p.pitch, p.pitch, 0}, {(const char *)p.q, p.rows, p.pitch, p.pitch, 0},
                           a0, b0, 1, lds, acc);
-    // four outputs of a point at once where every row keeps their alignment
+    // four outputs of a point at once where every row keeps their alignment;
+    // scales and biases are there in whole fours
     const bool wide = ((uintptr_t)p.y & (4 * sizeof(Y) - 1)) == 0 && (p.ldy & 3) == 0;
+    const int last = (p.n_out - 1) & ~3;
+    float s[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        s[b] = p.s[min(b0 + t.point_of(b), p.rows - 1)];
 #pragma unroll
     for (int a = 0; a < NA; ++a) {
         const int n = (int)a0 + t.out_of(a);
-        float sc[4], bias[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int j = min(n + e, p.n_out - 1);
-            sc[e] = p.t[j];
-            bias[e] = p.b ? p.b[j] : 0.f;
-        }
+        const f32x4 sc = *(const f32x4 *)(p.t + min(n, last)), bias = *(const f32x4 *)(p.b + min(n, last));
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const int64_t r = b0 + t.point_of(b);
-            if (r >= p.rows || n >= p.n_out)
-                continue;
-            const float s = p.s[r];
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[e] = (float)acc[a][b][e] * s * sc[e] + bias[e];
+                v[e] = (float)acc[a][b][e] * s[b] * sc[e] + bias[e];
                 if (p.relu)
                     v[e] = relu_keep_nan(v[e]);
             }
-            store_four((Y *)p.y + r * p.ldy + n, v, p.n_out - n, wide && n + 4 <= p.n_out);
+            if (r < p.rows && n < p.n_out)
+                store_four((Y *)p.y + r * p.ldy + n, v, p.n_out - n, wide && n + 4 <= p.n_out);
         }
     }
 }
