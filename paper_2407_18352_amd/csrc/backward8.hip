@@ -32,20 +32,22 @@ __global__ void __launch_bounds__(kThreads) planes_kernel(const T *__restrict__ 
     }
 }
 
-// planes [planes][n_in][pitch] of W's transpose, zero beyond n_out
+// planes of W's transpose [n_in][n_out], blocked, zero beyond n_out
 template <typename T>
 __global__ void __launch_bounds__(kThreads) transpose_kernel(const T *__restrict__ W, int64_t ldw, int32_t n_out,
-                                                             int32_t n_in, uint16_t *__restrict__ out, int64_t pitch) {
+                                                             int32_t n_in, char *__restrict__ out, int32_t slabs) {
+    const int64_t plane = blocked_bytes(n_in, slabs), pitch = (int64_t)slabs * (kSlabBytes / 2);
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n_in * pitch; i += (int64_t)gridDim.x * kThreads) {
         const int64_t k = i / pitch, j = i - k * pitch;
+        char *at = out + blocked_offset(k, 2 * j, slabs);
         if constexpr (sizeof(T) == 4) {
             uint16_t t[3] = {0, 0, 0};
             if (j < n_out)
                 split3(W[j * ldw + k], t);
             for (int q = 0; q < 3; ++q)
-                out[q * n_in * pitch + i] = t[q];
+                *(uint16_t *)(at + q * plane) = t[q];
         } else {
-            out[i] = j < n_out ? W[j * ldw + k] : (uint16_t)0;
+            *(uint16_t *)at = j < n_out ? W[j * ldw + k] : (uint16_t)0;
         }
     }
 }
@@ -53,7 +55,7 @@ __global__ void __launch_bounds__(kThreads) transpose_kernel(const T *__restrict
 // ---- dx -------------------------------------------------------------------------
 
 struct DxArgs {
-    nt::Operand wt, g;          // planes of W's transpose [n_in][pitch] and of dy
+    nt::Operand wt, g;          // W's transpose [n_in][n_out], blocked, and dy, in rows
     const uint8_t *codes;       // NULL: everything is let through
     void *dx;
     int64_t ld_codes, lddx;
@@ -61,7 +63,7 @@ struct DxArgs {
     uint32_t in_tiles, point_tiles;
 };
 
-template <typename X, bool EDGE, int WA, int WB, int NA, int NB>
+template <typename X, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB) dx_kernel(DxArgs p) {
     typedef nt::Tile<nt::Bf16, WA, WB, NA, NB> T;
     __shared__ __align__(1024) char lds[T::kLds];
@@ -69,7 +71,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dx_kernel(DxArgs p) {
     const int64_t a0 = at.out * T::kA, b0 = at.point * T::kB;
     f32x4 acc[NA][NB] = {};
     T t;
-    t.template run<EDGE>(p.wt, p.g, a0, b0, p.terms, lds, acc);
+    t.template run<false>(p.wt, p.g, a0, b0, p.terms, lds, acc);
     const bool wide = ((uintptr_t)p.dx & (4 * sizeof(X) - 1)) == 0 && (p.lddx & 3) == 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -299,7 +301,7 @@ int dw_tile(int32_t n_out, int32_t n_in) {
     return n_out <= 64 || n_in <= 64 ? 64 : tiles_of(n_out, n_in, 256) < 16 ? 128 : 256;
 }
 
-template <typename X, bool EDGE, int WA, int WB, int NA, int NB>
+template <typename X, int WA, int WB, int NA, int NB>
 void launch_dx_tile(const DxArgs &a, hipStream_t st) {
     typedef nt::Tile<nt::Bf16, WA, WB, NA, NB> T;
     DxArgs d = a;
@@ -311,18 +313,18 @@ void launch_dx_tile(const DxArgs &a, hipStream_t st) {
         d.codes = a.codes ? a.codes + r * a.ld_codes : nullptr;
         d.dx = (X *)a.dx + r * a.lddx;
         d.point_tiles = (uint32_t)((d.g.rows + T::kB - 1) / T::kB);
-        dx_kernel<X, EDGE, WA, WB, NA, NB><<<dim3(d.in_tiles * d.point_tiles), T::kThreads, 0, st>>>(d);
+        dx_kernel<X, WA, WB, NA, NB><<<dim3(d.in_tiles * d.point_tiles), T::kThreads, 0, st>>>(d);
     }
 }
 
-template <typename X, bool EDGE>
+template <typename X>
 void launch_dx(const DxArgs &d, hipStream_t st) {
-    if (tiles_of(d.g.rows, d.n_in, 256) >= 512 && d.wt.pitch >= 2048)
-        launch_dx_tile<X, EDGE, 4, 2, 4, 8>(d, st);
+    if (tiles_of(d.g.rows, d.n_in, 256) >= 512 && d.wt.width >= 2048)
+        launch_dx_tile<X, 4, 2, 4, 8>(d, st);
     else if (tiles_of(d.g.rows, d.n_in, 128) >= 256 && d.n_in > 64)
-        launch_dx_tile<X, EDGE, 2, 2, 4, 4>(d, st);
+        launch_dx_tile<X, 2, 2, 4, 4>(d, st);
     else
-        launch_dx_tile<X, EDGE, 2, 2, 2, 2>(d, st);
+        launch_dx_tile<X, 2, 2, 2, 2>(d, st);
 }
 
 template <bool RELU>
@@ -342,7 +344,8 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
     Backward8Plan p{};
     p.planes = dtype == HPACML_F32 ? 3 : 1;
     p.direct = dtype == HPACML_BF16 && ((uintptr_t)dy & 15) == 0 && lddy % 8 == 0 && n_out % 8 == 0;
-    p.pitch = slab_pitch16(n_out);
+    p.slabs = (int32_t)slabs_of(2 * n_out);
+    p.pitch = (int64_t)p.slabs * (kSlabBytes / 2);
     p.tile = dw_tile(n_out, c.width);
     p.splits = 1;
     if (want_dw) {
@@ -362,7 +365,7 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
         at += whole((size_t)p.planes * c.rows * p.pitch * 2);
     p.off_wt = at;
     if (want_dx)
-        at += whole((size_t)p.planes * c.width * p.pitch * 2);
+        at += whole((size_t)p.planes * blocked_bytes(c.width, p.slabs));
     p.off_dw = at;
     if (want_dw)
         at += whole((size_t)p.splits * n_out * c.width * 4);
@@ -376,7 +379,8 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
 hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipStream_t st) {
     const int64_t rows = a.c.rows;
     const bool f32 = a.dtype == HPACML_F32;
-    uint16_t *planes = (uint16_t *)(a.scratch + p.off_dy), *wt = (uint16_t *)(a.scratch + p.off_wt);
+    uint16_t *planes = (uint16_t *)(a.scratch + p.off_dy);
+    char *wt = a.scratch + p.off_wt;
     nt::Operand g{(const char *)planes, rows, p.pitch * 2, p.pitch * 2, rows * p.pitch * 2};
     if (p.direct)
         g = {(const char *)a.dy, rows, a.lddy * 2, (int64_t)a.n_out * 2, 0};
@@ -386,11 +390,11 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
         planes_kernel<uint16_t><<<blocks_for(rows * p.pitch), kThreads, 0, st>>>((const uint16_t *)a.dy, a.lddy, rows, a.n_out, planes, p.pitch);
     if (a.dx && rows > 0) {
         if (f32)
-            transpose_kernel<float><<<blocks_for(a.c.width * p.pitch), kThreads, 0, st>>>((const float *)a.W, a.ldw, a.n_out, a.c.width, wt, p.pitch);
+            transpose_kernel<float><<<blocks_for(a.c.width * p.pitch), kThreads, 0, st>>>((const float *)a.W, a.ldw, a.n_out, a.c.width, wt, p.slabs);
         else
-            transpose_kernel<uint16_t><<<blocks_for(a.c.width * p.pitch), kThreads, 0, st>>>((const uint16_t *)a.W, a.ldw, a.n_out, a.c.width, wt, p.pitch);
+            transpose_kernel<uint16_t><<<blocks_for(a.c.width * p.pitch), kThreads, 0, st>>>((const uint16_t *)a.W, a.ldw, a.n_out, a.c.width, wt, p.slabs);
         DxArgs d{};
-        d.wt = {(const char *)wt, a.c.width, p.pitch * 2, p.pitch * 2, a.c.width * p.pitch * 2};
+        d.wt = {wt, a.c.width, (int64_t)p.slabs * 1024, (int64_t)p.slabs * kSlabBytes, blocked_bytes(a.c.width, p.slabs)};
         d.g = g;
         d.codes = a.c.act == HPACML_ACT_RELU ? (const uint8_t *)a.c.codes : nullptr;
         d.dx = a.dx;
@@ -399,11 +403,9 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
         d.n_in = a.c.width;
         d.terms = p.planes;
         if (f32)
-            launch_dx<float, false>(d, st);
-        else if (g.width % kSlabBytes == 0)
-            launch_dx<uint16_t, false>(d, st);
+            launch_dx<float>(d, st);
         else
-            launch_dx<uint16_t, true>(d, st);
+            launch_dx<uint16_t>(d, st);
     }
     if (a.dw || a.db) {
         DwArgs d{};

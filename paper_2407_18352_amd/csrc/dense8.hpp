@@ -8,27 +8,33 @@
 
 namespace hpacml {
 
-// Row pitch of int8 codes and of bf16 planes laid out for the products: whole
-// slabs of 64 bytes, so that a product's loop over k has no remainder.
+// Operands laid out for the products: slabs of 64 bytes of k (64 codes, 32
+// bf16), 16 rows of a slab after one another (1 KB), the slabs of 16 rows after
+// one another.  Of a row's four 16-byte chunks, chunk c is at c ^ chunk_turn(row).
 constexpr int kSlabBytes = 64;
-constexpr int64_t slab_pitch8(int64_t k) { return (k + 63) / 64 * 64; }
-constexpr int64_t slab_pitch16(int64_t k) { return (k + 31) / 32 * 32; }
+constexpr int64_t slabs_of(int64_t bytes) { return (bytes + kSlabBytes - 1) / kSlabBytes; }
+constexpr int64_t blocked_bytes(int64_t rows, int64_t slabs) { return (rows + 15) / 16 * slabs * 1024; }
+__host__ __device__ constexpr int chunk_turn(int row) { return (row >> 2) & 3; }
+// of byte k of a row
+__host__ __device__ constexpr int64_t blocked_offset(int64_t row, int64_t k, int64_t slabs) {
+    return ((row >> 4) * slabs + (k >> 6)) * 1024 + (row & 15) * kSlabBytes + ((((int)(k >> 4) & 3) ^ chunk_turn((int)row)) * 16) + (k & 15);
+}
 
-// codes [rows][pitch] and scales [rows] of x [rows][width]; columns from
-// width to pitch are written as 0.
+// codes, blocked, and scales [rows] of x [rows][width]; columns from width to
+// the end of the last slab are written as 0.
 hipError_t launch_codes_by_row(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t width, int8_t *codes,
-                               int64_t pitch, float *scales, hipStream_t stream);
+                               float *scales, hipStream_t stream);
 
 // y = act(s_i t_j sum_k q_ik w_jk + b_j)
 struct Linear8Args {
-    const int8_t *q;      // [rows][pitch]
+    const int8_t *q;      // codes of the rows, blocked
     const float *s;       // [rows]
-    const int8_t *w;      // [n_out][pitch]
+    const int8_t *w;      // codes of the weights, blocked
     const float *t;       // [n_out], to a multiple of four
     const float *b;       // the same; zeros without a bias
     void *y;
-    int64_t rows, pitch, ldy;
-    int32_t n_out, relu;
+    int64_t rows, ldy;
+    int32_t slabs, n_out, relu;
 };
 hipError_t launch_linear8(const Linear8Args &a, int32_t y_dtype, hipStream_t stream);
 
@@ -41,7 +47,8 @@ hipError_t launch_checkpoint_load(const hpacml8_checkpoint &c, void *a, int32_t 
 struct Backward8Plan {
     int32_t planes;       // bf16 terms of an operand: 1 (bf16) or 3 (fp32)
     bool direct;          // dy is read in place
-    int64_t pitch;        // of dy's planes and W's transposed planes (elements)
+    int32_t slabs;        // of dy and of W's transpose along the outputs
+    int64_t pitch;        // of dy's planes (elements)
     int32_t tile;         // of dw
     int32_t splits;       // parts of the rows that sum into dw apart
     int64_t rows_per_split;

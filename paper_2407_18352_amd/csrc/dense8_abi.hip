@@ -11,8 +11,8 @@ using namespace hpacml;
 struct hpacml8_linear_s {
     int device = 0;
     int32_t n_in = 0, n_out = 0;
-    int64_t pitch = 0;
-    char *buf = nullptr;      // codes [n_out][pitch], then scales and biases, each to a multiple of four
+    int32_t slabs = 0;
+    char *buf = nullptr;      // codes, blocked, then scales and biases, each to a multiple of four
     int8_t *w = nullptr;
     float *t = nullptr, *b = nullptr;
 };
@@ -117,7 +117,7 @@ void add_checkpoint(Operands *o, const hpacml8_checkpoint &c, bool written) {
 }
 
 // scratch of hpacml8_linear_run: codes, then scales
-size_t linear_codes_bytes(const hpacml8_linear *l, int64_t rows) { return (size_t)(rows * l->pitch + 255) / 256 * 256; }
+size_t linear_codes_bytes(const hpacml8_linear *l, int64_t rows) { return (size_t)blocked_bytes(rows, l->slabs); }
 size_t linear_scratch_bytes(const hpacml8_linear *l, int64_t rows) { return linear_codes_bytes(l, rows) + (size_t)rows * 4; }
 
 }  // namespace
@@ -137,9 +137,9 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
         return HPACML_E_NOMEM;
     l->n_in = n_in;
     l->n_out = n_out;
-    l->pitch = slab_pitch8(n_in);
+    l->slabs = (int32_t)slabs_of(n_in);
     float *staged = nullptr;
-    const size_t codes = (size_t)n_out * l->pitch, wbytes = (size_t)n_out * n_in * 4, outs = ((size_t)n_out + 3) / 4 * 4;
+    const size_t codes = (size_t)blocked_bytes(n_out, l->slabs), wbytes = (size_t)n_out * n_in * 4, outs = ((size_t)n_out + 3) / 4 * 4;
     hipError_t e = hipGetDevice(&l->device);
     if (e == hipSuccess)
         e = hipDeviceSynchronize();
@@ -158,7 +158,7 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
     if (e == hipSuccess && b)
         e = hipMemcpy(l->b, b, (size_t)n_out * 4, hipMemcpyDefault);
     if (e == hipSuccess)
-        e = launch_codes_by_row(staged, HPACML_F32, n_in, n_out, n_in, l->w, l->pitch, l->t, nullptr);
+        e = launch_codes_by_row(staged, HPACML_F32, n_in, n_out, n_in, l->w, l->t, nullptr);
     if (e == hipSuccess)
         e = hipDeviceSynchronize();
     if (staged)
@@ -213,9 +213,9 @@ hpacml_status hpacml8_linear_run(const hpacml8_linear *l, const void *x, int32_t
     hipStream_t st = (hipStream_t)stream;
     int8_t *q = (int8_t *)scratch;
     float *s = (float *)((char *)scratch + linear_codes_bytes(l, n_rows));
-    hipError_t e = launch_codes_by_row(x, x_dtype, ldx, n_rows, l->n_in, q, l->pitch, s, st);
+    hipError_t e = launch_codes_by_row(x, x_dtype, ldx, n_rows, l->n_in, q, s, st);
     if (e == hipSuccess)
-        e = launch_linear8({q, s, l->w, l->t, l->b, y, n_rows, l->pitch, ldy, l->n_out, act == HPACML_ACT_RELU}, y_dtype, st);
+        e = launch_linear8({q, s, l->w, l->t, l->b, y, n_rows, ldy, l->slabs, l->n_out, act == HPACML_ACT_RELU}, y_dtype, st);
     return status_of(e);
 }
 

@@ -10,10 +10,13 @@
 // One barrier per slab publishes slab s + 1 (its loads have been waited for)
 // and frees slab s (its fragments are in registers).
 //
-// A row of a slab is four 16-byte chunks, chunk c stored at c ^ swizzle(row),
+// A row of a slab is four 16-byte chunks, chunk c stored at c ^ chunk_turn(row),
 // so that the 16 rows a matrix instruction reads at one chunk fall on different
-// banks; the direct loads can't permute what they write, so each lane fetches
-// the chunk that belongs where its bytes land.  A holds the outputs and B the
+// banks.  An operand that this library lays out itself lies in memory as in LDS:
+// a direct load then reads 1 KB in one piece, whatever k is, where rows of a
+// power of two would meet in the same few channels of the L2.  From an operand
+// in rows each lane fetches the chunk that belongs where its bytes land (the
+// direct loads can't permute what they write).  A holds the outputs and B the
 // points: a lane of the matrix instruction's result then has four consecutive
 // outputs of one point, which is what a row-major store wants.
 //
@@ -61,13 +64,15 @@ __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory
 __device__ __forceinline__ uint32_t lds_offset(const void *p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
 }
-__device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
 
 // what a load beyond an operand's width reads
 __device__ __align__(16) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
 
-// One operand: rows `pitch` bytes apart, of which `width` bytes count (the
-// rest of the slabs is zero), in `terms` planes `plane` bytes apart.
+// One operand, in `terms` planes `plane` bytes apart.  BLOCKED: as the LDS
+// image has it, 16 rows x 64 bytes after one another (1 KB, chunks swizzled),
+// `pitch` bytes per 16 rows; what pads the last rows and slab is there.
+// Otherwise rows `pitch` bytes apart, of which `width` bytes count (the rest
+// of the last slab reads as zero).
 struct Operand {
     const char *base;
     int64_t rows, pitch, width, plane;
@@ -91,38 +96,38 @@ struct Tile {
     // acc[a][b]: outputs a0 + 16 (WA-wave * NA + a) + 4 (lane / 16) + e of
     // point b0 + 16 (WB-wave * NB + b) + lane % 16
     // terms: 1, or 3 planes of each operand of which the products of ranks
-    // that sum to at most 2 are taken, the smallest first.  EDGE: the
-    // operands' widths may end inside a slab.
-    template <bool EDGE>
+    // that sum to at most 2 are taken, the smallest first.  A is BLOCKED.
+    template <bool BLOCKED_B>
     __device__ __forceinline__ void run(const Operand &A, const Operand &B, int64_t a0, int64_t b0, int terms, char *lds,
                                         Acc (&acc)[NA][NB]) {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int row16 = lane >> 2, chunk = (lane & 3) ^ swizzle(row16);   // swizzle(row) depends on row % 16 alone
+        const int row16 = lane >> 2, chunk = (lane & 3) ^ chunk_turn(row16);   // chunk_turn(row) depends on row % 16 alone
         int64_t oa[kLoadsA], ob[kLoadsB];
 #pragma unroll
         for (int i = 0; i < kLoadsA; ++i)
-            oa[i] = min(a0 + (i * kWaves + wave) * 16 + row16, A.rows - 1) * A.pitch + chunk * 16;
+            oa[i] = min(a0 / 16 + i * kWaves + wave, (A.rows - 1) / 16) * A.pitch + lane * 16;
 #pragma unroll
         for (int i = 0; i < kLoadsB; ++i)
-            ob[i] = min(b0 + (i * kWaves + wave) * 16 + row16, B.rows - 1) * B.pitch + chunk * 16;
+            ob[i] = BLOCKED_B ? min(b0 / 16 + i * kWaves + wave, (B.rows - 1) / 16) * B.pitch + lane * 16
+                              : min(b0 + (i * kWaves + wave) * 16 + row16, B.rows - 1) * B.pitch + chunk * 16;
         const uint32_t base = lds_offset(lds) + wave * 1024;
         const int wa = wave / WB, wb = wave % WB;
-        const int fr = (lane & 15) * kSlabBytes + ((lane >> 4) ^ swizzle(lane & 15)) * 16;
+        const int fr = (lane & 15) * kSlabBytes + ((lane >> 4) ^ chunk_turn(lane & 15)) * 16;
         const char *fa = lds + wa * NA * 16 * kSlabBytes + fr, *fb = lds + (kA + wb * NB * 16) * kSlabBytes + fr;
 
-        const int slabs = (int)((max(A.width, B.width) + kSlabBytes - 1) / kSlabBytes);
+        const int slabs = (int)((A.width + kSlabBytes - 1) / kSlabBytes);
         const int total = slabs * (terms * (terms + 1) / 2);
         int rank = terms - 1, term = 0, slab = 0, loaded = 0;   // what is loaded next
         const char *ga = A.base + term * A.plane, *gb = B.base + (rank - term) * B.plane;
         // one of the direct loads of the slab loaded next
         auto load_part = [&](int i) {
             const uint32_t to = base + (loaded & (kRing - 1)) * kBuf;
-            const int64_t k = (int64_t)slab * kSlabBytes;
             const bool of_a = i < kLoadsA;
             const int n = of_a ? i : i - kLoadsA;
-            const void *g = of_a ? ga + oa[of_a ? n : 0] + k : gb + ob[of_a ? 0 : n] + k;
-            if (EDGE && k + chunk * 16 >= (of_a ? A.width : B.width))
+            const void *g = of_a ? ga + oa[of_a ? n : 0] + (int64_t)slab * 1024
+                                 : gb + ob[of_a ? 0 : n] + (int64_t)slab * (BLOCKED_B ? 1024 : kSlabBytes);
+            if (!BLOCKED_B && !of_a && slab * kSlabBytes + chunk * 16 >= B.width)
                 g = zero_chunk;
             load_to_lds(g, to + (of_a ? 0 : kA * kSlabBytes) + n * kWaves * 1024);
         };

@@ -94,10 +94,10 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 // caches) for their codes.
 template <typename T, int LANES, int HELD>
 __global__ void __launch_bounds__(kThreads) codes_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows,
-                                                         int32_t width, int8_t *__restrict__ codes, int64_t pitch,
+                                                         int32_t width, int8_t *__restrict__ codes, int32_t slabs,
                                                          float *__restrict__ scales) {
     constexpr int kRows = kThreads / LANES;
-    const int lane = threadIdx.x % LANES, chunks = (int)(pitch / kChunk);
+    const int lane = threadIdx.x % LANES, chunks = slabs * (kSlabBytes / kChunk);
     for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; r < rows; r += (int64_t)gridDim.x * kRows) {
         const T *row = x + r * ldx;
         float v[HELD][kChunk];
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kThreads) codes_kernel(const T *__restrict__ x
                     for (int e = 0; e < kChunk; ++e)
                         q[e / 4] |= ((uint32_t)(int32_t)rintf(v[h][e] * inv) & 0xFFu) << (8 * (e % 4));
                 }
-                *(uint2 *)(codes + r * pitch + at * kChunk) = uint2{q[0], q[1]};
+                *(uint2 *)(codes + blocked_offset(r, at * kChunk, slabs)) = uint2{q[0], q[1]};
             }
         }
     }
@@ -193,30 +193,29 @@ dim3 blocks_for(int64_t rows, int64_t per_block) {
 }
 
 template <typename T, int LANES, int HELD>
-void codes_as(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *codes, int64_t pitch, float *scales,
+void codes_as(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *codes, int32_t slabs, float *scales,
               hipStream_t stream) {
     codes_kernel<T, LANES, HELD><<<blocks_for(rows, kThreads / LANES), kThreads, 0, stream>>>((const T *)x, ldx, rows,
-                                                                                             width, codes, pitch, scales);
+                                                                                             width, codes, slabs, scales);
 }
 
 template <typename T>
-void codes_of(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *codes, int64_t pitch, float *scales,
-              hipStream_t st) {
-    const int64_t chunks = pitch / kChunk;   // a multiple of 8
+void codes_of(const void *x, int64_t ldx, int64_t rows, int32_t width, int8_t *codes, float *scales, hipStream_t st) {
+    const int32_t slabs = (int32_t)slabs_of(width), chunks = slabs * (kSlabBytes / kChunk);
     if (chunks <= 8)
-        codes_as<T, 8, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+        codes_as<T, 8, 1>(x, ldx, rows, width, codes, slabs, scales, st);
     else if (chunks <= 16)
-        codes_as<T, 16, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+        codes_as<T, 16, 1>(x, ldx, rows, width, codes, slabs, scales, st);
     else if (chunks <= 32)
-        codes_as<T, 32, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+        codes_as<T, 32, 1>(x, ldx, rows, width, codes, slabs, scales, st);
     else if (chunks <= 64)
-        codes_as<T, 64, 1>(x, ldx, rows, width, codes, pitch, scales, st);
+        codes_as<T, 64, 1>(x, ldx, rows, width, codes, slabs, scales, st);
     else if (chunks <= 128)
-        codes_as<T, 64, 2>(x, ldx, rows, width, codes, pitch, scales, st);
+        codes_as<T, 64, 2>(x, ldx, rows, width, codes, slabs, scales, st);
     else if (chunks <= 256)
-        codes_as<T, 64, 4>(x, ldx, rows, width, codes, pitch, scales, st);
+        codes_as<T, 64, 4>(x, ldx, rows, width, codes, slabs, scales, st);
     else
-        codes_as<T, 64, 8>(x, ldx, rows, width, codes, pitch, scales, st);
+        codes_as<T, 64, 8>(x, ldx, rows, width, codes, slabs, scales, st);
 }
 
 // log2 of the chunks a row of a block of threads covers: 4 .. 256
@@ -249,11 +248,11 @@ void load_as(const hpacml8_checkpoint &c, void *a, int64_t lda, hipStream_t stre
 }  // namespace
 
 hipError_t launch_codes_by_row(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t width, int8_t *codes,
-                               int64_t pitch, float *scales, hipStream_t stream) {
+                               float *scales, hipStream_t stream) {
     if (dtype == HPACML_F32)
-        codes_of<float>(x, ldx, rows, width, codes, pitch, scales, stream);
+        codes_of<float>(x, ldx, rows, width, codes, scales, stream);
     else
-        codes_of<uint16_t>(x, ldx, rows, width, codes, pitch, scales, stream);
+        codes_of<uint16_t>(x, ldx, rows, width, codes, scales, stream);
     return hipGetLastError();
 }
 

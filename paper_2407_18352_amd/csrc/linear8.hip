@@ -14,8 +14,9 @@ __global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, ui
     const int64_t a0 = at.out * T::kA, b0 = at.point * T::kB;
     i32x4 acc[NA][NB] = {};
     T t;
-    t.template run<false>({(const char *)p.w, p.n_out, p.pitch, p.pitch, 0}, {(const char *)p.q, p.rows, p.pitch, p.pitch, 0},
-                          a0, b0, 1, lds, acc);
+    const int64_t pitch = (int64_t)p.slabs * 1024, width = (int64_t)p.slabs * kSlabBytes;
+    t.template run<true>({(const char *)p.w, p.n_out, pitch, width, 0}, {(const char *)p.q, p.rows, pitch, width, 0}, a0, b0, 1,
+                         lds, acc);
     // four outputs of a point at once where every row keeps their alignment;
     // scales and biases are there in whole fours
     const bool wide = ((uintptr_t)p.y & (4 * sizeof(Y) - 1)) == 0 && (p.ldy & 3) == 0;
@@ -52,7 +53,7 @@ void launch_tile(const Linear8Args &a, hipStream_t stream) {
     for (int64_t r = 0; r < a.rows; r += step) {
         Linear8Args p = a;
         p.rows = a.rows - r < step ? a.rows - r : step;
-        p.q += r * a.pitch;
+        p.q += blocked_bytes(r, a.slabs);
         p.s += r;
         p.y = (Y *)a.y + r * a.ldy;
         const uint32_t point_tiles = (uint32_t)((p.rows + T::kB - 1) / T::kB);
@@ -64,7 +65,7 @@ template <typename Y>
 void launch_as(const Linear8Args &a, hipStream_t stream) {
     const int64_t big = ((a.n_out + 255) / 256) * ((a.rows + 255) / 256);
     const int64_t mid = ((a.n_out + 127) / 128) * ((a.rows + 127) / 128);
-    if (big >= 512 && a.pitch >= 2048)
+    if (big >= 512 && a.slabs >= 32)
         launch_tile<Y, 4, 2, 4, 8>(a, stream);
     else if (mid >= 256 && a.n_out > 64)
         launch_tile<Y, 2, 2, 4, 4>(a, stream);
