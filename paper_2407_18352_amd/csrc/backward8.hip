@@ -72,26 +72,31 @@ __global__ void __launch_bounds__(64 * WA * WB) dx_kernel(DxArgs p) {
     f32x4 acc[NA][NB] = {};
     T t;
     t.template run<false>(p.wt, p.g, a0, b0, p.terms, lds, acc);
-    const bool wide = ((uintptr_t)p.dx & (4 * sizeof(X) - 1)) == 0 && (p.lddx & 3) == 0;
+    t.store((X *)p.dx, p.lddx, a0, p.n_in, b0, p.g.rows, lds,
+            [&](int a, int64_t, int b, int64_t, float (&v)[4]) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int64_t r = b0 + t.point_of(b);
-        if (r >= p.g.rows)
-            continue;
+                for (int e = 0; e < 4; ++e)
+                    v[e] = acc[a][b][e];
+            },
+            [&](int64_t r, int64_t k, u32x4 &u) {
+                if (!p.codes)
+                    return;
+                // rows of codes are whole blocks of channels: all of these exist
+                const uint8_t *c = p.codes + r * p.ld_codes + k;
+                if constexpr (sizeof(X) == 2) {
+                    const uint2 q = *(const uint2 *)c;
 #pragma unroll
-        for (int a = 0; a < NA; ++a) {
-            const int k = (int)a0 + t.out_of(a);
-            if (k >= p.n_in)
-                continue;
-            // a pitch of codes covers whole blocks of channels: four codes exist
-            const uint32_t c = p.codes ? *(const uint32_t *)(p.codes + r * p.ld_codes + k) : 0x01010101u;
-            float v[4];
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t two = (e < 2 ? q.x : q.y) >> (16 * (e & 1));
+                        u[e] &= (two & 0xFFu ? 0x0000FFFFu : 0u) | (two & 0xFF00u ? 0xFFFF0000u : 0u);
+                    }
+                } else {
+                    const uint32_t q = *(const uint32_t *)c;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = (c >> (8 * e)) & 0xFFu ? acc[a][b][e] : 0.f;
-            store_four((X *)p.dx + r * p.lddx + k, v, p.n_in - k, wide && k + 4 <= p.n_in);
-        }
-    }
+                    for (int e = 0; e < 4; ++e)
+                        u[e] = (q >> (8 * e)) & 0xFFu ? u[e] : 0u;
+                }
+            });
 }
 
 // ---- dw and db ------------------------------------------------------------------

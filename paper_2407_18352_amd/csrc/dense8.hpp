@@ -97,27 +97,14 @@ __device__ __forceinline__ float load_value(const uint16_t *p) { return bf16_bit
 __device__ __forceinline__ void store_value(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_value(uint16_t *p, float v) { *p = bf16_bits(v); }
 
-// Up to n of four values at p: in one store where `whole` says that all four
-// exist and p is aligned to them.
-__device__ __forceinline__ void store_four(float *p, const float (&v)[4], int n, bool whole) {
-    if (whole) {
-        *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < n)
-                p[e] = v[e];
-    }
-}
-__device__ __forceinline__ void store_four(uint16_t *p, const float (&v)[4], int n, bool whole) {
-    if (whole) {
-        *(uint2 *)p = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < n)
-                p[e] = bf16_bits(v[e]);
-    }
+// 16 bytes at any element's address
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+
+// four values at p, aligned to four
+__device__ __forceinline__ void store_four(float *p, const float (&v)[4]) { *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void store_four(uint16_t *p, const float (&v)[4]) {
+    *(uint2 *)p = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
 // max(x, 0) that keeps a NaN

@@ -68,6 +68,18 @@ __device__ __forceinline__ uint32_t lds_offset(const void *p) {
 // what a load beyond an operand's width reads
 __device__ __align__(16) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
 
+// element e of 16 bytes
+template <typename Y>
+__device__ __forceinline__ Y element(const u32x4 &u, int e) {
+    if constexpr (sizeof(Y) == 4) {
+        const uint32_t w = u[e];
+        return __builtin_bit_cast(Y, w);
+    } else {
+        const uint32_t w = u[e / 2];
+        return (Y)(w >> (16 * (e & 1)));
+    }
+}
+
 // One operand, in `terms` planes `plane` bytes apart.  BLOCKED: as the LDS
 // image has it, 16 rows x 64 bytes after one another (1 KB, chunks swizzled),
 // `pitch` bytes per 16 rows; what pads the last rows and slab is there.
@@ -79,9 +91,9 @@ struct Operand {
 };
 
 // Blocks of WA x WB waves, each NA x NB tiles of 16 x 16.
-template <typename Mma, int WA, int WB, int NA, int NB>
+template <typename Mma, int WA, int WB, int NA, int NB, int RING = 4>
 struct Tile {
-    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRing = 4;
+    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRing = RING;
     static constexpr int kA = 16 * NA * WA, kB = 16 * NB * WB;
     static constexpr int kBuf = (kA + kB) * kSlabBytes, kLds = kRing * kBuf;
     static constexpr int kLoadsA = kA / (16 * kWaves), kLoadsB = kB / (16 * kWaves), kLoads = kLoadsA + kLoadsB;
@@ -118,11 +130,11 @@ struct Tile {
 
         const int slabs = (int)((A.width + kSlabBytes - 1) / kSlabBytes);
         const int total = slabs * (terms * (terms + 1) / 2);
-        int rank = terms - 1, term = 0, slab = 0, loaded = 0;   // what is loaded next
+        int rank = terms - 1, term = 0, slab = 0, to_slot = 0, from_slot = 0;   // what is loaded and read next
         const char *ga = A.base + term * A.plane, *gb = B.base + (rank - term) * B.plane;
         // one of the direct loads of the slab loaded next
         auto load_part = [&](int i) {
-            const uint32_t to = base + (loaded & (kRing - 1)) * kBuf;
+            const uint32_t to = base + to_slot * kBuf;
             const bool of_a = i < kLoadsA;
             const int n = of_a ? i : i - kLoadsA;
             const void *g = of_a ? ga + oa[of_a ? n : 0] + (int64_t)slab * 1024
@@ -132,7 +144,7 @@ struct Tile {
             load_to_lds(g, to + (of_a ? 0 : kA * kSlabBytes) + n * kWaves * 1024);
         };
         auto load_done = [&]() {
-            ++loaded;
+            to_slot = to_slot + 1 == kRing ? 0 : to_slot + 1;
             if (++slab == slabs) {
                 slab = 0;
                 if (++term > rank) {
@@ -149,16 +161,19 @@ struct Tile {
                 load_part(i);
             load_done();
         };
-        auto read_part = [&](int at, int i, Frags &f) {
+        auto read_part = [&](int i, Frags &f) {
+            const int at = from_slot * kBuf;
             if (i < NA)
                 f.a[i < NA ? i : 0] = *(const u32x4 *)(fa + at + i * 16 * kSlabBytes);
             else
                 f.b[i < NA ? 0 : i - NA] = *(const u32x4 *)(fb + at + (i - NA) * 16 * kSlabBytes);
         };
-        auto read = [&](int s, Frags &f) {
+        auto read_done = [&]() { from_slot = from_slot + 1 == kRing ? 0 : from_slot + 1; };
+        auto read = [&](Frags &f) {
 #pragma unroll
             for (int i = 0; i < NA + NB; ++i)
-                read_part((s & (kRing - 1)) * kBuf, i, f);
+                read_part(i, f);
+            read_done();
         };
         auto multiply = [&](const Frags &f, int i) {
             acc[i % NA][i / NA] = Mma::mul(f.a[i % NA], f.b[i / NA], acc[i % NA][i / NA]);
@@ -168,31 +183,31 @@ struct Tile {
         // that may still be under way.  The LDS reads and loads go out evenly
         // between the matrix instructions: issued in one block they would
         // hold up the waves, all of which come from the barrier together.
-        auto step = [&](int s, const Frags &now, Frags &next) {
+        auto step = [&](const Frags &now, Frags &next) {
             constexpr int kOps = NA + NB + kLoads, kMul = NA * NB;
             wait_loads<(kRing - 2) * kLoads>();
             barrier();
-            const int at = ((s + 1) & (kRing - 1)) * kBuf;
 #pragma unroll
             for (int i = 0, op = 0; i < kMul; ++i) {
                 multiply(now, i);
 #pragma unroll
                 for (; op < kOps * (i + 1) / kMul; ++op) {
                     if (op < NA + NB)
-                        read_part(at, op, next);
+                        read_part(op, next);
                     else
                         load_part(op - NA - NB);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
             load_done();
+            read_done();
         };
         // the same near the end, where no more loads follow
         auto last_step = [&](int s, const Frags &now, Frags &next) {
             wait_loads<0>();
             if (s + 1 < total) {
                 barrier();
-                read(s + 1, next);
+                read(next);
             }
 #pragma unroll
             for (int i = 0; i < NA * NB; ++i)
@@ -208,14 +223,14 @@ struct Tile {
         else
             wait_loads<0>();
         barrier();
-        read(0, f0);
+        read(f0);
         int s = 0;
         for (; s + 1 + kRing < total; s += 2) {
-            step(s, f0, f1);
-            step(s + 1, f1, f0);
+            step(f0, f1);
+            step(f1, f0);
         }
         if (s + kRing < total) {
-            step(s, f0, f1);
+            step(f0, f1);
             ++s;
             f0 = f1;
         }
@@ -225,9 +240,59 @@ struct Tile {
                 last_step(s + 1, f1, f0);
         }
     }
-    // first output and point of this lane's acc[t][u]
-    __device__ __forceinline__ int out_of(int t) const { return (wave / WB * NA + t) * 16 + (lane >> 4) * 4; }
-    __device__ __forceinline__ int point_of(int u) const { return (wave % WB * NB + u) * 16 + (lane & 15); }
+    // the point of acc[..][b], from the tile's first
+    __device__ __forceinline__ int point_of(int b) const { return (wave % WB * NB + b) * 16 + (lane & 15); }
+
+    // The results, as rows of Y.  value(a, n, b, r, v): the four results of
+    // acc[a][b], outputs n.. (a multiple of 4 and below A.rows rounded up to
+    // one; past the last ones if the tile is) of point r (not above the last).
+    // mask(r, n, chunk): changes the 16 bytes that are about to be stored as
+    // outputs n.. of point r.  A wave turns 16 points at a time in LDS, so that
+    // its stores are 16-byte pieces of long runs of a row; they bypass the
+    // caches (the results are read by a later kernel, if at all): 131,072 x
+    // 1024 -> 1024 in 8 bits takes 146 us, 187 us without that, 227 us with
+    // stores as the matrix instruction leaves its results.
+    template <typename Y, typename Value, typename Mask>
+    __device__ __forceinline__ void store(Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0, int64_t rows, char *lds,
+                                          Value value, Mask mask) const {
+        constexpr int kPer = 16 / sizeof(Y), kRow = NA * 16 * sizeof(Y), kPitch = kRow + 16, kChunks = kRow / 16;
+        static_assert(kWaves * 16 * kPitch <= kLds, "room for the waves' rows");
+        const int wa = wave / WB, wb = wave % WB;
+        wait_loads<0>();
+        barrier();                       // the ring is free
+        char *own = lds + wave * 16 * kPitch;
+        const int64_t last = (n_out - 1) & ~(int64_t)3;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int64_t p0 = b0 + (wb * NB + b) * 16;
+#pragma unroll
+            for (int a = 0; a < NA; ++a) {
+                float v[4];
+                value(a, min(a0 + (wa * NA + a) * 16 + (lane >> 4) * 4, last), b, min(p0 + (lane & 15), rows - 1), v);
+                store_four((Y *)(own + (lane & 15) * kPitch) + a * 16 + (lane >> 4) * 4, v);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // one wave's LDS accesses are in order
+#pragma unroll
+            for (int i = 0; i < kChunks / 4; ++i) {
+                const int at = i * 64 + lane, row = at / kChunks, c = at % kChunks;
+                u32x4 u = *(const u32x4 *)(own + row * kPitch + c * 16);
+                const int64_t r = p0 + row, n = a0 + wa * NA * 16 + c * kPer;
+                if (r < rows && n < n_out) {
+                    mask(r, n, u);
+                    Y *to = y + r * ldy + n;
+                    if (n + kPer <= n_out) {
+                        __builtin_nontemporal_store(u, (u32x4_any *)to);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e)
+                            if (n + e < n_out)
+                                to[e] = element<Y>(u, e);
+                    }
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    }
 };
 
 // Rows of one launch: a launch of more than 2^22 blocks is split (a grid holds

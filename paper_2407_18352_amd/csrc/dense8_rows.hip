@@ -15,9 +15,6 @@ constexpr int kThreads = 256;
 constexpr int kMaxBlocks = 1 << 14;   // the kernels loop beyond them
 constexpr int kChunk = 8;
 
-typedef u32x4 __attribute__((aligned(2))) u32x4_any;
-typedef f32x4 __attribute__((aligned(4))) f32x4_any;
-
 // chunk at `p`, of which the first n values exist (the others become 0)
 __device__ __forceinline__ void load_chunk(const float *p, int n, float (&v)[kChunk]) {
     if (n >= kChunk) {

@@ -17,32 +17,21 @@ __global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, ui
     const int64_t pitch = (int64_t)p.slabs * 1024, width = (int64_t)p.slabs * kSlabBytes;
     t.template run<true>({(const char *)p.w, p.n_out, pitch, width, 0}, {(const char *)p.q, p.rows, pitch, width, 0}, a0, b0, 1,
                          lds, acc);
-    // four outputs of a point at once where every row keeps their alignment;
-    // scales and biases are there in whole fours
-    const bool wide = ((uintptr_t)p.y & (4 * sizeof(Y) - 1)) == 0 && (p.ldy & 3) == 0;
-    const int last = (p.n_out - 1) & ~3;
-    float s[NB];
+    float s[NB];   // asked for before the stores begin
 #pragma unroll
     for (int b = 0; b < NB; ++b)
         s[b] = p.s[min(b0 + t.point_of(b), p.rows - 1)];
+    t.store((Y *)p.y, p.ldy, a0, p.n_out, b0, p.rows, lds,
+            [&](int a, int64_t n, int b, int64_t, float (&v)[4]) {
+                const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
 #pragma unroll
-    for (int a = 0; a < NA; ++a) {
-        const int n = (int)a0 + t.out_of(a);
-        const f32x4 sc = *(const f32x4 *)(p.t + min(n, last)), bias = *(const f32x4 *)(p.b + min(n, last));
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int64_t r = b0 + t.point_of(b);
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = (float)acc[a][b][e] * s[b] * sc[e] + bias[e];
-                if (p.relu)
-                    v[e] = relu_keep_nan(v[e]);
-            }
-            if (r < p.rows && n < p.n_out)
-                store_four((Y *)p.y + r * p.ldy + n, v, p.n_out - n, wide && n + 4 <= p.n_out);
-        }
-    }
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = (float)acc[a][b][e] * s[b] * sc[e] + bias[e];
+                    if (p.relu)
+                        v[e] = relu_keep_nan(v[e]);
+                }
+            },
+            [](int64_t, int64_t, u32x4 &) {});
 }
 
 template <typename Y, int WA, int WB, int NA, int NB>
