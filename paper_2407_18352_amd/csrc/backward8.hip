@@ -4,6 +4,8 @@
 // dw's products are exact on v_mfma_f32_16x16x32_bf16 and summed in fp32.  An
 // fp32 operand is the exact sum of three bf16 terms: three products for dw,
 // for dx those six of nine whose terms' ranks sum to at most 2.
+#include <type_traits>
+
 #include "dense8_nt.hpp"
 
 namespace hpacml {
@@ -104,14 +106,20 @@ __global__ void __launch_bounds__(64 * WA * WB) dx_kernel(DxArgs p) {
 // The sum runs over the rows, along which neither operand is contiguous: both
 // go to LDS as they lie, [row][column] in bf16, and the fragments come out
 // transposed (ds_read_tr16_b64: 16 lanes read 4 rows x 16 columns and get one
-// column's 4 rows each).  dy is loaded straight to LDS; the codes pass through
-// registers, where they become bf16 values.  Slabs of 64 rows, double-buffered:
-// during a slab the next one's dy loads, its codes (loaded a slab earlier) are
-// converted and written, and the codes of the one after are fetched.
+// column's 4 rows each).  Slabs of 32 rows, one matrix instruction's depth.
+// Everything comes from memory by direct loads: dy to where its fragments are
+// read, the codes and their exponents to a place of the thread's own, from
+// where it takes them two slabs later, turns them into bf16 values and writes
+// those among the fragments.  During slab s (whose dy fragments are in
+// registers) a wave reads slab s's value fragments two ahead of their use and
+// slab s + 1's dy fragments, converts slab s + 2's codes, and asks for slab
+// s + 4's dy and slab s + 5's codes: three slabs pass before a load is waited
+// for.  One barrier per slab.
 //
 // A row of a slab is pairs of 16-byte chunks (16 columns); pair p is stored at
 // p ^ turn(row), so that the rows a transposing read touches at one pair lie
-// on different banks.
+// on different banks, and its two chunks change places with swap(p, row), so
+// that the threads that write one chunk each do not meet on half the banks.
 struct DwArgs {
     const char *g;              // dy's planes
     int64_t g_pitch, g_width;   // bytes; columns from the width on read as 0
@@ -123,40 +131,54 @@ struct DwArgs {
     uint32_t out_tiles, in_tiles;
 };
 
-template <bool RELU, int WA, int WB, int NA, int NB>
+template <int WA, int WB, int NA, int NB>
 struct DwTile {
-    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRows = 64;
+    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRows = 32;
     static constexpr int kA = 16 * NA * WA, kB = 16 * NB * WB;          // outputs, channels
-    static constexpr int kPitchA = 2 * kA, kPitchB = 2 * kB;            // bytes of an LDS row
-    static constexpr int kBufA = kRows * kPitchA, kBufB = kRows * kPitchB, kBuf = kBufA + kBufB;
-    static constexpr int kLoadsA = kBufA / (1024 * kWaves);             // direct loads of a wave per slab
-    static constexpr int kChunks = kRows * kB / 16 / kThreads;          // 16 codes each, per thread and slab
-    static_assert(kLoadsA >= 1 && kChunks >= 1 && kChunks * 16 * kThreads == kRows * kB, "whole shares");
+    static constexpr int kPitchG = 2 * kA, kPitchX = 2 * kB;            // bytes of an LDS row
+    static constexpr int kG = kRows * kPitchG, kX = kRows * kPitchX;    // one slab's
+    static constexpr int kRingG = 4, kRingX = 3, kRingCodes = 4;
+    static constexpr int kCodes = kThreads * 16, kExps = kThreads * 4;  // 16 codes and an exponent per thread
+    static constexpr int kAtX = kRingG * kG, kAtCodes = kAtX + kRingX * kX, kAtExps = kAtCodes + kRingCodes * kCodes;
+    static constexpr int kLds = kAtExps + kRingCodes * kExps;
+    static constexpr int kLoadsG = kG / (1024 * kWaves), kLoads = kLoadsG + 2;
+    static constexpr int kActive = kRows * kB / 16;                     // threads with codes of their own
+    static_assert(kLoadsG >= 1 && kActive <= kThreads && kLds <= 160 * 1024, "shares of a slab");
 
-    // which pair of an LDS row column pair 0 is at
-    template <int PAIRS>
-    static __device__ __forceinline__ int turn(int row) {
-        return ((row & 3) | ((row >> 1) & 4)) & (PAIRS - 1);
-    }
-    // fragment of 16 columns from `col` on, 32 rows from `row` on: lane l gets column l % 16, rows 8 (l / 16) + 0..7
     template <int PITCH>
-    static __device__ __forceinline__ bf16x8 fragment(const char *buf, int row, int col, int lane) {
+    static __device__ __forceinline__ int turn(int row) {
+        return ((row & 3) | ((row >> 1) & 4)) & (PITCH / 32 - 1);
+    }
+    static __device__ __forceinline__ int swap(int pair, int row) { return ((pair >> 3) + row) & 1; }
+    // byte of a slab where column pair `pair`, chunk `half` of `row` is stored
+    template <int PITCH>
+    static __device__ __forceinline__ int place(int row, int pair, int half) {
+        return row * PITCH + (pair ^ turn<PITCH>(row)) * 32 + (half ^ swap(pair, row)) * 16;
+    }
+    // where a lane begins to read the fragment of column pair `pair`: lane l
+    // gets column l % 16, rows 8 (l / 16) + 0..3; rows + 4..7 are 4 * PITCH on
+    // (turn and swap are the same there)
+    template <int PITCH>
+    static __device__ __forceinline__ int fragment_at(int pair, int lane) {
+        const int row = (lane >> 4) * 8 + ((lane & 15) >> 2), eighth = lane & 3;
+        return place<PITCH>(row, pair, eighth >> 1) + (eighth & 1) * 8;
+    }
+    template <int PITCH>
+    static __device__ __forceinline__ bf16x8 fragment(const char *at) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) s16x4 *Lds;
-        const int r = row + (lane >> 4) * 8 + ((lane & 15) >> 2);
-        const char *a = buf + r * PITCH + (((col >> 4) ^ turn<PITCH / 32>(r)) * 32) + (lane & 3) * 8;
-        const char *b = buf + (r + 4) * PITCH + (((col >> 4) ^ turn<PITCH / 32>(r + 4)) * 32) + (lane & 3) * 8;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)a), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)b);
         typedef short s16x8 __attribute__((ext_vector_type(8)));
+        typedef __attribute__((address_space(3))) s16x4 *Lds;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * PITCH));
         return __builtin_bit_cast(bf16x8, (s16x8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     }
 };
 
 template <bool RELU, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
-    typedef DwTile<RELU, WA, WB, NA, NB> T;
-    __shared__ __align__(1024) char lds[2 * T::kBuf];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    typedef DwTile<WA, WB, NA, NB> T;
+    __shared__ __align__(1024) char lds[T::kLds];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa = wave / WB, wb = wave % WB;
 
     // the tiles of one part of the rows follow one another on one XCD
@@ -167,109 +189,209 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
     const int64_t from = part * p.rows_per_split, to = min(from + p.rows_per_split, p.c.rows);
     const int slabs = to > from ? (int)((to - from + T::kRows - 1) / T::kRows) : 0, total = slabs * p.planes;
 
-    // dy: lane's place in a direct load, and the column that belongs there
-    const uint32_t base = nt::lds_offset(lds);
-    auto load_g = [&](int s, int buf) {
-        const int plane = p.planes - 1 - s / slabs;          // the smallest terms first
-        const int64_t r0 = from + (int64_t)(s % slabs) * T::kRows;
-        const char *g = p.g + plane * p.g_plane;
-#pragma unroll
-        for (int i = 0; i < T::kLoadsA; ++i) {
-            const int at = (i * T::kWaves + wave) * 1024 + lane * 16;
-            const int row = at / T::kPitchA, chunk = at % T::kPitchA / 16;
-            const int col = ((chunk >> 1) ^ T::template turn<T::kPitchA / 32>(row)) * 32 + (chunk & 1) * 16 + j0 * 2;   // bytes
-            const void *src = g + (r0 + row) * p.g_pitch + col;
-            if (r0 + row >= to || col >= p.g_width)
-                src = nt::zero_chunk;
-            nt::load_to_lds(src, base + buf * T::kBuf + (i * T::kWaves + wave) * 1024);
-        }
-    };
-    // codes: 16 columns of a row each
-    u32x4 code[T::kChunks];
-    uint32_t byte[T::kChunks];
-    const int code_cols = (p.c.width + 31) / 32 * 32;
-    auto load_x = [&](int s) {
-        const int64_t r0 = from + (int64_t)(s % slabs) * T::kRows;
-#pragma unroll
-        for (int i = 0; i < T::kChunks; ++i) {
-            const int at = i * T::kThreads + threadIdx.x, row = at / (T::kB / 16);
-            const int64_t r = min(r0 + row, to - 1);
-            int col = k0 + at % (T::kB / 16) * 16;
-            col = col < code_cols ? col : 0;                 // beyond the width: any codes
-            code[i] = *(const u32x4 *)((const uint8_t *)p.c.codes + r * p.c.ld_codes + col);
-            byte[i] = r0 + row < to ? ((const uint8_t *)p.c.exps)[r * p.c.ld_exps + col / 32] : 0u;   // 0: 2^e reads as 0
-        }
-    };
-    auto write_x = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < T::kChunks; ++i) {
-            const int at = i * T::kThreads + threadIdx.x, row = at / (T::kB / 16), pair = at % (T::kB / 16);
-            const float s = block_scale(byte[i]);
-            uint32_t w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t q = code[i][e / 2] >> (16 * (e & 1));
-                const float lo = block_value<RELU>(q & 0xFFu, s), hi = block_value<RELU>((q >> 8) & 0xFFu, s);
-                // exact in bf16: the high halves
-                w[e] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
-            }
-            char *to_lds = lds + buf * T::kBuf + T::kBufA + row * T::kPitchB + ((pair ^ T::template turn<T::kPitchB / 32>(row)) * 32);
-            ((u32x4 *)to_lds)[0] = u32x4{w[0], w[1], w[2], w[3]};
-            ((u32x4 *)to_lds)[1] = u32x4{w[4], w[5], w[6], w[7]};
-        }
-    };
-
-    f32x4 acc[NA][NB] = {}, sum[NA] = {};
+    f32x4 acc[NA][NB] = {};
+    float sum[NA] = {};
     const bool sums = p.db && k0 == 0 && wb == 0;
-    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+
     if (total > 0) {
-        load_g(0, 0);
-        load_x(0);
-        write_x(0);
-        if (total > 1)
-            load_x(1);
-    }
-    for (int s = 0; s < total; ++s) {
-        nt::wait_loads<0>();
-        nt::barrier();
-        const char *buf = lds + (s & 1) * T::kBuf;
-        if (s + 1 < total) {
-            load_g(s + 1, (s + 1) & 1);
-            write_x((s + 1) & 1);
-            if (s + 2 < total)
-                load_x(s + 2);
+        const uint32_t base = nt::lds_offset(lds);
+        // dy: the column that belongs where this lane's bytes of a load land
+        int g_row[T::kLoadsG], g_col[T::kLoadsG];
+#pragma unroll
+        for (int i = 0; i < T::kLoadsG; ++i) {
+            const int at = (i * T::kWaves + wave) * 1024 + lane * 16, row = at / T::kPitchG, chunk = at % T::kPitchG / 16;
+            const int pair = (chunk >> 1) ^ T::template turn<T::kPitchG>(row);
+            g_row[i] = row;
+            g_col[i] = j0 * 2 + pair * 32 + ((chunk & 1) ^ T::swap(pair, row)) * 16;
         }
+        // codes: this thread's row and 16 columns
+        const int x_id = tid % T::kActive, x_row = x_id / (T::kB / 16), x_pair = x_id % (T::kB / 16);
+        int x_col = k0 + x_pair * 16;
+        x_col = x_col < (p.c.width + 31) / 32 * 32 ? x_col : 0;     // beyond the width: any codes
+        const int x_at = T::kAtX + T::template place<T::kPitchX>(x_row, x_pair, 0);
+        const int x_other = T::kAtX + T::template place<T::kPitchX>(x_row, x_pair, 1);
+
+        // the slabs loaded next, past the end the last one again or zeros (so
+        // that every step has the same loads under way)
+        int g_slab = 0, g_plane = p.planes - 1, g_slot = 0, x_slab = 0, x_slot = 0;   // the smallest terms first
+        auto load_g = [&](int i) {
+            const int64_t r = from + (int64_t)g_slab * T::kRows + g_row[i];
+            const char *src = p.g + g_plane * p.g_plane + r * p.g_pitch + g_col[i];
+            nt::load_to_lds(nt::chosen(r < to && g_col[i] < p.g_width && g_plane >= 0, src), base + g_slot * T::kG + (i * T::kWaves + wave) * 1024);
+        };
+        auto next_g = [&]() {
+            g_slot = g_slot + 1 == T::kRingG ? 0 : g_slot + 1;
+            if (++g_slab == slabs) {
+                g_slab = 0;
+                --g_plane;
+            }
+        };
+        auto x_source = [&]() { return min(from + (int64_t)x_slab * T::kRows + x_row, to - 1); };
+        auto load_codes = [&]() {
+            nt::load_to_lds((const uint8_t *)p.c.codes + x_source() * p.c.ld_codes + x_col,
+                            base + T::kAtCodes + x_slot * T::kCodes + wave * 1024);
+        };
+        auto load_exps = [&]() {
+            nt::load_byte_to_lds((const uint8_t *)p.c.exps + x_source() * p.c.ld_exps + (x_col >> 5),
+                                 base + T::kAtExps + x_slot * T::kExps + wave * 256);
+        };
+        auto next_x = [&]() {
+            x_slot = x_slot + 1 == T::kRingCodes ? 0 : x_slot + 1;
+            x_slab = x_slab + 1 == slabs ? 0 : x_slab + 1;
+        };
+
+        // codes to values: slab c_slab (its row may lie past the end: zeros)
+        int c_slab = 0, c_slot = 0, w_slot = 0;
+        u32x4 code;
+        float scale;
+        uint32_t word[8];
+        auto take = [&]() {
+            code = *(const u32x4 *)(lds + T::kAtCodes + c_slot * T::kCodes + tid * 16);
+            uint32_t e = *(const uint32_t *)(lds + T::kAtExps + c_slot * T::kExps + tid * 4);
+            asm("" : "+v"(e));                    // read it without a branch
+            scale = from + (int64_t)c_slab * T::kRows + x_row < to ? block_scale(e & 0xFFu) : 0.f;
+        };
+        auto convert = [&](int e) {
+            const uint32_t w = code[e / 2], q = w >> (16 * (e & 1));
+            const float lo = block_value<RELU>(q & 0xFFu, scale), hi = block_value<RELU>((q >> 8) & 0xFFu, scale);
+            // exact in bf16: the high halves
+            word[e] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+        };
+        auto put = [&]() {
+            if (T::kActive == T::kThreads || tid < T::kActive) {
+                *(u32x4 *)(lds + x_at + w_slot * T::kX) = u32x4{word[0], word[1], word[2], word[3]};
+                *(u32x4 *)(lds + x_other + w_slot * T::kX) = u32x4{word[4], word[5], word[6], word[7]};
+            }
+            c_slot = c_slot + 1 == T::kRingCodes ? 0 : c_slot + 1;
+            w_slot = w_slot + 1 == T::kRingX ? 0 : w_slot + 1;
+            c_slab = c_slab + 1 == slabs ? 0 : c_slab + 1;
+        };
+
+        // fragments
+        int a_at[NA], b_at[NB], a_slot = 0, b_slot = 0;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 a[NA], b[NB];
+        for (int t = 0; t < NA; ++t)
+            a_at[t] = T::template fragment_at<T::kPitchG>(wa * NA + t, lane);
 #pragma unroll
-            for (int t = 0; t < NA; ++t)
-                a[t] = T::template fragment<T::kPitchA>(buf, ks * 32, (wa * NA + t) * 16, lane);
+        for (int u = 0; u < NB; ++u)
+            b_at[u] = T::kAtX + T::template fragment_at<T::kPitchX>(wb * NB + u, lane);
+        bf16x8 a[2][NA], b[4];
+        auto read_a = [&](int t) { return T::template fragment<T::kPitchG>(lds + a_at[t] + a_slot * T::kG); };
+        auto read_b = [&](int u, int slot) { return T::template fragment<T::kPitchX>(lds + b_at[u] + slot * T::kX); };
+        auto next_slot = [](int slot, int ring) { return slot + 1 == ring ? 0 : slot + 1; };
+
+        // first: the place in `b` of the slab's first fragment
+        auto step = [&](auto first, const bf16x8 (&now)[NA], bf16x8 (&next)[NA]) {
+            constexpr int kFirst = decltype(first)::value;
+            nt::wait_loads<2 * T::kLoads>();      // what the step before the last two asked for
+            nt::barrier();
+            const int after = next_slot(b_slot, T::kRingX);
 #pragma unroll
-            for (int t = 0; t < NB; ++t)
-                b[t] = T::template fragment<T::kPitchB>(buf + T::kBufA, ks * 32, (wb * NB + t) * 16, lane);
+            for (int u = 0; u < NB; ++u) {
+                // fragments two tiles ahead; past the last, the next slab's first
+                b[(kFirst + u + 2) & 3] = u + 2 < NB ? read_b(u + 2, b_slot) : read_b(u + 2 - NB, after);
 #pragma unroll
-            for (int t = 0; t < NA; ++t)
+                for (int t = u * NA / NB; t < (u + 1) * NA / NB; ++t)
+                    next[t] = read_a(t);
+                if (u == 0)
+                    take();
+                constexpr int kWords = (8 + NB - 2) / (NB - 1);
 #pragma unroll
-                for (int u = 0; u < NB; ++u)
-                    acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b[u], acc[t][u], 0, 0, 0);
-            if (sums) {
+                for (int e = (u - 1) * kWords; e < u * kWords; ++e)
+                    if (e >= 0 && e < 8)
+                        convert(e);
+#pragma unroll
+                for (int i = u * T::kLoads / NB; i < (u + 1) * T::kLoads / NB; ++i) {
+                    if (i < T::kLoadsG)
+                        load_g(i);
+                    else if (i == T::kLoadsG)
+                        load_codes();
+                    else
+                        load_exps();
+                }
 #pragma unroll
                 for (int t = 0; t < NA; ++t)
-                    sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], ones, sum[t], 0, 0, 0);
+                    acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now[t], b[(kFirst + u) & 3], acc[t][u], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            put();
+            if (sums) {
+                // eight rows at a time, so that few roundings follow one another
+#pragma unroll
+                for (int t = 0; t < NA; ++t) {
+                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                    const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+                    float v = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        v = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{now[t][e], now[t][e + 1]}, ones, v, false);
+                    sum[t] += v;
+                }
+            }
+            next_g();
+            next_x();
+            a_slot = next_slot(a_slot, T::kRingG);
+            b_slot = after;
+        };
+
+        // slabs 0..3 of dy and 0..3 of the codes, of which 0 and 1 are converted here
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            load_codes();
+            load_exps();
+            next_x();
         }
+#pragma unroll
+        for (int i = 0; i < T::kRingG; ++i) {
+#pragma unroll
+            for (int l = 0; l < T::kLoadsG; ++l)
+                load_g(l);
+            next_g();
+        }
+        nt::wait_loads<0>();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            take();
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                convert(e);
+            put();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        load_codes();                             // slab 4, where slab 0's were
+        load_exps();
+        next_x();
+        nt::wait_loads<63>();
+        nt::barrier();
+#pragma unroll
+        for (int t = 0; t < NA; ++t)
+            a[0][t] = read_a(t);
+        a_slot = 1;
+        b[0] = read_b(0, 0);
+        b[1] = read_b(1, 0);
+        for (int s = 0; s < total; s += 2) {
+            step(std::integral_constant<int, 0>(), a[0], a[1]);
+            if (s + 1 >= total)
+                break;
+            step(std::integral_constant<int, NB & 3>(), a[1], a[0]);
+        }
+        nt::wait_loads<0>();
     }
 #pragma unroll
-    for (int t = 0; t < NA; ++t)
+    for (int t = 0; t < NA; ++t) {
+        if (sums) {
+            // lane l holds output l % 16's rows 8 (l / 16) + 0..7
+            float v = sum[t];
+            v += __shfl_xor(v, 16);
+            v += __shfl_xor(v, 32);
+            const int j = j0 + (wa * NA + t) * 16 + lane;
+            if (lane < 16 && j < p.n_out)
+                p.db[(int64_t)part * p.n_out + j] = v;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int j = j0 + (wa * NA + t) * 16 + (lane >> 4) * 4 + e;
-            if (j >= p.n_out)
-                continue;
-            if (sums && (lane & 15) == 0)
-                p.db[(int64_t)part * p.n_out + j] = sum[t][e];
-            if (p.dw) {
+            if (p.dw && j < p.n_out) {
 #pragma unroll
                 for (int u = 0; u < NB; ++u) {
                     const int k = k0 + (wb * NB + u) * 16 + (lane & 15);
@@ -278,6 +400,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
                 }
             }
         }
+    }
 }
 
 // out [rows][ld] (+)= the sum over the parts of parts [splits][rows][width]
@@ -355,9 +478,9 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
     p.splits = 1;
     if (want_dw) {
         // one round of the chip: a block of the largest tile fills a CU's LDS,
-        // two of the middle one and four of the smallest do
+        // two of the middle one and three of the smallest do
         const int64_t tiles = tiles_of(n_out, c.width, p.tile), least = p.tile == 64 ? 256 : 512;
-        int64_t splits = (p.tile == 256 ? 256 : p.tile == 128 ? 512 : 1024) / tiles;
+        int64_t splits = (p.tile == 256 ? 256 : p.tile == 128 ? 512 : 768) / tiles;
         const int64_t most = c.rows / least;
         splits = splits < most ? splits : most;
         splits = splits < 1 ? 1 : splits;

@@ -52,6 +52,14 @@ __device__ __forceinline__ void load_to_lds(const void *g, uint32_t lds) {
                  : "v"(g), "s"(lds)
                  : "memory");
 }
+// one byte per lane, to the low byte of the word at `lds` + 4 * lane
+__device__ __forceinline__ void load_byte_to_lds(const void *g, uint32_t lds) {
+    uint32_t save;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save)
+                 : "v"(g), "s"(lds)
+                 : "memory");
+}
 // at most N of this wave's vector-memory loads are still under way, and its
 // LDS reads are in registers
 template <int N>
@@ -67,6 +75,12 @@ __device__ __forceinline__ uint32_t lds_offset(const void *p) {
 
 // what a load beyond an operand's width reads
 __device__ __align__(16) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
+
+// `g`, or zeros, by selection: the address is computed either way
+__device__ __forceinline__ const void *chosen(bool exists, const char *g) {
+    asm("" : "+v"(g));
+    return exists ? g : (const char *)zero_chunk;
+}
 
 // element e of 16 bytes
 template <typename Y>
@@ -137,11 +151,10 @@ struct Tile {
             const uint32_t to = base + to_slot * kBuf;
             const bool of_a = i < kLoadsA;
             const int n = of_a ? i : i - kLoadsA;
-            const void *g = of_a ? ga + oa[of_a ? n : 0] + (int64_t)slab * 1024
+            const char *g = of_a ? ga + oa[of_a ? n : 0] + (int64_t)slab * 1024
                                  : gb + ob[of_a ? 0 : n] + (int64_t)slab * (BLOCKED_B ? 1024 : kSlabBytes);
-            if (!BLOCKED_B && !of_a && slab * kSlabBytes + chunk * 16 >= B.width)
-                g = zero_chunk;
-            load_to_lds(g, to + (of_a ? 0 : kA * kSlabBytes) + n * kWaves * 1024);
+            const bool rest = !BLOCKED_B && !of_a;
+            load_to_lds(rest ? chosen(slab * kSlabBytes + chunk * 16 < B.width, g) : g, to + (of_a ? 0 : kA * kSlabBytes) + n * kWaves * 1024);
         };
         auto load_done = [&]() {
             to_slot = to_slot + 1 == kRing ? 0 : to_slot + 1;
