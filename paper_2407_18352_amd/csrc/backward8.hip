@@ -66,39 +66,46 @@ struct DxArgs {
 };
 
 template <typename X, int WA, int WB, int NA, int NB>
-__global__ void __launch_bounds__(64 * WA * WB) dx_kernel(DxArgs p) {
-    typedef nt::Tile<nt::Bf16, WA, WB, NA, NB> T;
+__global__ void __launch_bounds__(64 * WA * WB, 2) dx_kernel(DxArgs p) {
+    typedef nt::Product<nt::Bf16, X, false, WA, WB, NA, NB> T;
     __shared__ __align__(1024) char lds[T::kLds];
-    const nt::TileAt at = nt::tile_at(blockIdx.x, gridDim.x, p.in_tiles, p.point_tiles);
-    const int64_t a0 = at.out * T::kA, b0 = at.point * T::kB;
-    f32x4 acc[NA][NB] = {};
     T t;
-    t.template run<false>(p.wt, p.g, a0, b0, p.terms, lds, acc);
-    t.store((X *)p.dx, p.lddx, a0, p.n_in, b0, p.g.rows, lds,
-            [&](int a, int64_t, int b, int64_t, float (&v)[4]) {
+    t.run(p.wt, p.g, p.in_tiles, p.point_tiles, p.terms, lds, [&](const f32x4 (&acc)[NA][NB], int64_t a0, int64_t b0) {
+        // the codes of the values that this lane stores, all asked for at
+        // once.  Rows of codes are whole blocks of channels: all of a piece's exist.
+        constexpr int kPieces = T::kChunks / 4;
+        uint2 code[NB][kPieces];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = acc[a][b][e];
-            },
-            [&](int64_t r, int64_t k, u32x4 &u) {
-                if (!p.codes)
-                    return;
-                // rows of codes are whole blocks of channels: all of these exist
-                const uint8_t *c = p.codes + r * p.ld_codes + k;
-                if constexpr (sizeof(X) == 2) {
-                    const uint2 q = *(const uint2 *)c;
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t two = (e < 2 ? q.x : q.y) >> (16 * (e & 1));
-                        u[e] &= (two & 0xFFu ? 0x0000FFFFu : 0u) | (two & 0xFF00u ? 0xFFFF0000u : 0u);
-                    }
+            for (int i = 0; i < kPieces; ++i) {
+                const typename T::Piece at = t.piece(b, i, a0, b0);
+                if (p.codes && at.point < p.g.rows && at.out < p.n_in) {
+                    const uint8_t *c = p.codes + at.point * p.ld_codes + at.out;
+                    code[b][i] = sizeof(X) == 2 ? *(const uint2 *)c : uint2{*(const uint32_t *)c, 0u};
                 } else {
-                    const uint32_t q = *(const uint32_t *)c;
+                    code[b][i] = uint2{~0u, ~0u};
+                }
+            }
+        t.store((X *)p.dx, p.lddx, a0, p.n_in, b0, p.g.rows,
+                [&](int a, int64_t, int b, float (&v)[4]) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        u[e] = (q >> (8 * e)) & 0xFFu ? u[e] : 0u;
-                }
-            });
+                        v[e] = acc[a][b][e];
+                },
+                [&](int b, int i, u32x4 &u) {
+                    const uint2 q = code[b][i];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (sizeof(X) == 2) {
+                            const uint32_t two = (e < 2 ? q.x : q.y) >> (16 * (e & 1));
+                            u[e] &= (two & 0xFFu ? 0x0000FFFFu : 0u) | (two & 0xFF00u ? 0xFFFF0000u : 0u);
+                        } else {
+                            u[e] = (q.x >> (8 * e)) & 0xFFu ? u[e] : 0u;
+                        }
+                    }
+                });
+    });
 }
 
 // ---- dw and db ------------------------------------------------------------------
@@ -430,19 +437,12 @@ int dw_tile(int32_t n_out, int32_t n_in) {
 }
 
 template <typename X, int WA, int WB, int NA, int NB>
-void launch_dx_tile(const DxArgs &a, hipStream_t st) {
-    typedef nt::Tile<nt::Bf16, WA, WB, NA, NB> T;
-    DxArgs d = a;
-    d.in_tiles = (uint32_t)((a.n_in + T::kA - 1) / T::kA);
-    const int64_t step = nt::rows_per_launch(d.in_tiles, T::kB);
-    for (int64_t r = 0; r < a.g.rows; r += step) {
-        d.g.rows = a.g.rows - r < step ? a.g.rows - r : step;
-        d.g.base = a.g.base + r * a.g.pitch;
-        d.codes = a.codes ? a.codes + r * a.ld_codes : nullptr;
-        d.dx = (X *)a.dx + r * a.lddx;
-        d.point_tiles = (uint32_t)((d.g.rows + T::kB - 1) / T::kB);
-        dx_kernel<X, WA, WB, NA, NB><<<dim3(d.in_tiles * d.point_tiles), T::kThreads, 0, st>>>(d);
-    }
+void launch_dx_tile(DxArgs d, hipStream_t st) {
+    typedef nt::Product<nt::Bf16, X, false, WA, WB, NA, NB> T;
+    d.in_tiles = (uint32_t)((d.n_in + T::kA - 1) / T::kA);
+    d.point_tiles = (uint32_t)((d.g.rows + T::kB - 1) / T::kB);
+    dx_kernel<X, WA, WB, NA, NB>
+        <<<nt::blocks_for_tiles((int64_t)d.in_tiles * d.point_tiles, T::kPerCu), T::kThreads, 0, st>>>(d);
 }
 
 template <typename X>
@@ -471,7 +471,7 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
                              bool want_dw, bool want_dx) {
     Backward8Plan p{};
     p.planes = dtype == HPACML_F32 ? 3 : 1;
-    p.direct = dtype == HPACML_BF16 && ((uintptr_t)dy & 15) == 0 && lddy % 8 == 0 && n_out % 8 == 0;
+    p.direct = dtype == HPACML_BF16 && ((uintptr_t)dy & 15) == 0 && lddy % 8 == 0 && lddy < (1 << 22) && n_out % 32 == 0;
     p.slabs = (int32_t)slabs_of(2 * n_out);
     p.pitch = (int64_t)p.slabs * (kSlabBytes / 2);
     p.tile = dw_tile(n_out, c.width);

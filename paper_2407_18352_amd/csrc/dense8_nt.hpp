@@ -1,14 +1,19 @@
 // The product both operands of which lie along k: C[a][b] = sum_k A[a][k] B[b][k],
 // int8 codes with 32-bit sums or bf16 with fp32 sums.
 //
-// A block computes a tile of C.  The operands pass through LDS in slabs of 64
-// bytes of k (64 codes, 32 bf16: one matrix instruction's depth), a ring of
-// kRing of them filled by direct global-to-LDS loads.  While the matrix cores
-// work on slab s from registers, a wave reads slab s + 1's fragments from LDS
-// and the loads of slabs up to s + kRing are under way; what a slab's loads
-// have to wait for in the memory system is covered by the slabs before it.
-// One barrier per slab publishes slab s + 1 (its loads have been waited for)
-// and frees slab s (its fragments are in registers).
+// The operands pass through LDS in slabs of 64 bytes of k (64 codes, 32 bf16:
+// one matrix instruction's depth), a ring of four filled by direct
+// global-to-LDS loads.  While the matrix cores work on slab s from registers,
+// a wave reads slab s + 1's fragments from LDS and the loads of slabs up to
+// s + 4 are under way: what a load waits for in the memory system is covered by
+// the slabs before it.  One barrier per slab publishes slab s + 1 (its loads
+// have been waited for) and frees slab s (its fragments are in registers).
+//
+// A block computes tiles of C one after another, and the slabs of its tiles
+// follow one another through the ring: during a tile's last slabs the next
+// tile's first ones load, and they arrive while the results are stored.  (A
+// block per tile began and ended every tile with nothing under way: with 256
+// blocks in step, 15 us of each 57 us at 4096 codes of k.)
 //
 // A row of a slab is four 16-byte chunks, chunk c stored at c ^ chunk_turn(row),
 // so that the 16 rows a matrix instruction reads at one chunk fall on different
@@ -50,6 +55,14 @@ __device__ __forceinline__ void load_to_lds(const void *g, uint32_t lds) {
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
                  : "=&s"(save)
                  : "v"(g), "s"(lds)
+                 : "memory");
+}
+// the same from `base` + `offset`, the base wave-uniform
+__device__ __forceinline__ void load_to_lds(uint64_t base, uint32_t offset, uint32_t lds) {
+    uint32_t save;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(save)
+                 : "v"(offset), "s"(base), "s"(lds)
                  : "memory");
 }
 // one byte per lane, to the low byte of the word at `lds` + 4 * lane
@@ -97,82 +110,136 @@ __device__ __forceinline__ Y element(const u32x4 &u, int e) {
 // One operand, in `terms` planes `plane` bytes apart.  BLOCKED: as the LDS
 // image has it, 16 rows x 64 bytes after one another (1 KB, chunks swizzled),
 // `pitch` bytes per 16 rows; what pads the last rows and slab is there.
-// Otherwise rows `pitch` bytes apart, of which `width` bytes count (the rest
-// of the last slab reads as zero).
+// Otherwise rows `pitch` bytes apart.  `width` bytes of k: whole slabs.
 struct Operand {
     const char *base;
     int64_t rows, pitch, width, plane;
 };
 
-// Blocks of WA x WB waves, each NA x NB tiles of 16 x 16.
-template <typename Mma, int WA, int WB, int NA, int NB, int RING = 4>
-struct Tile {
-    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRing = RING;
+// Block id -> tiles.  Blocks go to the eight XCDs in turn; each XCD takes a
+// contiguous run of tiles, its blocks one after another along the run, so that
+// what they share meets in its L2; a run goes through groups of kGroup point
+// tiles by all output tiles.
+constexpr int kGroup = 4;
+struct Tiles {
+    uint32_t out_tiles, point_tiles;
+    uint32_t at, end, step;
+
+    __device__ __forceinline__ Tiles(uint32_t outs, uint32_t points) : out_tiles(outs), point_tiles(points) {
+        const uint32_t tiles = outs * points, xcd = blockIdx.x & 7, per = tiles >> 3, more = tiles & 7;
+        const uint32_t first = xcd * per + min(xcd, more);
+        at = first + (blockIdx.x >> 3);
+        end = first + per + (xcd < more ? 1 : 0);
+        step = (gridDim.x - xcd + 7) >> 3;
+    }
+    __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ void next() { at += step; }
+    __device__ __forceinline__ void place(uint32_t &out, uint32_t &point) const {
+        const uint32_t group = at / (kGroup * out_tiles), r = at - group * kGroup * out_tiles;
+        const uint32_t high = min((uint32_t)kGroup, point_tiles - group * kGroup);
+        out = r / high;
+        point = group * kGroup + r % high;
+    }
+};
+// Blocks for `tiles` tiles when `per_cu` of them share a CU: one round of the
+// chip's 256 CUs at most.
+inline uint32_t blocks_for_tiles(int64_t tiles, int per_cu) { return (uint32_t)(tiles < 256 * per_cu ? tiles : 256 * per_cu); }
+
+// Blocks of WA x WB waves, each NA x NB tiles of 16 x 16; results of type Y.
+// A is blocked, B is if BLOCKED_B, and comes in rows otherwise.
+template <typename Mma, typename Y, bool BLOCKED_B, int WA, int WB, int NA, int NB>
+struct Product {
+    static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRing = 4;
     static constexpr int kA = 16 * NA * WA, kB = 16 * NB * WB;
-    static constexpr int kBuf = (kA + kB) * kSlabBytes, kLds = kRing * kBuf;
-    static constexpr int kLoadsA = kA / (16 * kWaves), kLoadsB = kB / (16 * kWaves), kLoads = kLoadsA + kLoadsB;
-    static_assert(kLoadsA * 16 * kWaves == kA && kLoadsB * 16 * kWaves == kB, "whole loads per wave");
+    static constexpr int kBuf = (kA + kB) * kSlabBytes, kLoadsA = kA / (16 * kWaves), kLoadsB = kB / (16 * kWaves);
+    static constexpr int kLoads = kLoadsA + kLoadsB;
+    // results of 16 points of a wave, on their way out
+    static constexpr int kPer = 16 / sizeof(Y), kRow = NA * 16 * sizeof(Y), kChunks = kRow / 16;
+    static constexpr int kAtOut = kRing * kBuf, kLds = kAtOut + kWaves * 16 * kRow;
+    static constexpr int kPerCu = 160 * 1024 / kLds;
+    static_assert(kLoadsA * 16 * kWaves == kA && kLoadsB * 16 * kWaves == kB && kPerCu >= 1, "whole loads per wave");
     typedef typename Mma::Acc Acc;
     struct Frags {
         u32x4 a[NA], b[NB];
     };
 
     int wave, lane;
+    char *lds;
 
-    // acc[a][b]: outputs a0 + 16 (WA-wave * NA + a) + 4 (lane / 16) + e of
-    // point b0 + 16 (WB-wave * NB + b) + lane % 16
-    // terms: 1, or 3 planes of each operand of which the products of ranks
-    // that sum to at most 2 are taken, the smallest first.  A is BLOCKED.
-    template <bool BLOCKED_B>
-    __device__ __forceinline__ void run(const Operand &A, const Operand &B, int64_t a0, int64_t b0, int terms, char *lds,
-                                        Acc (&acc)[NA][NB]) {
+    // `terms`: 1, or 3 planes of each operand of which the products of ranks
+    // that sum to at most 2 are taken, the smallest first.  finish(acc, a0,
+    // b0): the tile's results; acc[a][b]: outputs a0 + 16 (WA-wave * NA + a) +
+    // 4 (lane / 16) + e of point b0 + 16 (WB-wave * NB + b) + lane % 16.
+    template <typename Finish>
+    __device__ __forceinline__ void run(const Operand &A, const Operand &B, uint32_t out_tiles, uint32_t point_tiles, int terms,
+                                        char *shared, Finish finish) {
+        lds = shared;
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int row16 = lane >> 2, chunk = (lane & 3) ^ chunk_turn(row16);   // chunk_turn(row) depends on row % 16 alone
-        int64_t oa[kLoadsA], ob[kLoadsB];
-#pragma unroll
-        for (int i = 0; i < kLoadsA; ++i)
-            oa[i] = min(a0 / 16 + i * kWaves + wave, (A.rows - 1) / 16) * A.pitch + lane * 16;
-#pragma unroll
-        for (int i = 0; i < kLoadsB; ++i)
-            ob[i] = BLOCKED_B ? min(b0 / 16 + i * kWaves + wave, (B.rows - 1) / 16) * B.pitch + lane * 16
-                              : min(b0 + (i * kWaves + wave) * 16 + row16, B.rows - 1) * B.pitch + chunk * 16;
         const uint32_t base = lds_offset(lds) + wave * 1024;
         const int wa = wave / WB, wb = wave % WB;
         const int fr = (lane & 15) * kSlabBytes + ((lane >> 4) ^ chunk_turn(lane & 15)) * 16;
         const char *fa = lds + wa * NA * 16 * kSlabBytes + fr, *fb = lds + (kA + wb * NB * 16) * kSlabBytes + fr;
+        const int slabs = (int)(A.width / kSlabBytes), total = slabs * (terms * (terms + 1) / 2), pairs = (total + 1) / 2;
 
-        const int slabs = (int)((A.width + kSlabBytes - 1) / kSlabBytes);
-        const int total = slabs * (terms * (terms + 1) / 2);
-        int rank = terms - 1, term = 0, slab = 0, to_slot = 0, from_slot = 0;   // what is loaded and read next
-        const char *ga = A.base + term * A.plane, *gb = B.base + (rank - term) * B.plane;
+        Tiles tiles(out_tiles, point_tiles), ahead = tiles;   // the tile worked on, and the one loaded
+        if (!tiles.more())
+            return;
+        int rank = 0, term = 0, slab = 0, to_slot = 0, from_slot = 0;
+        uint64_t ga[kLoadsA], gb;         // first bytes of the tile loaded, in its plane: of each load of A, of B's rows
+        uint32_t ob[kLoadsB];             // this lane's offsets from there
+        auto begin_plane = [&]() {
+            uint32_t out, point;
+            ahead.place(out, point);
+            const uint64_t a = (uint64_t)(A.base + term * A.plane), b = (uint64_t)(B.base + (rank - term) * B.plane);
+            const int64_t b0 = (int64_t)point * kB;
+#pragma unroll
+            for (int i = 0; i < kLoadsA; ++i)
+                ga[i] = a + min((int64_t)out * (kA / 16) + i * kWaves + wave, (A.rows - 1) / 16) * A.pitch;
+            gb = b + (BLOCKED_B ? b0 / 16 : b0) * B.pitch;
+#pragma unroll
+            for (int i = 0; i < kLoadsB; ++i) {
+                const int at = i * kWaves + wave, left = (int)min(B.rows - 1 - b0, (int64_t)kB);   // rows after the tile's first
+                ob[i] = BLOCKED_B ? (uint32_t)min(at, left / 16) * (uint32_t)B.pitch + lane * 16
+                                  : (uint32_t)min(at * 16 + row16, left) * (uint32_t)B.pitch + chunk * 16;
+            }
+        };
+        auto begin_tile = [&]() {
+            rank = terms - 1;
+            term = 0;
+            begin_plane();
+        };
         // one of the direct loads of the slab loaded next
         auto load_part = [&](int i) {
             const uint32_t to = base + to_slot * kBuf;
-            const bool of_a = i < kLoadsA;
-            const int n = of_a ? i : i - kLoadsA;
-            const char *g = of_a ? ga + oa[of_a ? n : 0] + (int64_t)slab * 1024
-                                 : gb + ob[of_a ? 0 : n] + (int64_t)slab * (BLOCKED_B ? 1024 : kSlabBytes);
-            const bool rest = !BLOCKED_B && !of_a;
-            load_to_lds(rest ? chosen(slab * kSlabBytes + chunk * 16 < B.width, g) : g, to + (of_a ? 0 : kA * kSlabBytes) + n * kWaves * 1024);
+            if (i < kLoadsA)
+                load_to_lds(ga[i < kLoadsA ? i : 0] + (uint64_t)slab * 1024, lane * 16, to + i * kWaves * 1024);
+            else
+                load_to_lds(gb + (uint64_t)slab * (BLOCKED_B ? 1024 : kSlabBytes), ob[i < kLoadsA ? 0 : i - kLoadsA],
+                            to + kA * kSlabBytes + (i - kLoadsA) * kWaves * 1024);
         };
+        // the slab after it: of this tile, the next, or, past the last, the
+        // same tile again (every step has as many loads under way)
         auto load_done = [&]() {
-            to_slot = to_slot + 1 == kRing ? 0 : to_slot + 1;
+            to_slot = (to_slot + 1) & (kRing - 1);
             if (++slab == slabs) {
                 slab = 0;
                 if (++term > rank) {
                     term = 0;
                     --rank;
                 }
-                ga = A.base + term * A.plane;
-                gb = B.base + (rank - term) * B.plane;
+                if (rank >= 0) {
+                    if (terms > 1)
+                        begin_plane();
+                } else {
+                    Tiles t = ahead;
+                    t.next();
+                    if (t.more())
+                        ahead = t;
+                    begin_tile();
+                }
             }
-        };
-        auto load = [&]() {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                load_part(i);
-            load_done();
         };
         auto read_part = [&](int i, Frags &f) {
             const int at = from_slot * kBuf;
@@ -181,25 +248,27 @@ struct Tile {
             else
                 f.b[i < NA ? 0 : i - NA] = *(const u32x4 *)(fb + at + (i - NA) * 16 * kSlabBytes);
         };
-        auto read_done = [&]() { from_slot = from_slot + 1 == kRing ? 0 : from_slot + 1; };
-        auto read = [&](Frags &f) {
-#pragma unroll
-            for (int i = 0; i < NA + NB; ++i)
-                read_part(i, f);
-            read_done();
-        };
+        Acc acc[NA][NB];
         auto multiply = [&](const Frags &f, int i) {
             acc[i % NA][i / NA] = Mma::mul(f.a[i % NA], f.b[i / NA], acc[i % NA][i / NA]);
         };
-        // Slab s from `now`, slab s + 1 to `next`, slab s + kRing to where
-        // slab s was.  Slab s + 1's loads have kRing - 2 slabs behind them
-        // that may still be under way.  The LDS reads and loads go out evenly
+        // Slab s of the tile from `now`, slab s + 1 to `next`, the slab loaded
+        // next to where slab s was.  Slab s + 1's loads have those of the last
+        // two steps behind them, which may still be under way; in a tile's
+        // first three steps they have arrived before the last tile's stores,
+        // which are not waited for.  The LDS reads and loads go out evenly
         // between the matrix instructions: issued in one block they would
         // hold up the waves, all of which come from the barrier together.
+        int arrived = 0;                 // steps whose loads have
         auto step = [&](const Frags &now, Frags &next) {
             constexpr int kOps = NA + NB + kLoads, kMul = NA * NB;
-            wait_loads<(kRing - 2) * kLoads>();
+            if (arrived > 0)
+                wait_loads<63>();
+            else
+                wait_loads<(kRing - 2) * kLoads>();
+            --arrived;
             barrier();
+            from_slot = (from_slot + 1) & (kRing - 1);
 #pragma unroll
             for (int i = 0, op = 0; i < kMul; ++i) {
                 multiply(now, i);
@@ -213,92 +282,93 @@ struct Tile {
                 }
             }
             load_done();
-            read_done();
-        };
-        // the same near the end, where no more loads follow
-        auto last_step = [&](int s, const Frags &now, Frags &next) {
-            wait_loads<0>();
-            if (s + 1 < total) {
-                barrier();
-                read(next);
-            }
-#pragma unroll
-            for (int i = 0; i < NA * NB; ++i)
-                multiply(now, i);
         };
         Frags f0, f1;
+        begin_tile();
 #pragma unroll
-        for (int i = 0; i < kRing; ++i)
-            if (i < total)
-                load();
-        if (total >= kRing)
-            wait_loads<(kRing - 1) * kLoads>();
-        else
+        for (int i = 0; i < kRing; ++i) {
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l)
+                load_part(l);
+            load_done();
+        }
+        wait_loads<0>();
+        for (; tiles.more(); tiles.next()) {
+            // slabs 0..3 of the tile have arrived
+            barrier();
+#pragma unroll
+            for (int i = 0; i < NA + NB; ++i)
+                read_part(i, f0);
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    acc[a][b] = Acc{0, 0, 0, 0};
+            arrived = kRing - 1;
+            asm volatile("" : "+s"(arrived));   // one form of the step, not one for each value
+            for (int pair = 0; pair < pairs; ++pair) {
+                step(f0, f1);            // the last step's fragments are the next tile's; they are read again
+                int left = total - 2 * pair;
+                asm volatile("" : "+s"(left));   // one way out of the loop: with two, the results are copied
+                if (left > 1)
+                    step(f1, f0);
+            }
             wait_loads<0>();
-        barrier();
-        read(f0);
-        int s = 0;
-        for (; s + 1 + kRing < total; s += 2) {
-            step(f0, f1);
-            step(f1, f0);
-        }
-        if (s + kRing < total) {
-            step(f0, f1);
-            ++s;
-            f0 = f1;
-        }
-        for (; s < total; s += 2) {
-            last_step(s, f0, f1);
-            if (s + 1 < total)
-                last_step(s + 1, f1, f0);
+            uint32_t out, point;
+            tiles.place(out, point);
+            finish(acc, (int64_t)out * kA, (int64_t)point * kB);
         }
     }
     // the point of acc[..][b], from the tile's first
     __device__ __forceinline__ int point_of(int b) const { return (wave % WB * NB + b) * 16 + (lane & 15); }
 
-    // The results, as rows of Y.  value(a, n, b, r, v): the four results of
-    // acc[a][b], outputs n.. (a multiple of 4 and below A.rows rounded up to
-    // one; past the last ones if the tile is) of point r (not above the last).
-    // mask(r, n, chunk): changes the 16 bytes that are about to be stored as
-    // outputs n.. of point r.  A wave turns 16 points at a time in LDS, so that
-    // its stores are 16-byte pieces of long runs of a row; they bypass the
-    // caches (the results are read by a later kernel, if at all): 131,072 x
-    // 1024 -> 1024 in 8 bits takes 146 us, 187 us without that, 227 us with
-    // stores as the matrix instruction leaves its results.
-    template <typename Y, typename Value, typename Mask>
-    __device__ __forceinline__ void store(Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0, int64_t rows, char *lds,
-                                          Value value, Mask mask) const {
-        constexpr int kPer = 16 / sizeof(Y), kRow = NA * 16 * sizeof(Y), kPitch = kRow + 16, kChunks = kRow / 16;
-        static_assert(kWaves * 16 * kPitch <= kLds, "room for the waves' rows");
-        const int wa = wave / WB, wb = wave % WB;
-        wait_loads<0>();
-        barrier();                       // the ring is free
-        char *own = lds + wave * 16 * kPitch;
+    // 16 bytes of results that a lane stores: piece i of the points of acc[..][b]
+    struct Piece {
+        int64_t point;
+        int64_t out;
+        int at;            // in the wave's part of LDS
+    };
+    __device__ __forceinline__ Piece piece(int b, int i, int64_t a0, int64_t b0) const {
+        const int at = i * 64 + lane, row = at / kChunks, c = at % kChunks;
+        return {b0 + (wave % WB * NB + b) * 16 + row, a0 + wave / WB * NA * 16 + c * kPer, row * kRow + ((c ^ (row & (kChunks - 1))) * 16)};
+    }
+    // The results, as rows of Y.  value(a, n, b, v): the four results of
+    // acc[a][b], outputs n.. (a multiple of 4, not above the last).
+    // mask(b, i, chunk): changes the 16 bytes that are about to be stored as
+    // piece i of b.  A wave turns 16 points at a time in LDS, so that its
+    // stores are 16-byte pieces of long runs of a row; they bypass the caches
+    // (the results are read by a later kernel, if at all): 131,072 x 1024 ->
+    // 1024 in 8 bits took 146 us with a block per tile, 187 us without that,
+    // 227 us with stores as the matrix instruction leaves its results.
+    template <typename Value, typename Mask>
+    __device__ __forceinline__ void store(Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0, int64_t rows, Value value,
+                                          Mask mask) const {
+        char *own = lds + kAtOut + wave * 16 * kRow;
         const int64_t last = (n_out - 1) & ~(int64_t)3;
+        const int row = lane & 15, grp = lane >> 4;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const int64_t p0 = b0 + (wb * NB + b) * 16;
 #pragma unroll
             for (int a = 0; a < NA; ++a) {
                 float v[4];
-                value(a, min(a0 + (wa * NA + a) * 16 + (lane >> 4) * 4, last), b, min(p0 + (lane & 15), rows - 1), v);
-                store_four((Y *)(own + (lane & 15) * kPitch) + a * 16 + (lane >> 4) * 4, v);
+                value(a, min(a0 + (wave / WB * NA + a) * 16 + grp * 4, last), b, v);
+                const int byte = (a * 16 + grp * 4) * (int)sizeof(Y);
+                store_four((Y *)(own + row * kRow + (((byte >> 4) ^ (row & (kChunks - 1))) * 16) + (byte & 15)), v);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // one wave's LDS accesses are in order
 #pragma unroll
             for (int i = 0; i < kChunks / 4; ++i) {
-                const int at = i * 64 + lane, row = at / kChunks, c = at % kChunks;
-                u32x4 u = *(const u32x4 *)(own + row * kPitch + c * 16);
-                const int64_t r = p0 + row, n = a0 + wa * NA * 16 + c * kPer;
-                if (r < rows && n < n_out) {
-                    mask(r, n, u);
-                    Y *to = y + r * ldy + n;
-                    if (n + kPer <= n_out) {
+                const Piece p = piece(b, i, a0, b0);
+                u32x4 u = *(const u32x4 *)(own + p.at);
+                mask(b, i, u);
+                if (p.point < rows && p.out < n_out) {
+                    Y *to = y + p.point * ldy + p.out;
+                    if (p.out + kPer <= n_out) {
                         __builtin_nontemporal_store(u, (u32x4_any *)to);
                     } else {
 #pragma unroll
                         for (int e = 0; e < kPer; ++e)
-                            if (n + e < n_out)
+                            if (p.out + e < n_out)
                                 to[e] = element<Y>(u, e);
                     }
                 }
@@ -307,28 +377,6 @@ struct Tile {
         }
     }
 };
-
-// Rows of one launch: a launch of more than 2^22 blocks is split (a grid holds
-// fewer than 2^32 threads).
-inline int64_t rows_per_launch(uint32_t out_tiles, int64_t tile) {
-    const int64_t point_tiles = (int64_t)(1 << 22) / out_tiles;
-    return (point_tiles < 1 ? 1 : point_tiles) * tile;
-}
-
-// Block id -> tile.  Blocks go to the eight XCDs in turn; each XCD takes a
-// contiguous run of tiles, so that what its blocks share meets in its L2, and
-// a run goes through groups of `kGroup` point tiles by all output tiles.
-constexpr int kGroup = 4;
-struct TileAt {
-    int64_t out, point;
-};
-__device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint32_t out_tiles, uint32_t point_tiles) {
-    const uint32_t xcd = block & 7, in = block >> 3, per = blocks >> 3, more = blocks & 7;
-    const uint32_t t = xcd * per + min(xcd, more) + in;
-    const uint32_t group = t / (kGroup * out_tiles), r = t - group * kGroup * out_tiles;
-    const uint32_t high = min((uint32_t)kGroup, point_tiles - group * kGroup);
-    return {r / high, (int64_t)group * kGroup + r % high};
-}
 
 }  // namespace nt
 

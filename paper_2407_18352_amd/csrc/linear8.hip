@@ -7,47 +7,37 @@ namespace hpacml {
 namespace {
 
 template <typename Y, int WA, int WB, int NA, int NB>
-__global__ void __launch_bounds__(64 * WA * WB) linear8_kernel(Linear8Args p, uint32_t out_tiles, uint32_t point_tiles) {
-    typedef nt::Tile<nt::I8, WA, WB, NA, NB> T;
+__global__ void __launch_bounds__(64 * WA * WB, 2) linear8_kernel(Linear8Args p, uint32_t out_tiles, uint32_t point_tiles) {
+    typedef nt::Product<nt::I8, Y, true, WA, WB, NA, NB> T;
     __shared__ __align__(1024) char lds[T::kLds];
-    const nt::TileAt at = nt::tile_at(blockIdx.x, gridDim.x, out_tiles, point_tiles);
-    const int64_t a0 = at.out * T::kA, b0 = at.point * T::kB;
-    i32x4 acc[NA][NB] = {};
-    T t;
     const int64_t pitch = (int64_t)p.slabs * 1024, width = (int64_t)p.slabs * kSlabBytes;
-    t.template run<true>({(const char *)p.w, p.n_out, pitch, width, 0}, {(const char *)p.q, p.rows, pitch, width, 0}, a0, b0, 1,
-                         lds, acc);
-    float s[NB];   // asked for before the stores begin
+    T t;
+    t.run({(const char *)p.w, p.n_out, pitch, width, 0}, {(const char *)p.q, p.rows, pitch, width, 0}, out_tiles, point_tiles, 1,
+          lds, [&](const i32x4 (&acc)[NA][NB], int64_t a0, int64_t b0) {
+              float s[NB];   // asked for before the stores begin
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-        s[b] = p.s[min(b0 + t.point_of(b), p.rows - 1)];
-    t.store((Y *)p.y, p.ldy, a0, p.n_out, b0, p.rows, lds,
-            [&](int a, int64_t n, int b, int64_t, float (&v)[4]) {
-                const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
+              for (int b = 0; b < NB; ++b)
+                  s[b] = p.s[min(b0 + t.point_of(b), p.rows - 1)];
+              t.store((Y *)p.y, p.ldy, a0, p.n_out, b0, p.rows,
+                      [&](int a, int64_t n, int b, float (&v)[4]) {
+                          const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = (float)acc[a][b][e] * s[b] * sc[e] + bias[e];
-                    if (p.relu)
-                        v[e] = relu_keep_nan(v[e]);
-                }
-            },
-            [](int64_t, int64_t, u32x4 &) {});
+                          for (int e = 0; e < 4; ++e) {
+                              v[e] = (float)acc[a][b][e] * s[b] * sc[e] + bias[e];
+                              if (p.relu)
+                                  v[e] = relu_keep_nan(v[e]);
+                          }
+                      },
+                      [](int, int, u32x4 &) {});
+          });
 }
 
 template <typename Y, int WA, int WB, int NA, int NB>
 void launch_tile(const Linear8Args &a, hipStream_t stream) {
-    typedef nt::Tile<nt::I8, WA, WB, NA, NB> T;
-    const uint32_t out_tiles = (uint32_t)((a.n_out + T::kA - 1) / T::kA);
-    const int64_t step = nt::rows_per_launch(out_tiles, T::kB);
-    for (int64_t r = 0; r < a.rows; r += step) {
-        Linear8Args p = a;
-        p.rows = a.rows - r < step ? a.rows - r : step;
-        p.q += blocked_bytes(r, a.slabs);
-        p.s += r;
-        p.y = (Y *)a.y + r * a.ldy;
-        const uint32_t point_tiles = (uint32_t)((p.rows + T::kB - 1) / T::kB);
-        linear8_kernel<Y, WA, WB, NA, NB><<<dim3(out_tiles * point_tiles), T::kThreads, 0, stream>>>(p, out_tiles, point_tiles);
-    }
+    typedef nt::Product<nt::I8, Y, true, WA, WB, NA, NB> T;
+    const uint32_t out_tiles = (uint32_t)((a.n_out + T::kA - 1) / T::kA), point_tiles = (uint32_t)((a.rows + T::kB - 1) / T::kB);
+    linear8_kernel<Y, WA, WB, NA, NB>
+        <<<nt::blocks_for_tiles((int64_t)out_tiles * point_tiles, T::kPerCu), T::kThreads, 0, stream>>>(a, out_tiles, point_tiles);
 }
 
 template <typename Y>
