@@ -25,18 +25,22 @@ __host__ __device__ constexpr int64_t blocked_offset(int64_t row, int64_t k, int
 hipError_t launch_codes_by_row(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t width, int8_t *codes,
                                float *scales, hipStream_t stream);
 
-// y = act(s_i t_j sum_k q_ik w_jk + b_j)
+// y = act(s_i t_j sum_k q_ik w_jk + b_j); x's codes and scales go to q and s,
+// except where the product forms them itself.
 struct Linear8Args {
-    const int8_t *q;      // codes of the rows, blocked
-    const float *s;       // [rows]
+    const void *x;
+    int64_t ldx;
+    int8_t *q;            // codes of the rows, blocked
+    float *s;             // [rows]
     const int8_t *w;      // codes of the weights, blocked
     const float *t;       // [n_out], to a multiple of four
     const float *b;       // the same; zeros without a bias
     void *y;
     int64_t rows, ldy;
-    int32_t slabs, n_out, relu;
+    int32_t slabs, n_in, n_out, relu;
 };
-hipError_t launch_linear8(const Linear8Args &a, int32_t y_dtype, hipStream_t stream);
+bool linear8_fused(int64_t rows, int32_t n_in);   // q and s are not used
+hipError_t launch_linear8(const Linear8Args &a, int32_t x_dtype, int32_t y_dtype, hipStream_t stream);
 
 hipError_t launch_checkpoint_save(const hpacml8_checkpoint &c, const void *z, int32_t z_dtype, int64_t ldz, void *a,
                                   int32_t a_dtype, int64_t lda, hipStream_t stream);

@@ -213,10 +213,8 @@ hpacml_status hpacml8_linear_run(const hpacml8_linear *l, const void *x, int32_t
     hipStream_t st = (hipStream_t)stream;
     int8_t *q = (int8_t *)scratch;
     float *s = (float *)((char *)scratch + linear_codes_bytes(l, n_rows));
-    hipError_t e = launch_codes_by_row(x, x_dtype, ldx, n_rows, l->n_in, q, s, st);
-    if (e == hipSuccess)
-        e = launch_linear8({q, s, l->w, l->t, l->b, y, n_rows, ldy, l->slabs, l->n_out, act == HPACML_ACT_RELU}, y_dtype, st);
-    return status_of(e);
+    return status_of(launch_linear8({x, ldx, q, s, l->w, l->t, l->b, y, n_rows, ldy, l->slabs, l->n_in, l->n_out, act == HPACML_ACT_RELU},
+                                    x_dtype, y_dtype, st));
 }
 
 hpacml_status hpacml8_checkpoint_save(const hpacml8_checkpoint *c, const void *z, int32_t z_dtype, int64_t ldz, void *a,

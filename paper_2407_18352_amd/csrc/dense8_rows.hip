@@ -1,11 +1,6 @@
 // Row-wise kernels of the 8-bit dense layers: codes and scales of a row, and
 // activations put away in 8 bits and brought back.  All are bound by memory.
-//
-// A lane takes eight consecutive values at a time: 16 bytes of bf16 or 32 of
-// fp32, from any address (the hardware loads and stores 16 bytes at an
-// element's alignment), and 8 bytes of codes.  Only the chunk that crosses a
-// row's end goes value by value.
-#include "dense8.hpp"
+#include "dense8_rows.hpp"
 
 namespace hpacml {
 
@@ -13,77 +8,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxBlocks = 1 << 14;   // the kernels loop beyond them
-constexpr int kChunk = 8;
 
-// chunk at `p`, of which the first n values exist (the others become 0)
-__device__ __forceinline__ void load_chunk(const float *p, int n, float (&v)[kChunk]) {
-    if (n >= kChunk) {
-        const f32x4 a = ((const f32x4_any *)p)[0], b = ((const f32x4_any *)p)[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = a[e];
-            v[4 + e] = b[e];
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < kChunk; ++e)
-            v[e] = e < n ? p[e] : 0.f;
-    }
-}
-__device__ __forceinline__ void load_chunk(const uint16_t *p, int n, float (&v)[kChunk]) {
-    if (n >= kChunk) {
-        const u32x4 a = *(const u32x4_any *)p;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[2 * e] = __builtin_bit_cast(float, a[e] << 16);
-            v[2 * e + 1] = __builtin_bit_cast(float, a[e] & 0xFFFF0000u);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < kChunk; ++e)
-            v[e] = e < n ? bf16_bits_value(p[e]) : 0.f;
-    }
-}
-__device__ __forceinline__ void store_chunk(float *p, int n, const float (&v)[kChunk]) {
-    if (n >= kChunk) {
-        ((f32x4_any *)p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-        ((f32x4_any *)p)[1] = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-#pragma unroll
-        for (int e = 0; e < kChunk; ++e)
-            if (e < n)
-                p[e] = v[e];
-    }
-}
-__device__ __forceinline__ void store_chunk(uint16_t *p, int n, const float (&v)[kChunk]) {
-    if (n >= kChunk) {
-        u32x4 a;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            a[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-        *(u32x4_any *)p = a;
-    } else {
-#pragma unroll
-        for (int e = 0; e < kChunk; ++e)
-            if (e < n)
-                p[e] = bf16_bits(v[e]);
-    }
-}
-
-// largest magnitude as bits: an infinity is above every number, a NaN above it
-__device__ __forceinline__ uint32_t top_bits(const float (&v)[kChunk]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < kChunk; ++e)
-        m = max(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7FFFFFFFu);
-    return m;
-}
-template <int LANES>
-__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
-#pragma unroll
-    for (int d = LANES / 2; d > 0; d /= 2)
-        v = max(v, (uint32_t)__shfl_xor((int)v, d));
-    return v;
+dim3 blocks_for(int64_t rows, int64_t per_block) {
+    const int64_t n = (rows + per_block - 1) / per_block;
+    return dim3((uint32_t)(n < kMaxBlocks ? n : kMaxBlocks));
 }
 
 // LANES lanes per row, HELD chunks of each lane in registers: rows up to
@@ -110,11 +38,9 @@ __global__ void __launch_bounds__(kThreads) codes_kernel(const T *__restrict__ x
                 top = max(top, top_bits(v[h]));
         }
         top = lanes_max<LANES>(top);
-        const float amax = __builtin_bit_cast(float, top);
-        const bool finite = top < 0x7F800000u, live = finite && amax >= 0x1p-119f;
-        const float inv = live ? 127.f / amax : 0.f;
+        const RowScale sc(top);
         if (lane == 0)
-            scales[r] = !finite ? __builtin_nanf("") : live ? amax / 127.f : 0.f;
+            scales[r] = sc.scale;
         for (int c = lane; c < chunks; c += LANES * HELD) {
 #pragma unroll
             for (int h = 0; h < HELD; ++h) {
@@ -123,13 +49,7 @@ __global__ void __launch_bounds__(kThreads) codes_kernel(const T *__restrict__ x
                     break;
                 if (chunks > LANES * HELD)
                     load_chunk(row + at * kChunk, width - at * kChunk, v[h]);
-                uint32_t q[2] = {0, 0};
-                if (live) {   // rows that count as zeros, or are not finite: codes 0
-#pragma unroll
-                    for (int e = 0; e < kChunk; ++e)
-                        q[e / 4] |= ((uint32_t)(int32_t)rintf(v[h][e] * inv) & 0xFFu) << (8 * (e % 4));
-                }
-                *(uint2 *)(codes + blocked_offset(r, at * kChunk, slabs)) = uint2{q[0], q[1]};
+                *(uint2 *)(codes + blocked_offset(r, at * kChunk, slabs)) = sc.codes(v[h]);
             }
         }
     }
@@ -182,11 +102,6 @@ __global__ void __launch_bounds__(kThreads) load_kernel(hpacml8_checkpoint c, A 
                 v[e] = block_value<RELU>(((e < 4 ? q.x : q.y) >> (8 * (e % 4))) & 0xFFu, s);
             store_chunk(a + r * lda + k, c.width - k, v);
         }
-}
-
-dim3 blocks_for(int64_t rows, int64_t per_block) {
-    const int64_t n = (rows + per_block - 1) / per_block;
-    return dim3((uint32_t)(n < kMaxBlocks ? n : kMaxBlocks));
 }
 
 template <typename T, int LANES, int HELD>

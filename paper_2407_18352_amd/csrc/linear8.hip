@@ -1,6 +1,7 @@
 // y = act(s_i t_j sum_k q_ik w_jk + b_j): int8 codes on v_mfma_i32_16x16x64_i8,
 // exact 32-bit sums, fp32 epilogue.
 #include "dense8_nt.hpp"
+#include "dense8_rows.hpp"
 
 namespace hpacml {
 
@@ -40,25 +41,170 @@ void launch_tile(const Linear8Args &a, hipStream_t stream) {
         <<<nt::blocks_for_tiles((int64_t)out_tiles * point_tiles, T::kPerCu), T::kThreads, 0, stream>>>(a, out_tiles, point_tiles);
 }
 
+// ---- few points ---------------------------------------------------------------
+//
+// Up to 64 points: the weights are read once and what counts is how many of
+// their bytes are on the way at a time.  A block takes 16 outputs (one per
+// fragment row) and all points; its eight waves split k, read their fragments
+// straight into registers (the blocked layout is the fragment), and add their
+// exact integer sums through LDS.  FUSED (up to 4 points): every block forms
+// the points' codes itself, its weights already on the way, which saves a
+// launch: one point through 4096 -> 4096 takes 5 us instead of 8.
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewPoints = 64, kFusedPoints = 4, kFusedCodes = 16384;
+
+template <typename X, typename Y, int P, bool FUSED>
+__global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
+    constexpr int kAhead = P == 4 ? 4 : 8;           // slabs of a wave on the way at a time
+    __shared__ __align__(16) int32_t part[kFewWaves][P][256];
+    __shared__ __align__(16) int8_t codes[FUSED ? kFusedCodes : 16];
+    __shared__ float scales[kFusedPoints];
+    __shared__ uint32_t tops[kFewWaves][kFusedPoints];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = lane & 15;
+    const int at = row * kSlabBytes + (((lane >> 4) ^ chunk_turn(row)) * 16);
+    const int8_t *w = p.w + (int64_t)blockIdx.x * p.slabs * 1024 + at;
+    const int pitch = p.slabs * kSlabBytes;
+
+    u32x4 a[kAhead];
+    auto weights = [&](int s0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            a[i] = *(const u32x4 *)(w + (int64_t)min(s0 + i * kFewWaves, p.slabs - 1) * 1024);
+    };
+    weights(wave);
+
+    if constexpr (FUSED) {
+        constexpr int kHeld = kFusedCodes / 8 / kFewThreads;
+        float v[kHeld][kChunk];
+        for (int r = 0; r < p.rows; ++r) {
+            const X *x = (const X *)p.x + r * p.ldx;
+            uint32_t top = 0;
+#pragma unroll
+            for (int h = 0; h < kHeld; ++h) {
+                const int k = (h * kFewThreads + tid) * kChunk;
+                if (k < p.n_in) {
+                    load_chunk(x + k, p.n_in - k, v[h]);
+                    top = max(top, top_bits(v[h]));
+                }
+            }
+            top = lanes_max<64>(top);
+            if (lane == 0)
+                tops[wave][r] = top;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kFewWaves; ++i)
+                top = max(top, tops[i][r]);
+            const RowScale sc(top);
+            if (tid == 0)
+                scales[r] = sc.scale;
+#pragma unroll
+            for (int h = 0; h < kHeld; ++h) {
+                const int k = (h * kFewThreads + tid) * kChunk;
+                if (k < p.n_in)
+                    *(uint2 *)(codes + r * pitch + k) = sc.codes(v[h]);
+                else if (k < pitch)
+                    *(uint2 *)(codes + r * pitch + k) = uint2{0, 0};
+            }
+        }
+        __syncthreads();
+    }
+
+    i32x4 acc[P] = {};
+    for (int s0 = wave; s0 < p.slabs; s0 += kAhead * kFewWaves) {
+        if (s0 != wave)
+            weights(s0);
+        // past the last slab: weights of that one, codes of 0
+        u32x4 q[kAhead][P];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int s = min(s0 + i * kFewWaves, p.slabs - 1);
+#pragma unroll
+            for (int b = 0; b < P; ++b)
+                q[i][b] = FUSED ? *(const u32x4 *)(codes + min(row, (int)p.rows - 1) * pitch + s * kSlabBytes + (lane >> 4) * 16)
+                                : *(const u32x4 *)(p.q + ((int64_t)min(b, (int)((p.rows - 1) >> 4)) * p.slabs + s) * 1024 + at);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int b = 0; b < P; ++b)
+                acc[b] = nt::I8::mul(a[i], s0 + i * kFewWaves < p.slabs ? q[i][b] : u32x4{0, 0, 0, 0}, acc[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < P; ++b)
+        *(i32x4 *)&part[wave][b][lane * 4] = acc[b];
+    __syncthreads();
+    for (int i = tid; i < P * 256; i += kFewThreads) {
+        // 16 threads after one another store 16 outputs of a point
+        const int b = i >> 8, point = (i >> 4) & 15, o = i & 15, from = ((o >> 2) * 16 + point) * 4 + (o & 3);
+        const int64_t r = b * 16 + point;
+        const int n = blockIdx.x * 16 + o;
+        if (r >= p.rows || n >= p.n_out)
+            continue;
+        int32_t sum = 0;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k)
+            sum += part[k][b][from];
+        float v = (float)sum * (FUSED ? scales[r & (kFusedPoints - 1)] : p.s[r]) * p.t[n] + p.b[n];
+        if (p.relu)
+            v = relu_keep_nan(v);
+        store_value((Y *)p.y + r * p.ldy + n, v);
+    }
+}
+
 template <typename Y>
-void launch_as(const Linear8Args &a, hipStream_t stream) {
-    const int64_t big = ((a.n_out + 255) / 256) * ((a.rows + 255) / 256);
-    const int64_t mid = ((a.n_out + 127) / 128) * ((a.rows + 127) / 128);
-    if (big >= 512 && a.slabs >= 32)
-        launch_tile<Y, 4, 2, 4, 8>(a, stream);
-    else if (mid >= 256 && a.n_out > 64)
-        launch_tile<Y, 2, 2, 4, 4>(a, stream);
-    else
+void launch_product(const Linear8Args &a, hipStream_t stream) {
+    auto tiles = [&](int64_t outs, int64_t points) { return (a.n_out + outs - 1) / outs * ((a.rows + points - 1) / points); };
+    const dim3 few((a.n_out + 15) / 16);
+    if (a.rows <= 16)
+        few_kernel<float, Y, 1, false><<<few, kFewThreads, 0, stream>>>(a);
+    else if (a.rows <= 32)
+        few_kernel<float, Y, 2, false><<<few, kFewThreads, 0, stream>>>(a);
+    else if (a.rows <= kFewPoints)
+        few_kernel<float, Y, 4, false><<<few, kFewThreads, 0, stream>>>(a);
+    // the largest tile that leaves no CU without one (us, 8-bit outputs <- inputs):
+    //   rows x out <- in       64 x 64  128 x 128  128 x 256  256 x 256
+    //   4096 x 256 <- 256          4.6        7.5        8.1       13.8
+    //   262144 x 64 <- 64         15.0       23.0       18.5       35.0
+    //   4096 x 1024 <- 1024       11.7       10.9       12.5       20.5
+    //   1024 x 4096 <- 4096       29.1       23.5       29.5       46.9
+    //   65536 x 256 <- 256        17.9       15.8       13.8       15.1
+    //   16384 x 512 <- 512        14.0       11.6       10.5       16.6
+    //   16384 x 1024 <- 1024      37.0       26.8       24.0       23.3
+    //   4096 x 4096 <- 4096      109.0       70.7       73.3       59.4
+    //   65536 x 4096 <- 4096      2620       1280       1026        899
+    else if (a.n_out <= 64 || tiles(64, 64) <= 512)
         launch_tile<Y, 2, 2, 2, 2>(a, stream);
+    else if (tiles(128, 128) <= 256)
+        launch_tile<Y, 2, 2, 4, 4>(a, stream);
+    else if (tiles(256, 256) >= 200 && a.slabs >= 16)
+        launch_tile<Y, 4, 2, 4, 8>(a, stream);
+    else
+        launch_tile<Y, 2, 4, 4, 4>(a, stream);
+}
+
+template <typename X, typename Y>
+void launch_as(const Linear8Args &a, hipStream_t stream) {
+    if (linear8_fused(a.rows, a.n_in))
+        few_kernel<X, Y, 1, true><<<dim3((a.n_out + 15) / 16), kFewThreads, 0, stream>>>(a);
+    else
+        launch_product<Y>(a, stream);
 }
 
 }  // namespace
 
-hipError_t launch_linear8(const Linear8Args &a, int32_t y_dtype, hipStream_t stream) {
-    if (y_dtype == HPACML_F32)
-        launch_as<float>(a, stream);
+bool linear8_fused(int64_t rows, int32_t n_in) {
+    return rows <= kFusedPoints && rows * slabs_of(n_in) * kSlabBytes <= kFusedCodes;
+}
+
+hipError_t launch_linear8(const Linear8Args &a, int32_t x_dtype, int32_t y_dtype, hipStream_t stream) {
+    if (!linear8_fused(a.rows, a.n_in)) {
+        const hipError_t e = launch_codes_by_row(a.x, x_dtype, a.ldx, a.rows, a.n_in, a.q, a.s, stream);
+        if (e != hipSuccess)
+            return e;
+    }
+    if (x_dtype == HPACML_F32)
+        y_dtype == HPACML_F32 ? launch_as<float, float>(a, stream) : launch_as<float, uint16_t>(a, stream);
     else
-        launch_as<uint16_t>(a, stream);
+        y_dtype == HPACML_F32 ? launch_as<uint16_t, float>(a, stream) : launch_as<uint16_t, uint16_t>(a, stream);
     return hipGetLastError();
 }
 
