@@ -233,7 +233,8 @@ class CnnModel:
 def _stream(stream):
     if stream is None:
         import torch
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+        # the current stream's handle, without the Stream object around it
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     if isinstance(stream, int):
         return C.c_void_p(stream)
     return C.c_void_p(stream.cuda_stream)
@@ -358,21 +359,17 @@ def _matrix(t, what, rows=None, width=None, dtypes=None):
     return t.data_ptr(), kinds[t.dtype], stride[0] if shape[0] > 1 else max(shape[1], 1)
 
 
-def _scratch8(scratch, need):
-    """(pointer, bytes) of the caller's scratch tensor, or of one from torch's allocator (kept by the caller of this)."""
+def _scratch8(scratch, need, stream):
+    """(the scratch tensor to keep during the call, its address, bytes): the caller's, or, on torch's current stream, whose
+    order its allocator follows, one from there."""
     import torch
     if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+        if stream is not None:
+            raise ValueError("a call on a stream of its own needs scratch memory")
+        scratch = torch.empty(need(), dtype=torch.uint8, device="cuda")
     elif not scratch.is_cuda or not scratch.is_contiguous():
         raise TypeError("scratch must be a contiguous device tensor")
     return scratch, scratch.data_ptr(), scratch.numel() * scratch.element_size()
-
-
-def _own_scratch8(scratch, need, stream):
-    """Scratch for a call that was given none: only on torch's current stream, whose order the allocator follows."""
-    if scratch is None and stream is not None:
-        raise ValueError("a call on a stream of its own needs scratch memory")
-    return _scratch8(scratch, need())
 
 
 class Linear8:
@@ -418,7 +415,7 @@ def linear8(layer: Linear8, x, y, act: int = _abi.ACT_IDENTITY, scratch=None, st
     px, tx, ldx = _matrix(x, "x", width=layer.n_in)
     n = x.shape[0]
     py, ty, ldy = _matrix(y, "y", rows=n, width=layer.n_out)
-    keep, ps, bytes_ = _own_scratch8(scratch, lambda: layer.scratch_bytes(n), stream)
+    keep, ps, bytes_ = _scratch8(scratch, lambda: layer.scratch_bytes(n), stream)
     check(lib().hpacml8_linear_run(layer.handle, px, tx, ldx, n, py, ty, ldy, act, ps, bytes_, _stream(stream)),
           "hpacml8_linear_run")
 
@@ -491,7 +488,7 @@ def backward8(kept: Checkpoint8, dy, dw=None, db=None, W=None, dx=None, accumula
             raise ValueError("dx needs W")
         pW, _, ldW = _matrix(W, "W", n_out, kept.width, (ty,))
         px, _, ldx = _matrix(dx, "dx", kept.rows, kept.width, (ty,))
-    keep, ps, bytes_ = _own_scratch8(scratch, lambda: backward8_scratch_bytes(
+    keep, ps, bytes_ = _scratch8(scratch, lambda: backward8_scratch_bytes(
         kept, dy, W if dx is not None else None, dw is not None or db is not None), stream)
     check(lib().hpacml8_backward(C.byref(kept.desc), py, ty, ldy, n_out, pW, ldW or 0, pw, lddw or 0, pb, px, ldx or 0,
                                  1 if accumulate else 0, ps, bytes_, _stream(stream)), "hpacml8_backward")

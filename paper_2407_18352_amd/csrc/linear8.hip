@@ -47,22 +47,24 @@ void launch_tile(const Linear8Args &a, hipStream_t stream) {
 // their bytes are on the way at a time.  A block takes 16 outputs (one per
 // fragment row) and all points; its eight waves split k, read their fragments
 // straight into registers (the blocked layout is the fragment), and add their
-// exact integer sums through LDS.  FUSED (up to 4 points): every block forms
-// the points' codes itself, its weights already on the way, which saves a
-// launch: one point through 4096 -> 4096 takes 5 us instead of 8.
-constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewPoints = 64, kFusedPoints = 4, kFusedCodes = 16384;
+// exact integer sums through LDS.  FUSED (codes of up to 36 KB): every block
+// forms the points' codes itself, its weights already on the way, which saves
+// a launch.  One point through 4096 -> 4096: 4.9 us.
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewPoints = 64, kFusedBytes = 36 * 1024;
+// of a row of codes in LDS: 16 rows at one k lie on different banks
+constexpr int64_t fused_pitch(int64_t slabs) { return slabs * kSlabBytes + 16; }
 
 template <typename X, typename Y, int P, bool FUSED>
 __global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
     constexpr int kAhead = P == 4 ? 4 : 8;           // slabs of a wave on the way at a time
     __shared__ __align__(16) int32_t part[kFewWaves][P][256];
-    __shared__ __align__(16) int8_t codes[FUSED ? kFusedCodes : 16];
-    __shared__ float scales[kFusedPoints];
-    __shared__ uint32_t tops[kFewWaves][kFusedPoints];
+    __shared__ __align__(16) int8_t codes[FUSED ? kFusedBytes : 16];
+    __shared__ float scales[P * 16];
+    __shared__ uint32_t tops[kFewWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = lane & 15;
     const int at = row * kSlabBytes + (((lane >> 4) ^ chunk_turn(row)) * 16);
     const int8_t *w = p.w + (int64_t)blockIdx.x * p.slabs * 1024 + at;
-    const int pitch = p.slabs * kSlabBytes;
+    const int pitch = (int)fused_pitch(p.slabs), chunks = p.slabs * (kSlabBytes / kChunk);
 
     u32x4 a[kAhead];
     auto weights = [&](int s0) {
@@ -73,36 +75,45 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
     weights(wave);
 
     if constexpr (FUSED) {
-        constexpr int kHeld = kFusedCodes / 8 / kFewThreads;
+        // one point: by the whole block; more: a wave each
+        const bool one = p.rows == 1;
+        const int step = one ? kFewThreads : 64, first = one ? tid : lane;
+        constexpr int kHeld = 4;
         float v[kHeld][kChunk];
-        for (int r = 0; r < p.rows; ++r) {
+        for (int r = one ? 0 : wave; r < p.rows; r += kFewWaves) {
             const X *x = (const X *)p.x + r * p.ldx;
             uint32_t top = 0;
+            for (int c = first; c < chunks; c += kHeld * step) {
 #pragma unroll
-            for (int h = 0; h < kHeld; ++h) {
-                const int k = (h * kFewThreads + tid) * kChunk;
-                if (k < p.n_in) {
+                for (int h = 0; h < kHeld; ++h) {
+                    const int k = (c + h * step) * kChunk;
                     load_chunk(x + k, p.n_in - k, v[h]);
-                    top = max(top, top_bits(v[h]));
                 }
+#pragma unroll
+                for (int h = 0; h < kHeld; ++h)
+                    top = max(top, top_bits(v[h]));
             }
             top = lanes_max<64>(top);
-            if (lane == 0)
-                tops[wave][r] = top;
-            __syncthreads();
+            if (one) {
+                if (lane == 0)
+                    tops[wave] = top;
+                __syncthreads();
 #pragma unroll
-            for (int i = 0; i < kFewWaves; ++i)
-                top = max(top, tops[i][r]);
+                for (int i = 0; i < kFewWaves; ++i)
+                    top = max(top, tops[i]);
+            }
             const RowScale sc(top);
-            if (tid == 0)
+            if (first == 0)
                 scales[r] = sc.scale;
+            for (int c = first; c < chunks; c += kHeld * step) {
 #pragma unroll
-            for (int h = 0; h < kHeld; ++h) {
-                const int k = (h * kFewThreads + tid) * kChunk;
-                if (k < p.n_in)
-                    *(uint2 *)(codes + r * pitch + k) = sc.codes(v[h]);
-                else if (k < pitch)
-                    *(uint2 *)(codes + r * pitch + k) = uint2{0, 0};
+                for (int h = 0; h < kHeld; ++h) {
+                    const int k = (c + h * step) * kChunk;
+                    if (chunks > kHeld * step)
+                        load_chunk(x + k, p.n_in - k, v[h]);
+                    if (c + h * step < chunks)
+                        *(uint2 *)(codes + r * pitch + k) = sc.codes(v[h]);
+                }
             }
         }
         __syncthreads();
@@ -119,7 +130,7 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
             const int s = min(s0 + i * kFewWaves, p.slabs - 1);
 #pragma unroll
             for (int b = 0; b < P; ++b)
-                q[i][b] = FUSED ? *(const u32x4 *)(codes + min(row, (int)p.rows - 1) * pitch + s * kSlabBytes + (lane >> 4) * 16)
+                q[i][b] = FUSED ? *(const u32x4 *)(codes + min(b * 16 + row, (int)p.rows - 1) * pitch + s * kSlabBytes + (lane >> 4) * 16)
                                 : *(const u32x4 *)(p.q + ((int64_t)min(b, (int)((p.rows - 1) >> 4)) * p.slabs + s) * 1024 + at);
         }
 #pragma unroll
@@ -143,23 +154,29 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
 #pragma unroll
         for (int k = 0; k < kFewWaves; ++k)
             sum += part[k][b][from];
-        float v = (float)sum * (FUSED ? scales[r & (kFusedPoints - 1)] : p.s[r]) * p.t[n] + p.b[n];
+        float v = (float)sum * (FUSED ? scales[b * 16 + point] : p.s[r]) * p.t[n] + p.b[n];
         if (p.relu)
             v = relu_keep_nan(v);
         store_value((Y *)p.y + r * p.ldy + n, v);
     }
 }
 
+template <typename X, typename Y, bool FUSED>
+void launch_few(const Linear8Args &a, hipStream_t stream) {
+    const dim3 grid((a.n_out + 15) / 16);
+    if (a.rows <= 16)
+        few_kernel<X, Y, 1, FUSED><<<grid, kFewThreads, 0, stream>>>(a);
+    else if (a.rows <= 32)
+        few_kernel<X, Y, 2, FUSED><<<grid, kFewThreads, 0, stream>>>(a);
+    else
+        few_kernel<X, Y, 4, FUSED><<<grid, kFewThreads, 0, stream>>>(a);
+}
+
 template <typename Y>
 void launch_product(const Linear8Args &a, hipStream_t stream) {
     auto tiles = [&](int64_t outs, int64_t points) { return (a.n_out + outs - 1) / outs * ((a.rows + points - 1) / points); };
-    const dim3 few((a.n_out + 15) / 16);
-    if (a.rows <= 16)
-        few_kernel<float, Y, 1, false><<<few, kFewThreads, 0, stream>>>(a);
-    else if (a.rows <= 32)
-        few_kernel<float, Y, 2, false><<<few, kFewThreads, 0, stream>>>(a);
-    else if (a.rows <= kFewPoints)
-        few_kernel<float, Y, 4, false><<<few, kFewThreads, 0, stream>>>(a);
+    if (a.rows <= kFewPoints)
+        launch_few<float, Y, false>(a, stream);   // x is not read
     // the largest tile that leaves no CU without one (us, 8-bit outputs <- inputs):
     //   rows x out <- in       64 x 64  128 x 128  128 x 256  256 x 256
     //   4096 x 256 <- 256          4.6        7.5        8.1       13.8
@@ -184,7 +201,7 @@ void launch_product(const Linear8Args &a, hipStream_t stream) {
 template <typename X, typename Y>
 void launch_as(const Linear8Args &a, hipStream_t stream) {
     if (linear8_fused(a.rows, a.n_in))
-        few_kernel<X, Y, 1, true><<<dim3((a.n_out + 15) / 16), kFewThreads, 0, stream>>>(a);
+        launch_few<X, Y, true>(a, stream);
     else
         launch_product<Y>(a, stream);
 }
@@ -192,7 +209,7 @@ void launch_as(const Linear8Args &a, hipStream_t stream) {
 }  // namespace
 
 bool linear8_fused(int64_t rows, int32_t n_in) {
-    return rows <= kFusedPoints && rows * slabs_of(n_in) * kSlabBytes <= kFusedCodes;
+    return rows <= kFewPoints && rows * fused_pitch(slabs_of(n_in)) <= kFusedBytes;
 }
 
 hipError_t launch_linear8(const Linear8Args &a, int32_t x_dtype, int32_t y_dtype, hipStream_t stream) {
