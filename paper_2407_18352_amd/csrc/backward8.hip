@@ -4,9 +4,11 @@
 // dw's products are exact on v_mfma_f32_16x16x32_bf16 and summed in fp32.  An
 // fp32 operand is the exact sum of three bf16 terms: three products for dw,
 // for dx those six of nine whose terms' ranks sum to at most 2.
+#include <cmath>
 #include <type_traits>
 
 #include "dense8_nt.hpp"
+#include "dense8_rows.hpp"
 
 namespace hpacml {
 
@@ -15,42 +17,68 @@ namespace {
 constexpr int kThreads = 256;             // of the kernels that lay operands out and join parts
 constexpr int64_t kMaxBlocks = 1 << 16;   // they loop beyond them
 
-// planes [planes][rows][pitch] of v [rows][width], zero beyond the width
+// What the products read, laid out in scratch by one launch: dy's planes
+// [planes][rows][pitch], zero beyond n_out (unless dy is read in place), and
+// the planes of W's transpose [n_in][n_out], blocked, zero beyond n_out
+// (unless dx is not wanted).
 template <typename T>
-__global__ void __launch_bounds__(kThreads) planes_kernel(const T *__restrict__ v, int64_t ld, int64_t rows,
-                                                          int32_t width, uint16_t *__restrict__ out, int64_t pitch) {
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * pitch; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t r = i / pitch, k = i - r * pitch;
-        const T *at = v + r * ld + k;
-        if constexpr (sizeof(T) == 4) {
-            uint16_t t[3] = {0, 0, 0};
-            if (k < width)
-                split3(*at, t);
-            for (int q = 0; q < 3; ++q)
-                out[q * rows * pitch + i] = t[q];
-        } else {
-            out[i] = k < width ? *at : (uint16_t)0;
-        }
+struct LayoutArgs {
+    const T *dy;
+    int64_t lddy, rows, pitch;
+    uint16_t *planes;
+    uint32_t row_blocks;        // blocks that lay out dy; the others W
+    const T *W;
+    int64_t ldw;
+    char *wt;
+    int32_t n_out, n_in, slabs, cols_log;
+};
+constexpr int kTurn = 64;       // channels of a block of W, by one slab's outputs
+
+// a chunk of eight values as bf16, or as its three terms
+__device__ __forceinline__ void store_planes(char *at, int64_t plane, const float (&v)[kChunk], float) {
+    uint32_t w[3][4];
+#pragma unroll
+    for (int e = 0; e < kChunk; ++e) {
+        uint16_t t[3];
+        split3(v[e], t);
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+            w[q][e / 2] = e & 1 ? w[q][e / 2] | (uint32_t)t[q] << 16 : t[q];
     }
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+        *(u32x4 *)(at + q * plane) = u32x4{w[q][0], w[q][1], w[q][2], w[q][3]};
+}
+__device__ __forceinline__ void store_planes(char *at, int64_t, const float (&v)[kChunk], uint16_t) {
+    *(u32x4 *)at = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
 }
 
-// planes of W's transpose [n_in][n_out], blocked, zero beyond n_out
 template <typename T>
-__global__ void __launch_bounds__(kThreads) transpose_kernel(const T *__restrict__ W, int64_t ldw, int32_t n_out,
-                                                             int32_t n_in, char *__restrict__ out, int32_t slabs) {
-    const int64_t plane = blocked_bytes(n_in, slabs), pitch = (int64_t)slabs * (kSlabBytes / 2);
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n_in * pitch; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t k = i / pitch, j = i - k * pitch;
-        char *at = out + blocked_offset(k, 2 * j, slabs);
-        if constexpr (sizeof(T) == 4) {
-            uint16_t t[3] = {0, 0, 0};
-            if (j < n_out)
-                split3(W[j * ldw + k], t);
-            for (int q = 0; q < 3; ++q)
-                *(uint16_t *)(at + q * plane) = t[q];
-        } else {
-            *(uint16_t *)at = j < n_out ? W[j * ldw + k] : (uint16_t)0;
-        }
+__global__ void __launch_bounds__(kThreads) layout_kernel(LayoutArgs<T> p) {
+    __shared__ float tile[kSlabBytes / 2][kTurn + 1];
+    const int tid = threadIdx.x;
+    float v[kChunk];
+    if (blockIdx.x < p.row_blocks) {
+        const int col = tid & ((1 << p.cols_log) - 1), per = kThreads >> p.cols_log, chunks = (int)(p.pitch / kChunk);
+        for (int64_t r = (int64_t)blockIdx.x * per + (tid >> p.cols_log); r < p.rows; r += (int64_t)p.row_blocks * per)
+            for (int at = col; at < chunks; at += 1 << p.cols_log) {
+                load_chunk(p.dy + r * p.lddy + at * kChunk, p.n_out - at * kChunk, v);
+                store_planes((char *)(p.planes + r * p.pitch + at * kChunk), p.rows * p.pitch * 2, v, T{});
+            }
+        return;
+    }
+    const int id = (int)(blockIdx.x - p.row_blocks), slab = id % p.slabs, k0 = id / p.slabs * kTurn;
+    for (int i = tid; i < kSlabBytes / 2 * kTurn; i += kThreads) {
+        const int j = i / kTurn, k = i % kTurn, out = slab * (kSlabBytes / 2) + j;
+        tile[j][k] = out < p.n_out && k0 + k < p.n_in ? load_value(p.W + (int64_t)out * p.ldw + k0 + k) : 0.f;
+    }
+    __syncthreads();
+    const int k = tid / 4, c = tid % 4;      // eight outputs of a channel
+    if (k0 + k < p.n_in) {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e)
+            v[e] = tile[c * kChunk + e][k];
+        store_planes(p.wt + blocked_offset(k0 + k, slab * kSlabBytes + c * 16, p.slabs), blocked_bytes(p.n_in, p.slabs), v, T{});
     }
 }
 
@@ -132,9 +160,10 @@ struct DwArgs {
     int64_t g_pitch, g_width;   // bytes; columns from the width on read as 0
     int64_t g_plane;
     hpacml8_checkpoint c;
-    float *dw, *db;             // parts: dw [splits][n_out][n_in], db [splits][n_out]; NULL: not wanted
+    float *dw, *db;             // of the first part; NULL: not wanted
+    int64_t lddw, dw_part, db_part;   // pitch of dw, and from a part to the next
     int64_t rows_per_split;
-    int32_t n_out, planes;
+    int32_t n_out, planes, accumulate;
     uint32_t out_tiles, in_tiles;
 };
 
@@ -202,53 +231,75 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
 
     if (total > 0) {
         const uint32_t base = nt::lds_offset(lds);
-        // dy: the column that belongs where this lane's bytes of a load land
-        int g_row[T::kLoadsG], g_col[T::kLoadsG];
+        const int rows = (int)(to - from);
+        // dy: the row and column that belong where this lane's bytes of a load
+        // land; where there is no such row or column, zeros (a column past the
+        // last has a row past every last)
+        const char *g_at[T::kLoadsG];
+        int g_row[T::kLoadsG], g_plane = p.planes - 1;       // the smallest terms first
+        int64_t g_first[T::kLoadsG];
 #pragma unroll
         for (int i = 0; i < T::kLoadsG; ++i) {
             const int at = (i * T::kWaves + wave) * 1024 + lane * 16, row = at / T::kPitchG, chunk = at % T::kPitchG / 16;
             const int pair = (chunk >> 1) ^ T::template turn<T::kPitchG>(row);
-            g_row[i] = row;
-            g_col[i] = j0 * 2 + pair * 32 + ((chunk & 1) ^ T::swap(pair, row)) * 16;
+            const int col = j0 * 2 + pair * 32 + ((chunk & 1) ^ T::swap(pair, row)) * 16;
+            g_row[i] = col < p.g_width ? row : INT32_MAX;
+            g_first[i] = (from + row) * p.g_pitch + col;
+            g_at[i] = p.g + g_plane * p.g_plane + g_first[i];
         }
         // codes: this thread's row and 16 columns
         const int x_id = tid % T::kActive, x_row = x_id / (T::kB / 16), x_pair = x_id % (T::kB / 16);
         int x_col = k0 + x_pair * 16;
         x_col = x_col < (p.c.width + 31) / 32 * 32 ? x_col : 0;     // beyond the width: any codes
+        const int64_t x_first = min(from + x_row, to - 1);
+        const char *const codes_first = (const char *)p.c.codes + x_first * p.c.ld_codes + x_col;
+        const char *const exps_first = (const char *)p.c.exps + x_first * p.c.ld_exps + (x_col >> 5);
+        const char *codes_at = codes_first, *exps_at = exps_first;
         const int x_at = T::kAtX + T::template place<T::kPitchX>(x_row, x_pair, 0);
         const int x_other = T::kAtX + T::template place<T::kPitchX>(x_row, x_pair, 1);
 
-        // the slabs loaded next, past the end the last one again or zeros (so
-        // that every step has the same loads under way)
-        int g_slab = 0, g_plane = p.planes - 1, g_slot = 0, x_slab = 0, x_slot = 0;   // the smallest terms first
+        // What is loaded next, and how many rows are left there.  After the
+        // last slab come the next plane's, and after the last plane zeros and
+        // any codes: every step has the same loads under way.
+        int g_left = rows, g_slot = 0, x_left = rows, x_slot = 0;
         auto load_g = [&](int i) {
-            const int64_t r = from + (int64_t)g_slab * T::kRows + g_row[i];
-            const char *src = p.g + g_plane * p.g_plane + r * p.g_pitch + g_col[i];
-            nt::load_to_lds(nt::chosen(r < to && g_col[i] < p.g_width && g_plane >= 0, src), base + g_slot * T::kG + (i * T::kWaves + wave) * 1024);
+            nt::load_to_lds(nt::chosen(g_row[i] < g_left, g_at[i]), base + g_slot * T::kG + (i * T::kWaves + wave) * 1024);
         };
         auto next_g = [&]() {
             g_slot = g_slot + 1 == T::kRingG ? 0 : g_slot + 1;
-            if (++g_slab == slabs) {
-                g_slab = 0;
+            g_left -= T::kRows;
+#pragma unroll
+            for (int i = 0; i < T::kLoadsG; ++i)
+                g_at[i] += T::kRows * p.g_pitch;
+            if (g_left <= 0) {
                 --g_plane;
+                g_left = g_plane < 0 ? 0 : rows;
+#pragma unroll
+                for (int i = 0; i < T::kLoadsG; ++i)
+                    g_at[i] = p.g + g_plane * p.g_plane + g_first[i];
             }
         };
-        auto x_source = [&]() { return min(from + (int64_t)x_slab * T::kRows + x_row, to - 1); };
+        // (a row past the last reads the part's first again; it counts as zeros)
         auto load_codes = [&]() {
-            nt::load_to_lds((const uint8_t *)p.c.codes + x_source() * p.c.ld_codes + x_col,
-                            base + T::kAtCodes + x_slot * T::kCodes + wave * 1024);
+            nt::load_to_lds(x_row < x_left ? codes_at : codes_first, base + T::kAtCodes + x_slot * T::kCodes + wave * 1024);
         };
         auto load_exps = [&]() {
-            nt::load_byte_to_lds((const uint8_t *)p.c.exps + x_source() * p.c.ld_exps + (x_col >> 5),
-                                 base + T::kAtExps + x_slot * T::kExps + wave * 256);
+            nt::load_byte_to_lds(x_row < x_left ? exps_at : exps_first, base + T::kAtExps + x_slot * T::kExps + wave * 256);
         };
         auto next_x = [&]() {
             x_slot = x_slot + 1 == T::kRingCodes ? 0 : x_slot + 1;
-            x_slab = x_slab + 1 == slabs ? 0 : x_slab + 1;
+            x_left -= T::kRows;
+            codes_at += T::kRows * p.c.ld_codes;
+            exps_at += T::kRows * p.c.ld_exps;
+            if (x_left <= 0) {
+                x_left = rows;
+                codes_at = codes_first;
+                exps_at = exps_first;
+            }
         };
 
-        // codes to values: slab c_slab (its row may lie past the end: zeros)
-        int c_slab = 0, c_slot = 0, w_slot = 0;
+        // codes to values, zeros past the last row
+        int c_left = rows, c_slot = 0, w_slot = 0;
         u32x4 code;
         float scale;
         uint32_t word[8];
@@ -256,7 +307,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
             code = *(const u32x4 *)(lds + T::kAtCodes + c_slot * T::kCodes + tid * 16);
             uint32_t e = *(const uint32_t *)(lds + T::kAtExps + c_slot * T::kExps + tid * 4);
             asm("" : "+v"(e));                    // read it without a branch
-            scale = from + (int64_t)c_slab * T::kRows + x_row < to ? block_scale(e & 0xFFu) : 0.f;
+            scale = x_row < c_left ? block_scale(e & 0xFFu) : 0.f;
         };
         auto convert = [&](int e) {
             const uint32_t w = code[e / 2], q = w >> (16 * (e & 1));
@@ -271,7 +322,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
             }
             c_slot = c_slot + 1 == T::kRingCodes ? 0 : c_slot + 1;
             w_slot = w_slot + 1 == T::kRingX ? 0 : w_slot + 1;
-            c_slab = c_slab + 1 == slabs ? 0 : c_slab + 1;
+            c_left = c_left <= T::kRows ? rows : c_left - T::kRows;
         };
 
         // fragments
@@ -318,7 +369,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
                 }
 #pragma unroll
                 for (int t = 0; t < NA; ++t)
-                    acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now[t], b[(kFirst + u) & 3], acc[t][u], 0, 0, 0);
+                    acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[(kFirst + u) & 3], now[t], acc[t][u], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
             put();
@@ -384,6 +435,9 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
         }
         nt::wait_loads<0>();
     }
+    // acc[t][u]: channels 4 (lane / 16) + e of output lane % 16
+    float *dw = p.dw ? p.dw + part * p.dw_part : nullptr;
+    const bool four = ((uintptr_t)dw & 15) == 0 && p.lddw % 4 == 0;
 #pragma unroll
     for (int t = 0; t < NA; ++t) {
         if (sums) {
@@ -392,34 +446,69 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
             v += __shfl_xor(v, 16);
             v += __shfl_xor(v, 32);
             const int j = j0 + (wa * NA + t) * 16 + lane;
-            if (lane < 16 && j < p.n_out)
-                p.db[(int64_t)part * p.n_out + j] = v;
+            if (lane < 16 && j < p.n_out) {
+                float *to_db = p.db + part * p.db_part + j;
+                *to_db = p.accumulate ? *to_db + v : v;
+            }
         }
+        const int j = j0 + (wa * NA + t) * 16 + (lane & 15);
+        if (!dw || j >= p.n_out)
+            continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int j = j0 + (wa * NA + t) * 16 + (lane >> 4) * 4 + e;
-            if (p.dw && j < p.n_out) {
+        for (int u = 0; u < NB; ++u) {
+            const int k = k0 + (wb * NB + u) * 16 + (lane >> 4) * 4;
+            float *out = dw + j * p.lddw + k;
+            f32x4 v = acc[t][u];
+            if (four && k + 4 <= p.c.width) {
+                *(f32x4 *)out = p.accumulate ? *(const f32x4 *)out + v : v;
+            } else {
 #pragma unroll
-                for (int u = 0; u < NB; ++u) {
-                    const int k = k0 + (wb * NB + u) * 16 + (lane & 15);
-                    if (k < p.c.width)
-                        p.dw[((int64_t)part * p.n_out + j) * p.c.width + k] = acc[t][u][e];
-                }
+                for (int e = 0; e < 4; ++e)
+                    if (k + e < p.c.width)
+                        out[e] = p.accumulate ? out[e] + v[e] : v[e];
             }
         }
     }
 }
 
-// out [rows][ld] (+)= the sum over the parts of parts [splits][rows][width]
-__global__ void __launch_bounds__(kThreads) join_kernel(const float *__restrict__ parts, int32_t splits, int64_t rows,
-                                                        int64_t width, float *__restrict__ out, int64_t ld,
-                                                        int32_t accumulate) {
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * width; i += (int64_t)gridDim.x * kThreads) {
-        float v = 0.f;
-        for (int s = 0; s < splits; ++s)
-            v += parts[s * rows * width + i];
-        float *o = out + i / width * ld + i % width;
-        *o = accumulate ? *o + v : v;
+// dw [n_out][lddw] and db [n_out] (+)= the sums over their parts, which lie
+// after one another; four at a time where rows keep the alignment (FOUR).
+struct JoinArgs {
+    const float *dw_parts, *db_parts;
+    float *dw, *db;               // NULL: not wanted
+    int64_t lddw;
+    int32_t splits, n_out, n_in, accumulate;
+};
+template <typename V>
+__device__ __forceinline__ V sum_of_parts(const V *p, int splits, int64_t apart) {
+    V v = {};
+    int s = 0;
+    for (; s + 8 <= splits; s += 8) {
+        V w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = p[(s + i) * apart];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v += w[i];
+    }
+    for (; s < splits; ++s)
+        v += p[s * apart];
+    return v;
+}
+template <typename V>
+__global__ void __launch_bounds__(kThreads) join_kernel(JoinArgs p) {
+    constexpr int kPer = sizeof(V) / 4;
+    const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x, step = (int64_t)gridDim.x * kThreads;
+    const int64_t row = p.n_in / kPer, all = p.dw ? p.n_out * row : 0;
+    for (int64_t i = first; i < all; i += step) {
+        const V v = sum_of_parts((const V *)p.dw_parts + i, p.splits, (int64_t)p.n_out * row);
+        V *o = (V *)(p.dw + i / row * p.lddw) + i % row;
+        *o = p.accumulate ? *o + v : v;
+    }
+    for (int64_t i = first; p.db && i < p.n_out; i += step) {
+        const float v = sum_of_parts(p.db_parts + i, p.splits, p.n_out);
+        p.db[i] = p.accumulate ? p.db[i] + v : v;
     }
 }
 
@@ -436,6 +525,41 @@ int dw_tile(int32_t n_out, int32_t n_in) {
     return n_out <= 64 || n_in <= 64 ? 64 : tiles_of(n_out, n_in, 256) < 16 ? 128 : 256;
 }
 
+// Parts of the rows: more of them shorten the blocks' loops and lengthen the
+// join.  A slab of 32 rows takes a block about 0.5 us, a part of dw (written,
+// read) n_out * n_in * 8 bytes at about 4 TB/s: the square root of their ratio
+// is where the sum is least.  At most as many as the chip holds at once: a
+// block of the largest tile fills a CU's LDS, two of the middle one and three
+// of the smallest do.
+int64_t dw_splits(int64_t rows, int32_t n_out, int32_t n_in, int tile, int planes) {
+    const int64_t slabs = (rows + 31) / 32, tiles = tiles_of(n_out, n_in, tile);
+    const int64_t most = (tile == 256 ? 256 : tile == 128 ? 512 : 768) / tiles;
+    const double join_us = 0.05 + (double)n_out * n_in * 8 / 4e6;
+    int64_t s = (int64_t)(std::sqrt((double)slabs * planes * 0.5 / join_us) + 0.5);
+    s = s < most ? s : most;
+    s = s < slabs ? s : slabs;
+    return s < 1 ? 1 : s;
+}
+
+// log2 of the chunks a row of a block of threads covers: 4 .. 256
+int cols_log(int64_t chunks) {
+    int l = 2;
+    while (((int64_t)1 << l) < chunks && (1 << l) < kThreads)
+        ++l;
+    return l;
+}
+
+template <typename T>
+void launch_layout(const Backward8Args &a, const Backward8Plan &p, uint16_t *planes, char *wt, hipStream_t st) {
+    LayoutArgs<T> l{(const T *)a.dy, a.lddy, p.direct ? 0 : a.c.rows, p.pitch, planes, 0, (const T *)a.W, a.ldw, wt, a.n_out,
+                    a.c.width, p.slabs, cols_log(p.pitch / kChunk)};
+    const int64_t per = kThreads >> l.cols_log, blocks = (l.rows + per - 1) / per;
+    l.row_blocks = (uint32_t)(blocks < 8192 ? blocks : 8192);
+    const uint32_t turn = a.dx ? (uint32_t)((a.c.width + kTurn - 1) / kTurn * p.slabs) : 0;
+    if (l.row_blocks + turn > 0)
+        layout_kernel<T><<<l.row_blocks + turn, kThreads, 0, st>>>(l);
+}
+
 template <typename X, int WA, int WB, int NA, int NB>
 void launch_dx_tile(DxArgs d, hipStream_t st) {
     typedef nt::Product<nt::Bf16, X, false, WA, WB, NA, NB> T;
@@ -447,12 +571,12 @@ void launch_dx_tile(DxArgs d, hipStream_t st) {
 
 template <typename X>
 void launch_dx(const DxArgs &d, hipStream_t st) {
-    if (tiles_of(d.g.rows, d.n_in, 256) >= 512 && d.wt.width >= 2048)
-        launch_dx_tile<X, 4, 2, 4, 8>(d, st);
-    else if (tiles_of(d.g.rows, d.n_in, 128) >= 256 && d.n_in > 64)
-        launch_dx_tile<X, 2, 2, 4, 4>(d, st);
-    else
-        launch_dx_tile<X, 2, 2, 2, 2>(d, st);
+    switch (nt::tile_for(d.n_in, d.g.rows, d.wt.width / kSlabBytes * (d.terms * (d.terms + 1) / 2))) {
+    case nt::Size::k64x64: return launch_dx_tile<X, 2, 2, 2, 2>(d, st);
+    case nt::Size::k128x128: return launch_dx_tile<X, 2, 2, 4, 4>(d, st);
+    case nt::Size::k128x256: return launch_dx_tile<X, 2, 4, 4, 4>(d, st);
+    case nt::Size::k256x256: return launch_dx_tile<X, 4, 2, 4, 8>(d, st);
+    }
 }
 
 template <bool RELU>
@@ -471,20 +595,16 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
                              bool want_dw, bool want_dx) {
     Backward8Plan p{};
     p.planes = dtype == HPACML_F32 ? 3 : 1;
-    p.direct = dtype == HPACML_BF16 && ((uintptr_t)dy & 15) == 0 && lddy % 8 == 0 && lddy < (1 << 22) && n_out % 32 == 0;
+    // dw reads whole 16-byte chunks of dy's rows, dx whole slabs, both with 32-bit offsets in a tile
+    p.direct = dtype == HPACML_BF16 && ((uintptr_t)dy & 15) == 0 && lddy % 8 == 0 && lddy < (1 << 22) &&
+               n_out % (want_dx ? 32 : 8) == 0;
     p.slabs = (int32_t)slabs_of(2 * n_out);
     p.pitch = (int64_t)p.slabs * (kSlabBytes / 2);
     p.tile = dw_tile(n_out, c.width);
     p.splits = 1;
     if (want_dw) {
-        // one round of the chip: a block of the largest tile fills a CU's LDS,
-        // two of the middle one and three of the smallest do
-        const int64_t tiles = tiles_of(n_out, c.width, p.tile), least = p.tile == 64 ? 256 : 512;
-        int64_t splits = (p.tile == 256 ? 256 : p.tile == 128 ? 512 : 768) / tiles;
-        const int64_t most = c.rows / least;
-        splits = splits < most ? splits : most;
-        splits = splits < 1 ? 1 : splits;
-        p.rows_per_split = ((c.rows + splits - 1) / splits + 63) / 64 * 64;
+        const int64_t splits = dw_splits(c.rows, n_out, c.width, p.tile, p.planes);
+        p.rows_per_split = ((c.rows + splits - 1) / splits + 31) / 32 * 32;
         p.splits = p.rows_per_split ? (int32_t)((c.rows + p.rows_per_split - 1) / p.rows_per_split) : 1;
     }
     size_t at = 0;
@@ -495,10 +615,10 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
     if (want_dx)
         at += whole((size_t)p.planes * blocked_bytes(c.width, p.slabs));
     p.off_dw = at;
-    if (want_dw)
+    if (want_dw && p.splits > 1)
         at += whole((size_t)p.splits * n_out * c.width * 4);
     p.off_db = at;
-    if (want_dw)
+    if (want_dw && p.splits > 1)
         at += whole((size_t)p.splits * n_out * 4);
     p.bytes = at;
     return p;
@@ -509,18 +629,12 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
     const bool f32 = a.dtype == HPACML_F32;
     uint16_t *planes = (uint16_t *)(a.scratch + p.off_dy);
     char *wt = a.scratch + p.off_wt;
+    if (rows > 0)
+        f32 ? launch_layout<float>(a, p, planes, wt, st) : launch_layout<uint16_t>(a, p, planes, wt, st);
     nt::Operand g{(const char *)planes, rows, p.pitch * 2, p.pitch * 2, rows * p.pitch * 2};
     if (p.direct)
         g = {(const char *)a.dy, rows, a.lddy * 2, (int64_t)a.n_out * 2, 0};
-    else if (rows > 0 && f32)
-        planes_kernel<float><<<blocks_for(rows * p.pitch), kThreads, 0, st>>>((const float *)a.dy, a.lddy, rows, a.n_out, planes, p.pitch);
-    else if (rows > 0)
-        planes_kernel<uint16_t><<<blocks_for(rows * p.pitch), kThreads, 0, st>>>((const uint16_t *)a.dy, a.lddy, rows, a.n_out, planes, p.pitch);
     if (a.dx && rows > 0) {
-        if (f32)
-            transpose_kernel<float><<<blocks_for(a.c.width * p.pitch), kThreads, 0, st>>>((const float *)a.W, a.ldw, a.n_out, a.c.width, wt, p.slabs);
-        else
-            transpose_kernel<uint16_t><<<blocks_for(a.c.width * p.pitch), kThreads, 0, st>>>((const uint16_t *)a.W, a.ldw, a.n_out, a.c.width, wt, p.slabs);
         DxArgs d{};
         d.wt = {wt, a.c.width, (int64_t)p.slabs * 1024, (int64_t)p.slabs * kSlabBytes, blocked_bytes(a.c.width, p.slabs)};
         d.g = g;
@@ -530,34 +644,36 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
         d.lddx = a.lddx;
         d.n_in = a.c.width;
         d.terms = p.planes;
-        if (f32)
-            launch_dx<float>(d, st);
-        else
-            launch_dx<uint16_t>(d, st);
+        f32 ? launch_dx<float>(d, st) : launch_dx<uint16_t>(d, st);
     }
     if (a.dw || a.db) {
+        const bool join = p.splits > 1;
         DwArgs d{};
         d.g = g.base;
         d.g_pitch = g.pitch;
         d.g_width = g.width;
         d.g_plane = g.plane;
         d.c = a.c;
-        d.dw = a.dw ? (float *)(a.scratch + p.off_dw) : nullptr;
-        d.db = a.db ? (float *)(a.scratch + p.off_db) : nullptr;
+        d.dw = join && a.dw ? (float *)(a.scratch + p.off_dw) : a.dw;
+        d.db = join && a.db ? (float *)(a.scratch + p.off_db) : a.db;
+        d.lddw = join ? a.c.width : a.lddw;
+        d.dw_part = (int64_t)a.n_out * a.c.width;
+        d.db_part = a.n_out;
+        d.accumulate = join ? 0 : a.accumulate;
         d.rows_per_split = p.rows_per_split;
         d.n_out = a.n_out;
         d.planes = p.planes;
         d.out_tiles = (uint32_t)((a.n_out + p.tile - 1) / p.tile);
         d.in_tiles = a.dw ? (uint32_t)((a.c.width + p.tile - 1) / p.tile) : 1;
         const uint32_t blocks = d.out_tiles * d.in_tiles * p.splits;
-        if (a.c.act == HPACML_ACT_RELU)
-            launch_dw<true>(d, blocks, p.tile, st);
-        else
-            launch_dw<false>(d, blocks, p.tile, st);
-        if (d.dw)
-            join_kernel<<<blocks_for((int64_t)a.n_out * a.c.width), kThreads, 0, st>>>(d.dw, p.splits, a.n_out, a.c.width, a.dw, a.lddw, a.accumulate);
-        if (d.db)
-            join_kernel<<<blocks_for(a.n_out), kThreads, 0, st>>>(d.db, p.splits, 1, a.n_out, a.db, a.n_out, a.accumulate);
+        a.c.act == HPACML_ACT_RELU ? launch_dw<true>(d, blocks, p.tile, st) : launch_dw<false>(d, blocks, p.tile, st);
+        if (join) {
+            const JoinArgs j{d.dw, d.db, a.dw, a.db, a.lddw, p.splits, a.n_out, a.c.width, a.accumulate};
+            if (a.c.width % 4 == 0 && ((uintptr_t)a.dw & 15) == 0 && a.lddw % 4 == 0)
+                join_kernel<f32x4><<<blocks_for((int64_t)a.n_out * a.c.width / 4), kThreads, 0, st>>>(j);
+            else
+                join_kernel<float><<<blocks_for((int64_t)a.n_out * a.c.width), kThreads, 0, st>>>(j);
+        }
     }
     return hipGetLastError();
 }

@@ -145,6 +145,27 @@ struct Tiles {
 // chip's 256 CUs at most.
 inline uint32_t blocks_for_tiles(int64_t tiles, int per_cu) { return (uint32_t)(tiles < 256 * per_cu ? tiles : 256 * per_cu); }
 
+// The tile (outputs x points) of a product: the largest that leaves no CU
+// without one, by these times (us, 8-bit products):
+//   rows x out <- in       64 x 64  128 x 128  128 x 256  256 x 256
+//   4096 x 256 <- 256          4.6        7.5        8.1       13.8
+//   262144 x 64 <- 64         15.0       23.0       18.5       35.0
+//   4096 x 1024 <- 1024       11.7       10.9       12.5       20.5
+//   1024 x 4096 <- 4096       29.1       23.5       29.5       46.9
+//   65536 x 256 <- 256        17.9       15.8       13.8       15.1
+//   16384 x 512 <- 512        14.0       11.6       10.5       16.6
+//   16384 x 1024 <- 1024      37.0       26.8       24.0       23.3
+//   4096 x 4096 <- 4096      109.0       70.7       73.3       59.4
+//   65536 x 4096 <- 4096      2620       1280       1026        899
+enum class Size { k64x64, k128x128, k128x256, k256x256 };
+inline Size tile_for(int64_t n_out, int64_t rows, int64_t slabs) {
+    auto tiles = [&](int64_t outs, int64_t points) { return (n_out + outs - 1) / outs * ((rows + points - 1) / points); };
+    return n_out <= 64 || tiles(64, 64) <= 512               ? Size::k64x64
+           : tiles(128, 128) <= 256                          ? Size::k128x128
+           : tiles(256, 256) >= 200 && slabs >= 16           ? Size::k256x256
+                                                             : Size::k128x256;
+}
+
 // Blocks of WA x WB waves, each NA x NB tiles of 16 x 16; results of type Y.
 // A is blocked, B is if BLOCKED_B, and comes in rows otherwise.
 template <typename Mma, typename Y, bool BLOCKED_B, int WA, int WB, int NA, int NB>

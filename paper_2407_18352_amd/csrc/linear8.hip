@@ -174,28 +174,14 @@ void launch_few(const Linear8Args &a, hipStream_t stream) {
 
 template <typename Y>
 void launch_product(const Linear8Args &a, hipStream_t stream) {
-    auto tiles = [&](int64_t outs, int64_t points) { return (a.n_out + outs - 1) / outs * ((a.rows + points - 1) / points); };
     if (a.rows <= kFewPoints)
-        launch_few<float, Y, false>(a, stream);   // x is not read
-    // the largest tile that leaves no CU without one (us, 8-bit outputs <- inputs):
-    //   rows x out <- in       64 x 64  128 x 128  128 x 256  256 x 256
-    //   4096 x 256 <- 256          4.6        7.5        8.1       13.8
-    //   262144 x 64 <- 64         15.0       23.0       18.5       35.0
-    //   4096 x 1024 <- 1024       11.7       10.9       12.5       20.5
-    //   1024 x 4096 <- 4096       29.1       23.5       29.5       46.9
-    //   65536 x 256 <- 256        17.9       15.8       13.8       15.1
-    //   16384 x 512 <- 512        14.0       11.6       10.5       16.6
-    //   16384 x 1024 <- 1024      37.0       26.8       24.0       23.3
-    //   4096 x 4096 <- 4096      109.0       70.7       73.3       59.4
-    //   65536 x 4096 <- 4096      2620       1280       1026        899
-    else if (a.n_out <= 64 || tiles(64, 64) <= 512)
-        launch_tile<Y, 2, 2, 2, 2>(a, stream);
-    else if (tiles(128, 128) <= 256)
-        launch_tile<Y, 2, 2, 4, 4>(a, stream);
-    else if (tiles(256, 256) >= 200 && a.slabs >= 16)
-        launch_tile<Y, 4, 2, 4, 8>(a, stream);
-    else
-        launch_tile<Y, 2, 4, 4, 4>(a, stream);
+        return launch_few<float, Y, false>(a, stream);   // x is not read
+    switch (nt::tile_for(a.n_out, a.rows, a.slabs)) {
+    case nt::Size::k64x64: return launch_tile<Y, 2, 2, 2, 2>(a, stream);
+    case nt::Size::k128x128: return launch_tile<Y, 2, 2, 4, 4>(a, stream);
+    case nt::Size::k128x256: return launch_tile<Y, 2, 4, 4, 4>(a, stream);
+    case nt::Size::k256x256: return launch_tile<Y, 4, 2, 4, 8>(a, stream);
+    }
 }
 
 template <typename X, typename Y>
