@@ -185,7 +185,7 @@ struct DwTile {
     static __device__ __forceinline__ int turn(int row) {
         return ((row & 3) | ((row >> 1) & 4)) & (PITCH / 32 - 1);
     }
-    static __device__ __forceinline__ int swap(int pair, int row) { return ((pair >> 3) + row) & 1; }
+    static __device__ __forceinline__ int swap(int pair, int row) { return ((pair >> 2) + row) & 1; }
     // byte of a slab where column pair `pair`, chunk `half` of `row` is stored
     template <int PITCH>
     static __device__ __forceinline__ int place(int row, int pair, int half) {

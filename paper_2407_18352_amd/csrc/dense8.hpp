@@ -14,7 +14,7 @@ namespace hpacml {
 constexpr int kSlabBytes = 64;
 constexpr int64_t slabs_of(int64_t bytes) { return (bytes + kSlabBytes - 1) / kSlabBytes; }
 constexpr int64_t blocked_bytes(int64_t rows, int64_t slabs) { return (rows + 15) / 16 * slabs * 1024; }
-__host__ __device__ constexpr int chunk_turn(int row) { return (row >> 2) & 3; }
+__host__ __device__ constexpr int chunk_turn(int row) { return (row >> 1) & 3; }
 // of byte k of a row
 __host__ __device__ constexpr int64_t blocked_offset(int64_t row, int64_t k, int64_t slabs) {
     return ((row >> 4) * slabs + (k >> 6)) * 1024 + (row & 15) * kSlabBytes + ((((int)(k >> 4) & 3) ^ chunk_turn((int)row)) * 16) + (k & 15);
