@@ -68,10 +68,15 @@ __global__ void __launch_bounds__(kThreads) layout_kernel(LayoutArgs<T> p) {
         return;
     }
     const int id = (int)(blockIdx.x - p.row_blocks), slab = id % p.slabs, k0 = id / p.slabs * kTurn;
-    for (int i = tid; i < kSlabBytes / 2 * kTurn; i += kThreads) {
-        const int j = i / kTurn, k = i % kTurn, out = slab * (kSlabBytes / 2) + j;
-        tile[j][k] = out < p.n_out && k0 + k < p.n_in ? load_value(p.W + (int64_t)out * p.ldw + k0 + k) : 0.f;
+    float w[kSlabBytes / 2 * kTurn / kThreads];
+#pragma unroll
+    for (int n = 0; n < kSlabBytes / 2 * kTurn / kThreads; ++n) {
+        const int i = n * kThreads + tid, out = slab * (kSlabBytes / 2) + i / kTurn, k = k0 + i % kTurn;
+        w[n] = out < p.n_out && k < p.n_in ? load_value(p.W + (int64_t)out * p.ldw + k) : 0.f;
     }
+#pragma unroll
+    for (int n = 0; n < kSlabBytes / 2 * kTurn / kThreads; ++n)
+        tile[(n * kThreads + tid) / kTurn][tid % kTurn] = w[n];
     __syncthreads();
     const int k = tid / 4, c = tid % 4;      // eight outputs of a channel
     if (k0 + k < p.n_in) {
@@ -167,17 +172,21 @@ struct DwArgs {
     uint32_t out_tiles, in_tiles;
 };
 
-template <int WA, int WB, int NA, int NB>
+// PL: planes of dy that a slab takes at once.  Three at once convert the codes
+// once and have three times as much under way, but the largest tile has no
+// room for them in LDS and goes through the rows once for each.
+template <int PL, int WA, int WB, int NA, int NB>
 struct DwTile {
     static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRows = 32;
     static constexpr int kA = 16 * NA * WA, kB = 16 * NB * WB;          // outputs, channels
     static constexpr int kPitchG = 2 * kA, kPitchX = 2 * kB;            // bytes of an LDS row
-    static constexpr int kG = kRows * kPitchG, kX = kRows * kPitchX;    // one slab's
+    static constexpr int kPlane = kRows * kPitchG, kG = PL * kPlane, kX = kRows * kPitchX;    // one slab's
     static constexpr int kRingG = 4, kRingX = 3, kRingCodes = 4;
     static constexpr int kCodes = kThreads * 16, kExps = kThreads * 4;  // 16 codes and an exponent per thread
     static constexpr int kAtX = kRingG * kG, kAtCodes = kAtX + kRingX * kX, kAtExps = kAtCodes + kRingCodes * kCodes;
     static constexpr int kLds = kAtExps + kRingCodes * kExps;
-    static constexpr int kLoadsG = kG / (1024 * kWaves), kLoads = kLoadsG + 2;
+    static constexpr int kLoadsG = kG / (1024 * kWaves), kLoads = kLoadsG + 2;   // direct loads of a wave
+    static constexpr int kPerCu = 160 * 1024 / kLds;
     static constexpr int kActive = kRows * kB / 16;                     // threads with codes of their own
     static_assert(kLoadsG >= 1 && kActive <= kThreads && kLds <= 160 * 1024, "shares of a slab");
 
@@ -210,9 +219,9 @@ struct DwTile {
     }
 };
 
-template <bool RELU, int WA, int WB, int NA, int NB>
+template <bool RELU, int PL, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
-    typedef DwTile<WA, WB, NA, NB> T;
+    typedef DwTile<PL, WA, WB, NA, NB> T;
     __shared__ __align__(1024) char lds[T::kLds];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa = wave / WB, wb = wave % WB;
@@ -223,7 +232,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
     const uint32_t part = id / tiles, tile = id - part * tiles;
     const int j0 = (int)(tile / p.in_tiles) * T::kA, k0 = (int)(tile % p.in_tiles) * T::kB;
     const int64_t from = part * p.rows_per_split, to = min(from + p.rows_per_split, p.c.rows);
-    const int slabs = to > from ? (int)((to - from + T::kRows - 1) / T::kRows) : 0, total = slabs * p.planes;
+    const int slabs = to > from ? (int)((to - from + T::kRows - 1) / T::kRows) : 0, total = slabs * (p.planes / PL);
 
     f32x4 acc[NA][NB] = {};
     float sum[NA] = {};
@@ -236,15 +245,15 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
         // land; where there is no such row or column, zeros (a column past the
         // last has a row past every last)
         const char *g_at[T::kLoadsG];
-        int g_row[T::kLoadsG], g_plane = p.planes - 1;       // the smallest terms first
+        int g_row[T::kLoadsG], g_plane = p.planes - PL;      // (the first of PL) the smallest terms first
         int64_t g_first[T::kLoadsG];
 #pragma unroll
         for (int i = 0; i < T::kLoadsG; ++i) {
-            const int at = (i * T::kWaves + wave) * 1024 + lane * 16, row = at / T::kPitchG, chunk = at % T::kPitchG / 16;
+            const int at = (i * T::kWaves + wave) * 1024 + lane * 16, row = at % T::kPlane / T::kPitchG, chunk = at % T::kPitchG / 16;
             const int pair = (chunk >> 1) ^ T::template turn<T::kPitchG>(row);
             const int col = j0 * 2 + pair * 32 + ((chunk & 1) ^ T::swap(pair, row)) * 16;
             g_row[i] = col < p.g_width ? row : INT32_MAX;
-            g_first[i] = (from + row) * p.g_pitch + col;
+            g_first[i] = at / T::kPlane * p.g_plane + (from + row) * p.g_pitch + col;
             g_at[i] = p.g + g_plane * p.g_plane + g_first[i];
         }
         // codes: this thread's row and 16 columns
@@ -272,7 +281,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
             for (int i = 0; i < T::kLoadsG; ++i)
                 g_at[i] += T::kRows * p.g_pitch;
             if (g_left <= 0) {
-                --g_plane;
+                g_plane -= PL;
                 g_left = g_plane < 0 ? 0 : rows;
 #pragma unroll
                 for (int i = 0; i < T::kLoadsG; ++i)
@@ -333,13 +342,13 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
 #pragma unroll
         for (int u = 0; u < NB; ++u)
             b_at[u] = T::kAtX + T::template fragment_at<T::kPitchX>(wb * NB + u, lane);
-        bf16x8 a[2][NA], b[4];
-        auto read_a = [&](int t) { return T::template fragment<T::kPitchG>(lds + a_at[t] + a_slot * T::kG); };
+        bf16x8 a[2][PL * NA], b[4];      // a: plane by plane
+        auto read_a = [&](int t) { return T::template fragment<T::kPitchG>(lds + a_at[t % NA] + t / NA * T::kPlane + a_slot * T::kG); };
         auto read_b = [&](int u, int slot) { return T::template fragment<T::kPitchX>(lds + b_at[u] + slot * T::kX); };
         auto next_slot = [](int slot, int ring) { return slot + 1 == ring ? 0 : slot + 1; };
 
         // first: the place in `b` of the slab's first fragment
-        auto step = [&](auto first, const bf16x8 (&now)[NA], bf16x8 (&next)[NA]) {
+        auto step = [&](auto first, const bf16x8 (&now)[PL * NA], bf16x8 (&next)[PL * NA]) {
             constexpr int kFirst = decltype(first)::value;
             nt::wait_loads<2 * T::kLoads>();      // what the step before the last two asked for
             nt::barrier();
@@ -349,7 +358,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
                 // fragments two tiles ahead; past the last, the next slab's first
                 b[(kFirst + u + 2) & 3] = u + 2 < NB ? read_b(u + 2, b_slot) : read_b(u + 2 - NB, after);
 #pragma unroll
-                for (int t = u * NA / NB; t < (u + 1) * NA / NB; ++t)
+                for (int t = u * PL * NA / NB; t < (u + 1) * PL * NA / NB; ++t)
                     next[t] = read_a(t);
                 if (u == 0)
                     take();
@@ -368,22 +377,22 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
                         load_exps();
                 }
 #pragma unroll
-                for (int t = 0; t < NA; ++t)
-                    acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[(kFirst + u) & 3], now[t], acc[t][u], 0, 0, 0);
+                for (int t = PL * NA - 1; t >= 0; --t)
+                    acc[t % NA][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[(kFirst + u) & 3], now[t], acc[t % NA][u], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
             put();
             if (sums) {
                 // eight rows at a time, so that few roundings follow one another
 #pragma unroll
-                for (int t = 0; t < NA; ++t) {
+                for (int t = PL * NA - 1; t >= 0; --t) {
                     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
                     const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
                     float v = 0.f;
 #pragma unroll
                     for (int e = 0; e < 8; e += 2)
                         v = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{now[t][e], now[t][e + 1]}, ones, v, false);
-                    sum[t] += v;
+                    sum[t % NA] += v;
                 }
             }
             next_g();
@@ -422,7 +431,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
         nt::wait_loads<63>();
         nt::barrier();
 #pragma unroll
-        for (int t = 0; t < NA; ++t)
+        for (int t = 0; t < PL * NA; ++t)
             a[0][t] = read_a(t);
         a_slot = 1;
         b[0] = read_b(0, 0);
@@ -479,36 +488,58 @@ struct JoinArgs {
     int64_t lddw;
     int32_t splits, n_out, n_in, accumulate;
 };
-template <typename V>
-__device__ __forceinline__ V sum_of_parts(const V *p, int splits, int64_t apart) {
-    V v = {};
-    int s = 0;
-    for (; s + 8 <= splits; s += 8) {
-        V w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            w[i] = p[(s + i) * apart];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v += w[i];
-    }
-    for (; s < splits; ++s)
-        v += p[s * apart];
-    return v;
-}
-template <typename V>
+// V: four values where rows keep the alignment, or one.  PARTS threads share a
+// sum where there are many parts: each adds every PARTS-th, and the first adds
+// theirs (always in the same order).
+template <typename V, int PARTS>
 __global__ void __launch_bounds__(kThreads) join_kernel(JoinArgs p) {
-    constexpr int kPer = sizeof(V) / 4;
-    const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x, step = (int64_t)gridDim.x * kThreads;
-    const int64_t row = p.n_in / kPer, all = p.dw ? p.n_out * row : 0;
-    for (int64_t i = first; i < all; i += step) {
-        const V v = sum_of_parts((const V *)p.dw_parts + i, p.splits, (int64_t)p.n_out * row);
-        V *o = (V *)(p.dw + i / row * p.lddw) + i % row;
-        *o = p.accumulate ? *o + v : v;
+    constexpr int kPer = sizeof(V) / 4, kSums = kThreads / PARTS;
+    __shared__ V share[PARTS][kSums];
+    const int lane = threadIdx.x % kSums, first = threadIdx.x / kSums;
+    auto total = [&](auto *parts, int64_t i, int64_t all) {
+        typedef std::remove_cv_t<std::remove_reference_t<decltype(*parts)>> T;
+        T v = {};
+        if (i < all) {
+            const T *at = parts + i;
+            int s = first;
+            for (; s + 3 * PARTS < p.splits; s += 4 * PARTS) {
+                T w[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    w[n] = at[(s + n * PARTS) * all];
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    v += w[n];
+            }
+            for (; s < p.splits; s += PARTS)
+                v += at[s * all];
+        }
+        if (PARTS > 1) {
+            T(*to)[kSums] = (T(*)[kSums])share;
+            __syncthreads();
+            to[first][lane] = v;
+            __syncthreads();
+            if (first == 0)
+#pragma unroll
+                for (int n = 1; n < PARTS; ++n)
+                    v += to[n][lane];
+        }
+        return v;
+    };
+    const int64_t row = p.n_in / kPer, all = p.dw ? p.n_out * row : 0, step = (int64_t)gridDim.x * kSums;
+    for (int64_t i0 = (int64_t)blockIdx.x * kSums; i0 < all; i0 += step) {
+        const int64_t i = i0 + lane;
+        const V v = total((const V *)p.dw_parts, i, all);
+        if (first == 0 && i < all) {
+            V *o = (V *)(p.dw + i / row * p.lddw) + i % row;
+            *o = p.accumulate ? *o + v : v;
+        }
     }
-    for (int64_t i = first; p.db && i < p.n_out; i += step) {
-        const float v = sum_of_parts(p.db_parts + i, p.splits, p.n_out);
-        p.db[i] = p.accumulate ? p.db[i] + v : v;
+    for (int64_t i0 = (int64_t)blockIdx.x * kSums; p.db && i0 < p.n_out; i0 += step) {
+        const int64_t i = i0 + lane;
+        const float v = total(p.db_parts, i, p.n_out);
+        if (first == 0 && i < p.n_out)
+            p.db[i] = p.accumulate ? p.db[i] + v : v;
     }
 }
 
@@ -518,27 +549,43 @@ dim3 blocks_for(int64_t items) {
 }
 size_t whole(size_t b) { return (b + 255) / 256 * 256; }
 
-int64_t tiles_of(int64_t a, int64_t b, int64_t tile) { return (a + tile - 1) / tile * ((b + tile - 1) / tile); }
+// How dw is computed: the tile (outputs x channels), the planes at once, and
+// the parts of the rows.  More parts shorten the blocks' loops and lengthen the
+// join (a part of dw is written and read: n_out * n_in * 8 bytes at about 4.5
+// TB/s); at most as many as the chip holds at once.  The tile is the one whose
+// time is least by the times measured for a slab of 32 rows in a full chip, at
+// 131,072 rows: 1.10, 0.67, 0.68, 0.79 and 0.47 us (the larger tiles need
+// fewer of them), with three planes at once 1.9 and 0.9 us.
+struct DwTileTimes {
+    int outs, channels, planes, at_once;
+    double slab_us;
+};
+constexpr DwTileTimes kDwTiles[] = {{256, 256, 1, 256, 1.10}, {256, 128, 1, 256, 0.67}, {128, 256, 1, 256, 0.68},
+                                    {128, 128, 1, 512, 0.79}, {64, 64, 1, 768, 0.47},   {128, 128, 3, 256, 1.9},
+                                    {64, 64, 3, 512, 0.9}};
+constexpr double kStartUs = 4;     // until a block's first slabs are there; and of another launch
 
-// Tile of dw: the largest that a gradient of this size fills.
-int dw_tile(int32_t n_out, int32_t n_in) {
-    return n_out <= 64 || n_in <= 64 ? 64 : tiles_of(n_out, n_in, 256) < 16 ? 128 : 256;
-}
-
-// Parts of the rows: more of them shorten the blocks' loops and lengthen the
-// join.  A slab of 32 rows takes a block about 0.5 us, a part of dw (written,
-// read) n_out * n_in * 8 bytes at about 4 TB/s: the square root of their ratio
-// is where the sum is least.  At most as many as the chip holds at once: a
-// block of the largest tile fills a CU's LDS, two of the middle one and three
-// of the smallest do.
-int64_t dw_splits(int64_t rows, int32_t n_out, int32_t n_in, int tile, int planes) {
-    const int64_t slabs = (rows + 31) / 32, tiles = tiles_of(n_out, n_in, tile);
-    const int64_t most = (tile == 256 ? 256 : tile == 128 ? 512 : 768) / tiles;
-    const double join_us = 0.05 + (double)n_out * n_in * 8 / 4e6;
-    int64_t s = (int64_t)(std::sqrt((double)slabs * planes * 0.5 / join_us) + 0.5);
-    s = s < most ? s : most;
-    s = s < slabs ? s : slabs;
-    return s < 1 ? 1 : s;
+void choose_dw(int64_t rows, int32_t n_out, int32_t n_in, int planes, Backward8Plan *p) {
+    const double slabs = (double)((rows + 31) / 32), part_us = (double)n_out * n_in * 8 / 4.5e6;
+    double best = 0;
+    for (int i = 0; i < (int)(sizeof(kDwTiles) / sizeof(kDwTiles[0])); ++i) {
+        const DwTileTimes &t = kDwTiles[i];
+        if (t.planes > planes)
+            continue;
+        const double tiles = (double)((n_out + t.outs - 1) / t.outs) * ((n_in + t.channels - 1) / t.channels);
+        const double us = t.slab_us * (planes / t.planes), most = std::floor(t.at_once / tiles);
+        double splits = std::floor(std::sqrt(slabs * us / (part_us + 0.02)) + 0.5);
+        splits = std::fmax(1, std::fmin(splits, std::fmin(most, slabs)));
+        const double rounds = std::ceil(tiles * splits / t.at_once);
+        const double time = rounds * (kStartUs + std::ceil(slabs / splits) * us) + (splits > 1 ? kStartUs + splits * part_us : 0);
+        if (i == 0 || time < best) {
+            best = time;
+            p->tile = i;
+            p->splits = (int32_t)splits;
+        }
+    }
+    p->rows_per_split = ((rows + p->splits - 1) / p->splits + 31) / 32 * 32;
+    p->splits = p->rows_per_split ? (int32_t)((rows + p->rows_per_split - 1) / p->rows_per_split) : 1;
 }
 
 // log2 of the chunks a row of a block of threads covers: 4 .. 256
@@ -579,14 +626,34 @@ void launch_dx(const DxArgs &d, hipStream_t st) {
     }
 }
 
+template <bool RELU, int PL, int WA, int WB, int NA, int NB>
+void launch_dw_tile(DwArgs d, int splits, hipStream_t st) {
+    typedef DwTile<PL, WA, WB, NA, NB> T;
+    d.out_tiles = (uint32_t)((d.n_out + T::kA - 1) / T::kA);
+    d.in_tiles = d.dw ? (uint32_t)((d.c.width + T::kB - 1) / T::kB) : 1;
+    dw_kernel<RELU, PL, WA, WB, NA, NB><<<d.out_tiles * d.in_tiles * splits, T::kThreads, 0, st>>>(d);
+}
+
 template <bool RELU>
-void launch_dw(const DwArgs &d, uint32_t blocks, int tile, hipStream_t st) {
-    if (tile == 256)
-        dw_kernel<RELU, 4, 2, 4, 8><<<blocks, 512, 0, st>>>(d);
-    else if (tile == 128)
-        dw_kernel<RELU, 2, 2, 4, 4><<<blocks, 256, 0, st>>>(d);
+void launch_dw(const DwArgs &d, const Backward8Plan &p, hipStream_t st) {
+    switch (p.tile) {   // of kDwTiles
+    case 0: return launch_dw_tile<RELU, 1, 4, 2, 4, 8>(d, p.splits, st);
+    case 1: return launch_dw_tile<RELU, 1, 4, 2, 4, 4>(d, p.splits, st);
+    case 2: return launch_dw_tile<RELU, 1, 2, 4, 4, 4>(d, p.splits, st);
+    case 3: return launch_dw_tile<RELU, 1, 2, 2, 4, 4>(d, p.splits, st);
+    case 4: return launch_dw_tile<RELU, 1, 2, 2, 2, 2>(d, p.splits, st);
+    case 5: return launch_dw_tile<RELU, 3, 2, 2, 4, 4>(d, p.splits, st);
+    case 6: return launch_dw_tile<RELU, 3, 2, 2, 2, 2>(d, p.splits, st);
+    }
+}
+
+template <typename V>
+void launch_join(const JoinArgs &j, hipStream_t st) {
+    const int64_t sums = (int64_t)j.n_out * (j.n_in * 4 / (int)sizeof(V));
+    if (j.splits >= 16)
+        join_kernel<V, 16><<<blocks_for(sums * 16), kThreads, 0, st>>>(j);
     else
-        dw_kernel<RELU, 2, 2, 2, 2><<<blocks, 256, 0, st>>>(d);
+        join_kernel<V, 1><<<blocks_for(sums), kThreads, 0, st>>>(j);
 }
 
 }  // namespace
@@ -600,13 +667,9 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
                n_out % (want_dx ? 32 : 8) == 0;
     p.slabs = (int32_t)slabs_of(2 * n_out);
     p.pitch = (int64_t)p.slabs * (kSlabBytes / 2);
-    p.tile = dw_tile(n_out, c.width);
     p.splits = 1;
-    if (want_dw) {
-        const int64_t splits = dw_splits(c.rows, n_out, c.width, p.tile, p.planes);
-        p.rows_per_split = ((c.rows + splits - 1) / splits + 31) / 32 * 32;
-        p.splits = p.rows_per_split ? (int32_t)((c.rows + p.rows_per_split - 1) / p.rows_per_split) : 1;
-    }
+    if (want_dw)
+        choose_dw(c.rows, n_out, c.width, p.planes, &p);
     size_t at = 0;
     p.off_dy = at;
     if (!p.direct)
@@ -663,16 +726,13 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
         d.rows_per_split = p.rows_per_split;
         d.n_out = a.n_out;
         d.planes = p.planes;
-        d.out_tiles = (uint32_t)((a.n_out + p.tile - 1) / p.tile);
-        d.in_tiles = a.dw ? (uint32_t)((a.c.width + p.tile - 1) / p.tile) : 1;
-        const uint32_t blocks = d.out_tiles * d.in_tiles * p.splits;
-        a.c.act == HPACML_ACT_RELU ? launch_dw<true>(d, blocks, p.tile, st) : launch_dw<false>(d, blocks, p.tile, st);
+        a.c.act == HPACML_ACT_RELU ? launch_dw<true>(d, p, st) : launch_dw<false>(d, p, st);
         if (join) {
             const JoinArgs j{d.dw, d.db, a.dw, a.db, a.lddw, p.splits, a.n_out, a.c.width, a.accumulate};
             if (a.c.width % 4 == 0 && ((uintptr_t)a.dw & 15) == 0 && a.lddw % 4 == 0)
-                join_kernel<f32x4><<<blocks_for((int64_t)a.n_out * a.c.width / 4), kThreads, 0, st>>>(j);
+                launch_join<f32x4>(j, st);
             else
-                join_kernel<float><<<blocks_for((int64_t)a.n_out * a.c.width), kThreads, 0, st>>>(j);
+                launch_join<float>(j, st);
         }
     }
     return hipGetLastError();

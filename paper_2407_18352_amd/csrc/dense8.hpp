@@ -53,7 +53,7 @@ struct Backward8Plan {
     bool direct;          // dy is read in place
     int32_t slabs;        // of dy and of W's transpose along the outputs
     int64_t pitch;        // of dy's planes (elements)
-    int32_t tile;         // of dw
+    int32_t tile;         // of dw: which of the table in backward8.hip
     int32_t splits;       // parts of the rows that sum into dw apart
     int64_t rows_per_split;
     size_t off_dy, off_wt, off_dw, off_db, bytes;
