@@ -10,7 +10,8 @@ namespace hpacml {
 
 constexpr int kChunk = 8;
 
-// chunk at `p`, of which the first n values exist (the others become 0)
+// chunk at `p`, of which the first n values exist (the others become 0); n may
+// be negative, value n - 1 is the row's last in any case
 __device__ __forceinline__ void load_chunk(const float *p, int n, float (&v)[kChunk]) {
     if (n >= kChunk) {
         const f32x4 a = ((const f32x4_any *)p)[0], b = ((const f32x4_any *)p)[1];
@@ -22,7 +23,10 @@ __device__ __forceinline__ void load_chunk(const float *p, int n, float (&v)[kCh
     } else {
 #pragma unroll
         for (int e = 0; e < kChunk; ++e)
-            v[e] = e < n ? p[e] : 0.f;
+            v[e] = p[min(e, n - 1)];
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e)
+            v[e] = e < n ? v[e] : 0.f;
     }
 }
 __device__ __forceinline__ void load_chunk(const uint16_t *p, int n, float (&v)[kChunk]) {
@@ -36,7 +40,10 @@ __device__ __forceinline__ void load_chunk(const uint16_t *p, int n, float (&v)[
     } else {
 #pragma unroll
         for (int e = 0; e < kChunk; ++e)
-            v[e] = e < n ? bf16_bits_value(p[e]) : 0.f;
+            v[e] = bf16_bits_value(p[min(e, n - 1)]);
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e)
+            v[e] = e < n ? v[e] : 0.f;
     }
 }
 __device__ __forceinline__ void store_chunk(float *p, int n, const float (&v)[kChunk]) {
