@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) dx_kernel(DxArgs p) {
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
-                const typename T::Piece at = t.piece(b, i, a0, b0);
+                const auto at = t.piece(b, i, a0, b0);
                 if (p.codes && at.point < p.g.rows && at.out < p.n_in) {
                     const uint8_t *c = p.codes + at.point * p.ld_codes + at.out;
                     code[b][i] = sizeof(X) == 2 ? *(const uint2 *)c : uint2{*(const uint32_t *)c, 0u};

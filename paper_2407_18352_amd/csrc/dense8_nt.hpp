@@ -166,6 +166,66 @@ inline Size tile_for(int64_t n_out, int64_t rows, int64_t slabs) {
                                                              : Size::k128x256;
 }
 
+// A wave's results on their way out, as rows of Y, NA * 16 outputs of 16 points
+// at a time.  They are turned in LDS, so that the stores are 16-byte pieces of
+// long runs of a row, and bypass the caches (a later kernel reads them, if
+// any): 131,072 x 1024 -> 1024 in 8 bits took 146 us with a block per tile, 187
+// us without that, 227 us with stores as the matrix instruction leaves its
+// results.
+template <typename Y, int NA>
+struct Out {
+    static constexpr int kPer = 16 / sizeof(Y), kRow = NA * 16 * sizeof(Y), kChunks = kRow / 16;
+    // 16 bytes that a lane stores
+    struct Piece {
+        int64_t point, out;
+        int at;            // in the wave's part of LDS
+    };
+    // piece i of the 16 points from p0 on, of the outputs from a0 on
+    static __device__ __forceinline__ Piece piece(int lane, int i, int64_t a0, int64_t p0) {
+        const int at = i * 64 + lane, row = at / kChunks, c = at % kChunks;
+        return {p0 + row, a0 + c * kPer, row * kRow + ((c ^ (row & (kChunks - 1))) * 16)};
+    }
+    // own: the wave's 16 * kRow bytes of LDS.  value(a, n, b, v): the four
+    // results of acc[a][b], outputs n.. (a multiple of 4, not above the last).
+    // mask(b, i, chunk): changes the 16 bytes that are about to be stored as
+    // piece i of acc[..][b].
+    template <int NB, typename Value, typename Mask>
+    static __device__ __forceinline__ void store(char *own, int lane, Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0,
+                                                 int64_t rows, Value value, Mask mask) {
+        const int64_t last = (n_out - 1) & ~(int64_t)3;
+        const int row = lane & 15, grp = lane >> 4;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int a = 0; a < NA; ++a) {
+                float v[4];
+                value(a, min(a0 + a * 16 + grp * 4, last), b, v);
+                const int byte = (a * 16 + grp * 4) * (int)sizeof(Y);
+                store_four((Y *)(own + row * kRow + (((byte >> 4) ^ (row & (kChunks - 1))) * 16) + (byte & 15)), v);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // one wave's LDS accesses are in order
+#pragma unroll
+            for (int i = 0; i < kChunks / 4; ++i) {
+                const Piece p = piece(lane, i, a0, b0 + b * 16);
+                u32x4 u = *(const u32x4 *)(own + p.at);
+                mask(b, i, u);
+                if (p.point < rows && p.out < n_out) {
+                    Y *to = y + p.point * ldy + p.out;
+                    if (p.out + kPer <= n_out) {
+                        __builtin_nontemporal_store(u, (u32x4_any *)to);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e)
+                            if (p.out + e < n_out)
+                                to[e] = element<Y>(u, e);
+                    }
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    }
+};
+
 // Blocks of WA x WB waves, each NA x NB tiles of 16 x 16; results of type Y.
 // A is blocked, B is if BLOCKED_B, and comes in rows otherwise.
 template <typename Mma, typename Y, bool BLOCKED_B, int WA, int WB, int NA, int NB>
@@ -174,8 +234,7 @@ struct Product {
     static constexpr int kA = 16 * NA * WA, kB = 16 * NB * WB;
     static constexpr int kBuf = (kA + kB) * kSlabBytes, kLoadsA = kA / (16 * kWaves), kLoadsB = kB / (16 * kWaves);
     static constexpr int kLoads = kLoadsA + kLoadsB;
-    // results of 16 points of a wave, on their way out
-    static constexpr int kPer = 16 / sizeof(Y), kRow = NA * 16 * sizeof(Y), kChunks = kRow / 16;
+    static constexpr int kRow = Out<Y, NA>::kRow, kChunks = Out<Y, NA>::kChunks;
     static constexpr int kAtOut = kRing * kBuf, kLds = kAtOut + kWaves * 16 * kRow;
     static constexpr int kPerCu = 160 * 1024 / kLds;
     static_assert(kLoadsA * 16 * kWaves == kA && kLoadsB * 16 * kWaves == kB && kPerCu >= 1, "whole loads per wave");
@@ -343,59 +402,16 @@ struct Product {
     // the point of acc[..][b], from the tile's first
     __device__ __forceinline__ int point_of(int b) const { return (wave % WB * NB + b) * 16 + (lane & 15); }
 
-    // 16 bytes of results that a lane stores: piece i of the points of acc[..][b]
-    struct Piece {
-        int64_t point;
-        int64_t out;
-        int at;            // in the wave's part of LDS
-    };
-    __device__ __forceinline__ Piece piece(int b, int i, int64_t a0, int64_t b0) const {
-        const int at = i * 64 + lane, row = at / kChunks, c = at % kChunks;
-        return {b0 + (wave % WB * NB + b) * 16 + row, a0 + wave / WB * NA * 16 + c * kPer, row * kRow + ((c ^ (row & (kChunks - 1))) * 16)};
+    // The results, as rows of Y: see store_results.
+    typedef Out<Y, NA> O;
+    __device__ __forceinline__ typename O::Piece piece(int b, int i, int64_t a0, int64_t b0) const {
+        return O::piece(lane, i, a0 + wave / WB * NA * 16, b0 + (wave % WB * NB + b) * 16);
     }
-    // The results, as rows of Y.  value(a, n, b, v): the four results of
-    // acc[a][b], outputs n.. (a multiple of 4, not above the last).
-    // mask(b, i, chunk): changes the 16 bytes that are about to be stored as
-    // piece i of b.  A wave turns 16 points at a time in LDS, so that its
-    // stores are 16-byte pieces of long runs of a row; they bypass the caches
-    // (the results are read by a later kernel, if at all): 131,072 x 1024 ->
-    // 1024 in 8 bits took 146 us with a block per tile, 187 us without that,
-    // 227 us with stores as the matrix instruction leaves its results.
     template <typename Value, typename Mask>
     __device__ __forceinline__ void store(Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0, int64_t rows, Value value,
                                           Mask mask) const {
-        char *own = lds + kAtOut + wave * 16 * kRow;
-        const int64_t last = (n_out - 1) & ~(int64_t)3;
-        const int row = lane & 15, grp = lane >> 4;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-#pragma unroll
-            for (int a = 0; a < NA; ++a) {
-                float v[4];
-                value(a, min(a0 + (wave / WB * NA + a) * 16 + grp * 4, last), b, v);
-                const int byte = (a * 16 + grp * 4) * (int)sizeof(Y);
-                store_four((Y *)(own + row * kRow + (((byte >> 4) ^ (row & (kChunks - 1))) * 16) + (byte & 15)), v);
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // one wave's LDS accesses are in order
-#pragma unroll
-            for (int i = 0; i < kChunks / 4; ++i) {
-                const Piece p = piece(b, i, a0, b0);
-                u32x4 u = *(const u32x4 *)(own + p.at);
-                mask(b, i, u);
-                if (p.point < rows && p.out < n_out) {
-                    Y *to = y + p.point * ldy + p.out;
-                    if (p.out + kPer <= n_out) {
-                        __builtin_nontemporal_store(u, (u32x4_any *)to);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < kPer; ++e)
-                            if (p.out + e < n_out)
-                                to[e] = element<Y>(u, e);
-                    }
-                }
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
+        O::template store<NB>(lds + kAtOut + wave * 16 * kRow, lane, y, ldy, a0 + wave / WB * NA * 16, n_out,
+                              b0 + wave % WB * NB * 16, rows, value, mask);
     }
 };
 

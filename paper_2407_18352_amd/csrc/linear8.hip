@@ -184,22 +184,160 @@ void launch_product(const Linear8Args &a, hipStream_t stream) {
     }
 }
 
+// ---- narrow layers --------------------------------------------------------------
+//
+// Up to SLABS * 64 inputs and many points: a block takes its points' rows whole,
+// forms their codes in LDS, and goes through all outputs with them, so that the
+// codes never lie in memory, which is what bounds these products.  The weights
+// come as fragments straight from the L2, a slab ahead.
+template <typename Y, int SLABS, int WA, int WB, int NA, int NB>
+struct Narrow {
+    static constexpr int kPoints = 16 * NB * WB, kRows = kPoints / 4, kOuts = 16 * NA * WA;
+    static constexpr int kCodes = kPoints / 16 * SLABS * 1024, kOut = 4 * 16 * nt::Out<Y, NA>::kRow;
+    static constexpr int kFit = 160 * 1024 / (kCodes + kOut), kPerCu = kPoints == 128 ? 2 : kFit < 4 ? kFit : 4;
+    static_assert(WA * WB == 4 && kPerCu >= 2, "four waves, two blocks");
+};
+
+template <typename X, typename Y, int SLABS, int WA, int WB, int NA, int NB>
+__global__ void __launch_bounds__(256, (Narrow<Y, SLABS, WA, WB, NA, NB>::kPerCu)) narrow_kernel(Linear8Args p) {
+    typedef Narrow<Y, SLABS, WA, WB, NA, NB> N;
+    constexpr int kPoints = N::kPoints, kRows = N::kRows, kOuts = N::kOuts, kBatch = 8;
+    typedef nt::Out<Y, NA> Out;
+    __shared__ __align__(1024) char codes[N::kCodes];
+    __shared__ __align__(16) char out[N::kOut];      // the points' scales first
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t p0 = (int64_t)blockIdx.x * kPoints;
+    float *scales = (float *)out;
+
+    // codes: 2^lanes_log lanes per row, a chunk each
+    const int chunks = p.slabs * (kSlabBytes / kChunk);
+    int lanes_log = 3;
+    while ((1 << lanes_log) < chunks)
+        ++lanes_log;
+    const int lanes = 1 << lanes_log, per = 64 >> lanes_log, c = lane & (lanes - 1), k = c * kChunk;
+    for (int r0 = wave * kRows; r0 < wave * kRows + kRows; r0 += per * kBatch) {
+        float v[kBatch][kChunk];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int64_t r = min(p0 + min(r0 + i * per + (lane >> lanes_log), kPoints - 1), p.rows - 1);
+            load_chunk((const X *)p.x + r * p.ldx + k, p.n_in - k, v[i]);
+        }
+        uint32_t top[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            top[i] = top_bits(v[i]);
+        for (int d = lanes / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], d));
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const RowScale sc(top[i]);
+            const int r = r0 + i * per + (lane >> lanes_log);
+            if (r < wave * kRows + kRows) {
+                if (c == 0)
+                    scales[r] = sc.scale;
+                if (c < chunks)
+                    *(uint2 *)(codes + blocked_offset(r, k, p.slabs)) = sc.codes(v[i]);
+            }
+        }
+    }
+    __syncthreads();
+
+    const int wa = wave / WB, wb = wave % WB, row = lane & 15;
+    const int at = row * kSlabBytes + (((lane >> 4) ^ chunk_turn(row)) * 16);
+    float s[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        s[b] = scales[(wb * NB + b) * 16 + row];
+    __syncthreads();                                   // the scales' place is the results' now
+
+    const int last = (p.n_out - 1) / 16;               // 16 outputs
+    auto weights = [&](int pass, int slab, u32x4 (&a)[NA]) {
+#pragma unroll
+        for (int t = 0; t < NA; ++t)
+            a[t] = *(const u32x4 *)(p.w + ((int64_t)min(pass * (kOuts / 16) + wa * NA + t, last) * p.slabs + slab) * 1024 + at);
+    };
+    u32x4 a[NA], next[NA];
+    weights(0, 0, a);
+    const int passes = (p.n_out + kOuts - 1) / kOuts;
+    for (int pass = 0; pass < passes; ++pass) {
+        i32x4 acc[NA][NB] = {};
+        for (int slab = 0; slab < p.slabs; ++slab) {
+            const bool more = slab + 1 < p.slabs;
+            weights(more ? pass : min(pass + 1, passes - 1), more ? slab + 1 : 0, next);
+            u32x4 b[NB];
+#pragma unroll
+            for (int u = 0; u < NB; ++u)
+                b[u] = *(const u32x4 *)(codes + ((wb * NB + u) * p.slabs + slab) * 1024 + at);
+#pragma unroll
+            for (int u = 0; u < NB; ++u)
+#pragma unroll
+                for (int t = 0; t < NA; ++t)
+                    acc[t][u] = nt::I8::mul(a[t], b[u], acc[t][u]);
+#pragma unroll
+            for (int t = 0; t < NA; ++t)
+                a[t] = next[t];
+        }
+        const int64_t a0 = (int64_t)pass * kOuts + wa * NA * 16;
+        if (a0 < p.n_out)
+            Out::template store<NB>(out + wave * 16 * Out::kRow, lane, (Y *)p.y, p.ldy, a0, p.n_out, p0 + wb * NB * 16, p.rows,
+                                    [&](int t, int64_t n, int u, float (&v)[4]) {
+                                        const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e) {
+                                            v[e] = (float)acc[t][u][e] * s[u] * sc[e] + bias[e];
+                                            if (p.relu)
+                                                v[e] = relu_keep_nan(v[e]);
+                                        }
+                                    },
+                                    [](int, int, u32x4 &) {});
+    }
+}
+
+template <typename X, typename Y, int SLABS, int WA, int WB, int NB>
+void launch_narrow_tile(const Linear8Args &a, hipStream_t stream) {
+    constexpr int kPoints = Narrow<Y, SLABS, WA, WB, 4, NB>::kPoints;
+    narrow_kernel<X, Y, SLABS, WA, WB, 4, NB><<<dim3((uint32_t)((a.rows + kPoints - 1) / kPoints)), 256, 0, stream>>>(a);
+}
+
+// Points of a block: 64, of which four share a CU; with few outputs and enough
+// rows for as many larger blocks 128 (us, 64 and 128, and with the codes in
+// memory: 65536 x 512 <- 512 45.9, 48.3, 54.3; 262144 x 64 <- 64 26.8, 19.3,
+// 28.6; 65521 x 50 <- 201 in fp32 19.0, 22.4, 24.5).
+template <typename X, typename Y, int SLABS>
+void launch_narrow(const Linear8Args &a, hipStream_t stream) {
+    const bool many = a.rows >= 131072;
+    if (a.n_out <= 64)
+        many ? launch_narrow_tile<X, Y, SLABS, 1, 4, 2>(a, stream) : launch_narrow_tile<X, Y, SLABS, 1, 4, 1>(a, stream);
+    else if (a.n_out <= 128)
+        many ? launch_narrow_tile<X, Y, SLABS, 2, 2, 4>(a, stream) : launch_narrow_tile<X, Y, SLABS, 2, 2, 2>(a, stream);
+    else
+        launch_narrow_tile<X, Y, SLABS, 4, 1, 4>(a, stream);
+}
+
+bool few_fused(int64_t rows, int32_t n_in) {
+    return rows <= kFewPoints && rows * fused_pitch(slabs_of(n_in)) <= kFusedBytes;
+}
+// (16384 x 512 <- 512 takes 24.5 us this way and 20.7 us with the codes in memory)
+bool narrow(int64_t rows, int32_t n_in, int32_t n_out) { return rows >= 32768 && rows <= (1 << 30) && n_in <= 512 && n_out <= 1024; }
+
 template <typename X, typename Y>
 void launch_as(const Linear8Args &a, hipStream_t stream) {
-    if (linear8_fused(a.rows, a.n_in))
+    if (few_fused(a.rows, a.n_in))
         launch_few<X, Y, true>(a, stream);
+    else if (narrow(a.rows, a.n_in, a.n_out))
+        a.slabs <= 4 ? launch_narrow<X, Y, 4>(a, stream) : launch_narrow<X, Y, 8>(a, stream);
     else
         launch_product<Y>(a, stream);
 }
 
 }  // namespace
 
-bool linear8_fused(int64_t rows, int32_t n_in) {
-    return rows <= kFewPoints && rows * fused_pitch(slabs_of(n_in)) <= kFusedBytes;
-}
+bool linear8_fused(int64_t rows, int32_t n_in, int32_t n_out) { return few_fused(rows, n_in) || narrow(rows, n_in, n_out); }
 
 hipError_t launch_linear8(const Linear8Args &a, int32_t x_dtype, int32_t y_dtype, hipStream_t stream) {
-    if (!linear8_fused(a.rows, a.n_in)) {
+    if (!linear8_fused(a.rows, a.n_in, a.n_out)) {
         const hipError_t e = launch_codes_by_row(a.x, x_dtype, a.ldx, a.rows, a.n_in, a.q, a.s, stream);
         if (e != hipSuccess)
             return e;

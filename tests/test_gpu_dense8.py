@@ -118,6 +118,15 @@ def test_linear_larger(rows, n_in, n_out, x_kind, y_kind):
     _check_linear(_rand(4, (rows, n_in), x_kind), _rand(5, (n_out, n_in), scale=n_in ** -0.5), None, IDENT, y_kind)
 
 
+@pytest.mark.parametrize("rows, n_in, n_out", [(32768, 5, 16), (32769, 64, 64), (33001, 65, 65), (40000, 201, 50), (32770, 256, 128),
+                                               (32768, 257, 130), (33007, 320, 300), (32801, 512, 512), (32768, 511, 1024),
+                                               (32790, 512, 1025), (32768, 513, 100), (131073, 40, 33), (131100, 130, 127)])
+@pytest.mark.parametrize("x_kind, y_kind", [("bf16", "bf16"), ("f32", "f32")])
+def test_linear_many_rows_of_narrow_layers(rows, n_in, n_out, x_kind, y_kind):
+    _check_linear(_rand(40, (rows, n_in), x_kind, pad=rows % 5), _rand(41, (n_out, n_in), scale=n_in ** -0.5),
+                  _rand(42, (1, n_out))[0], RELU, y_kind)
+
+
 @pytest.mark.parametrize("x_kind", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [0, 1, 4, 8])
 def test_linear_alignment(x_kind, pad):
@@ -127,7 +136,7 @@ def test_linear_alignment(x_kind, pad):
         _check_linear(wide[:, off:off + 65], _rand(7, (40, 65)), None, RELU, "f32", "pad %d offset %d" % (pad, off))
 
 
-@pytest.mark.parametrize("rows", [1, 4, 40, 300])
+@pytest.mark.parametrize("rows", [1, 4, 40, 300, 33000])
 def test_linear_special_rows(rows):
     """Rows of zeros, of tiny and of huge values, with an infinity or a NaN;
     the same in the weights."""
