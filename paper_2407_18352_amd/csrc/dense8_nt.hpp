@@ -189,11 +189,14 @@ struct Out {
     // results of acc[a][b], outputs n.. (a multiple of 4, not above the last).
     // mask(b, i, chunk): changes the 16 bytes that are about to be stored as
     // piece i of acc[..][b].
-    template <int NB, typename Value, typename Mask>
+    // MERGE: rows that share cache lines go through the L2, which puts them together
+    // (fp32 rows of 201: dx of 30,011 rows 22.7 -> 19.6 us).
+    template <int NB, bool MERGE, typename Value, typename Mask>
     static __device__ __forceinline__ void store(char *own, int lane, Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0,
                                                  int64_t rows, Value value, Mask mask) {
         const int64_t last = (n_out - 1) & ~(int64_t)3;
         const int row = lane & 15, grp = lane >> 4;
+        const bool whole_lines = !MERGE || (((uintptr_t)y | (uint64_t)ldy * sizeof(Y)) & 63) == 0;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -212,7 +215,10 @@ struct Out {
                 if (p.point < rows && p.out < n_out) {
                     Y *to = y + p.point * ldy + p.out;
                     if (p.out + kPer <= n_out) {
-                        __builtin_nontemporal_store(u, (u32x4_any *)to);
+                        if (whole_lines)
+                            __builtin_nontemporal_store(u, (u32x4_any *)to);
+                        else
+                            *(u32x4_any *)to = u;
                     } else {
 #pragma unroll
                         for (int e = 0; e < kPer; ++e)
@@ -410,7 +416,7 @@ struct Product {
     template <typename Value, typename Mask>
     __device__ __forceinline__ void store(Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0, int64_t rows, Value value,
                                           Mask mask) const {
-        O::template store<NB>(lds + kAtOut + wave * 16 * kRow, lane, y, ldy, a0 + wave / WB * NA * 16, n_out,
+        O::template store<NB, true>(lds + kAtOut + wave * 16 * kRow, lane, y, ldy, a0 + wave / WB * NA * 16, n_out,
                               b0 + wave % WB * NB * 16, rows, value, mask);
     }
 };

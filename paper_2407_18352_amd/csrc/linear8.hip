@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(256, (Narrow<Y, SLABS, WA, WB, NA, NB>::kPerCu
         }
         const int64_t a0 = (int64_t)pass * kOuts + wa * NA * 16;
         if (a0 < p.n_out)
-            Out::template store<NB>(out + wave * 16 * Out::kRow, lane, (Y *)p.y, p.ldy, a0, p.n_out, p0 + wb * NB * 16, p.rows,
+            Out::template store<NB, false>(out + wave * 16 * Out::kRow, lane, (Y *)p.y, p.ldy, a0, p.n_out, p0 + wb * NB * 16, p.rows,
                                     [&](int t, int64_t n, int u, float (&v)[4]) {
                                         const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
 #pragma unroll
