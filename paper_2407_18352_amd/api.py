@@ -343,29 +343,36 @@ class Region:
 
 # ---- dense layers in 8 bits (include/hpacml8.h) -----------------------------
 
-def _matrix(t, what, rows=None, width=None, dtypes=None):
+_kinds8 = {}       # torch's types -> the ABI's, filled by the first call
+
+
+def _matrix(t, what, rows=None, width=None, kind=None):
     """(pointer, ABI type, row pitch) of a device matrix with contiguous rows."""
-    import torch
-    kinds = {torch.float32: _abi.F32, torch.bfloat16: _abi.BF16}
-    if not t.is_cuda or t.dtype not in kinds or (dtypes is not None and kinds[t.dtype] not in dtypes):
-        raise TypeError("%s must be a %s device tensor" % (what, "float32" if dtypes == (_abi.F32,) else
-                                                           "float32 or bfloat16" if dtypes is None else "bfloat16"))
-    shape, stride = t.shape, t.stride()
+    if not _kinds8:
+        import torch
+        _kinds8.update({torch.float32: _abi.F32, torch.bfloat16: _abi.BF16})
+    own = _kinds8.get(t.dtype)
+    if own is None or not t.is_cuda or (kind is not None and own != kind):
+        raise TypeError("%s must be a %s device tensor" % (what, "float32 or bfloat16" if kind is None else
+                                                           "float32" if kind == _abi.F32 else "bfloat16"))
+    shape = t.shape
     if len(shape) != 2 or (rows is not None and shape[0] != rows) or (width is not None and shape[1] != width):
         raise ValueError("%s: shape %s, expected %s x %s" % (what, tuple(shape), "rows" if rows is None else rows,
                                                              "width" if width is None else width))
-    if shape[1] > 1 and shape[0] > 0 and stride[1] != 1:
+    n, m = shape
+    ld, step = t.stride()
+    if m > 1 and n > 0 and step != 1:
         raise ValueError("%s: the values of a row must be contiguous" % what)
-    return t.data_ptr(), kinds[t.dtype], stride[0] if shape[0] > 1 else max(shape[1], 1)
+    return t.data_ptr(), own, ld if n > 1 else max(m, 1)
 
 
 def _scratch8(scratch, need, stream):
     """(the scratch tensor to keep during the call, its address, bytes): the caller's, or, on torch's current stream, whose
     order its allocator follows, one from there."""
-    import torch
     if scratch is None:
         if stream is not None:
             raise ValueError("a call on a stream of its own needs scratch memory")
+        import torch
         scratch = torch.empty(need(), dtype=torch.uint8, device="cuda")
     elif not scratch.is_cuda or not scratch.is_contiguous():
         raise TypeError("scratch must be a contiguous device tensor")
@@ -461,13 +468,17 @@ def checkpoint8_load(kept: Checkpoint8, a, stream=None) -> None:
     check(lib().hpacml8_checkpoint_load(C.byref(kept.desc), pa, ta, lda, _stream(stream)), "hpacml8_checkpoint_load")
 
 
+def _backward8_need(kept, dy, dw, dx):
+    """Bytes of scratch; dy: (pointer, type, pitch, width)."""
+    n = C.c_size_t()
+    check(lib().hpacml8_backward_scratch(kept.desc, *dy, dw, dx, n), "hpacml8_backward_scratch")
+    return n.value
+
+
 def backward8_scratch_bytes(kept: Checkpoint8, dy, W=None, dw: bool = True) -> int:
     """Bytes of scratch ``backward8`` needs (``W``: given when dx is wanted)."""
-    _, t, ld = _matrix(dy, "dy", rows=kept.rows)
-    n = C.c_size_t()
-    check(lib().hpacml8_backward_scratch(C.byref(kept.desc), dy.data_ptr(), t, ld, dy.shape[1], 1 if dw else 0,
-                                         0 if W is None else 1, C.byref(n)), "hpacml8_backward_scratch")
-    return n.value
+    p, t, ld = _matrix(dy, "dy", kept.rows)
+    return _backward8_need(kept, (p, t, ld, dy.shape[1]), 1 if dw else 0, 0 if W is None else 1)
 
 
 def backward8(kept: Checkpoint8, dy, dw=None, db=None, W=None, dx=None, accumulate: bool = False, scratch=None,
@@ -476,19 +487,24 @@ def backward8(kept: Checkpoint8, dy, dw=None, db=None, W=None, dx=None, accumula
     ``kept``, from ``dy`` [n][out] (float32 or bfloat16): ``dw`` [out][in] and
     ``db`` [out] in float32, ``dx`` [n][in] in dy's type from ``W`` [out][in]
     (dy's type).  Gradients not given are not computed."""
-    py, ty, ldy = _matrix(dy, "dy", rows=kept.rows)
+    py, ty, ldy = _matrix(dy, "dy", kept.rows)
     n_out = dy.shape[1]
-    pw = lddw = pb = pW = ldW = px = ldx = None
+    pw = pb = pW = px = None
+    lddw = ldW = ldx = 0
     if dw is not None:
-        pw, _, lddw = _matrix(dw, "dw", n_out, kept.width, (_abi.F32,))
+        pw, _, lddw = _matrix(dw, "dw", n_out, kept.width, _abi.F32)
     if db is not None:
-        pb, _, _ = _matrix(db.unsqueeze(0), "db", 1, n_out, (_abi.F32,))
+        if _kinds8.get(db.dtype) != _abi.F32 or not db.is_cuda:
+            raise TypeError("db must be a float32 device tensor")
+        if db.shape != (n_out,) or not db.is_contiguous():
+            raise ValueError("db: shape %s, expected %s contiguous" % (tuple(db.shape), (n_out,)))
+        pb = db.data_ptr()
     if dx is not None:
         if W is None:
             raise ValueError("dx needs W")
-        pW, _, ldW = _matrix(W, "W", n_out, kept.width, (ty,))
-        px, _, ldx = _matrix(dx, "dx", kept.rows, kept.width, (ty,))
-    keep, ps, bytes_ = _scratch8(scratch, lambda: backward8_scratch_bytes(
-        kept, dy, W if dx is not None else None, dw is not None or db is not None), stream)
-    check(lib().hpacml8_backward(C.byref(kept.desc), py, ty, ldy, n_out, pW, ldW or 0, pw, lddw or 0, pb, px, ldx or 0,
+        pW, _, ldW = _matrix(W, "W", n_out, kept.width, ty)
+        px, _, ldx = _matrix(dx, "dx", kept.rows, kept.width, ty)
+    keep, ps, bytes_ = _scratch8(scratch, lambda: _backward8_need(
+        kept, (py, ty, ldy, n_out), 1 if dw is not None or db is not None else 0, 0 if dx is None else 1), stream)
+    check(lib().hpacml8_backward(kept.desc, py, ty, ldy, n_out, pW, ldW, pw, lddw, pb, px, ldx,
                                  1 if accumulate else 0, ps, bytes_, _stream(stream)), "hpacml8_backward")

@@ -50,6 +50,7 @@ hipError_t launch_checkpoint_load(const hpacml8_checkpoint &c, void *a, int32_t 
 // The backward pass.  Everything it puts into scratch, as byte offsets.
 struct Backward8Plan {
     int32_t planes;       // bf16 terms of an operand: 1 (bf16) or 3 (fp32)
+    bool few;             // one launch that reads everything in place, without scratch
     bool direct;          // dy is read in place
     int32_t slabs;        // of dy and of W's transpose along the outputs
     int64_t pitch;        // of dy's planes (elements)
@@ -77,6 +78,7 @@ struct Backward8Args {
     char *scratch;
 };
 hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipStream_t stream);
+hipError_t launch_backward8_few(const Backward8Args &a, hipStream_t stream);
 
 // ---- device arithmetic --------------------------------------------------------
 

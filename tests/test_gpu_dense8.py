@@ -467,6 +467,36 @@ def test_backward_larger(rows, n_in, n_out, kind, act):
     _check_backward(kept, dy, W, a, t, kind)
 
 
+@pytest.mark.parametrize("rows, n_in, n_out", [(1024, 40, 70), (1025, 40, 70), (1, 1000, 900), (3, 1100, 511), (33, 1100, 513),
+                                               (512, 64, 1111), (700, 333, 222), (65, 4097, 33), (17, 31, 4099)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_backward_of_few_rows(rows, n_in, n_out, kind):
+    """On both sides of the sizes that one launch takes."""
+    act = (RELU, IDENT)[rows % 2]
+    kept, dy, W, a, t = _case(rows, n_in, n_out, act, kind, pad=rows % 3)
+    _check_backward(kept, dy, W, a, t, kind)
+
+
+def test_backward_of_few_rows_beside_infinite_weights_and_rows():
+    """The rows of W that lie beyond a block of outputs' end, and the rows of dy
+    beyond a block of rows' end, do not take part."""
+    torch = _torch()
+    kept, dy, W, a, t = _case(35, 40, 37, IDENT, "f32")
+    W[36, 3] = float("inf")
+    dy[:, 36] = torch.where(dy[:, 36] == 0, 1.0, dy[:, 36])
+    dx = torch.empty((35, 40), device="cuda")
+    api.backward8(kept, dy, W=W, dx=dx)
+    rest = [k for k in range(40) if k != 3]
+    assert torch.isfinite(dx[:, rest]).all() and not torch.isfinite(dx[:, 3]).any()
+    W[36, 3] = 0.0
+    dy[34, 5] = float("nan")
+    dw = torch.empty((37, 40), device="cuda")
+    api.backward8(kept, dy, dw, W=W, dx=dx)
+    assert torch.isnan(dx[34]).all() and torch.isfinite(dx[:34]).all()
+    rest = [j for j in range(37) if j != 5]
+    assert torch.isnan(dw[5]).all() and torch.isfinite(dw[rest]).all()
+
+
 @pytest.mark.parametrize("parts", [("dw",), ("db",), ("dx",), ("dw", "db"), ("dw", "dx"), ("db", "dx")])
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_backward_wanted_parts(parts, kind):
