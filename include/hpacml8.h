@@ -125,8 +125,10 @@ hpacml_status hpacml8_backward(const hpacml8_checkpoint *c, const void *dy, int3
 
 /* Bytes of scratch (16-byte aligned) hpacml8_backward needs for these
  * operands; want_dw (dw or db) and want_dx say which of its outputs are
- * wanted.  A dy with 16-byte aligned rows (pointer, pitch and n_out) in bf16
- * is read in place; any other is first laid out in the scratch memory. */
+ * wanted.  With many rows a dy is read in place if it is bf16, its pointer
+ * 16-byte aligned, lddy a multiple of 8 (below 2^22) and n_out one of 32 (of 8
+ * where dx is not wanted); any other is first laid out in the scratch memory.
+ * A smaller number of rows may need more: ask for each. */
 hpacml_status hpacml8_backward_scratch(const hpacml8_checkpoint *c, const void *dy, int32_t dtype, int64_t lddy,
                                        int32_t n_out, int32_t want_dw, int32_t want_dx, size_t *bytes);
 

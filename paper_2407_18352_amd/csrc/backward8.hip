@@ -4,6 +4,13 @@
 // dw's products are exact on v_mfma_f32_16x16x32_bf16 and summed in fp32.  An
 // fp32 operand is the exact sum of three bf16 terms: three products for dw,
 // for dx those six of nine whose terms' ranks sum to at most 2.
+//
+// Few rows take one launch (backward8_few.hip); otherwise up to four follow one
+// another.  131,072 rows of 2048 <- 2048 in bf16: W laid out 8 us, dx 0.92 ms,
+// dw 1.07-1.14 ms (1.0 PFLOP/s; the matrix cores work in 44% of its cycles, held
+// up by the conversion of the codes between them), parts joined 14 us.  262,144
+// rows of 256 <- 256: 5, 70, 62 and 7 us; dx and dw are bound by memory (335 MB
+// at 4.8 TB/s; 201 MB at 3.2 TB/s).
 #include <cmath>
 #include <type_traits>
 
@@ -98,9 +105,9 @@ struct DxArgs {
     uint32_t in_tiles, point_tiles;
 };
 
-template <typename X, int WA, int WB, int NA, int NB>
+template <typename X, bool MERGE, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB, 2) dx_kernel(DxArgs p) {
-    typedef nt::Product<nt::Bf16, X, false, WA, WB, NA, NB> T;
+    typedef nt::Product<nt::Bf16, X, false, MERGE, WA, WB, NA, NB> T;
     __shared__ __align__(1024) char lds[T::kLds];
     T t;
     t.run(p.wt, p.g, p.in_tiles, p.point_tiles, p.terms, lds, [&](const f32x4 (&acc)[NA][NB], int64_t a0, int64_t b0) {
@@ -607,22 +614,22 @@ void launch_layout(const Backward8Args &a, const Backward8Plan &p, uint16_t *pla
         layout_kernel<T><<<l.row_blocks + turn, kThreads, 0, st>>>(l);
 }
 
-template <typename X, int WA, int WB, int NA, int NB>
+template <typename X, bool MERGE, int WA, int WB, int NA, int NB>
 void launch_dx_tile(DxArgs d, hipStream_t st) {
-    typedef nt::Product<nt::Bf16, X, false, WA, WB, NA, NB> T;
+    typedef nt::Product<nt::Bf16, X, false, MERGE, WA, WB, NA, NB> T;
     d.in_tiles = (uint32_t)((d.n_in + T::kA - 1) / T::kA);
     d.point_tiles = (uint32_t)((d.g.rows + T::kB - 1) / T::kB);
-    dx_kernel<X, WA, WB, NA, NB>
+    dx_kernel<X, MERGE, WA, WB, NA, NB>
         <<<nt::blocks_for_tiles((int64_t)d.in_tiles * d.point_tiles, T::kPerCu), T::kThreads, 0, st>>>(d);
 }
 
-template <typename X>
+template <typename X, bool MERGE>
 void launch_dx(const DxArgs &d, hipStream_t st) {
     switch (nt::tile_for(d.n_in, d.g.rows, d.wt.width / kSlabBytes * (d.terms * (d.terms + 1) / 2))) {
-    case nt::Size::k64x64: return launch_dx_tile<X, 2, 2, 2, 2>(d, st);
-    case nt::Size::k128x128: return launch_dx_tile<X, 2, 2, 4, 4>(d, st);
-    case nt::Size::k128x256: return launch_dx_tile<X, 2, 4, 4, 4>(d, st);
-    case nt::Size::k256x256: return launch_dx_tile<X, 4, 2, 4, 8>(d, st);
+    case nt::Size::k64x64: return launch_dx_tile<X, MERGE, 2, 2, 2, 2>(d, st);
+    case nt::Size::k128x128: return launch_dx_tile<X, MERGE, 2, 2, 4, 4>(d, st);
+    case nt::Size::k128x256: return launch_dx_tile<X, MERGE, 2, 4, 4, 4>(d, st);
+    case nt::Size::k256x256: return launch_dx_tile<X, MERGE, 4, 2, 4, 8>(d, st);
     }
 }
 
@@ -729,7 +736,11 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
         d.lddx = a.lddx;
         d.n_in = a.c.width;
         d.terms = p.planes;
-        f32 ? launch_dx<float>(d, st) : launch_dx<uint16_t>(d, st);
+        const bool shared = nt::shared_lines(a.dx, a.lddx * (f32 ? 4 : 2));
+        if (f32)
+            shared ? launch_dx<float, true>(d, st) : launch_dx<float, false>(d, st);
+        else
+            shared ? launch_dx<uint16_t, true>(d, st) : launch_dx<uint16_t, false>(d, st);
     }
     if (a.dw || a.db) {
         const bool join = p.splits > 1;

@@ -169,9 +169,9 @@ inline Size tile_for(int64_t n_out, int64_t rows, int64_t slabs) {
 // A wave's results on their way out, as rows of Y, NA * 16 outputs of 16 points
 // at a time.  They are turned in LDS, so that the stores are 16-byte pieces of
 // long runs of a row, and bypass the caches (a later kernel reads them, if
-// any): 131,072 x 1024 -> 1024 in 8 bits took 146 us with a block per tile, 187
-// us without that, 227 us with stores as the matrix instruction leaves its
-// results.
+// any).  131,072 x 1024 -> 1024 in 8 bits, measured with a block per tile: 146
+// us so, 187 us through the caches, 227 us with stores as the matrix
+// instruction leaves its results.
 template <typename Y, int NA>
 struct Out {
     static constexpr int kPer = 16 / sizeof(Y), kRow = NA * 16 * sizeof(Y), kChunks = kRow / 16;
@@ -189,14 +189,16 @@ struct Out {
     // results of acc[a][b], outputs n.. (a multiple of 4, not above the last).
     // mask(b, i, chunk): changes the 16 bytes that are about to be stored as
     // piece i of acc[..][b].
-    // MERGE: rows that share cache lines go through the L2, which puts them together
-    // (fp32 rows of 201: dx of 30,011 rows 22.7 -> 19.6 us).
+    // MERGE: for rows that share cache lines (shared_lines): the stores go
+    // through the L2, which puts the lines together (fp32 rows of 201: dx of
+    // 30,011 rows 22.7 -> 19.6 us).  A form of its own: with a test at each
+    // store dx of 262,144 rows, 256 <- 256 in bf16, its inputs read before, took
+    // 86 us, not 70.
     template <int NB, bool MERGE, typename Value, typename Mask>
     static __device__ __forceinline__ void store(char *own, int lane, Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0,
                                                  int64_t rows, Value value, Mask mask) {
         const int64_t last = (n_out - 1) & ~(int64_t)3;
         const int row = lane & 15, grp = lane >> 4;
-        const bool whole_lines = !MERGE || (((uintptr_t)y | (uint64_t)ldy * sizeof(Y)) & 63) == 0;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -215,10 +217,10 @@ struct Out {
                 if (p.point < rows && p.out < n_out) {
                     Y *to = y + p.point * ldy + p.out;
                     if (p.out + kPer <= n_out) {
-                        if (whole_lines)
-                            __builtin_nontemporal_store(u, (u32x4_any *)to);
-                        else
+                        if constexpr (MERGE)
                             *(u32x4_any *)to = u;
+                        else
+                            __builtin_nontemporal_store(u, (u32x4_any *)to);
                     } else {
 #pragma unroll
                         for (int e = 0; e < kPer; ++e)
@@ -232,9 +234,11 @@ struct Out {
     }
 };
 
+inline bool shared_lines(const void *y, int64_t pitch_bytes) { return (((uintptr_t)y | (uint64_t)pitch_bytes) & 63) != 0; }
+
 // Blocks of WA x WB waves, each NA x NB tiles of 16 x 16; results of type Y.
 // A is blocked, B is if BLOCKED_B, and comes in rows otherwise.
-template <typename Mma, typename Y, bool BLOCKED_B, int WA, int WB, int NA, int NB>
+template <typename Mma, typename Y, bool BLOCKED_B, bool MERGE, int WA, int WB, int NA, int NB>
 struct Product {
     static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, kRing = 4;
     static constexpr int kA = 16 * NA * WA, kB = 16 * NB * WB;
@@ -408,7 +412,7 @@ struct Product {
     // the point of acc[..][b], from the tile's first
     __device__ __forceinline__ int point_of(int b) const { return (wave % WB * NB + b) * 16 + (lane & 15); }
 
-    // The results, as rows of Y: see store_results.
+    // The results, as rows of Y: see Out.
     typedef Out<Y, NA> O;
     __device__ __forceinline__ typename O::Piece piece(int b, int i, int64_t a0, int64_t b0) const {
         return O::piece(lane, i, a0 + wave / WB * NA * 16, b0 + (wave % WB * NB + b) * 16);
@@ -416,8 +420,8 @@ struct Product {
     template <typename Value, typename Mask>
     __device__ __forceinline__ void store(Y *y, int64_t ldy, int64_t a0, int64_t n_out, int64_t b0, int64_t rows, Value value,
                                           Mask mask) const {
-        O::template store<NB, true>(lds + kAtOut + wave * 16 * kRow, lane, y, ldy, a0 + wave / WB * NA * 16, n_out,
-                              b0 + wave % WB * NB * 16, rows, value, mask);
+        O::template store<NB, MERGE>(lds + kAtOut + wave * 16 * kRow, lane, y, ldy, a0 + wave / WB * NA * 16, n_out,
+                                     b0 + wave % WB * NB * 16, rows, value, mask);
     }
 };
 

@@ -1,5 +1,14 @@
 // y = act(s_i t_j sum_k q_ik w_jk + b_j): int8 codes on v_mfma_i32_16x16x64_i8,
 // exact 32-bit sums, fp32 epilogue.
+//
+// Three ways, by the number of points and the widths:
+//   up to 64 points: few_kernel; one point through 4096 -> 4096 takes 5-6 us of
+//     the device (3.4 us are the 16.8 MB of weights at a copy's rate);
+//   many points of a narrow layer: narrow_kernel, bound by memory; 65,536 x 512
+//     -> 512 in bf16 takes 41 us (27 us at a copy's rate);
+//   otherwise the codes are formed by a launch of their own and the product is
+//     the general one, bound by the matrix cores: 131,072 x 4096 -> 4096 takes
+//     0.31 ms for the codes (1.6 GB, 5.1 TB/s) and 1.7-1.85 ms for the product.
 #include "dense8_nt.hpp"
 #include "dense8_rows.hpp"
 
@@ -7,9 +16,9 @@ namespace hpacml {
 
 namespace {
 
-template <typename Y, int WA, int WB, int NA, int NB>
+template <typename Y, bool MERGE, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB, 2) linear8_kernel(Linear8Args p, uint32_t out_tiles, uint32_t point_tiles) {
-    typedef nt::Product<nt::I8, Y, true, WA, WB, NA, NB> T;
+    typedef nt::Product<nt::I8, Y, true, MERGE, WA, WB, NA, NB> T;
     __shared__ __align__(1024) char lds[T::kLds];
     const int64_t pitch = (int64_t)p.slabs * 1024, width = (int64_t)p.slabs * kSlabBytes;
     T t;
@@ -33,12 +42,22 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) linear8_kernel(Linear8Args p,
           });
 }
 
-template <typename Y, int WA, int WB, int NA, int NB>
+template <typename Y, bool MERGE, int WA, int WB, int NA, int NB>
 void launch_tile(const Linear8Args &a, hipStream_t stream) {
-    typedef nt::Product<nt::I8, Y, true, WA, WB, NA, NB> T;
+    typedef nt::Product<nt::I8, Y, true, MERGE, WA, WB, NA, NB> T;
     const uint32_t out_tiles = (uint32_t)((a.n_out + T::kA - 1) / T::kA), point_tiles = (uint32_t)((a.rows + T::kB - 1) / T::kB);
-    linear8_kernel<Y, WA, WB, NA, NB>
+    linear8_kernel<Y, MERGE, WA, WB, NA, NB>
         <<<nt::blocks_for_tiles((int64_t)out_tiles * point_tiles, T::kPerCu), T::kThreads, 0, stream>>>(a, out_tiles, point_tiles);
+}
+
+template <typename Y, bool MERGE>
+void launch_tiled(const Linear8Args &a, hipStream_t stream) {
+    switch (nt::tile_for(a.n_out, a.rows, a.slabs)) {
+    case nt::Size::k64x64: return launch_tile<Y, MERGE, 2, 2, 2, 2>(a, stream);
+    case nt::Size::k128x128: return launch_tile<Y, MERGE, 2, 2, 4, 4>(a, stream);
+    case nt::Size::k128x256: return launch_tile<Y, MERGE, 2, 4, 4, 4>(a, stream);
+    case nt::Size::k256x256: return launch_tile<Y, MERGE, 4, 2, 4, 8>(a, stream);
+    }
 }
 
 // ---- few points ---------------------------------------------------------------
@@ -49,7 +68,7 @@ void launch_tile(const Linear8Args &a, hipStream_t stream) {
 // straight into registers (the blocked layout is the fragment), and add their
 // exact integer sums through LDS.  FUSED (codes of up to 36 KB): every block
 // forms the points' codes itself, its weights already on the way, which saves
-// a launch.  One point through 4096 -> 4096: 4.9 us.
+// a launch.
 constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewPoints = 64, kFusedBytes = 36 * 1024;
 // of a row of codes in LDS: 16 rows at one k lie on different banks
 constexpr int64_t fused_pitch(int64_t slabs) { return slabs * kSlabBytes + 16; }
@@ -176,12 +195,7 @@ template <typename Y>
 void launch_product(const Linear8Args &a, hipStream_t stream) {
     if (a.rows <= kFewPoints)
         return launch_few<float, Y, false>(a, stream);   // x is not read
-    switch (nt::tile_for(a.n_out, a.rows, a.slabs)) {
-    case nt::Size::k64x64: return launch_tile<Y, 2, 2, 2, 2>(a, stream);
-    case nt::Size::k128x128: return launch_tile<Y, 2, 2, 4, 4>(a, stream);
-    case nt::Size::k128x256: return launch_tile<Y, 2, 4, 4, 4>(a, stream);
-    case nt::Size::k256x256: return launch_tile<Y, 4, 2, 4, 8>(a, stream);
-    }
+    nt::shared_lines(a.y, a.ldy * (int64_t)sizeof(Y)) ? launch_tiled<Y, true>(a, stream) : launch_tiled<Y, false>(a, stream);
 }
 
 // ---- narrow layers --------------------------------------------------------------
