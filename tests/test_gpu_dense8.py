@@ -118,6 +118,14 @@ def test_linear_larger(rows, n_in, n_out, x_kind, y_kind):
     _check_linear(_rand(4, (rows, n_in), x_kind), _rand(5, (n_out, n_in), scale=n_in ** -0.5), None, IDENT, y_kind)
 
 
+@pytest.mark.parametrize("rows, n_in, n_out", [(13001, 1040, 1100), (12950, 1024, 1088), (50011, 70, 1300), (25100, 130, 1024)])
+@pytest.mark.parametrize("x_kind, y_kind", [("bf16", "bf16"), ("f32", "f32")])
+def test_linear_in_the_largest_tiles(rows, n_in, n_out, x_kind, y_kind):
+    """Enough of them for every CU; rows whose ends share cache lines and rows
+    whose ends do not."""
+    _check_linear(_rand(24, (rows, n_in), x_kind), _rand(25, (n_out, n_in), scale=n_in ** -0.5), None, RELU, y_kind)
+
+
 @pytest.mark.parametrize("rows, n_in, n_out", [(32768, 5, 16), (32769, 64, 64), (33001, 65, 65), (40000, 201, 50), (32770, 256, 128),
                                                (32768, 257, 130), (33007, 320, 300), (32801, 512, 512), (32768, 511, 1024),
                                                (32790, 512, 1025), (32768, 513, 100), (131073, 40, 33), (131100, 130, 127)])
@@ -464,6 +472,13 @@ def test_backward_sizes(rows, n_in, n_out, kind):
 @pytest.mark.parametrize("kind, act", [("f32", RELU), ("bf16", RELU), ("bf16", IDENT)])
 def test_backward_larger(rows, n_in, n_out, kind, act):
     kept, dy, W, a, t = _case(rows, n_in, n_out, act, kind)
+    _check_backward(kept, dy, W, a, t, kind)
+
+
+@pytest.mark.parametrize("rows, n_in, n_out", [(13001, 1100, 550), (12950, 1088, 512), (100101, 256, 40), (99001, 250, 33)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_backward_in_the_largest_tiles(rows, n_in, n_out, kind):
+    kept, dy, W, a, t = _case(rows, n_in, n_out, RELU, kind)
     _check_backward(kept, dy, W, a, t, kind)
 
 
