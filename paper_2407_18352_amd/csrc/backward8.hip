@@ -9,8 +9,8 @@
 // another.  131,072 rows of 2048 <- 2048 in bf16: W laid out 8 us, dx 0.92 ms,
 // dw 1.07-1.14 ms (1.0 PFLOP/s; the matrix cores work in 44% of its cycles, held
 // up by the conversion of the codes between them), parts joined 14 us.  262,144
-// rows of 256 <- 256: 5, 70, 62 and 7 us; dx and dw are bound by memory (335 MB
-// at 4.8 TB/s; 201 MB at 3.2 TB/s).
+// rows of 256 <- 256: 5, 66, 64 and 7 us; dx and dw are bound by memory (337 MB
+// at 5.1 TB/s; 203 MB at 3.2 TB/s).
 #include <cmath>
 #include <type_traits>
 
