@@ -672,3 +672,87 @@ def test_backward_refusals():
     n_out = _abi.MAX_WIDTH8 + 1
     assert _abi.lib().hpacml8_backward(kept.desc, dy.data_ptr(), 0, n_out, n_out, None, 0, dw.data_ptr(), 32, None, None,
                                        0, 0, None, 0, None) == _abi.E_UNSUPPORTED
+
+
+# ---- graphs and long offsets -------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows, n_in, n_out", [(3, 200, 96), (60, 64, 64), (700, 96, 130), (5000, 256, 192), (33000, 128, 64)])
+def test_replayed_from_a_graph(rows, n_in, n_out):
+    """Every replay, with other inputs and eager work in between, has the eager
+    calls' bits."""
+    torch = _torch()
+    layer = api.Linear8(_rand(70, (n_out, n_in)))
+    z, dy = torch.empty((rows, n_in), dtype=torch.bfloat16, device="cuda"), torch.empty((rows, n_out), dtype=torch.bfloat16, device="cuda")
+    W = _rand(71, (n_out, n_in), "bf16")
+    kept = api.Checkpoint8(rows, n_in, RELU)
+
+    def outputs():
+        return (torch.empty((rows, n_out), device="cuda"), torch.empty((rows, n_in), dtype=torch.bfloat16, device="cuda"),
+                torch.empty((n_out, n_in), device="cuda"), torch.empty(n_out, device="cuda"), torch.empty_like(z))
+
+    def calls(o, scratch, stream):
+        y, a, dw, db, dx = o
+        api.checkpoint8_save(kept, z, a, stream=stream)
+        api.linear8(layer, a, y, RELU, scratch=scratch, stream=stream)
+        api.backward8(kept, dy, dw, db, W=W, dx=dx, scratch=scratch, stream=stream)
+
+    z.copy_(_rand(72, (rows, n_in)))
+    dy.copy_(_rand(73, (rows, n_out)))
+    scratch = torch.empty(max(layer.scratch_bytes(rows), api.backward8_scratch_bytes(kept, dy, W)), dtype=torch.uint8, device="cuda")
+    replayed, s = outputs(), torch.cuda.Stream()
+    calls(replayed, scratch, None)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        calls(replayed, scratch, s)
+    for i in range(4):
+        z.copy_(_rand(80 + i, (rows, n_in)))
+        dy.copy_(_rand(90 + i, (rows, n_out)))
+        for t in replayed:
+            t.fill_(-3)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = outputs()
+        calls(eager, torch.empty_like(scratch), None)
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(replayed, eager)), i
+
+
+# (rows, pitch): offsets in the last rows pass 2^32 bytes; few rows, many rows, pitches beyond what a tile's offsets hold
+@pytest.mark.parametrize("rows, pitch", [(40, 1 << 26), (70001, 1 << 15), (1100, 1 << 22)])
+@pytest.mark.parametrize("n_in, n_out", [(64, 64), (70, 40)])
+def test_rows_far_apart(rows, pitch, n_in, n_out):
+    torch = _torch()
+
+    def far(width, kind=torch.bfloat16, like=None):
+        t = torch.empty((rows, pitch), dtype=kind, device="cuda")[:, pitch - 128:][:, :width]
+        if like is not None:
+            t.copy_(like)
+        return t
+
+    x, dy, W = _rand(74, (rows, n_in), "bf16"), _rand(75, (rows, n_out), "bf16"), _rand(76, (n_out, n_in), "bf16")
+    layer = api.Linear8(_rand(77, (n_out, n_in)))
+    blocks = -(-n_in // 32)
+    results = []
+    for apart in (False, True):
+        y = far(n_out) if apart else torch.empty((rows, n_out), dtype=torch.bfloat16, device="cuda")
+        api.linear8(layer, far(n_in, like=x) if apart else x, y, RELU)
+        results.append([y.clone()])
+        del y
+        kept = api.Checkpoint8(rows, n_in, RELU, far(blocks * 32, torch.uint8), far(blocks, torch.uint8)) if apart else \
+            api.Checkpoint8(rows, n_in, RELU)
+        a = far(n_in) if apart else torch.empty((rows, n_in), dtype=torch.bfloat16, device="cuda")
+        api.checkpoint8_save(kept, x, a)
+        back = far(n_in) if apart else torch.empty_like(x)
+        api.checkpoint8_load(kept, back)
+        results[-1] += [a.clone(), back.clone(), kept.codes[:, :blocks * 32].clone(), kept.exps[:, :blocks].clone()]
+        del a, back
+        dw, db = torch.empty((n_out, n_in), device="cuda"), torch.empty(n_out, device="cuda")
+        dx = far(n_in) if apart else torch.empty_like(x)
+        api.backward8(kept, far(n_out, like=dy) if apart else dy, dw, db, W=W, dx=dx)
+        results[-1] += [dw, db, dx.clone()]
+        torch.cuda.synchronize()
+        del dx, kept
+    torch.cuda.empty_cache()
+    assert all(torch.equal(u, v) for u, v in zip(*results)), [torch.equal(u, v) for u, v in zip(*results)]
