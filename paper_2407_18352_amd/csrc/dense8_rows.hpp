@@ -46,6 +46,50 @@ __device__ __forceinline__ void load_chunk(const uint16_t *p, int n, float (&v)[
             v[e] = e < n ? v[e] : 0.f;
     }
 }
+// N chunks of rows of `width` values at once: all their loads go out before
+// the first is waited for (load_chunk's branch makes each wait for its own).
+// Chunk h is at at(h) and has left(h) values in front of its row's end; where
+// that is less than a chunk the row's last eight values are read and moved
+// down.  N chunks one by one where a row has no eight values.
+template <typename T, int N, typename At, typename Left>
+__device__ __forceinline__ void load_chunks(int width, At at, Left left, float (&v)[N][kChunk]) {
+    if (width < kChunk) {
+#pragma unroll
+        for (int h = 0; h < N; ++h)
+            load_chunk(at(h), left(h), v[h]);
+        return;
+    }
+    constexpr int kParts = sizeof(T) / 2;
+    u32x4 raw[N][kParts];
+#pragma unroll
+    for (int h = 0; h < N; ++h) {
+        const T *p = at(h) + min(left(h) - kChunk, 0);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+            raw[h][i] = ((const u32x4_any *)p)[i];
+    }
+#pragma unroll
+    for (int h = 0; h < N; ++h) {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            const uint32_t w = raw[h][sizeof(T) == 4 ? e / 4 : 0][sizeof(T) == 4 ? e % 4 : e / 2];
+            v[h][e] = __builtin_bit_cast(float, sizeof(T) == 4 ? w : e % 2 ? w & 0xFFFF0000u : w << 16);
+        }
+        const int down = kChunk - left(h);
+        if (__any(down > 0)) {
+#pragma unroll
+            for (int d = 4; d > 0; d /= 2)
+#pragma unroll
+                for (int e = 0; e < kChunk; ++e) {
+                    const float from = e + d < kChunk ? v[h][e + d] : 0.f;
+                    v[h][e] = down > 0 && (down & d) ? from : v[h][e];
+                }
+#pragma unroll
+            for (int e = 0; e < kChunk; ++e)
+                v[h][e] = down >= kChunk ? 0.f : v[h][e];
+        }
+    }
+}
 __device__ __forceinline__ void store_chunk(float *p, int n, const float (&v)[kChunk]) {
     if (n >= kChunk) {
         ((f32x4_any *)p)[0] = f32x4{v[0], v[1], v[2], v[3]};

@@ -2,13 +2,15 @@
 // exact 32-bit sums, fp32 epilogue.
 //
 // Three ways, by the number of points and the widths:
-//   up to 64 points: few_kernel; one point through 4096 -> 4096 takes 5-6 us of
-//     the device (3.4 us are the 16.8 MB of weights at a copy's rate);
+//   up to 64 points: few_kernel; one point through 4096 -> 4096 takes 4.1 us of
+//     the device, the weights in the caches (16.8 MB, 3.4 us at a copy's rate);
 //   many points of a narrow layer: narrow_kernel, bound by memory; 65,536 x 512
 //     -> 512 in bf16 takes 41 us (27 us at a copy's rate);
 //   otherwise the codes are formed by a launch of their own and the product is
 //     the general one, bound by the matrix cores: 131,072 x 4096 -> 4096 takes
 //     0.31 ms for the codes (1.6 GB, 5.1 TB/s) and 1.7-1.85 ms for the product.
+#include <type_traits>
+
 #include "dense8_nt.hpp"
 #include "dense8_rows.hpp"
 
@@ -66,10 +68,14 @@ void launch_tiled(const Linear8Args &a, hipStream_t stream) {
 // their bytes are on the way at a time.  A block takes 16 outputs (one per
 // fragment row) and all points; its eight waves split k, read their fragments
 // straight into registers (the blocked layout is the fragment), and add their
-// exact integer sums through LDS.  FUSED (codes of up to 36 KB): every block
-// forms the points' codes itself, its weights already on the way, which saves
-// a launch.
-constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewPoints = 64, kFusedBytes = 36 * 1024;
+// exact integer sums through LDS.  FUSED (up to 32 points, codes of up to 36
+// KB): every block forms the points' codes itself, its weights already on the
+// way, which saves a launch: 512 -> 512 in bf16, device us and us of a call from
+// the host, so and with a launch for the codes: 8 points 3.5 and 6.6, 5.4 and
+// 9.5; 24 points 5.6 and 6.6, 6.0 and 9.6; 48 points 7.9 and 7.8, 6.2 and 9.4.
+// Its code is kept short, a chunk or two of a row at a time: with eight of them
+// (so that all points' loads were on the way at once) 9 points took 7.3 us.
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewPoints = 64, kFusedPoints = 32, kFusedBytes = 36 * 1024;
 // of a row of codes in LDS: 16 rows at one k lie on different banks
 constexpr int64_t fused_pitch(int64_t slabs) { return slabs * kSlabBytes + 16; }
 
@@ -94,47 +100,74 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
     weights(wave);
 
     if constexpr (FUSED) {
-        // one point: by the whole block; more: a wave each
+        // one point: by the whole block; more: a wave each, kHeld chunks of a
+        // lane at a time: of one point (per of them), or of kHeld points
         const bool one = p.rows == 1;
-        const int step = one ? kFewThreads : 64, first = one ? tid : lane;
-        constexpr int kHeld = 4;
-        float v[kHeld][kChunk];
-        for (int r = one ? 0 : wave; r < p.rows; r += kFewWaves) {
-            const X *x = (const X *)p.x + r * p.ldx;
-            uint32_t top = 0;
-            for (int c = first; c < chunks; c += kHeld * step) {
+        const int step = one ? kFewThreads : 64, first = one ? tid : lane, points = (int)p.rows;
+        auto form = [&](auto held) {
+            constexpr int kHeld = decltype(held)::value;
+            int per_log = 0;
+            while ((1 << per_log) < kHeld && (step << per_log) < chunks)
+                ++per_log;
+            const int per = 1 << per_log, at_once = kHeld >> per_log;
+            float v[kHeld][kChunk];
+            for (int r0 = one ? 0 : wave; r0 < points; r0 += kFewWaves * at_once) {
+                auto point = [&](int h) { return r0 + (h >> per_log) * kFewWaves; };
+                auto load = [&](int c) {
+                    auto k = [&](int h) { return (c + (h & (per - 1)) * step) * kChunk; };
+                    load_chunks<X>(
+                        p.n_in, [&](int h) { return (const X *)p.x + min(point(h), points - 1) * p.ldx + k(h); },
+                        [&](int h) { return p.n_in - k(h); }, v);
+                };
+                uint32_t top[kHeld] = {};
+                for (int c = first; c < chunks; c += step << per_log) {
+                    load(c);
 #pragma unroll
-                for (int h = 0; h < kHeld; ++h) {
-                    const int k = (c + h * step) * kChunk;
-                    load_chunk(x + k, p.n_in - k, v[h]);
+                    for (int h = 0; h < kHeld; ++h)
+                        top[h] = max(top[h], top_bits(v[h]));
                 }
+                // a row's largest: at its first chunk, and from there at the others
+#pragma unroll
+                for (int d = 1; d < kHeld; d *= 2)
+                    if (d < per)
+#pragma unroll
+                        for (int h = 0; h < kHeld; h += 2 * d)
+                            top[h] = max(top[h], top[h + d]);
 #pragma unroll
                 for (int h = 0; h < kHeld; ++h)
-                    top = max(top, top_bits(v[h]));
-            }
-            top = lanes_max<64>(top);
-            if (one) {
-                if (lane == 0)
-                    tops[wave] = top;
-                __syncthreads();
+                    top[h] = h & (per - 1) ? top[h > 0 ? h - 1 : 0] : lanes_max<64>(top[h]);
+                if (one) {
+                    if (lane == 0)
+                        tops[wave] = top[0];
+                    __syncthreads();
+                    uint32_t all = 0;
 #pragma unroll
-                for (int i = 0; i < kFewWaves; ++i)
-                    top = max(top, tops[i]);
-            }
-            const RowScale sc(top);
-            if (first == 0)
-                scales[r] = sc.scale;
-            for (int c = first; c < chunks; c += kHeld * step) {
+                    for (int i = 0; i < kFewWaves; ++i)
+                        all = max(all, tops[i]);
 #pragma unroll
-                for (int h = 0; h < kHeld; ++h) {
-                    const int k = (c + h * step) * kChunk;
-                    if (chunks > kHeld * step)
-                        load_chunk(x + k, p.n_in - k, v[h]);
-                    if (c + h * step < chunks)
-                        *(uint2 *)(codes + r * pitch + k) = sc.codes(v[h]);
+                    for (int h = 0; h < kHeld; ++h)
+                        top[h] = all;
+                }
+                for (int c = first; c < chunks; c += step << per_log) {
+                    if (chunks > step << per_log)
+                        load(c);
+#pragma unroll
+                    for (int h = 0; h < kHeld; ++h) {
+                        const RowScale sc(top[h]);
+                        const int at = c + (h & (per - 1)) * step;
+                        if (point(h) < points && at < chunks) {
+                            if (at == 0)
+                                scales[point(h)] = sc.scale;
+                            *(uint2 *)(codes + point(h) * pitch + at * kChunk) = sc.codes(v[h]);
+                        }
+                    }
                 }
             }
-        }
+        };
+        if (chunks <= step)
+            form(std::integral_constant<int, 1>());
+        else
+            form(std::integral_constant<int, 2>());
         __syncthreads();
     }
 
@@ -185,9 +218,9 @@ void launch_few(const Linear8Args &a, hipStream_t stream) {
     const dim3 grid((a.n_out + 15) / 16);
     if (a.rows <= 16)
         few_kernel<X, Y, 1, FUSED><<<grid, kFewThreads, 0, stream>>>(a);
-    else if (a.rows <= 32)
+    else if (FUSED || a.rows <= 32)
         few_kernel<X, Y, 2, FUSED><<<grid, kFewThreads, 0, stream>>>(a);
-    else
+    else if constexpr (!FUSED)
         few_kernel<X, Y, 4, FUSED><<<grid, kFewThreads, 0, stream>>>(a);
 }
 
@@ -331,7 +364,7 @@ void launch_narrow(const Linear8Args &a, hipStream_t stream) {
 }
 
 bool few_fused(int64_t rows, int32_t n_in) {
-    return rows <= kFewPoints && rows * fused_pitch(slabs_of(n_in)) <= kFusedBytes;
+    return rows <= kFusedPoints && rows * fused_pitch(slabs_of(n_in)) <= kFusedBytes;
 }
 // (16384 x 512 <- 512 takes 24.5 us this way and 20.7 us with the codes in memory)
 bool narrow(int64_t rows, int32_t n_in, int32_t n_out) { return rows >= 32768 && rows <= (1 << 30) && n_in <= 512 && n_out <= 1024; }
