@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kTile = 32;
 constexpr int kStep = 32;        // of a sum, per matrix instruction
-constexpr int kAhead = 2;        // steps of a wave on the way at a time
+constexpr int kAhead = 1;        // steps of a wave on the way at a time
 
 struct FewArgs {
     hpacml8_checkpoint c;
