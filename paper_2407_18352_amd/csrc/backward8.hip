@@ -668,18 +668,19 @@ void launch_join(const JoinArgs &j, hipStream_t st) {
 // block each; that launch reads an operand again for every 32 results across.
 // Device us, one launch and the general form, of (rows) outputs <- inputs:
 //                                fp32           bf16
-//   (256) 64 <- 64             7.2   16.5      5.3  12.9
-//   (256) 512 <- 512 (384)    14.0   34.4      8.8  17.6
-//   (1024) 256 <- 256 (320)   23.6   27.5     15.6  16.1
-//   (256) 64 <- 2048 (640)    18.6   18.1     11.4  13.9
-//   (512) 64 <- 2048 (1152)   30.4   20.4     18.4  15.2
-//   (1) 1024 <- 1024 (1056)   20.6   46.1     14.4  16.3
-//   (256) 1024 <- 1024 (1280) 38.8   57.6     23.2  19.2
-//   (4096) 64 <- 64 (260)     50.6   18.2     34.2  15.5
-// (fp32 with many outputs: the general form's dx takes six products in turn.)
-bool few_rows(int64_t rows, int32_t n_out, int32_t n_in, bool f32) {
+//   (256) 64 <- 64             5.2   16.5      4.3  12.9
+//   (256) 512 <- 512 (384)    10.1   34.4      5.9  17.6
+//   (1024) 256 <- 256 (320)   16.0   27.5     10.7  16.1
+//   (256) 64 <- 2048 (640)     8.3   18.1      6.2  13.9
+//   (1024) 512 <- 512 (768)   23.5   41.2     13.9  21.5
+//   (1) 1024 <- 1024 (1056)   13.5   46.1      7.2  16.3
+//   (512) 64 <- 2048 (1152)   14.0   20.4     10.0  15.2
+//   (256) 1024 <- 1024 (1280) 24.5   57.6     13.3  19.2
+// and, of an earlier form that took up to twice as long, (4096) 64 <- 64 50.6
+// and 18.2 in fp32, (64) 2048 <- 2048 (4224) 58 and 34 in bf16.
+bool few_rows(int64_t rows, int32_t n_out, int32_t n_in) {
     auto tiles = [](int64_t n) { return (n + 31) / 32; };
-    return rows <= 1024 && tiles(n_in) * (tiles(rows) + tiles(n_out)) <= (f32 && n_out >= 512 ? 1280 : 640);
+    return rows <= 1024 && tiles(n_in) * (tiles(rows) + tiles(n_out)) <= 1280;
 }
 
 }  // namespace
@@ -687,7 +688,7 @@ bool few_rows(int64_t rows, int32_t n_out, int32_t n_in, bool f32) {
 Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_t dtype, int64_t lddy, int32_t n_out,
                              bool want_dw, bool want_dx) {
     Backward8Plan p{};
-    p.few = few_rows(c.rows, n_out, c.width, dtype == HPACML_F32);   // (the scratch asked for does not depend on it)
+    p.few = few_rows(c.rows, n_out, c.width);   // (the scratch asked for does not depend on it)
     p.planes = dtype == HPACML_F32 ? 3 : 1;
     // dw reads whole 16-byte chunks of dy's rows, dx whole slabs, both with 32-bit offsets in a tile
     p.direct = dtype == HPACML_BF16 && ((uintptr_t)dy & 15) == 0 && lddy % 8 == 0 && lddy < (1 << 22) &&
