@@ -5,6 +5,7 @@
 #include <new>
 
 #include "dense8.hpp"
+#include "span.hpp"
 
 using namespace hpacml;
 
@@ -27,27 +28,6 @@ bool is_type(int32_t t) { return t == HPACML_F32 || t == HPACML_BF16; }
 int64_t size_of(int32_t t) { return t == HPACML_F32 ? 4 : 2; }
 bool is_act(int32_t a) { return a == HPACML_ACT_IDENTITY || a == HPACML_ACT_RELU; }
 constexpr int64_t kMaxRows = INT32_MAX, kMaxPitch = INT32_MAX;
-
-// A matrix operand: `rows` rows of `width` bytes, `pitch` bytes apart.
-struct Span {
-    const char *at;
-    int64_t rows, pitch, width;
-    bool written;
-    const char *end() const { return at + (rows - 1) * pitch + width; }
-};
-
-// No element in common: ranges that do not meet, or rows of equal pitch that
-// keep to columns of their own.
-bool disjoint(const Span &a, const Span &b) {
-    if (a.end() <= b.at || b.end() <= a.at)
-        return true;
-    if (a.pitch != b.pitch)
-        return false;
-    int64_t r = (b.at - a.at) % a.pitch;
-    if (r < 0)
-        r += a.pitch;
-    return a.width <= r && r + b.width <= a.pitch;
-}
 
 // The operands of one call.  `add` checks one: aligned device memory of the
 // current device, inside its allocation.
@@ -82,7 +62,7 @@ struct Operands {
             status = HPACML_E_INVAL;
             return;
         }
-        if (v.end() > (const char *)base + size) {
+        if (!inside(v, (const char *)base, size)) {
             status = HPACML_E_RANGE;
             return;
         }

@@ -75,3 +75,56 @@ def test_null_arguments():
     assert L.hpacml8_checkpoint_save(None, FAKE, 0, 40, None, 0, 0, None) == _abi.E_INVAL
     assert L.hpacml8_checkpoint_load(None, FAKE, 0, 40, None) == _abi.E_INVAL
     L.hpacml8_linear_destroy(None)
+
+
+SPANS = r"""
+#include <cstdio>
+#include "span.hpp"
+using namespace hpacml;
+int main() {
+    const char *base = (const char *)0x7f0000000000;
+    long long at, rows, pitch, width, size, at2;
+    while (std::scanf("%lld %lld %lld %lld %lld %lld", &at, &rows, &pitch, &width, &size, &at2) == 6) {
+        const Span s{base + at, rows, pitch, width, false};
+        const bool in = inside(s, base, (uint64_t)size);
+        std::printf("%d %d\n", in, in && disjoint(s, Span{base + at2, rows, pitch, width, true}));
+    }
+}
+"""
+
+
+def _compiled(tmp_path, source):
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text(source)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"),
+                    "-I", os.path.join(ROOT, "paper_2407_18352_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    return lambda text: subprocess.run([str(exe)], input=text, capture_output=True, text=True, check=True).stdout
+
+
+def test_operands_against_their_allocations(tmp_path):
+    """Inside exactly where the last row's end is, in whole numbers of any
+    length: rows times pitch passes 64 bits for 2^31 rows of 2^31 fp32 values."""
+    big, cases = 2 ** 31 - 1, []
+    for size in (0, 1, 64, 1 << 20, 1 << 38, 1 << 47):
+        for at in (0, 1, 63, 64, size - 1, size, size + 1):
+            for rows in (1, 2, 3, 1000, 1 << 20, big - 1, big):
+                for pitch in (1, 16, 64, 1 << 20, big, 2 * big, 4 * big, 4 * big - 3):
+                    for width in {1, min(16, pitch), pitch}:
+                        if at >= 0:
+                            cases.append((at, rows, pitch, width, size, at + width))
+    # the end itself, a byte less, a byte more
+    for rows, pitch, width in ((7, 100, 30), (big, 64, 64), (big, 4 * big, 16), (3, 4 * big, 4 * big)):
+        for more in (-1, 0, 1):
+            size = (rows - 1) * pitch + width + more
+            if size < 2 ** 62:
+                cases.append((0, rows, pitch, width, size, width))
+    out = _compiled(tmp_path, SPANS)("".join("%d %d %d %d %d %d\n" % c for c in cases)).split("\n")
+    accepted = 0
+    for c, line in zip(cases, out):
+        at, rows, pitch, width, size, at2 = c
+        fits = at + (rows - 1) * pitch + width <= size
+        # the second begins `width` after the first: beside it in its rows or past its end
+        apart = fits and (rows == 1 or 2 * width <= pitch)
+        assert line == "%d %d" % (fits, apart), c
+        accepted += fits
+    assert len(out) == len(cases) + 1 and accepted > 300
