@@ -35,8 +35,9 @@ extern "C" {
  *     s_i = max_k |x_ik| / 127,  q_ik = rint(x_ik * (127 / max_k |x_ik|))
  * (fp32 arithmetic, ties to even), t_j and w_jk the same of W_j, and
  *     y_ij = act(s_i * t_j * sum_k q_ik w_jk + b_j),
- * the sum in exact 32-bit integers, the rest in fp32, rounded once to y's
- * type.  A row whose largest magnitude is below 2^-119 counts as zeros; a row
+ * the sum in exact 32-bit integers, the rest in fp32 (what lies between the sum
+ * and the result leaves fp32's range only where the result does), rounded once
+ * to y's type.  A row whose largest magnitude is below 2^-119 counts as zeros; a row
  * of inputs or weights that holds an infinity or a NaN makes the results it
  * reaches NaN (a ReLU keeps a NaN). */
 typedef struct hpacml8_linear_s hpacml8_linear;

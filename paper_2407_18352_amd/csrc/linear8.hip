@@ -18,6 +18,30 @@ namespace hpacml {
 
 namespace {
 
+// A result in fp32 before its activation.  A sum of codes (below 2^29) times a
+// point's scale passes fp32's range where the scale is above 2^99, though the
+// output's scale may bring it back: a far point's scale is taken in two factors
+// (FAR; a rounding of the other points' results may change by it).  Waves with
+// such a point run a form of their own: 65,536 x 256 <- 256 in bf16 takes 18.1 us
+// so, 22.5 with two factors everywhere, 23.5 with a choice at each value.
+constexpr float kFar = 0x1p90f;
+template <bool FAR>
+__device__ __forceinline__ float scaled(int32_t sum, float s, float t, float bias) {
+    if (!FAR)
+        return (float)sum * s * t + bias;
+    const bool two = s > kFar;
+    return (float)sum * (two ? s * 0x1p-64f : s) * t * (two ? 0x1p64f : 1.f) + bias;
+}
+// one of the wave's points is such a one (not by a NaN)
+template <int N>
+__device__ __forceinline__ bool any_far(const float (&s)[N]) {
+    float most = s[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i)
+        most = fmaxf(most, s[i]);
+    return __any(most > kFar);
+}
+
 template <typename Y, bool MERGE, int WA, int WB, int NA, int NB>
 __global__ void __launch_bounds__(64 * WA * WB, 2) linear8_kernel(Linear8Args p, uint32_t out_tiles, uint32_t point_tiles) {
     typedef nt::Product<nt::I8, Y, true, MERGE, WA, WB, NA, NB> T;
@@ -30,17 +54,23 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) linear8_kernel(Linear8Args p,
 #pragma unroll
               for (int b = 0; b < NB; ++b)
                   s[b] = p.s[min(b0 + t.point_of(b), p.rows - 1)];
-              t.store((Y *)p.y, p.ldy, a0, p.n_out, b0, p.rows,
-                      [&](int a, int64_t n, int b, float (&v)[4]) {
-                          const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
+              auto store = [&](auto far) {
+                  t.store((Y *)p.y, p.ldy, a0, p.n_out, b0, p.rows,
+                          [&](int a, int64_t n, int b, float (&v)[4]) {
+                              const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
 #pragma unroll
-                          for (int e = 0; e < 4; ++e) {
-                              v[e] = (float)acc[a][b][e] * s[b] * sc[e] + bias[e];
-                              if (p.relu)
-                                  v[e] = relu_keep_nan(v[e]);
-                          }
-                      },
-                      [](int, int, u32x4 &) {});
+                              for (int e = 0; e < 4; ++e) {
+                                  v[e] = scaled<decltype(far)::value>(acc[a][b][e], s[b], sc[e], bias[e]);
+                                  if (p.relu)
+                                      v[e] = relu_keep_nan(v[e]);
+                              }
+                          },
+                          [](int, int, u32x4 &) {});
+              };
+              if (any_far(s))
+                  store(std::true_type());
+              else
+                  store(std::false_type());
           });
 }
 
@@ -206,7 +236,8 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
 #pragma unroll
         for (int k = 0; k < kFewWaves; ++k)
             sum += part[k][b][from];
-        float v = (float)sum * (FUSED ? scales[b * 16 + point] : p.s[r]) * p.t[n] + p.b[n];
+        const float scale = FUSED ? scales[b * 16 + point] : p.s[r];
+        float v = scaled<true>(sum, scale, p.t[n], p.b[n]);
         if (p.relu)
             v = relu_keep_nan(v);
         store_value((Y *)p.y + r * p.ldy + n, v);
@@ -241,7 +272,12 @@ template <typename Y, int SLABS, int WA, int WB, int NA, int NB>
 struct Narrow {
     static constexpr int kPoints = 16 * NB * WB, kRows = kPoints / 4, kOuts = 16 * NA * WA;
     static constexpr int kCodes = kPoints / 16 * SLABS * 1024, kOut = 4 * 16 * nt::Out<Y, NA>::kRow;
-    static constexpr int kFit = 160 * 1024 / (kCodes + kOut), kPerCu = kPoints == 128 ? 2 : kFit < 4 ? kFit : 4;
+    static constexpr int kFit = 160 * 1024 / (kCodes + kOut);
+    // 64 points of fp32 results have no room in a quarter of a CU's registers:
+    // 65,536 x 256 <- 256 in fp32 takes 32.9 us with four blocks of them a CU, 27.1
+    // with three
+    static constexpr int kMost = sizeof(Y) == 4 && NB == 4 ? 3 : 4;
+    static constexpr int kPerCu = kPoints == 128 ? 2 : kFit < kMost ? kFit : kMost;
     static_assert(WA * WB == 4 && kPerCu >= 2, "four waves, two blocks");
 };
 
@@ -305,41 +341,47 @@ __global__ void __launch_bounds__(256, (Narrow<Y, SLABS, WA, WB, NA, NB>::kPerCu
         for (int t = 0; t < NA; ++t)
             a[t] = *(const u32x4 *)(p.w + ((int64_t)min(pass * (kOuts / 16) + wa * NA + t, last) * p.slabs + slab) * 1024 + at);
     };
-    u32x4 a[NA], next[NA];
-    weights(0, 0, a);
-    const int passes = (p.n_out + kOuts - 1) / kOuts;
-    for (int pass = 0; pass < passes; ++pass) {
-        i32x4 acc[NA][NB] = {};
-        for (int slab = 0; slab < p.slabs; ++slab) {
-            const bool more = slab + 1 < p.slabs;
-            weights(more ? pass : min(pass + 1, passes - 1), more ? slab + 1 : 0, next);
-            u32x4 b[NB];
+    auto go = [&](auto far) {
+        u32x4 a[NA], next[NA];
+        weights(0, 0, a);
+        const int passes = (p.n_out + kOuts - 1) / kOuts;
+        for (int pass = 0; pass < passes; ++pass) {
+            i32x4 acc[NA][NB] = {};
+            for (int slab = 0; slab < p.slabs; ++slab) {
+                const bool more = slab + 1 < p.slabs;
+                weights(more ? pass : min(pass + 1, passes - 1), more ? slab + 1 : 0, next);
+                u32x4 b[NB];
 #pragma unroll
-            for (int u = 0; u < NB; ++u)
-                b[u] = *(const u32x4 *)(codes + ((wb * NB + u) * p.slabs + slab) * 1024 + at);
+                for (int u = 0; u < NB; ++u)
+                    b[u] = *(const u32x4 *)(codes + ((wb * NB + u) * p.slabs + slab) * 1024 + at);
 #pragma unroll
-            for (int u = 0; u < NB; ++u)
+                for (int u = 0; u < NB; ++u)
+#pragma unroll
+                    for (int t = 0; t < NA; ++t)
+                        acc[t][u] = nt::I8::mul(a[t], b[u], acc[t][u]);
 #pragma unroll
                 for (int t = 0; t < NA; ++t)
-                    acc[t][u] = nt::I8::mul(a[t], b[u], acc[t][u]);
+                    a[t] = next[t];
+            }
+            const int64_t a0 = (int64_t)pass * kOuts + wa * NA * 16;
+            if (a0 < p.n_out)
+                Out::template store<NB, false>(out + wave * 16 * Out::kRow, lane, (Y *)p.y, p.ldy, a0, p.n_out, p0 + wb * NB * 16, p.rows,
+                                        [&](int t, int64_t n, int u, float (&v)[4]) {
+                                            const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
 #pragma unroll
-            for (int t = 0; t < NA; ++t)
-                a[t] = next[t];
+                                            for (int e = 0; e < 4; ++e) {
+                                                v[e] = scaled<decltype(far)::value>(acc[t][u][e], s[u], sc[e], bias[e]);
+                                                if (p.relu)
+                                                    v[e] = relu_keep_nan(v[e]);
+                                            }
+                                        },
+                                        [](int, int, u32x4 &) {});
         }
-        const int64_t a0 = (int64_t)pass * kOuts + wa * NA * 16;
-        if (a0 < p.n_out)
-            Out::template store<NB, false>(out + wave * 16 * Out::kRow, lane, (Y *)p.y, p.ldy, a0, p.n_out, p0 + wb * NB * 16, p.rows,
-                                    [&](int t, int64_t n, int u, float (&v)[4]) {
-                                        const f32x4 sc = *(const f32x4 *)(p.t + n), bias = *(const f32x4 *)(p.b + n);
-#pragma unroll
-                                        for (int e = 0; e < 4; ++e) {
-                                            v[e] = (float)acc[t][u][e] * s[u] * sc[e] + bias[e];
-                                            if (p.relu)
-                                                v[e] = relu_keep_nan(v[e]);
-                                        }
-                                    },
-                                    [](int, int, u32x4 &) {});
-    }
+    };
+    if (any_far(s))
+        go(std::true_type());
+    else
+        go(std::false_type());
 }
 
 template <typename X, typename Y, int SLABS, int WA, int WB, int NB>

@@ -41,3 +41,30 @@ def test_the_longest_operands_are_refused():
                               1 << 60, None) == _abi.E_RANGE
     torch.cuda.synchronize()
     assert not any(t.any() for t in (x, y, s))
+
+
+@pytest.mark.parametrize("rows, n_in, n_out", [(1, 70, 50), (20, 70, 50), (24, 1100, 40), (60, 70, 50), (300, 130, 200),
+                                               (5000, 600, 300), (33001, 70, 50), (33001, 300, 150)])
+@pytest.mark.parametrize("x_kind, y_kind", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("large", ["x", "W"])
+def test_linear_of_values_whose_sums_alone_leave_the_range(rows, n_in, n_out, x_kind, y_kind, large):
+    """A scale times the sum of codes passes 3.4e38 long before the result
+    does, when the other scale is small: points of magnitudes up to 3e38
+    against weights from 1e-36, and the other way round."""
+    import torch
+    from test_gpu_dense8 import _check_linear, _dtype, _rand
+    high = lambda n: 10.0 ** torch.linspace(38.4, 25, n, device="cuda", dtype=torch.float64)[:, None]
+    low = lambda n: 10.0 ** torch.linspace(-36, -5, n, device="cuda", dtype=torch.float64)[:, None]
+    unit = lambda seed, n: (_rand(seed, (n, n_in)) / 8).clamp(-1, 1).double()      # results stay below 3e38
+    x = unit(1, rows) * (high if large == "x" else low)(rows)
+    W = unit(2, n_out) * (low if large == "x" else high)(n_out)
+    if large == "x":
+        x[:, 0], W[:, 0] = x.abs().amax(1), W.abs().amax(1)      # sums that are not 0
+    limit = 3.0e38 / n_in
+    W *= (limit / (x.abs().max() * W.abs().max())).clamp(max=1)
+    W = W.float()
+    if large == "x" and rows >= 3 and n_out >= 3:
+        W[2] = 0
+        x[2], W[1] = 0, 0
+        x[2, 1], W[1, 2] = 3e38, 3e38 * 2.0 ** -128              # a sum of 0, of a large point
+    _check_linear(x.to(_dtype(x_kind)), W, _rand(3, (1, n_out))[0], IDENT, y_kind)
