@@ -43,18 +43,13 @@ constexpr int kTurn = 64;       // channels of a block of W, by one slab's outpu
 
 // a chunk of eight values as bf16, or as its three terms
 __device__ __forceinline__ void store_planes(char *at, int64_t plane, const float (&v)[kChunk], float) {
-    uint32_t w[3][4];
+    uint32_t w[4][3];
 #pragma unroll
-    for (int e = 0; e < kChunk; ++e) {
-        uint16_t t[3];
-        split3(v[e], t);
-#pragma unroll
-        for (int q = 0; q < 3; ++q)
-            w[q][e / 2] = e & 1 ? w[q][e / 2] | (uint32_t)t[q] << 16 : t[q];
-    }
+    for (int e = 0; e < kChunk; e += 2)
+        split3(v[e], v[e + 1], w[e / 2]);
 #pragma unroll
     for (int q = 0; q < 3; ++q)
-        *(u32x4 *)(at + q * plane) = u32x4{w[q][0], w[q][1], w[q][2], w[q][3]};
+        *(u32x4 *)(at + q * plane) = u32x4{w[0][q], w[1][q], w[2][q], w[3][q]};
 }
 __device__ __forceinline__ void store_planes(char *at, int64_t, const float (&v)[kChunk], uint16_t) {
     *(u32x4 *)at = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};

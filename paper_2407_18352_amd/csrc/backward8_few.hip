@@ -42,12 +42,11 @@ __device__ __forceinline__ void terms_of(const float (&v)[kChunk], bf16x8 (&t)[T
     } else {
 #pragma unroll
         for (int e = 0; e < kChunk; e += 2) {
-            uint16_t lo[3], hi[3];
-            split3(v[e], lo);
-            split3(v[e + 1], hi);
+            uint32_t two[3];
+            split3(v[e], v[e + 1], two);
 #pragma unroll
             for (int q = 0; q < TERMS; ++q)
-                w[q][e / 2] = lo[q] | (uint32_t)hi[q] << 16;
+                w[q][e / 2] = two[q];
         }
     }
 #pragma unroll

@@ -143,20 +143,21 @@ __device__ __forceinline__ float block_value(uint32_t code, float scale) {
     return RELU ? (float)code * scale : ((float)code - 128.f) * scale;
 }
 
-// x as the exact sum of three bf16 terms, each the nearest to what is left
-// (a term that would round up to infinity is cut instead; infinities and
-// NaNs are the first term alone).
-__device__ __forceinline__ void split3(float x, uint16_t out[3]) {
-    uint16_t hi = bf16_bits(x);
-    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
-    const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
-    if (finite && (hi & 0x7F80u) == 0x7F80u)
-        hi = (uint16_t)(bits >> 16);
-    const float r = x - bf16_bits_value(hi);
-    const uint16_t mid = bf16_bits(r);
-    out[0] = hi;
-    out[1] = finite ? mid : (uint16_t)0;
-    out[2] = finite ? bf16_bits(r - bf16_bits_value(mid)) : (uint16_t)0;
+// x and y, each as the exact sum of three bf16 terms, each the nearest to what
+// is left (the first at most the largest finite one); a word holds a term of
+// both, x's in the low half.  An infinity is 1 of its sign, 0 and itself: the
+// products taken are those of terms whose ranks sum to at most 2, so it meets
+// the other operand's first term alone, which has that operand's sign and is 0
+// only for a 0, and a sum with it is what the operands' own would be (as a first
+// term it would meet second and third ones that are 0 or of the other sign).  A
+// NaN's second and third terms are NaN.
+__device__ __forceinline__ void split3(float x, float y, uint32_t out[3]) {
+    const bool inf_x = __builtin_isinf(x), inf_y = __builtin_isinf(y);
+    const float most_x = inf_x ? 1.f : 0x1.FEp127f, most_y = inf_y ? 1.f : 0x1.FEp127f;
+    out[0] = pack_bf16(__builtin_amdgcn_fmed3f(x, -most_x, most_x), __builtin_amdgcn_fmed3f(y, -most_y, most_y));
+    const float rx = x - __builtin_bit_cast(float, out[0] << 16), ry = y - __builtin_bit_cast(float, out[0] & 0xFFFF0000u);
+    out[1] = pack_bf16(inf_x ? 0.f : rx, inf_y ? 0.f : ry);
+    out[2] = pack_bf16(rx - __builtin_bit_cast(float, out[1] << 16), ry - __builtin_bit_cast(float, out[1] & 0xFFFF0000u));
 }
 
 }  // namespace hpacml

@@ -68,3 +68,76 @@ def test_linear_of_values_whose_sums_alone_leave_the_range(rows, n_in, n_out, x_
         x[2], W[1] = 0, 0
         x[2, 1], W[1, 2] = 3e38, 3e38 * 2.0 ** -128              # a sum of 0, of a large point
     _check_linear(x.to(_dtype(x_kind)), W, _rand(3, (1, n_out))[0], IDENT, y_kind)
+
+
+def _sums(a, b):
+    """sum_j a_ij b_jk in 64 bits, product by product (a library's product need
+    not treat infinities as sums do)."""
+    with np.errstate(invalid="ignore"):
+        return np.concatenate([(a[:, :, None] * b[None, :, k:k + 1]).sum(1) for k in range(b.shape[1])], 1)
+
+
+def _same(got, want, tol):
+    with np.errstate(invalid="ignore"):
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        inf = np.isinf(want)
+        assert np.array_equal(np.isinf(got), inf) and np.array_equal(got[inf], want[inf])
+        ok = np.isfinite(want)
+        assert (np.abs(got - want)[ok] <= np.broadcast_to(tol, want.shape)[ok]).all()
+
+
+@pytest.mark.parametrize("rows, n_in, n_out", [(70, 40, 8), (33, 70, 200), (1100, 72, 40), (1500, 70, 100), (40000, 24, 16)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("act", [RELU, IDENT])
+def test_backward_infinities_follow_the_formula(rows, n_in, n_out, kind, act):
+    """Infinities of either sign and NaNs in dy and W, beside zeros, values
+    exact in 8 bits and others: the results are infinite, and NaN, where the
+    sums of the formulas are."""
+    import torch
+    from test_gpu_dense8 import EPS_SUM, EPSBF, _case, _np
+    inf, nan = float("inf"), float("nan")
+    kept, dy, W, a, through = _case(rows, n_in, n_out, act, kind)
+    dy, W = dy.clone(), W.clone()
+    dy[::3] = (dy[::3] * 256).round() / 256        # few bits, zeros among them
+    W[:, ::2] = (W[:, ::2] * 16).round() / 16
+    dy[5, 1], dy[9, 2], dy[30, 3], dy[rows - 1, 4], dy[31, 1], dy[12, 7] = inf, -inf, inf, -inf, inf, nan
+    W[3, 7], W[4, 9], W[1, 11], W[6, 13], W[1, 15], W[2, 15] = inf, -inf, inf, nan, -inf, inf
+    W[1, 17] = 0.0
+    dw, db = torch.empty((n_out, n_in), device="cuda"), torch.empty(n_out, device="cuda")
+    dx = torch.empty((rows, n_in), dtype=dy.dtype, device="cuda")
+    api.backward8(kept, dy, dw, db, W=W, dx=dx)
+    g, w = _np(dy), _np(W)
+    fin = lambda v: np.abs(np.where(np.isfinite(v), v, 0))
+    terms = 3 if kind == "f32" else 1
+    want = np.where(through, _sums(g, w), 0)
+    tol = (2 * terms * n_out + 2) * EPS_SUM * (fin(g) @ fin(w)) + 1e-37 + (EPSBF * fin(want) if kind == "bf16" else 0)
+    _same(_np(dx), want, tol)
+    _same(_np(dw), _sums(g.T, a), (terms * rows + 2) * EPS_SUM * (fin(g).T @ np.abs(a)) + 1e-37)
+    with np.errstate(invalid="ignore"):
+        _same(_np(db), g.sum(0), (terms * rows + 2) * EPS_SUM * fin(g).sum(0) + 1e-37)
+
+
+@pytest.mark.parametrize("rows", [1, 1100])
+def test_backward_terms_of_fp32_values_add_up(rows):
+    """One row of values of every exponent against a kept 1 and W = 1: the sum of
+    an operand's three terms, exact from 2^-110 on, within 2^-134 below."""
+    import torch
+    z = torch.zeros((rows, 64), device="cuda")
+    z[0] = 1.0
+    kept = api.Checkpoint8(rows, 64, IDENT)
+    api.checkpoint8_save(kept, z)
+    n = 256 * 128
+    bits = torch.randint(0, 1 << 23, (n,), generator=torch.Generator().manual_seed(7), dtype=torch.int32)
+    v = (bits | (torch.arange(n, dtype=torch.int32) // 128 % 255) << 23).view(torch.float32)
+    v[::5] *= -1
+    v[-1], v[-2] = 3.4028234663852886e38, -3.4028234663852886e38
+    eye, dx = torch.eye(64, device="cuda"), torch.empty((rows, 64), device="cuda")
+    dw, db = torch.empty((64, 64), device="cuda"), torch.empty(64, device="cuda")
+    for part in v.split(64):
+        dy = torch.zeros((rows, 64), device="cuda")
+        dy[0] = part.cuda()
+        api.backward8(kept, dy, dw, db, W=eye, dx=dx)
+        want = part.double()
+        tol = torch.where(want.abs() >= 2.0 ** -110, 0.0, 2.0 ** -134)
+        for got in (dw[:, 0], dw[:, 63], db, dx[0]):
+            assert ((got.cpu().double() - want).abs() <= tol).all()
