@@ -117,9 +117,12 @@ hpacml_status hpacml8_checkpoint_load(const hpacml8_checkpoint *c, void *a, int3
  * bf16: products of exact bf16 values on the matrix cores, fp32 sums; dx
  * rounded once.  fp32: each fp32 operand is the exact sum of three bf16 terms
  * (below 2^-110: to within 2^-134, so that less than that counts as 0); dw takes
- * all three products, dx the six largest of nine (what is left out is
- * below 2^-23 of a product).  Infinities and NaNs in dy and W give what the sums
- * above give.  Zero rows: dw and db are set to 0 (accumulate: left).  Asynchronous on `stream`. */
+ * all three products, dx the six largest of nine (what is left out is below
+ * 2^-23 of a product).  Infinities and NaNs in dy and W give what the sums above
+ * give; so do those that `c` stands for in bf16, while in fp32 a block of `c`
+ * with exponent byte 255 counts as NaN in dw.
+ * Zero rows: dw and db are set to 0 (accumulate: left).  Asynchronous on
+ * `stream`. */
 hpacml_status hpacml8_backward(const hpacml8_checkpoint *c, const void *dy, int32_t dtype, int64_t lddy,
                                int32_t n_out, const void *W, int64_t ldw, float *dw, int64_t lddw, float *db,
                                void *dx, int64_t lddx, int32_t accumulate, void *scratch, size_t scratch_bytes,

@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(64 * WA * WB) dw_kernel(DwArgs p) {
             code = *(const u32x4 *)(lds + T::kAtCodes + c_slot * T::kCodes + tid * 16);
             uint32_t e = *(const uint32_t *)(lds + T::kAtExps + c_slot * T::kExps + tid * 4);
             asm("" : "+v"(e));                    // read it without a branch
-            scale = x_row < c_left ? block_scale(e & 0xFFu) : 0.f;
+            scale = x_row < c_left ? block_scale(e & 0xFFu, p.planes) : 0.f;
         };
         auto convert = [&](int e) {
             const uint32_t w = code[e / 2], q = w >> (16 * (e & 1));

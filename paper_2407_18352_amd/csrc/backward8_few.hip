@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) few_backward_kernel(FewArgs p) {
                 const int64_t r = min(r0 + e, rows - 1);
                 // rows of codes are whole blocks of channels: all of a tile's exist
                 const uint32_t exp = exps[r * p.c.ld_exps + k0 / 32];
-                scale[i][e] = r0 + e < rows ? block_scale(exp) : 0.f;
+                scale[i][e] = r0 + e < rows ? block_scale(exp, kTerms) : 0.f;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     code[i][t][e] = codes[r * p.c.ld_codes + k0 + t * 16 + l16];

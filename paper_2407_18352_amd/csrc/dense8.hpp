@@ -129,6 +129,13 @@ __device__ __forceinline__ float block_factor(uint32_t byte) {
 }
 // 2^e of an exponent byte (infinite for 255)
 __device__ __forceinline__ float block_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+// the same for products with an operand's `terms` terms: with three, second and
+// third ones that are 0 or of the other sign make NaN of an infinite value's
+// products by chance, so there 255 is a NaN (in one instruction: the byte comes
+// into the fraction as well, below 2^-15 of a value, which bf16 drops)
+__device__ __forceinline__ float block_scale(uint32_t byte, int terms) {
+    return __builtin_bit_cast(float, __umul24(byte, terms > 1 ? 0x800001u : 0x800000u));
+}
 
 template <bool RELU>
 __device__ __forceinline__ uint32_t block_code(float a, float factor) {

@@ -141,3 +141,32 @@ def test_backward_terms_of_fp32_values_add_up(rows):
         tol = torch.where(want.abs() >= 2.0 ** -110, 0.0, 2.0 ** -134)
         for got in (dw[:, 0], dw[:, 63], db, dx[0]):
             assert ((got.cpu().double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("rows, n_in, n_out", [(70, 100, 8), (1500, 100, 70), (40000, 96, 24), (1200, 600, 600)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("act", [RELU, IDENT])
+def test_backward_of_kept_infinities(rows, n_in, n_out, kind, act):
+    """A block of channels that was kept with an infinity or a NaN: dw is that of
+    the values it stands for in bf16, and NaN in fp32; db, dx and the other
+    blocks are as ever."""
+    import torch
+    from test_gpu_dense8 import EPS_SUM, _np, _rand
+    z = _rand(51, (rows, n_in)).clone()
+    z[7, 3], z[rows - 1, 70] = float("inf"), float("nan") if rows % 3 else float("inf")
+    kept, back = api.Checkpoint8(rows, n_in, act), torch.empty((rows, n_in), device="cuda")
+    api.checkpoint8_save(kept, z)
+    api.checkpoint8_load(kept, back)
+    dy, W = _rand(52, (rows, n_out), kind, 0, 1e-2).clone(), _rand(53, (n_out, n_in), kind)
+    dy[7, 1] = 0
+    dw, db = torch.empty((n_out, n_in), device="cuda"), torch.empty(n_out, device="cuda")
+    dx = torch.empty((rows, n_in), dtype=dy.dtype, device="cuda")
+    api.backward8(kept, dy, dw, db, W=W, dx=dx)
+    a, g, w = _np(back), _np(dy), _np(W)
+    channels = [k for k in range(n_in) if k // 32 in (0, 2)]
+    assert not np.isfinite(a).all(0)[channels].any() and np.isfinite(a).all(0).sum() == n_in - len(channels)
+    want = _sums(g.T, a)
+    if kind == "f32":
+        want[:, channels] = np.nan
+    _same(_np(dw), want, (3 * rows + 2) * EPS_SUM * (np.abs(g).T @ np.abs(np.where(np.isfinite(a), a, 0))) + 1e-37)
+    assert np.isfinite(_np(db)).all() and np.isfinite(_np(dx)).all()
