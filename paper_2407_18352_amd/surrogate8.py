@@ -55,8 +55,12 @@ class Surrogate8:
 
     @torch.no_grad()
     def backward(self, dy, accumulate: bool = False):
-        """Gradients of the loss in ``.grad`` from that of the outputs."""
+        """Gradients of the loss in ``.grad`` (made where an optimizer has taken
+        them away) from that of the outputs."""
         dy = dy.to(torch.bfloat16)
+        for p in self.parameters():
+            if p.grad is None:
+                p.grad = torch.zeros_like(p)
         for l in range(len(self.W) - 1, -1, -1):
             W = self.Wh[l] if l else None
             dx = torch.empty((dy.shape[0], self.dims[l]), dtype=torch.bfloat16, device="cuda") if l else None

@@ -170,3 +170,36 @@ def test_backward_of_kept_infinities(rows, n_in, n_out, kind, act):
         want[:, channels] = np.nan
     _same(_np(dw), want, (3 * rows + 2) * EPS_SUM * (np.abs(g).T @ np.abs(np.where(np.isfinite(a), a, 0))) + 1e-37)
     assert np.isfinite(_np(db)).all() and np.isfinite(_np(dx)).all()
+
+
+# ---- a training loop ----------------------------------------------------------
+
+
+def _model_and_batch(dims=(6, 64, 96, 2), n=300, seed=0):
+    import torch
+    from paper_2407_18352_amd.surrogate8 import Surrogate8
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((n, dims[0]), generator=g, device="cuda")
+    return Surrogate8(dims, seed=1), x, torch.randn((n, dims[-1]), generator=g, device="cuda") / n
+
+
+def _grads(m):
+    return [p.grad.clone() for p in m.parameters()]
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_training_after_zero_grad(accumulate):
+    """An optimizer's zero_grad takes the gradients away (None) or fills them
+    with 0: the next pass has all of them, equal to a new model's."""
+    import torch
+    m, x, dy = _model_and_batch()
+    m.forward(x)
+    m.backward(dy)
+    want = _grads(m)
+    opt = torch.optim.SGD(m.parameters(), lr=0.0)
+    for to_none in (True, False):
+        opt.zero_grad(set_to_none=to_none)
+        m.forward(x)
+        m.backward(dy, accumulate=accumulate)
+        assert all(torch.equal(u, v) for u, v in zip(_grads(m), want))
+        opt.step()
