@@ -21,6 +21,11 @@ import torch
 from . import _abi, api
 
 
+def _rows(t):
+    """`t` with the values of a row after one another and rows of their own."""
+    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
+
+
 class Surrogate8:
     """A ReLU perceptron of the widths ``dims``: fp32 weights ``W[l]``
     [out][in] and biases ``b[l]`` with gradients in ``.grad``; products in
@@ -43,7 +48,7 @@ class Surrogate8:
     def forward(self, x):
         """Outputs [n][dims[-1]] (fp32) of inputs [n][dims[0]]; keeps what
         ``backward`` reads."""
-        n, a = x.shape[0], x.to(torch.bfloat16)
+        n, a = x.shape[0], _rows(x.to(torch.bfloat16))
         if not self.kept or self.kept[0].rows != n:
             self.kept = [api.Checkpoint8(n, d, _abi.ACT_RELU if l else _abi.ACT_IDENTITY) for l, d in enumerate(self.dims[:-1])]
         self.Wh = [w.to(torch.bfloat16) for w in self.W]
@@ -57,7 +62,7 @@ class Surrogate8:
     def backward(self, dy, accumulate: bool = False):
         """Gradients of the loss in ``.grad`` (made where an optimizer has taken
         them away) from that of the outputs."""
-        dy = dy.to(torch.bfloat16)
+        dy = _rows(dy.to(torch.bfloat16))
         for p in self.parameters():
             if p.grad is None:
                 p.grad = torch.zeros_like(p)
@@ -80,7 +85,7 @@ class Surrogate8:
 @torch.no_grad()
 def answer(layers, x):
     """Outputs (fp32) of a surrogate's 8-bit layers for inputs [n][in]."""
-    n = x.shape[0]
+    n, x = x.shape[0], _rows(x)
     scratch = torch.empty(max(l.scratch_bytes(n) for l in layers), dtype=torch.uint8, device="cuda")
     for i, layer in enumerate(layers):
         last = i + 1 == len(layers)
