@@ -29,7 +29,9 @@ def _rows(t):
 class Surrogate8:
     """A ReLU perceptron of the widths ``dims``: fp32 weights ``W[l]``
     [out][in] and biases ``b[l]`` with gradients in ``.grad``; products in
-    bf16."""
+    bf16.  ``backward`` is that of the last ``forward``: another one in between
+    replaces what was kept.  Calls may come on one stream after another, each
+    works after the one before; from several threads at a time they may not."""
 
     def __init__(self, dims, seed: int = 0):
         g = torch.Generator().manual_seed(seed)
@@ -39,15 +41,29 @@ class Surrogate8:
         self.b = [torch.zeros(o, device="cuda").requires_grad_() for o in self.dims[1:]]
         for p in self.parameters():
             p.grad = torch.zeros_like(p)
-        self.kept, self.scratch = [], None
+        self.kept, self.scratch, self.Wh, self.stream = [], None, [], torch.cuda.current_stream()
 
     def parameters(self):
         return self.W + self.b
+
+    def _in_order(self):
+        """Kept values, weights in bf16 and scratch memory are used again by
+        every call: a call on another stream than the last waits for it.  (A
+        capture into a graph begins after a synchronization, and a stream in it
+        may not wait for one outside.)"""
+        now = torch.cuda.current_stream()
+        if now != self.stream and not torch.cuda.is_current_stream_capturing():
+            now.wait_stream(self.stream)
+            for t in [t for k in self.kept for t in (k.codes, k.exps)] + self.Wh + [self.scratch]:
+                if t is not None:
+                    t.record_stream(now)
+        self.stream = now
 
     @torch.no_grad()
     def forward(self, x):
         """Outputs [n][dims[-1]] (fp32) of inputs [n][dims[0]]; keeps what
         ``backward`` reads."""
+        self._in_order()
         n, a = x.shape[0], _rows(x.to(torch.bfloat16))
         if not self.kept or self.kept[0].rows != n:
             self.kept = [api.Checkpoint8(n, d, _abi.ACT_RELU if l else _abi.ACT_IDENTITY) for l, d in enumerate(self.dims[:-1])]
@@ -62,6 +78,7 @@ class Surrogate8:
     def backward(self, dy, accumulate: bool = False):
         """Gradients of the loss in ``.grad`` (made where an optimizer has taken
         them away) from that of the outputs."""
+        self._in_order()
         dy = _rows(dy.to(torch.bfloat16))
         for p in self.parameters():
             if p.grad is None:

@@ -223,3 +223,29 @@ def test_inputs_and_gradients_of_any_layout(kind):
         results.append([y, surrogate8.answer(layers, u)] + _grads(m))
     for r in results[1:]:
         assert all(torch.equal(a, b) for a, b in zip(r, results[0]))
+
+
+def test_a_model_used_on_one_stream_after_another():
+    """Steps that follow one another on streams of their own, the first held up:
+    each has the gradients it has alone."""
+    import torch
+    batches = [_model_and_batch(n=n, seed=n)[1:] for n in (700, 700, 300, 700)]
+    m = _model_and_batch()[0]
+    want = []
+    for x, dy in batches:
+        m.forward(x)
+        m.backward(dy)
+        want.append(_grads(m))
+    torch.cuda.synchronize()
+    forwards, backwards = [torch.cuda.Stream() for _ in batches], [torch.cuda.Stream() for _ in batches]
+    got = []
+    for (x, dy), f, b in zip(batches, forwards, backwards):
+        with torch.cuda.stream(f):
+            torch.cuda._sleep(20_000_000)
+            m.forward(x)
+        with torch.cuda.stream(b):
+            m.backward(dy)
+            got.append(_grads(m))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(u, v) for u, v in zip(w, g))
