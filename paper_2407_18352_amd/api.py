@@ -504,6 +504,8 @@ def backward8(kept: Checkpoint8, dy, dw=None, db=None, W=None, dx=None, accumula
             raise ValueError("dx needs W")
         pW, _, ldW = _matrix(W, "W", n_out, kept.width, ty)
         px, _, ldx = _matrix(dx, "dx", kept.rows, kept.width, ty)
+        if kept.rows == 0 and dw is None and db is None:
+            return        # an empty tensor has no address, which would read as "not wanted"
     keep, ps, bytes_ = _scratch8(scratch, lambda: _backward8_need(
         kept, (py, ty, ldy, n_out), 1 if dw is not None or db is not None else 0, 0 if dx is None else 1), stream)
     check(lib().hpacml8_backward(kept.desc, py, ty, ldy, n_out, pW, ldW, pw, lddw, pb, px, ldx,

@@ -172,6 +172,26 @@ def test_backward_of_kept_infinities(rows, n_in, n_out, kind, act):
     assert np.isfinite(_np(db)).all() and np.isfinite(_np(dx)).all()
 
 
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n_in, n_out", [(2048, 2048), (40, 20)])
+def test_backward_without_rows_on_either_side_of_the_rule(kind, n_in, n_out):
+    """Sizes that one launch takes and that take several; dx alone as well, whose
+    empty tensor has no address."""
+    import torch
+    kind = getattr(torch, kind)
+    kept = api.Checkpoint8(0, n_in, RELU)
+    dw, db = torch.full((n_out, n_in), 3.0, device="cuda"), torch.full((n_out,), 3.0, device="cuda")
+    dy, dx = (torch.empty((0, n), dtype=kind, device="cuda") for n in (n_out, n_in))
+    W = torch.ones((n_out, n_in), dtype=kind, device="cuda")
+    api.backward8(kept, dy, dw, db, W=W, dx=dx, accumulate=True)
+    assert (dw == 3).all() and (db == 3).all()
+    api.backward8(kept, dy, W=W, dx=dx)
+    api.backward8(kept, dy, db=db)
+    assert (dw == 3).all() and (db == 0).all()
+    api.backward8(kept, dy, dw, db, W=W, dx=dx)
+    assert (dw == 0).all() and (db == 0).all()
+
+
 # ---- a training loop ----------------------------------------------------------
 
 
