@@ -11,7 +11,6 @@
 // up by the conversion of the codes between them), parts joined 14 us.  262,144
 // rows of 256 <- 256: 5, 66, 64 and 7 us; dx and dw are bound by memory (337 MB
 // at 5.1 TB/s; 203 MB at 3.2 TB/s).
-#include <cmath>
 #include <type_traits>
 
 #include "dense8_nt.hpp"
@@ -551,45 +550,6 @@ dim3 blocks_for(int64_t items) {
 }
 size_t whole(size_t b) { return (b + 255) / 256 * 256; }
 
-// How dw is computed: the tile (outputs x channels), the planes at once, and
-// the parts of the rows.  More parts shorten the blocks' loops and lengthen the
-// join (a part of dw is written and read: n_out * n_in * 8 bytes at about 4.5
-// TB/s); at most as many as the chip holds at once.  The tile is the one whose
-// time is least by the times measured for a slab of 32 rows in a full chip, at
-// 131,072 rows: 1.10, 0.67, 0.68, 0.79 and 0.47 us (the larger tiles need
-// fewer of them), with three planes at once 1.9 and 0.9 us.
-struct DwTileTimes {
-    int outs, channels, planes, at_once;
-    double slab_us;
-};
-constexpr DwTileTimes kDwTiles[] = {{256, 256, 1, 256, 1.10}, {256, 128, 1, 256, 0.67}, {128, 256, 1, 256, 0.68},
-                                    {128, 128, 1, 512, 0.79}, {64, 64, 1, 768, 0.47},   {128, 128, 3, 256, 1.9},
-                                    {64, 64, 3, 512, 0.9}};
-constexpr double kStartUs = 4;     // until a block's first slabs are there; and of another launch
-
-void choose_dw(int64_t rows, int32_t n_out, int32_t n_in, int planes, Backward8Plan *p) {
-    const double slabs = (double)((rows + 31) / 32), part_us = (double)n_out * n_in * 8 / 4.5e6;
-    double best = 0;
-    for (int i = 0; i < (int)(sizeof(kDwTiles) / sizeof(kDwTiles[0])); ++i) {
-        const DwTileTimes &t = kDwTiles[i];
-        if (t.planes > planes)
-            continue;
-        const double tiles = (double)((n_out + t.outs - 1) / t.outs) * ((n_in + t.channels - 1) / t.channels);
-        const double us = t.slab_us * (planes / t.planes), most = std::floor(t.at_once / tiles);
-        double splits = std::floor(std::sqrt(slabs * us / (part_us + 0.02)) + 0.5);
-        splits = std::fmax(1, std::fmin(splits, std::fmin(most, slabs)));
-        const double rounds = std::ceil(tiles * splits / t.at_once);
-        const double time = rounds * (kStartUs + std::ceil(slabs / splits) * us) + (splits > 1 ? kStartUs + splits * part_us : 0);
-        if (i == 0 || time < best) {
-            best = time;
-            p->tile = i;
-            p->splits = (int32_t)splits;
-        }
-    }
-    p->rows_per_split = ((rows + p->splits - 1) / p->splits + 31) / 32 * 32;
-    p->splits = p->rows_per_split ? (int32_t)((rows + p->rows_per_split - 1) / p->rows_per_split) : 1;
-}
-
 // log2 of the chunks a row of a block of threads covers: 4 .. 256
 int cols_log(int64_t chunks) {
     int l = 2;
@@ -638,14 +598,14 @@ void launch_dw_tile(DwArgs d, int splits, hipStream_t st) {
 
 template <bool RELU>
 void launch_dw(const DwArgs &d, const Backward8Plan &p, hipStream_t st) {
-    switch (p.tile) {   // of kDwTiles
-    case 0: return launch_dw_tile<RELU, 1, 4, 2, 4, 8>(d, p.splits, st);
-    case 1: return launch_dw_tile<RELU, 1, 4, 2, 4, 4>(d, p.splits, st);
-    case 2: return launch_dw_tile<RELU, 1, 2, 4, 4, 4>(d, p.splits, st);
-    case 3: return launch_dw_tile<RELU, 1, 2, 2, 4, 4>(d, p.splits, st);
-    case 4: return launch_dw_tile<RELU, 1, 2, 2, 2, 2>(d, p.splits, st);
-    case 5: return launch_dw_tile<RELU, 3, 2, 2, 4, 4>(d, p.splits, st);
-    case 6: return launch_dw_tile<RELU, 3, 2, 2, 2, 2>(d, p.splits, st);
+    switch (p.dw.tile) {   // of kDwTiles
+    case 0: return launch_dw_tile<RELU, 1, 4, 2, 4, 8>(d, p.dw.splits, st);
+    case 1: return launch_dw_tile<RELU, 1, 4, 2, 4, 4>(d, p.dw.splits, st);
+    case 2: return launch_dw_tile<RELU, 1, 2, 4, 4, 4>(d, p.dw.splits, st);
+    case 3: return launch_dw_tile<RELU, 1, 2, 2, 4, 4>(d, p.dw.splits, st);
+    case 4: return launch_dw_tile<RELU, 1, 2, 2, 2, 2>(d, p.dw.splits, st);
+    case 5: return launch_dw_tile<RELU, 3, 2, 2, 4, 4>(d, p.dw.splits, st);
+    case 6: return launch_dw_tile<RELU, 3, 2, 2, 2, 2>(d, p.dw.splits, st);
     }
 }
 
@@ -656,26 +616,6 @@ void launch_join(const JoinArgs &j, hipStream_t st) {
         join_kernel<V, 16><<<blocks_for(sums * 16), kThreads, 0, st>>>(j);
     else
         join_kernel<V, 1><<<blocks_for(sums), kThreads, 0, st>>>(j);
-}
-
-// One launch for dx, dw and db (backward8_few.hip), or operands laid out, dx,
-// dw and their join apart.  What counts is the number of 32 x 32 results, a
-// block each; that launch reads an operand again for every 32 results across.
-// Device us, one launch and the general form, of (rows) outputs <- inputs:
-//                                fp32           bf16
-//   (256) 64 <- 64             5.2   16.5      4.3  12.9
-//   (256) 512 <- 512 (384)    10.1   34.4      5.9  17.6
-//   (1024) 256 <- 256 (320)   16.0   27.5     10.7  16.1
-//   (256) 64 <- 2048 (640)     8.3   18.1      6.2  13.9
-//   (1024) 512 <- 512 (768)   23.5   41.2     13.9  21.5
-//   (1) 1024 <- 1024 (1056)   13.5   46.1      7.2  16.3
-//   (512) 64 <- 2048 (1152)   14.0   20.4     10.0  15.2
-//   (256) 1024 <- 1024 (1280) 24.5   57.6     13.3  19.2
-// and, of an earlier form that took up to twice as long, (4096) 64 <- 64 50.6
-// and 18.2 in fp32, (64) 2048 <- 2048 (4224) 58 and 34 in bf16.
-bool few_rows(int64_t rows, int32_t n_out, int32_t n_in) {
-    auto tiles = [](int64_t n) { return (n + 31) / 32; };
-    return rows <= 1024 && tiles(n_in) * (tiles(rows) + tiles(n_out)) <= 1280;
 }
 
 }  // namespace
@@ -690,9 +630,7 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
                n_out % (want_dx ? 32 : 8) == 0;
     p.slabs = (int32_t)slabs_of(2 * n_out);
     p.pitch = (int64_t)p.slabs * (kSlabBytes / 2);
-    p.splits = 1;
-    if (want_dw)
-        choose_dw(c.rows, n_out, c.width, p.planes, &p);
+    p.dw = want_dw ? choose_dw(c.rows, n_out, c.width, p.planes) : DwForm{0, 1, 0};
     size_t at = 0;
     p.off_dy = at;
     if (!p.direct)
@@ -701,11 +639,11 @@ Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_
     if (want_dx)
         at += whole((size_t)p.planes * blocked_bytes(c.width, p.slabs));
     p.off_dw = at;
-    if (want_dw && p.splits > 1)
-        at += whole((size_t)p.splits * n_out * c.width * 4);
+    if (want_dw && p.dw.splits > 1)
+        at += whole((size_t)p.dw.splits * n_out * c.width * 4);
     p.off_db = at;
-    if (want_dw && p.splits > 1)
-        at += whole((size_t)p.splits * n_out * 4);
+    if (want_dw && p.dw.splits > 1)
+        at += whole((size_t)p.dw.splits * n_out * 4);
     p.bytes = at;
     return p;
 }
@@ -739,7 +677,7 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
             shared ? launch_dx<uint16_t, true>(d, st) : launch_dx<uint16_t, false>(d, st);
     }
     if (a.dw || a.db) {
-        const bool join = p.splits > 1;
+        const bool join = p.dw.splits > 1;
         DwArgs d{};
         d.g = g.base;
         d.g_pitch = g.pitch;
@@ -752,12 +690,12 @@ hipError_t launch_backward8(const Backward8Args &a, const Backward8Plan &p, hipS
         d.dw_part = (int64_t)a.n_out * a.c.width;
         d.db_part = a.n_out;
         d.accumulate = join ? 0 : a.accumulate;
-        d.rows_per_split = p.rows_per_split;
+        d.rows_per_split = p.dw.rows_per_split;
         d.n_out = a.n_out;
         d.planes = p.planes;
         a.c.act == HPACML_ACT_RELU ? launch_dw<true>(d, p, st) : launch_dw<false>(d, p, st);
         if (join) {
-            const JoinArgs j{d.dw, d.db, a.dw, a.db, a.lddw, p.splits, a.n_out, a.c.width, a.accumulate};
+            const JoinArgs j{d.dw, d.db, a.dw, a.db, a.lddw, p.dw.splits, a.n_out, a.c.width, a.accumulate};
             if (a.c.width % 4 == 0 && ((uintptr_t)a.dw & 15) == 0 && a.lddw % 4 == 0)
                 launch_join<f32x4>(j, st);
             else

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "dense8_rules.hpp"
 #include "hpacml8.h"
 
 namespace hpacml {
@@ -54,9 +55,7 @@ struct Backward8Plan {
     bool direct;          // dy is read in place
     int32_t slabs;        // of dy and of W's transpose along the outputs
     int64_t pitch;        // of dy's planes (elements)
-    int32_t tile;         // of dw: which of the table in backward8.hip
-    int32_t splits;       // parts of the rows that sum into dw apart
-    int64_t rows_per_split;
+    DwForm dw;
     size_t off_dy, off_wt, off_dw, off_db, bytes;
 };
 Backward8Plan backward8_plan(const hpacml8_checkpoint &c, const void *dy, int32_t dtype, int64_t lddy, int32_t n_out,

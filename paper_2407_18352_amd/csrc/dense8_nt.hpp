@@ -30,6 +30,7 @@
 #pragma once
 
 #include "dense8.hpp"
+#include "dense8_rules.hpp"
 
 namespace hpacml {
 
@@ -144,40 +145,6 @@ struct Tiles {
 // Blocks for `tiles` tiles when `per_cu` of them share a CU: one round of the
 // chip's 256 CUs at most.
 inline uint32_t blocks_for_tiles(int64_t tiles, int per_cu) { return (uint32_t)(tiles < 256 * per_cu ? tiles : 256 * per_cu); }
-
-// The tile (outputs x points) of a product: the largest that leaves no CU
-// without one, by these times (us, 8-bit products):
-//   rows x out <- in       64 x 64  128 x 128  128 x 256  256 x 256
-//   4096 x 256 <- 256          4.6        7.5        8.1       13.8
-//   262144 x 64 <- 64         15.0       23.0       18.5       35.0
-//   4096 x 1024 <- 1024       11.7       10.9       12.5       20.5
-//   1024 x 4096 <- 4096       29.1       23.5       29.5       46.9
-//   65536 x 256 <- 256        17.9       15.8       13.8       15.1
-//   16384 x 512 <- 512        14.0       11.6       10.5       16.6
-//   16384 x 1024 <- 1024      37.0       26.8       24.0       23.3
-//   4096 x 4096 <- 4096      109.0       70.7       73.3       59.4
-//   65536 x 4096 <- 4096      2620       1280       1026        899
-// The largest needs more tiles where k is short, and outputs of which it does
-// not pad more than a quarter away (with the launch that forms the codes):
-//   65536 x 2048 <- 512        190        147        141        127
-//   131072 x 1280 <- 64        110         96         93         87
-//   100000 x 256 <- 600         90         84         87         83
-//   100000 x 300 <- 600         99         97         98        119
-//   100000 x 300 <- 2048       258        225        215        241
-//   65536 x 640 <- 2048        230        176        170        173
-// and the same in bf16, dx of (rows, its outputs <- its inputs):
-//   262144 x 256 <- 256        123         93         87         79
-//   65536 x 2048 <- 64         146        112        108         91
-//   200000 x 300 <- 128         91         78         77         91
-enum class Size { k64x64, k128x128, k128x256, k256x256 };
-inline Size tile_for(int64_t n_out, int64_t rows, int64_t slabs) {
-    auto tiles = [&](int64_t outs, int64_t points) { return (n_out + outs - 1) / outs * ((rows + points - 1) / points); };
-    const bool many = tiles(256, 256) >= (slabs >= 16 ? 200 : 384);
-    return n_out <= 64 || tiles(64, 64) <= 512                     ? Size::k64x64
-           : tiles(128, 128) <= 256                                ? Size::k128x128
-           : many && 8 * tiles(256, 256) <= 5 * tiles(128, 256)    ? Size::k256x256
-                                                                   : Size::k128x256;
-}
 
 // A wave's results on their way out, as rows of Y, NA * 16 outputs of 16 points
 // at a time.  They are turned in LDS, so that the stores are 16-byte pieces of

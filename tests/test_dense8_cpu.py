@@ -128,3 +128,65 @@ def test_operands_against_their_allocations(tmp_path):
         assert line == "%d %d" % (fits, apart), c
         accepted += fits
     assert len(out) == len(cases) + 1 and accepted > 300
+
+
+FORMS = r"""
+#include <cstdio>
+#include "dense8_rules.hpp"
+using namespace hpacml;
+int main() {
+    long rows, n_in, n_out;
+    int planes;
+    while (std::scanf("%ld %ld %ld %d", &rows, &n_in, &n_out, &planes) == 4) {
+        const DwForm f = choose_dw(rows, (int)n_out, (int)n_in, planes);
+        const int dx = (int)nt::tile_for(n_in, rows, (2 * n_out + 63) / 64 * (planes * (planes + 1) / 2));
+        std::printf("%d %d %d %ld %d\n", few_rows(rows, (int)n_out, (int)n_in), f.tile, f.splits, (long)f.rows_per_split / 32, dx);
+    }
+    std::printf("%zu\n", sizeof(kDwTiles) / sizeof(kDwTiles[0]));
+}
+"""
+
+
+def test_the_exact_tests_reach_every_form(tmp_path):
+    """Of dw: each tile of the table with four slabs of rows or more (its rings
+    go round), in one type at least each with the rows in one part, in several
+    and in many; of dx: each tile, in both types; the one launch for few rows."""
+    from test_gpu_dense8_exact import GENERAL, SHAPES
+    run = _compiled(tmp_path, FORMS)
+
+    def forms(shapes, planes):
+        lines = run("".join("%d %d %d %d\n" % (s + (planes,)) for s in shapes)).split("\n")
+        return [tuple(map(int, l.split())) for l in lines[:len(shapes)]], int(lines[len(shapes)])
+
+    parts = lambda splits: 0 if splits == 1 else 1 if splits < 16 else 2
+    seen = set()
+    for planes in (1, 3):
+        got, tiles = forms(SHAPES, planes)
+        general = [f for f in got if not f[0]]
+        assert len(got) - len(general) >= 3
+        long = {t for _, t, _, slabs, _ in general if slabs >= 4}
+        # three planes at once are of fp32 alone
+        assert long == ({0, 1, 2, 3, 4} if planes == 1 else set(range(tiles))), (planes, long)
+        whole = [n_in % 32 == 0 for _, n_in, _ in SHAPES]      # dx in whole cache lines, and not
+        for lines in (True, False):
+            assert {f[4] for f, w in zip(got, whole) if not f[0] and w == lines} == {0, 1, 2, 3}, (planes, lines)
+        seen |= {(t, parts(splits)) for _, t, splits, slabs, _ in general}
+        few, t = forms(GENERAL, planes)
+        assert not any(f[0] for f in few) and {parts(f[2]) for f in few} == {0, 1, 2}, few
+    assert tiles == 7 and {t for t, _ in seen} == set(range(7)) and {p for _, p in seen} == {0, 1, 2}
+    # the largest tile, which large batches take, with its parts joined by one thread and by many
+    assert {p for t, p in seen if t == 0} == {0, 1, 2}
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_the_exact_tests_tell_a_lost_slab(kind):
+    """Any 32 rows that do not take part, or take part twice, change dw."""
+    import torch
+    from test_gpu_dense8_exact import RELU, results, whole_numbers
+    for shape in ((70001, 64, 8), (100003, 35, 5), (3001, 150, 47)):
+        codes, exps, dy, W = whole_numbers(*shape, kind, RELU, "cpu")
+        a, dw, db, _ = results(codes, exps, dy, W, RELU)
+        rows = -(-shape[0] // 32) * 32
+        pad = lambda t: torch.nn.functional.pad(t.double(), (0, 0, 0, rows - shape[0])).view(rows // 32, 32, -1)
+        slabs = torch.matmul(pad(dy).transpose(1, 2).contiguous(), pad(a))
+        assert torch.equal(slabs.sum(0), dw) and (slabs != 0).any(2).any(1).all()
