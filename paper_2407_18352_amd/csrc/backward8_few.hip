@@ -21,7 +21,6 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kTile = 32;
 constexpr int kStep = 32;        // of a sum, per matrix instruction
-constexpr int kAhead = 1;        // steps of a wave on the way at a time
 
 struct FewArgs {
     hpacml8_checkpoint c;
@@ -94,41 +93,35 @@ __global__ void __launch_bounds__(kThreads) few_backward_kernel(FewArgs p) {
             w_at[t] = (const T *)p.W + min(k0 + t * 16 + l16, n_in - 1);
             g_at[t] = dy + min(p0 + t * 16 + l16, rows - 1) * p.lddy;
         }
-        for (int s0 = wave; s0 < steps; s0 += kAhead * kWaves) {
-            float w[kAhead][2][kChunk], g[kAhead][2][kChunk];
+        for (int step = wave; step < steps; step += kWaves) {
+            float w[2][kChunk], g[2][kChunk];
+            const int o = step * kStep + grp * kChunk;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int o = (s0 + i * kWaves) * kStep + grp * kChunk;
+            for (int t = 0; t < 2; ++t) {
+                load_chunk(g_at[t] + o, p.n_out - o, g[t]);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    load_chunk(g_at[t] + o, p.n_out - o, g[i][t]);
-#pragma unroll
-                    for (int e = 0; e < kChunk; ++e)
-                        w[i][t][e] = load_value(w_at[t] + min(o + e, p.n_out - 1) * p.ldw);
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < kChunk; ++e)
-                        w[i][t][e] = o + e < p.n_out ? w[i][t][e] : 0.f;
+                for (int e = 0; e < kChunk; ++e)
+                    w[t][e] = load_value(w_at[t] + min(o + e, p.n_out - 1) * p.ldw);
             }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                bf16x8 a[2][kTerms], b[2][kTerms];
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    terms_of(w[i][t], a[t]);
-                    terms_of(g[i][t], b[t]);
-                }
-                // the products whose ranks sum to at most 2, the smallest first
+                for (int e = 0; e < kChunk; ++e)
+                    w[t][e] = o + e < p.n_out ? w[t][e] : 0.f;
+            bf16x8 a[2][kTerms], b[2][kTerms];
 #pragma unroll
-                for (int rank = kTerms - 1; rank >= 0; --rank)
-#pragma unroll
-                    for (int q = 0; q <= rank; ++q)
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-                            mul(a[t & 1][q], b[t >> 1][rank - q], acc[t & 1][t >> 1]);
+            for (int t = 0; t < 2; ++t) {
+                terms_of(w[t], a[t]);
+                terms_of(g[t], b[t]);
             }
+            // the products whose ranks sum to at most 2, the smallest first
+#pragma unroll
+            for (int rank = kTerms - 1; rank >= 0; --rank)
+#pragma unroll
+                for (int q = 0; q <= rank; ++q)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        mul(a[t & 1][q], b[t >> 1][rank - q], acc[t & 1][t >> 1]);
         }
         share();
 #pragma unroll
@@ -148,51 +141,45 @@ __global__ void __launch_bounds__(kThreads) few_backward_kernel(FewArgs p) {
     const int j0 = (int)(id / p.dw_in_tiles) * kTile, k0 = (int)(id % p.dw_in_tiles) * kTile;
     const int64_t steps = (rows + kStep - 1) / kStep;
     const bool sums = p.db && k0 == 0;
-    for (int64_t s0 = wave; s0 < steps; s0 += kAhead * kWaves) {
-        float g[kAhead][2][kChunk], scale[kAhead][kChunk];
-        uint32_t code[kAhead][2][kChunk];
+    for (int64_t step = wave; step < steps; step += kWaves) {
+        float g[2][kChunk], scale[kChunk];
+        uint32_t code[2][kChunk];
+        const int64_t r0 = step * kStep + grp * kChunk;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int64_t r0 = (s0 + i * kWaves) * kStep + grp * kChunk;
-#pragma unroll
-            for (int e = 0; e < kChunk; ++e) {
-                const int64_t r = min(r0 + e, rows - 1);
-                // rows of codes are whole blocks of channels: all of a tile's exist
-                const uint32_t exp = exps[r * p.c.ld_exps + k0 / 32];
-                scale[i][e] = r0 + e < rows ? block_scale(exp, kTerms) : 0.f;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    code[i][t][e] = codes[r * p.c.ld_codes + k0 + t * 16 + l16];
-                    const float v = load_value(dy + r * p.lddy + min(j0 + t * 16 + l16, p.n_out - 1));
-                    g[i][t][e] = r0 + e < rows ? v : 0.f;
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            bf16x8 a[2][1], b[2][kTerms];
+        for (int e = 0; e < kChunk; ++e) {
+            const int64_t r = min(r0 + e, rows - 1);
+            // rows of codes are whole blocks of channels: all of a tile's exist
+            const uint32_t exp = exps[r * p.c.ld_exps + k0 / 32];
+            scale[e] = r0 + e < rows ? block_scale(exp, kTerms) : 0.f;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                float v[kChunk];
-#pragma unroll
-                for (int e = 0; e < kChunk; ++e)
-                    v[e] = block_value<RELU>(code[i][t][e], scale[i][e]);
-                terms_of(v, a[t]);       // exact
-                terms_of(g[i][t], b[t]);
+                code[t][e] = codes[r * p.c.ld_codes + k0 + t * 16 + l16];
+                const float v = load_value(dy + r * p.lddy + min(j0 + t * 16 + l16, p.n_out - 1));
+                g[t][e] = r0 + e < rows ? v : 0.f;
             }
+        }
+        bf16x8 a[2][1], b[2][kTerms];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            float v[kChunk];
+#pragma unroll
+            for (int e = 0; e < kChunk; ++e)
+                v[e] = block_value<RELU>(code[t][e], scale[e]);
+            terms_of(v, a[t]);       // exact
+            terms_of(g[t], b[t]);
+        }
+#pragma unroll
+        for (int q = kTerms - 1; q >= 0; --q)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                mul(a[t & 1][0], b[t >> 1][q], acc[t & 1][t >> 1]);
+        if (sums) {
+            const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
 #pragma unroll
             for (int q = kTerms - 1; q >= 0; --q)
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    mul(a[t & 1][0], b[t >> 1][q], acc[t & 1][t >> 1]);
-            if (sums) {
-                const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
-#pragma unroll
-                for (int q = kTerms - 1; q >= 0; --q)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        mul(ones, b[t][q], sum[t]);
-            }
+                for (int t = 0; t < 2; ++t)
+                    mul(ones, b[t][q], sum[t]);
         }
     }
     if (lane < 16) {

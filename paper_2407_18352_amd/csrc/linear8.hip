@@ -130,66 +130,46 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Linear8Args p) {
     weights(wave);
 
     if constexpr (FUSED) {
-        // one point: by the whole block; more: a wave each, kHeld chunks of a
-        // lane at a time: of one point (per of them), or of kHeld points
+        // one point: by the whole block; more: a wave each.  A lane takes kHeld
+        // chunks of the row at a time
         const bool one = p.rows == 1;
         const int step = one ? kFewThreads : 64, first = one ? tid : lane, points = (int)p.rows;
         auto form = [&](auto held) {
             constexpr int kHeld = decltype(held)::value;
-            int per_log = 0;
-            while ((1 << per_log) < kHeld && (step << per_log) < chunks)
-                ++per_log;
-            const int per = 1 << per_log, at_once = kHeld >> per_log;
             float v[kHeld][kChunk];
-            for (int r0 = one ? 0 : wave; r0 < points; r0 += kFewWaves * at_once) {
-                auto point = [&](int h) { return r0 + (h >> per_log) * kFewWaves; };
+            for (int r = one ? 0 : wave; r < points; r += kFewWaves) {
+                const X *row_at = (const X *)p.x + r * p.ldx;
                 auto load = [&](int c) {
-                    auto k = [&](int h) { return (c + (h & (per - 1)) * step) * kChunk; };
-                    load_chunks<X>(
-                        p.n_in, [&](int h) { return (const X *)p.x + min(point(h), points - 1) * p.ldx + k(h); },
-                        [&](int h) { return p.n_in - k(h); }, v);
+                    auto k = [&](int h) { return (c + h * step) * kChunk; };
+                    load_chunks<X>(p.n_in, [&](int h) { return row_at + k(h); }, [&](int h) { return p.n_in - k(h); }, v);
                 };
-                uint32_t top[kHeld] = {};
-                for (int c = first; c < chunks; c += step << per_log) {
+                uint32_t top = 0;
+                for (int c = first; c < chunks; c += step * kHeld) {
                     load(c);
 #pragma unroll
                     for (int h = 0; h < kHeld; ++h)
-                        top[h] = max(top[h], top_bits(v[h]));
+                        top = max(top, top_bits(v[h]));
                 }
-                // a row's largest: at its first chunk, and from there at the others
-#pragma unroll
-                for (int d = 1; d < kHeld; d *= 2)
-                    if (d < per)
-#pragma unroll
-                        for (int h = 0; h < kHeld; h += 2 * d)
-                            top[h] = max(top[h], top[h + d]);
-#pragma unroll
-                for (int h = 0; h < kHeld; ++h)
-                    top[h] = h & (per - 1) ? top[h > 0 ? h - 1 : 0] : lanes_max<64>(top[h]);
+                top = lanes_max<64>(top);
                 if (one) {
                     if (lane == 0)
-                        tops[wave] = top[0];
+                        tops[wave] = top;
                     __syncthreads();
-                    uint32_t all = 0;
 #pragma unroll
                     for (int i = 0; i < kFewWaves; ++i)
-                        all = max(all, tops[i]);
-#pragma unroll
-                    for (int h = 0; h < kHeld; ++h)
-                        top[h] = all;
+                        top = max(top, tops[i]);
                 }
-                for (int c = first; c < chunks; c += step << per_log) {
-                    if (chunks > step << per_log)
+                const RowScale sc(top);
+                for (int c = first; c < chunks; c += step * kHeld) {
+                    if (chunks > step * kHeld)
                         load(c);
 #pragma unroll
                     for (int h = 0; h < kHeld; ++h) {
-                        const RowScale sc(top[h]);
-                        const int at = c + (h & (per - 1)) * step;
-                        if (point(h) < points && at < chunks) {
-                            if (at == 0)
-                                scales[point(h)] = sc.scale;
-                            *(uint2 *)(codes + point(h) * pitch + at * kChunk) = sc.codes(v[h]);
-                        }
+                        const int at = c + h * step;
+                        if (at == 0)
+                            scales[r] = sc.scale;
+                        if (at < chunks)
+                            *(uint2 *)(codes + r * pitch + at * kChunk) = sc.codes(v[h]);
                     }
                 }
             }
