@@ -53,7 +53,7 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
 void hpacml8_linear_destroy(hpacml8_linear *layer);
 
 /* Bytes of scratch hpacml8_linear_run needs for n_rows rows (never shrinking
- * with n_rows; 0 is possible). */
+ * with n_rows; 0 for no rows). */
 hpacml_status hpacml8_linear_scratch(const hpacml8_linear *layer, int64_t n_rows, size_t *bytes);
 
 /* y [n_rows][n_out] from x [n_rows][n_in].

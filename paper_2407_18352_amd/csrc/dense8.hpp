@@ -40,7 +40,8 @@ struct Linear8Args {
     int64_t rows, ldy;
     int32_t slabs, n_in, n_out, relu;
 };
-bool linear8_fused(int64_t rows, int32_t n_in, int32_t n_out);   // q and s are not used
+// rows that q and s need room for: of these, or of fewer where these use neither
+int64_t linear8_scratch_rows(int64_t rows, int32_t n_in, int32_t n_out);
 hipError_t launch_linear8(const Linear8Args &a, int32_t x_dtype, int32_t y_dtype, hipStream_t stream);
 
 hipError_t launch_checkpoint_save(const hpacml8_checkpoint &c, const void *z, int32_t z_dtype, int64_t ldz, void *a,

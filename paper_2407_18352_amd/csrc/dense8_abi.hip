@@ -97,8 +97,11 @@ void add_checkpoint(Operands *o, const hpacml8_checkpoint &c, bool written) {
 }
 
 // scratch of hpacml8_linear_run: codes, then scales
-size_t linear_codes_bytes(const hpacml8_linear *l, int64_t rows) { return (size_t)blocked_bytes(rows, l->slabs); }
-size_t linear_scratch_bytes(const hpacml8_linear *l, int64_t rows) { return linear_codes_bytes(l, rows) + (size_t)rows * 4; }
+int64_t linear_scratch_rows(const hpacml8_linear *l, int64_t rows) { return linear8_scratch_rows(rows, l->n_in, l->n_out); }
+size_t linear_codes_bytes(const hpacml8_linear *l, int64_t rows) { return (size_t)blocked_bytes(linear_scratch_rows(l, rows), l->slabs); }
+size_t linear_scratch_bytes(const hpacml8_linear *l, int64_t rows) {
+    return linear_codes_bytes(l, rows) + (size_t)linear_scratch_rows(l, rows) * 4;
+}
 
 }  // namespace
 

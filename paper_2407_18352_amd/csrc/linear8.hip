@@ -389,7 +389,8 @@ bool few_fused(int64_t rows, int32_t n_in) {
     return rows <= kFusedPoints && rows * fused_pitch(slabs_of(n_in)) <= kFusedBytes;
 }
 // (16384 x 512 <- 512 takes 24.5 us this way and 20.7 us with the codes in memory)
-bool narrow(int64_t rows, int32_t n_in, int32_t n_out) { return rows >= 32768 && rows <= (1 << 30) && n_in <= 512 && n_out <= 1024; }
+constexpr int64_t kNarrowPoints = 32768;
+bool narrow(int64_t rows, int32_t n_in, int32_t n_out) { return rows >= kNarrowPoints && rows <= (1 << 30) && n_in <= 512 && n_out <= 1024; }
 
 template <typename X, typename Y>
 void launch_as(const Linear8Args &a, hipStream_t stream) {
@@ -403,10 +404,12 @@ void launch_as(const Linear8Args &a, hipStream_t stream) {
 
 }  // namespace
 
-bool linear8_fused(int64_t rows, int32_t n_in, int32_t n_out) { return few_fused(rows, n_in) || narrow(rows, n_in, n_out); }
+int64_t linear8_scratch_rows(int64_t rows, int32_t n_in, int32_t n_out) {
+    return narrow(rows, n_in, n_out) ? kNarrowPoints - 1 : rows;
+}
 
 hipError_t launch_linear8(const Linear8Args &a, int32_t x_dtype, int32_t y_dtype, hipStream_t stream) {
-    if (!linear8_fused(a.rows, a.n_in, a.n_out)) {
+    if (!few_fused(a.rows, a.n_in) && !narrow(a.rows, a.n_in, a.n_out)) {
         const hipError_t e = launch_codes_by_row(a.x, x_dtype, a.ldx, a.rows, a.n_in, a.q, a.s, stream);
         if (e != hipSuccess)
             return e;

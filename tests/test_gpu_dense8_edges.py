@@ -269,3 +269,28 @@ def test_a_model_used_on_one_stream_after_another():
     torch.cuda.synchronize()
     for w, g in zip(want, got):
         assert all(torch.equal(u, v) for u, v in zip(w, g))
+
+
+# ---- scratch memory -------------------------------------------------------------
+
+
+def test_linear_scratch_is_what_the_products_read():
+    """Many points of a narrow layer form their codes where they multiply them:
+    the scratch memory asked for stops growing there, and never shrinks."""
+    import torch
+    from test_gpu_dense8 import _linear, _np, _rand
+    rows = [0, 1, 32, 33, 1000, 32767, 32768, 40000, 1 << 20, 1 << 30, (1 << 30) + 1, 2 ** 31 - 1]
+    for n_in, n_out, fixed in ((512, 512, True), (200, 1024, True), (513, 64, False), (64, 1025, False)):
+        layer = api.Linear8(torch.ones((n_out, n_in)))
+        need = [layer.scratch_bytes(n) for n in rows]
+        assert need[0] == 0 and need == sorted(need)
+        assert (need[8] < 2 ** 25) == fixed and need[10] >= (1 << 30) * n_in
+    W, x = _rand(81, (96, 130)), _rand(82, (40000, 130), "bf16")
+    layer, y = api.Linear8(W), torch.empty((40000, 96), device="cuda")
+    scratch = torch.full((layer.scratch_bytes(40000) + 64,), 7, dtype=torch.uint8, device="cuda")
+    api.linear8(layer, x, y, RELU, scratch=scratch[:-64])
+    want, size = _linear(x.float().cpu().numpy(), W.cpu().numpy(), None, RELU)
+    assert (np.abs(_np(y) - want) <= 6 * 2.0 ** -24 * size + 1e-37).all() and (scratch[-64:] == 7).all()
+    with pytest.raises(_abi.HpacmlError) as e:
+        api.linear8(layer, x, y, RELU, scratch=scratch[:-80])
+    assert e.value.status == _abi.E_RANGE
