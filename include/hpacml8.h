@@ -44,8 +44,9 @@ typedef struct hpacml8_linear_s hpacml8_linear;
 
 /* Lays a layer's weights out in device memory.
  *   W: fp32 [n_out][n_in], b: fp32 [n_out] or NULL (no bias); HOST or DEVICE
- *   memory, copied.  n_in, n_out: 1..HPACML8_MAX_WIDTH (above:
- *   HPACML_E_UNSUPPORTED).  Synchronises the device (also before it reads W). */
+ *   memory, copied (beyond its allocation on the device: HPACML_E_RANGE).
+ *   n_in, n_out: 1..HPACML8_MAX_WIDTH (above: HPACML_E_UNSUPPORTED).
+ * Synchronises the device (also before it reads W). */
 hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W, const float *b,
                                     hpacml8_linear **out);
 

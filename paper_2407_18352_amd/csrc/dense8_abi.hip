@@ -96,6 +96,25 @@ void add_checkpoint(Operands *o, const hpacml8_checkpoint &c, bool written) {
     o->add(c.exps, c.rows, blocks, c.ld_exps, 1, 1, written);
 }
 
+// A host or device array to be copied: in device memory it has to lie inside
+// its allocation.
+hpacml_status source_status(const void *p, int64_t bytes) {
+    hipPointerAttribute_t attr;
+    hipDeviceptr_t base = nullptr;
+    size_t size = 0;
+    if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
+        (void)hipGetLastError();       // host memory that the runtime does not know
+        return HPACML_OK;
+    }
+    if (attr.type != hipMemoryTypeDevice)
+        return HPACML_OK;
+    if (hipMemGetAddressRange(&base, &size, (hipDeviceptr_t)p) != hipSuccess) {
+        (void)hipGetLastError();
+        return HPACML_E_INVAL;
+    }
+    return inside({(const char *)p, 1, bytes, bytes, false}, (const char *)base, size) ? HPACML_OK : HPACML_E_RANGE;
+}
+
 // scratch of hpacml8_linear_run: codes, then scales
 int64_t linear_scratch_rows(const hpacml8_linear *l, int64_t rows) { return linear8_scratch_rows(rows, l->n_in, l->n_out); }
 size_t linear_codes_bytes(const hpacml8_linear *l, int64_t rows) { return (size_t)blocked_bytes(linear_scratch_rows(l, rows), l->slabs); }
@@ -115,6 +134,11 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
         return HPACML_E_INVAL;
     if (n_in > HPACML8_MAX_WIDTH || n_out > HPACML8_MAX_WIDTH)
         return HPACML_E_UNSUPPORTED;
+    hpacml_status source = source_status(W, (int64_t)n_out * n_in * 4);
+    if (source == HPACML_OK && b)
+        source = source_status(b, (int64_t)n_out * 4);
+    if (source != HPACML_OK)
+        return source;
     hpacml8_linear *l = new (std::nothrow) hpacml8_linear_s;
     if (!l)
         return HPACML_E_NOMEM;

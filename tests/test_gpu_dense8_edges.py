@@ -294,3 +294,22 @@ def test_linear_scratch_is_what_the_products_read():
     with pytest.raises(_abi.HpacmlError) as e:
         api.linear8(layer, x, y, RELU, scratch=scratch[:-80])
     assert e.value.status == _abi.E_RANGE
+
+
+def test_linear_weights_beyond_their_allocation_are_refused():
+    """Device weights and biases that would be read past the end of what was
+    allocated for them."""
+    import ctypes as C
+    import torch
+    L, h = _abi.lib(), C.c_void_p()
+    small, host = torch.zeros(256, device="cuda"), torch.zeros(1 << 15)
+    n = _abi.MAX_WIDTH8
+    assert L.hpacml8_linear_create(n, n, small.data_ptr(), None, C.byref(h)) == _abi.E_RANGE and not h.value
+    torch.cuda.empty_cache()
+    big = torch.zeros(64 << 18, device="cuda")            # 64 MB: not a piece of what torch holds, so an allocation of its own
+    assert L.hpacml8_linear_create(1, 8, small.data_ptr(), big.data_ptr() + big.numel() * 4 - 28, C.byref(h)) == _abi.E_RANGE
+    assert not h.value
+    for W, b in ((small, big[-8:]), (host, host), (host, small), (host.pin_memory(), None)):
+        assert L.hpacml8_linear_create(1, 8, W.data_ptr(), None if b is None else b.data_ptr(), C.byref(h)) == _abi.OK
+        L.hpacml8_linear_destroy(h)
+        h = C.c_void_p()
