@@ -96,9 +96,10 @@ void add_checkpoint(Operands *o, const hpacml8_checkpoint &c, bool written) {
     o->add(c.exps, c.rows, blocks, c.ld_exps, 1, 1, written);
 }
 
-// A host or device array to be copied: in device memory it has to lie inside
-// its allocation.
-hpacml_status source_status(const void *p, int64_t bytes) {
+// A host or device array to be read once: in device memory it has to lie inside
+// its allocation.  here (may be NULL): floats of device `device`, which its
+// kernels can read where they are.
+hpacml_status source_status(const void *p, int64_t bytes, int device, bool *here) {
     hipPointerAttribute_t attr;
     hipDeviceptr_t base = nullptr;
     size_t size = 0;
@@ -112,6 +113,8 @@ hpacml_status source_status(const void *p, int64_t bytes) {
         (void)hipGetLastError();
         return HPACML_E_INVAL;
     }
+    if (here)
+        *here = attr.device == device && ((uintptr_t)p & 3) == 0;
     return inside({(const char *)p, 1, bytes, bytes, false}, (const char *)base, size) ? HPACML_OK : HPACML_E_RANGE;
 }
 
@@ -134,9 +137,16 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
         return HPACML_E_INVAL;
     if (n_in > HPACML8_MAX_WIDTH || n_out > HPACML8_MAX_WIDTH)
         return HPACML_E_UNSUPPORTED;
-    hpacml_status source = source_status(W, (int64_t)n_out * n_in * 4);
+    int device = 0;
+    bool w_here = false;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        return status_of(e);
+    }
+    hpacml_status source = source_status(W, (int64_t)n_out * n_in * 4, device, &w_here);
     if (source == HPACML_OK && b)
-        source = source_status(b, (int64_t)n_out * 4);
+        source = source_status(b, (int64_t)n_out * 4, device, nullptr);
     if (source != HPACML_OK)
         return source;
     hpacml8_linear *l = new (std::nothrow) hpacml8_linear_s;
@@ -147,12 +157,11 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
     l->slabs = (int32_t)slabs_of(n_in);
     float *staged = nullptr;
     const size_t codes = (size_t)blocked_bytes(n_out, l->slabs), wbytes = (size_t)n_out * n_in * 4, outs = ((size_t)n_out + 3) / 4 * 4;
-    hipError_t e = hipGetDevice(&l->device);
-    if (e == hipSuccess)
-        e = hipDeviceSynchronize();
+    l->device = device;
+    e = hipDeviceSynchronize();
     if (e == hipSuccess)
         e = hipMalloc((void **)&l->buf, codes + outs * 8);
-    if (e == hipSuccess)
+    if (e == hipSuccess && !w_here)
         e = hipMalloc((void **)&staged, wbytes);
     if (e == hipSuccess) {
         l->w = (int8_t *)l->buf;
@@ -160,12 +169,12 @@ hpacml_status hpacml8_linear_create(int32_t n_in, int32_t n_out, const float *W,
         l->b = l->t + outs;
         e = hipMemset(l->t, 0, outs * 8);
     }
-    if (e == hipSuccess)
+    if (e == hipSuccess && !w_here)
         e = hipMemcpy(staged, W, wbytes, hipMemcpyDefault);
     if (e == hipSuccess && b)
         e = hipMemcpy(l->b, b, (size_t)n_out * 4, hipMemcpyDefault);
     if (e == hipSuccess)
-        e = launch_codes_by_row(staged, HPACML_F32, n_in, n_out, n_in, l->w, l->t, nullptr);
+        e = launch_codes_by_row(w_here ? W : staged, HPACML_F32, n_in, n_out, n_in, l->w, l->t, nullptr);
     if (e == hipSuccess)
         e = hipDeviceSynchronize();
     if (staged)

@@ -313,3 +313,34 @@ def test_linear_weights_beyond_their_allocation_are_refused():
         assert L.hpacml8_linear_create(1, 8, W.data_ptr(), None if b is None else b.data_ptr(), C.byref(h)) == _abi.OK
         L.hpacml8_linear_destroy(h)
         h = C.c_void_p()
+
+
+def test_linear_weights_of_the_device():
+    """They give the layer that the same weights on the host give, also where
+    another stream is still writing them, or they begin at an odd address."""
+    import ctypes as C
+    import torch
+    from test_gpu_dense8 import _rand
+    W, x = _rand(91, (2048, 4096)), _rand(92, (9, 4096), "bf16")
+    want, y = torch.empty((9, 2048), device="cuda"), torch.empty((9, 2048), device="cuda")
+    api.linear8(api.Linear8(W.cpu()), x, want)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(10_000_000)
+        late = W.clone()
+    torch.cuda.empty_cache()
+    layer = api.Linear8(late)
+    late.zero_()                                    # nothing of it is needed any more
+    api.linear8(layer, x, y)
+    assert torch.equal(y, want)
+    odd = torch.zeros(W.numel() * 4 + 64, dtype=torch.uint8, device="cuda")
+    odd[2:2 + W.numel() * 4] = W.contiguous().view(-1).view(torch.uint8)
+    torch.cuda.synchronize()
+    h = C.c_void_p()
+    assert _abi.lib().hpacml8_linear_create(4096, 2048, odd.data_ptr() + 2, None, C.byref(h)) == _abi.OK
+    layer.close()
+    layer.handle = h
+    y.zero_()
+    api.linear8(layer, x, y)
+    assert torch.equal(y, want)
