@@ -6,11 +6,11 @@
 // for dx those six of nine whose terms' ranks sum to at most 2.
 //
 // Few rows take one launch (backward8_few.hip); otherwise up to four follow one
-// another.  131,072 rows of 2048 <- 2048 in bf16: W laid out 8 us, dx 0.92 ms,
-// dw 1.07-1.14 ms (1.0 PFLOP/s; the matrix cores work in 44% of its cycles, held
-// up by the conversion of the codes between them), parts joined 14 us.  262,144
-// rows of 256 <- 256: 5, 66, 64 and 7 us; dx and dw are bound by memory (337 MB
-// at 5.1 TB/s; 203 MB at 3.2 TB/s).
+// another.  131,072 rows of 2048 <- 2048 in bf16: W laid out 8 us, dx 0.9 ms, dw
+// 1.05-1.15 ms (1.0 PFLOP/s; the matrix cores work in 43% of its cycles, held up
+// by the conversion of the codes between them), parts joined 14 us.  262,144
+// rows of 256 <- 256: 5, 65, 68 and 7 us; dx and dw are bound by memory (337 MB
+// at 5.2 TB/s; 203 MB at 3.0 TB/s).
 #include <type_traits>
 
 #include "dense8_nt.hpp"

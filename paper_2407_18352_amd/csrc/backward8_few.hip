@@ -5,10 +5,11 @@
 // waves split the sum (over the outputs, or over the rows), load what their
 // share needs straight into registers, form the bf16 terms there, multiply, and
 // add their results through LDS, always in the same order.  256 rows, 64 -> 64
-// in fp32: 5.2 us of the device where the general form takes 16.5.  What bounds
+// in fp32: 4.7 us of the device where the general form takes 16.7.  What bounds
 // it is one wait for memory and the loads' issue, a column's values being a
 // load each.  A wave takes one step of a sum at a time: with two on the way at
-// once, and their code, 7.2 us (256 <- 256: 5.6 and 11.4).
+// once, and their code, it took 7.2 us where one took 5.2 (256 <- 256: 11.4 and
+// 5.6).
 //
 // The products are those of the general form: a kept value is exact in bf16, an
 // fp32 value is three bf16 terms; dw takes three products, dx the six whose

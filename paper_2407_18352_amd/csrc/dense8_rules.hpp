@@ -96,17 +96,24 @@ inline DwForm choose_dw(int64_t rows, int32_t n_out, int32_t n_in, int planes) {
 // dw and their join apart.  What counts is the number of 32 x 32 results, a
 // block each; that launch reads an operand again for every 32 results across.
 // Device us, one launch and the general form, of (rows) outputs <- inputs:
-//                                fp32           bf16
-//   (256) 64 <- 64             5.2   16.5      4.3  12.9
-//   (256) 512 <- 512 (384)    10.1   34.4      5.9  17.6
-//   (1024) 256 <- 256 (320)   16.0   27.5     10.7  16.1
-//   (256) 64 <- 2048 (640)     8.3   18.1      6.2  13.9
-//   (1024) 512 <- 512 (768)   23.5   41.2     13.9  21.5
-//   (1) 1024 <- 1024 (1056)   13.5   46.1      7.2  16.3
-//   (512) 64 <- 2048 (1152)   14.0   20.4     10.0  15.2
-//   (256) 1024 <- 1024 (1280) 24.5   57.6     13.3  19.2
-// and, of an earlier form that took up to twice as long, (4096) 64 <- 64 50.6
-// and 18.2 in fp32, (64) 2048 <- 2048 (4224) 58 and 34 in bf16.
+//                                 fp32           bf16
+//   (256) 64 <- 64              4.7   16.7      4.3  13.0
+//   (256) 512 <- 512 (384)      8.5   34.4      6.0  18.0
+//   (1024) 256 <- 256 (320)    13.1   27.4     10.6  16.3
+//   (256) 64 <- 2048 (640)      7.2   17.7      6.2  13.9
+//   (1024) 512 <- 512 (768)    19.0   41.1     13.8  21.6
+//   (1) 1024 <- 1024 (1056)     9.4   46.5      7.1  16.2
+//   (512) 64 <- 2048 (1152)    11.8   20.1      9.9  15.1
+//   (256) 1024 <- 1024 (1280)  19.1   58.0     13.3  19.2
+// and beyond the limits, where they cross:
+//   (512) 1024 <- 1024 (1536)  30.2   60.2     20.9  28.6
+//   (1024) 1024 <- 1024 (2048) 62.7   65.4     37.6  35.2
+//   (1024) 1024 <- 2048 (4096)  118   82.2     88.0  41.1
+//   (256) 2048 <- 2048 (4608)  66.5   91.2     46.7  36.1
+//   (1500) 64 <- 64            15.9   18.3     13.5  14.2
+//   (2048) 64 <- 64            20.6   18.1     17.4  14.4
+//   (2048) 512 <- 512 (1280)   44.9   45.9     25.3  24.6
+//   (4096) 64 <- 64            36.8   18.1     31.6  15.6
 inline bool few_rows(int64_t rows, int32_t n_out, int32_t n_in) {
     auto tiles = [](int64_t n) { return (n + 31) / 32; };
     return rows <= 1024 && tiles(n_in) * (tiles(rows) + tiles(n_out)) <= 1280;

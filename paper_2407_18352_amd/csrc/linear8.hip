@@ -2,13 +2,14 @@
 // exact 32-bit sums, fp32 epilogue.
 //
 // Three ways, by the number of points and the widths:
-//   up to 64 points: few_kernel; one point through 4096 -> 4096 takes 4.1 us of
-//     the device, the weights in the caches (16.8 MB, 3.4 us at a copy's rate);
+//   up to 64 points: few_kernel; one point through 4096 -> 4096 takes 4.4 us of
+//     the device when its weights are in the caches, as they are when the same
+//     layer is asked again and again (16.8 MB, 3.4 us at a copy's rate);
 //   many points of a narrow layer: narrow_kernel, bound by memory; 65,536 x 512
-//     -> 512 in bf16 takes 41 us (27 us at a copy's rate);
+//     -> 512 in bf16 takes 40 us (27 us at a copy's rate);
 //   otherwise the codes are formed by a launch of their own and the product is
 //     the general one, bound by the matrix cores: 131,072 x 4096 -> 4096 takes
-//     0.31 ms for the codes (1.6 GB, 5.1 TB/s) and 1.7-1.85 ms for the product.
+//     0.31 ms for the codes (1.6 GB, 5.2 TB/s) and 1.66-1.8 ms for the product.
 #include <type_traits>
 
 #include "dense8_nt.hpp"
@@ -103,6 +104,9 @@ void launch_tiled(const Linear8Args &a, hipStream_t stream) {
 // way, which saves a launch: 512 -> 512 in bf16, device us and us of a call from
 // the host, so and with a launch for the codes: 8 points 3.5 and 6.6, 5.4 and
 // 9.5; 24 points 5.6 and 6.6, 6.0 and 9.6; 48 points 7.9 and 7.8, 6.2 and 9.4.
+// 64 points, so and as tiles, device us with the launch for the codes: 512 ->
+// 512 6.4 and 7.3, 1024 -> 1024 6.7 and 8.7, 4096 -> 4096 12.7 and 17.1 (128
+// points, which have no form here, as tiles 7.3, 8.8 and 17.5).
 // Its code is kept short, a chunk or two of a row at a time: with eight of them
 // (so that all points' loads were on the way at once) 9 points took 7.3 us.
 constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewPoints = 64, kFusedPoints = 32, kFusedBytes = 36 * 1024;
@@ -371,9 +375,11 @@ void launch_narrow_tile(const Linear8Args &a, hipStream_t stream) {
 }
 
 // Points of a block: 64, of which four share a CU; with few outputs and enough
-// rows for as many larger blocks 128 (us, 64 and 128, and with the codes in
-// memory: 65536 x 512 <- 512 45.9, 48.3, 54.3; 262144 x 64 <- 64 26.8, 19.3,
-// 28.6; 65521 x 50 <- 201 in fp32 19.0, 22.4, 24.5).
+// rows for as many larger blocks 128 (device us, 64 and 128, and with the codes
+// in memory: 262144 x 64 <- 64 27.2, 20.2, 28.9; 131072 x 64 <- 64 13.3, 9.8,
+// 19.9; 262144 x 128 <- 128 38.1, 34.3, 45.5; 100000 x 128 <- 128 16.2, 17.9,
+// 23.1; 65521 x 50 <- 201 in fp32 18.6, 21.2, 23.3; against the rule 131072 x
+// 100 <- 300 54.4, 82.2, 63.7).
 template <typename X, typename Y, int SLABS>
 void launch_narrow(const Linear8Args &a, hipStream_t stream) {
     const bool many = a.rows >= 131072;
@@ -388,7 +394,14 @@ void launch_narrow(const Linear8Args &a, hipStream_t stream) {
 bool few_fused(int64_t rows, int32_t n_in) {
     return rows <= kFusedPoints && rows * fused_pitch(slabs_of(n_in)) <= kFusedBytes;
 }
-// (16384 x 512 <- 512 takes 24.5 us this way and 20.7 us with the codes in memory)
+// Device us this way and with the codes in memory, in bf16:
+//   16384 x 512 <- 512     23.6  20.0      24576 x 512 <- 512    26.6  26.7
+//   32768 x 512 <- 512     28.9  30.0      65536 x 512 <- 512    40.1  49.6
+//   32768 x 1024 <- 256    27.4  32.5      65536 x 1024 <- 256   45.0  54.1
+//   32768 x 1024 <- 512    44.7  40.6      65536 x 1024 <- 512   64.8  73.8
+//   32768 x 1500 <- 512    79.6  57.2      65536 x 1500 <- 512    160   110
+//   16384 x 64 <- 64        5.5   7.2      16384 x 1024 <- 256   23.5  19.8
+// (in fp32 32768 x 1024 <- 512 48.7 and 52.6)
 constexpr int64_t kNarrowPoints = 32768;
 bool narrow(int64_t rows, int32_t n_in, int32_t n_out) { return rows >= kNarrowPoints && rows <= (1 << 30) && n_in <= 512 && n_out <= 1024; }
 
