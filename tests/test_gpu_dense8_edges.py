@@ -344,3 +344,36 @@ def test_linear_weights_of_the_device():
     y.zero_()
     api.linear8(layer, x, y)
     assert torch.equal(y, want)
+
+
+def test_a_training_step_replayed_from_a_graph():
+    """A step captured after one on another stream, replayed between eager steps
+    with other inputs: each has the eager steps' gradients."""
+    import torch
+    m, x, dy = _model_and_batch(n=1100)
+    batches = [_model_and_batch(n=1100, seed=s)[1:] for s in (3, 4, 5)]
+    want = []
+    for u, d in batches:
+        m.forward(u)
+        m.backward(d)
+        want.append(_grads(m))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        m.forward(x)
+        m.backward(dy)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = m.forward(x)
+        m.backward(dy)
+    for again in range(2):
+        for (u, d), w in zip(batches, want):
+            x.copy_(u)
+            dy.copy_(d)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(_grads(m), w))
+            eager = m.forward(u)
+            m.backward(d)
+            assert torch.equal(eager, y) and all(torch.equal(p, q) for p, q in zip(_grads(m), w))
