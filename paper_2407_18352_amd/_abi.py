@@ -44,6 +44,17 @@ class Checkpoint8(C.Structure):
                 ("ld_exps", C.c_int64), ("width", C.c_int32), ("act", C.c_int32)]
 
 
+class Matrix(C.Structure):
+    """``hpacmlt_matrix``"""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("width", C.c_int64)]
+
+
+class Gradient(C.Structure):
+    """``hpacmlt_gradient``"""
+    _fields_ = [("from_", C.c_void_p), ("to", C.c_void_p), ("count", C.c_int64), ("from_dtype", C.c_int32),
+                ("to_dtype", C.c_int32)]
+
+
 class Layer(C.Structure):
     _fields_ = [("kind", C.c_int32), ("out_channels", C.c_int32), ("kernel", C.c_int32 * 2),
                 ("stride", C.c_int32 * 2), ("padding", C.c_int32), ("pad_mode", C.c_int32), ("act", C.c_int32)]
@@ -106,6 +117,38 @@ SIGNATURES8 = {
                                    C.c_size_t, C.c_void_p]),
 }
 
+# every symbol of include/hpacmlt.h (layers in 8-bit floating point, group norm, gradients)
+ACT_SILU = 2
+NORM_2, NORM_MAX = 0, 1
+BLOCKF8, MAX_CHANNELS = 128, 16384
+_GN = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
+SIGNATURES_T = {
+    "hpacmlt_matrix_bytes": (C.c_int, [C.c_int64, C.c_int64, _P(C.c_size_t), _P(C.c_size_t)]),
+    "hpacmlt_quantize": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P(Matrix), _P(Matrix), C.c_int32,
+                                   C.c_void_p]),
+    "hpacmlt_load": (C.c_int, [_P(Matrix), C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]),
+    "hpacmlt_product": (C.c_int, [_P(Matrix), _P(Matrix), C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_int32,
+                                  C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hpacmlt_product_scratch": (C.c_int, [C.c_int64, C.c_int64, C.c_int64, _P(C.c_size_t)]),
+    "hpacmlt_linear_run": (C.c_int, [_P(Matrix), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
+                                     C.c_int64, C.c_int32, _P(Matrix), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hpacmlt_linear_scratch": (C.c_int, [_P(Matrix), C.c_int64, _P(C.c_size_t)]),
+    "hpacmlt_backward": (C.c_int, [_P(Matrix), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _P(Matrix),
+                                   C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_size_t,
+                                   C.c_void_p]),
+    "hpacmlt_backward_scratch": (C.c_int, [C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P(C.c_size_t)]),
+    "hpacmlt_group_norm": (C.c_int, _GN + [C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                           C.c_size_t, C.c_void_p]),
+    "hpacmlt_group_norm_backward": (C.c_int, _GN + [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                                    C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hpacmlt_group_norm_scratch": (C.c_int, [C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _P(C.c_size_t)]),
+    "hpacmlt_gradients_create": (C.c_int, [_P(Gradient), C.c_int64, _P(C.c_void_p)]),
+    "hpacmlt_gradients_destroy": (None, [C.c_void_p]),
+    "hpacmlt_gradients_scratch": (C.c_int, [C.c_void_p, _P(C.c_size_t)]),
+    "hpacmlt_gradients_norm": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hpacmlt_gradients_clip": (C.c_int, [C.c_void_p, C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+}
+
 _lib = None
 
 
@@ -117,7 +160,7 @@ def lib():
             raise RuntimeError("libhpacml.so is not built: run `python -m paper_2407_18352_amd.build` "
                                "(or __graft_entry__.build())")
         L = C.CDLL(LIB_PATH)
-        for name, (res, args) in list(SIGNATURES.items()) + list(SIGNATURES8.items()):
+        for name, (res, args) in [*SIGNATURES.items(), *SIGNATURES8.items(), *SIGNATURES_T.items()]:
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args

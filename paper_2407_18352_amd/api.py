@@ -510,3 +510,322 @@ def backward8(kept: Checkpoint8, dy, dw=None, db=None, W=None, dx=None, accumula
         kept, (py, ty, ldy, n_out), 1 if dw is not None or db is not None else 0, 0 if dx is None else 1), stream)
     check(lib().hpacml8_backward(kept.desc, py, ty, ldy, n_out, pW, ldW, pw, lddw, pb, px, ldx,
                                  1 if accumulate else 0, ps, bytes_, _stream(stream)), "hpacml8_backward")
+
+
+# ---- layers in 8-bit floating point (include/hpacmlt.h) ----------------------
+
+
+class MatrixF8:
+    """Buffers of a matrix [rows][width] in 8-bit floating point with a scale
+    for each block of 128 values of a row (``hpacmlt_matrix``), in the library's
+    own order.  ``codes`` and ``scales`` may be given (contiguous uint8 device
+    tensors of at least ``MatrixF8.bytes(rows, width)``)."""
+
+    @staticmethod
+    def bytes(rows: int, width: int):
+        c, s = C.c_size_t(), C.c_size_t()
+        check(lib().hpacmlt_matrix_bytes(int(rows), int(width), C.byref(c), C.byref(s)), "hpacmlt_matrix_bytes")
+        return c.value, s.value
+
+    def __init__(self, rows: int, width: int, codes=None, scales=None):
+        import torch
+        need = self.bytes(rows, width)
+        if codes is None:
+            codes = torch.empty(need[0], dtype=torch.uint8, device="cuda")
+        if scales is None:
+            scales = torch.empty(need[1], dtype=torch.uint8, device="cuda")
+        for t, what, least in ((codes, "codes", need[0]), (scales, "scales", need[1])):
+            if t.dtype != torch.uint8 or not t.is_cuda:
+                raise TypeError("%s must be a uint8 device tensor" % what)
+            if t.numel() < least or not t.is_contiguous():
+                raise ValueError("%s: %d values, expected at least %d, contiguous" % (what, t.numel(), least))
+        self.rows, self.width, self.codes, self.scales = int(rows), int(width), codes, scales
+        self.desc = _abi.Matrix(codes.data_ptr(), scales.data_ptr(), self.rows, self.width)
+
+
+def quantizef8(x, by_row: MatrixF8 = None, by_column: MatrixF8 = None, square: bool = False, stream=None) -> None:
+    """``hpacmlt_quantize``: ``x`` [n][m] (float32 or bfloat16) as ``by_row``
+    [n][m], in blocks of 128 columns of a row, and as its transpose
+    ``by_column`` [m][n], in blocks of 128 rows of a column; ``square``: both in
+    blocks of 128 x 128 (weights)."""
+    px, tx, ldx = _matrix(x, "x")
+    check(lib().hpacmlt_quantize(px, tx, ldx, x.shape[0], x.shape[1], None if by_row is None else by_row.desc,
+                                 None if by_column is None else by_column.desc, 1 if square else 0, _stream(stream)),
+          "hpacmlt_quantize")
+
+
+def loadf8(m: MatrixF8, x, stream=None) -> None:
+    """``hpacmlt_load``: what ``m`` stands for, as ``x`` [rows][width]."""
+    px, tx, ldx = _matrix(x, "x", m.rows, m.width)
+    check(lib().hpacmlt_load(m.desc, px, tx, ldx, _stream(stream)), "hpacmlt_load")
+
+
+def _vector(t, what, n):
+    """The address of a contiguous float32 device vector of n values (None: none)."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.float32 or not t.is_cuda:
+        raise TypeError("%s must be a float32 device tensor" % what)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: shape %s, expected %d values, contiguous" % (what, tuple(t.shape), n))
+    return t.data_ptr()
+
+
+def productf8_scratch_bytes(p: MatrixF8, q: MatrixF8) -> int:
+    """Bytes of scratch ``productf8`` needs."""
+    n = C.c_size_t()
+    check(lib().hpacmlt_product_scratch(p.rows, q.rows, p.width, C.byref(n)), "hpacmlt_product_scratch")
+    return n.value
+
+
+def productf8(p: MatrixF8, q: MatrixF8, y, b=None, act: int = _abi.ACT_IDENTITY, accumulate: bool = False, scratch=None,
+              stream=None) -> None:
+    """``hpacmlt_product``: ``y`` [p.rows][q.rows] (float32 or bfloat16) =
+    act(``p`` ``q``^T + ``b``), or, with ``accumulate``, added to ``y``
+    (float32)."""
+    py, ty, ldy = _matrix(y, "y", p.rows, q.rows)
+    keep, ps, bytes_ = _scratch8(scratch, lambda: productf8_scratch_bytes(p, q), stream)
+    check(lib().hpacmlt_product(p.desc, q.desc, _vector(b, "b", q.rows), act, py, ty, ldy, 1 if accumulate else 0, ps, bytes_,
+                                _stream(stream)), "hpacmlt_product")
+
+
+class LinearF8:
+    """A dense layer's weights in 8-bit floating point, a scale for each 128 x
+    128 of them: ``W`` [out][in] and ``b`` [out] or None (float32 or bfloat16
+    W, on the CPU or the device), on the current stream; ``learn``: the weights
+    by column as well, as ``backwardf8`` reads them for dx."""
+
+    def __init__(self, W, b=None, learn: bool = False):
+        import numpy as np
+        import torch
+        W = torch.as_tensor(np.asarray(W) if not isinstance(W, torch.Tensor) else W)
+        if W.dim() != 2 or W.numel() == 0:
+            raise ValueError("W: shape %s, expected out x in" % (tuple(W.shape),))
+        self.n_out, self.n_in = int(W.shape[0]), int(W.shape[1])
+        self.W = MatrixF8(self.n_out, self.n_in)
+        self.Wt = MatrixF8(self.n_in, self.n_out) if learn else None
+        self.b = None if b is None else torch.empty(self.n_out, device="cuda")
+        if b is not None and not isinstance(b, torch.Tensor):
+            b = torch.as_tensor(np.asarray(b))
+        if W.dtype not in (torch.float32, torch.bfloat16):
+            W = W.to(torch.float32)
+        self.update(W.detach().cuda(), b)
+
+    def update(self, W, b=None, stream=None) -> None:
+        """Other weights (and biases, which a layer made without has none of)
+        in the same buffers: ``hpacmlt_quantize`` on ``stream``."""
+        import torch
+        if tuple(W.shape) != (self.n_out, self.n_in):
+            raise ValueError("W: shape %s, expected %s" % (tuple(W.shape), (self.n_out, self.n_in)))
+        if (b is None) != (self.b is None):
+            raise ValueError("b: a layer keeps its biases, or has none")
+        if b is not None and tuple(b.shape) != (self.n_out,):
+            raise ValueError("b: shape %s, expected %d" % (tuple(b.shape), self.n_out))
+        W = W.detach()
+        if (W.stride(1) != 1 and W.shape[1] > 1) or (W.shape[0] > 1 and W.stride(0) < W.shape[1]):
+            if stream is not None:
+                raise ValueError("W: the values of a row must be contiguous in a call on a stream of its own")
+            W = W.contiguous()
+        quantizef8(W, self.W, self.Wt, square=True, stream=stream)
+        if b is not None:
+            if stream is None:
+                self.b.copy_(b.detach(), non_blocking=True)
+            else:
+                with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
+                    self.b.copy_(b.detach(), non_blocking=True)
+
+    def scratch_bytes(self, n_rows: int) -> int:
+        n = C.c_size_t()
+        check(lib().hpacmlt_linear_scratch(self.W.desc, int(n_rows), C.byref(n)), "hpacmlt_linear_scratch")
+        return n.value
+
+
+def linearf8(layer: LinearF8, x, y, act: int = _abi.ACT_IDENTITY, kept: MatrixF8 = None, scratch=None, stream=None) -> None:
+    """``hpacmlt_linear_run``: ``y`` [n][out] = act(``x`` [n][in] W^T + b) with
+    x in 8-bit floating point, a scale for each 128 values of a row; float32 or
+    bfloat16 device tensors, rows may lie inside wider ones.  ``kept``
+    [in][n]: x by column, for ``backwardf8``.  ``scratch``: at least
+    ``layer.scratch_bytes(n)`` bytes (None: from torch's allocator, on its
+    current stream)."""
+    px, tx, ldx = _matrix(x, "x", width=layer.n_in)
+    n = x.shape[0]
+    py, ty, ldy = _matrix(y, "y", rows=n, width=layer.n_out)
+    keep, ps, bytes_ = _scratch8(scratch, lambda: layer.scratch_bytes(n), stream)
+    check(lib().hpacmlt_linear_run(layer.W.desc, None if layer.b is None else layer.b.data_ptr(), px, tx, ldx, n, py, ty, ldy, act,
+                                   None if kept is None else kept.desc, ps, bytes_, _stream(stream)), "hpacmlt_linear_run")
+
+
+def backwardf8_scratch_bytes(kept: MatrixF8, dy, dw: bool = True, db: bool = True, dx: bool = True) -> int:
+    """Bytes of scratch ``backwardf8`` needs for the gradients wanted."""
+    n = C.c_size_t()
+    check(lib().hpacmlt_backward_scratch(kept.width, kept.rows, dy.shape[1], 1 if dw else 0, 1 if db else 0, 1 if dx else 0,
+                                         C.byref(n)), "hpacmlt_backward_scratch")
+    return n.value
+
+
+def backwardf8(kept: MatrixF8, dy, dw=None, db=None, layer: LinearF8 = None, dx=None, y=None, accumulate: bool = False,
+               scratch=None, stream=None) -> None:
+    """``hpacmlt_backward``: the gradients of a layer whose input is ``kept``
+    by column, from ``dy`` [n][out] (float32 or bfloat16), which counts as 0
+    where ``y`` [n][out] (dy's type; the layer's outputs behind a ReLU) is not
+    above 0: ``dw`` [out][in] and ``db`` [out] in float32, ``dx`` [n][in] in
+    dy's type from ``layer`` (made with ``learn``).  Gradients not given are not
+    computed."""
+    n, n_in = kept.width, kept.rows
+    pg, tg, ldg = _matrix(dy, "dy", n)
+    n_out = dy.shape[1]
+    py = pw = px = None
+    ldy = lddw = ldx = 0
+    if y is not None:
+        py, _, ldy = _matrix(y, "y", n, n_out, tg)
+    if dw is not None:
+        pw, _, lddw = _matrix(dw, "dw", n_out, n_in, _abi.F32)
+    pb = _vector(db, "db", n_out)
+    if dx is not None:
+        if layer is None or layer.Wt is None:
+            raise ValueError("dx needs a layer made with learn")
+        if layer.n_out != n_out or layer.n_in != n_in:
+            raise ValueError("layer: %d -> %d, expected %d -> %d" % (layer.n_in, layer.n_out, n_in, n_out))
+        px, _, ldx = _matrix(dx, "dx", n, n_in, tg)
+        if n == 0 and dw is None and db is None:
+            return        # an empty tensor has no address, which would read as "not wanted"
+    keep, ps, bytes_ = _scratch8(scratch, lambda: backwardf8_scratch_bytes(kept, dy, dw is not None, db is not None, dx is not None),
+                                 stream)
+    check(lib().hpacmlt_backward(kept.desc, pg, py, tg, ldg, ldy, n_out, None if dx is None else layer.Wt.desc, pw, lddw, pb, px,
+                                 ldx, 1 if accumulate else 0, ps, bytes_, _stream(stream)), "hpacmlt_backward")
+
+
+# ---- group norm with an activation, channels last -----------------------------
+
+
+def _images(x, points):
+    if points < 1 or x.shape[0] % points:
+        raise ValueError("x: %d rows, expected a multiple of %d points" % (x.shape[0], points))
+    return x.shape[0] // int(points)
+
+
+def group_norm_scratch_bytes(x, points: int, groups: int, backward: bool = False) -> int:
+    """Bytes of scratch ``group_norm`` (``backward``: ``group_norm_backward``)
+    needs for ``x``."""
+    _, kind, _ = _matrix(x, "x")
+    n = C.c_size_t()
+    check(lib().hpacmlt_group_norm_scratch(kind, _images(x, points), int(points), x.shape[1], int(groups), 1 if backward else 0,
+                                           C.byref(n)), "hpacmlt_group_norm_scratch")
+    return n.value
+
+
+def group_norm(x, y, points: int, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: int = _abi.ACT_IDENTITY, mean=None,
+               rstd=None, scratch=None, stream=None) -> None:
+    """``hpacmlt_group_norm``: ``y`` = act(the group norm of ``x``) for rows
+    [images * points][channels] of float32 or bfloat16 (one type; rows may lie
+    inside wider ones): the ``points`` rows of an image share their statistics.
+    ``gamma``, ``beta`` [channels]; ``act`` also ACT_SILU; ``mean`` and ``rstd``
+    [images][groups] are written where given (both or none)."""
+    px, kind, ldx = _matrix(x, "x")
+    py, _, ldy = _matrix(y, "y", x.shape[0], x.shape[1], kind)
+    images, channels = _images(x, points), x.shape[1]
+    if images == 0:
+        return
+    stats = images * int(groups)
+    keep, ps, bytes_ = _scratch8(scratch, lambda: group_norm_scratch_bytes(x, points, groups), stream)
+    check(lib().hpacmlt_group_norm(px, kind, ldx, images, int(points), channels, int(groups), _vector(gamma, "gamma", channels),
+                                   _vector(beta, "beta", channels), eps, act, py, ldy, _vector(mean, "mean", stats),
+                                   _vector(rstd, "rstd", stats), ps, bytes_, _stream(stream)), "hpacmlt_group_norm")
+
+
+def group_norm_backward(x, dy, points: int, groups: int, mean, rstd, dx=None, dgamma=None, dbeta=None, gamma=None, beta=None,
+                        act: int = _abi.ACT_IDENTITY, accumulate: bool = False, scratch=None, stream=None) -> None:
+    """``hpacmlt_group_norm_backward``: from the gradient ``dy`` of
+    ``group_norm``'s ``y`` that of ``x`` (``dx``) and of ``gamma`` and ``beta``
+    (``dgamma``, ``dbeta`` [channels], float32), each if given; ``mean`` and
+    ``rstd`` as ``group_norm`` wrote them, the rest as given to it."""
+    px, kind, ldx = _matrix(x, "x")
+    pg, _, ldg = _matrix(dy, "dy", x.shape[0], x.shape[1], kind)
+    images, channels = _images(x, points), x.shape[1]
+    pd, ldd = None, 0
+    if dx is not None:
+        pd, _, ldd = _matrix(dx, "dx", x.shape[0], channels, kind)
+        if images == 0 and dgamma is None and dbeta is None:
+            return
+    stats = images * int(groups)
+    keep, ps, bytes_ = _scratch8(scratch, lambda: group_norm_scratch_bytes(x, points, groups, True), stream)
+    check(lib().hpacmlt_group_norm_backward(px, kind, ldx, images, int(points), channels, int(groups),
+                                            _vector(gamma, "gamma", channels), _vector(beta, "beta", channels), act,
+                                            _vector(mean, "mean", stats), _vector(rstd, "rstd", stats), pg, ldg, pd, ldd,
+                                            _vector(dgamma, "dgamma", channels), _vector(dbeta, "dbeta", channels),
+                                            1 if accumulate else 0, ps, bytes_, _stream(stream)), "hpacmlt_group_norm_backward")
+
+
+# ---- the norm of many gradients, and clipping -----------------------------------
+
+
+def _dense(t):
+    """Whether t's values are one after another in memory, in any order of its dimensions."""
+    expected = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != expected:
+            return False
+        expected *= size
+    return True
+
+
+class GradientSet:
+    """Gradients whose norm is taken together (``hpacmlt_gradients_create``):
+    float32 or bfloat16 device tensors whose values are one after another in
+    memory; ``into``: as many tensors of the same shapes and strides that
+    clipping writes to (None: in place).  The set holds the tensors: gradients
+    that an optimizer replaces need a new set."""
+
+    def __init__(self, gradients, into=None):
+        if not _kinds8:
+            import torch
+            _kinds8.update({torch.float32: _abi.F32, torch.bfloat16: _abi.BF16})
+        gradients = list(gradients)
+        into = gradients if into is None else list(into)
+        if len(into) != len(gradients):
+            raise ValueError("into: %d tensors, expected %d" % (len(into), len(gradients)))
+        table = (_abi.Gradient * max(1, len(gradients)))()
+        for e, g, t in zip(table, gradients, into):
+            for v in (g, t):
+                if v.dtype not in _kinds8 or not v.is_cuda:
+                    raise TypeError("gradients must be float32 or bfloat16 device tensors")
+                if v.numel() and not _dense(v):
+                    raise ValueError("gradients must have their values one after another in memory: strides %s of shape %s"
+                                     % (tuple(v.stride()), tuple(v.shape)))
+            if g.shape != t.shape or (g.numel() and any(a != b for a, b, n in zip(g.stride(), t.stride(), g.shape) if n != 1)):
+                raise ValueError("into: shape %s, strides %s, expected %s, %s"
+                                 % (tuple(t.shape), tuple(t.stride()), tuple(g.shape), tuple(g.stride())))
+            e.from_, e.to, e.count = g.data_ptr(), t.data_ptr(), g.numel()
+            e.from_dtype, e.to_dtype = _kinds8[g.dtype], _kinds8[t.dtype]
+        h = C.c_void_p()
+        check(lib().hpacmlt_gradients_create(table, len(gradients), C.byref(h)), "hpacmlt_gradients_create")
+        self.handle, self.gradients, self.into = h, gradients, into
+
+    def scratch_bytes(self) -> int:
+        n = C.c_size_t()
+        check(lib().hpacmlt_gradients_scratch(self.handle, C.byref(n)), "hpacmlt_gradients_scratch")
+        return n.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().hpacmlt_gradients_destroy(self.handle)
+            self.handle = None
+
+    __del__ = Model.__del__
+
+
+def gradient_norm(gradients: GradientSet, norm, kind: int = _abi.NORM_2, scratch=None, stream=None) -> None:
+    """``hpacmlt_gradients_norm``: the common norm of the set, into ``norm``
+    [1] (float32): Euclidean (NORM_2) or the largest magnitude (NORM_MAX)."""
+    keep, ps, bytes_ = _scratch8(scratch, gradients.scratch_bytes, stream)
+    check(lib().hpacmlt_gradients_norm(gradients.handle, kind, _vector(norm, "norm", 1), ps, bytes_, _stream(stream)),
+          "hpacmlt_gradients_norm")
+
+
+def clip_gradients(gradients: GradientSet, most: float, norm, kind: int = _abi.NORM_2, scratch=None, stream=None) -> None:
+    """``hpacmlt_gradients_clip``: ``gradient_norm``, and every gradient times
+    min(1, most / (norm + 1e-6)), in place or into the set's ``into``."""
+    keep, ps, bytes_ = _scratch8(scratch, gradients.scratch_bytes, stream)
+    check(lib().hpacmlt_gradients_clip(gradients.handle, kind, most, _vector(norm, "norm", 1), ps, bytes_, _stream(stream)),
+          "hpacmlt_gradients_clip")

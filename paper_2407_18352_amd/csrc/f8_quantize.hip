@@ -1,0 +1,260 @@
+// Codes and scales of a matrix by row, by column, or both in one reading.
+//
+// A block of 256 threads takes 128 x 128 values: a thread four rows by 16
+// columns, in registers.  The largest magnitude of a row's 128 columns joins
+// eight lanes, that of a column's 128 rows the threads of a wave and, through
+// LDS, the four waves.  The codes by row (16 of a thread are one store) and by
+// column (four rows of a column are one word) are laid out in LDS as they lie in
+// memory, 16 KB each, and copied out in whole pieces.  16-byte slots are turned
+// by what the lanes of one LDS write differ in (turn_row, turn_column), so that
+// they fall on different banks.
+#include "f8.hpp"
+
+namespace hpacml {
+namespace f8 {
+
+namespace {
+
+// slot of 16 bytes in a 16 KB image: unit * 128 + half * 64 + group * 32 + row
+__device__ __forceinline__ int turn_row(int slot) { return slot ^ (((slot >> 4) & 1) | (((slot >> 6) & 1) << 1)); }
+__device__ __forceinline__ int turn_column(int slot) {
+    return slot ^ (((slot >> 4) & 1) | (((slot >> 8) & 3) << 1) | (((slot >> 6) & 1) << 3));
+}
+
+template <typename X, bool ROW, bool COLUMN, bool MASK, bool SUMS>
+__global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a) {
+    __shared__ u32x4 image[ROW && COLUMN ? 2048 : 1024];
+    __shared__ uint32_t most_of[4][128];
+    __shared__ float sum_of[SUMS ? 4 : 1][128];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int rg = lane & 7, tc = lane >> 3;                 // rows 32 wave + 4 rg + j, columns 16 tc + i
+    const int64_t row_tile = blockIdx.x / blocks_of(a.width), col_tile = blockIdx.x % blocks_of(a.width);
+    const int64_t row0 = row_tile * 128 + wave * 32 + rg * 4, col0 = col_tile * 128 + tc * 16;
+    const int64_t left = a.width - col0;
+    const int have = left > 16 ? 16 : left < 0 ? 0 : (int)left;
+
+    float v[4][16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t row = row0 + j;
+        const int n = row < a.rows ? have : 0;
+        load16((const X *)a.x + row * a.ldx + col0, n, v[j]);
+        if (MASK) {
+            float y[16];
+            load16((const X *)a.y + row * a.ldy + col0, n, y);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                v[j][i] = y[i] <= 0.f ? 0.f : v[j][i];
+        }
+    }
+    uint32_t row_most[4], col_most[16];
+    if (ROW) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                m = max(m, magnitude(v[j][i]));
+#pragma unroll
+            for (int s = 8; s < 64; s *= 2)
+                m = max(m, (uint32_t)__shfl_xor((int)m, s));
+            row_most[j] = m;
+        }
+    }
+    if (COLUMN || SUMS) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            uint32_t m = 0;
+            float t = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                m = max(m, magnitude(v[j][i]));
+                t += v[j][i];
+            }
+#pragma unroll
+            for (int s = 1; s < 8; s *= 2) {
+                if (COLUMN)
+                    m = max(m, (uint32_t)__shfl_xor((int)m, s));
+                if (SUMS)
+                    t += __shfl_xor(t, s);
+            }
+            if (rg == 0) {
+                if (COLUMN)
+                    most_of[wave][tc * 16 + i] = m;
+                if (SUMS)
+                    sum_of[wave][tc * 16 + i] = t;
+            }
+        }
+        __syncthreads();
+        if (COLUMN) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int c = tc * 16 + i;
+                col_most[i] = max(max(most_of[0][c], most_of[1][c]), max(most_of[2][c], most_of[3][c]));
+            }
+        }
+        if (SUMS && threadIdx.x < 128 && col_tile * 128 + threadIdx.x < a.width)
+            a.sums[row_tile * a.width + col_tile * 128 + threadIdx.x] =
+                (sum_of[0][threadIdx.x] + sum_of[1][threadIdx.x]) + (sum_of[2][threadIdx.x] + sum_of[3][threadIdx.x]);
+    }
+    if (a.square) {
+        // the largest of all: of the columns where those are known, of the rows otherwise
+        uint32_t m = 0;
+        if (COLUMN) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                m = max(m, col_most[i]);
+#pragma unroll
+            for (int s = 8; s < 64; s *= 2)
+                m = max(m, (uint32_t)__shfl_xor((int)m, s));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                m = max(m, row_most[j]);
+#pragma unroll
+            for (int s = 1; s < 8; s *= 2)
+                m = max(m, (uint32_t)__shfl_xor((int)m, s));
+            if (lane == 0)
+                most_of[wave][0] = m;
+            __syncthreads();
+            m = max(max(most_of[0][0], most_of[1][0]), max(most_of[2][0], most_of[3][0]));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            row_most[j] = m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            col_most[i] = m;
+    }
+    if (ROW) {
+        const int64_t blocks = blocks_of(a.width);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t byte = scale_byte(row_most[j]);
+            const float f = scale_factor(byte);
+            u32x4 c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                c[e] = byte == 255u ? kNanCodes : codes4(v[j][4 * e], v[j][4 * e + 1], v[j][4 * e + 2], v[j][4 * e + 3], f);
+            // unit (32 rows: wave) * 2 + tc / 4, half tc % 2, group (tc / 2) % 2, row 4 rg + j
+            image[turn_row((wave * 2 + (tc >> 2)) * 128 + (tc & 1) * 64 + ((tc >> 1) & 1) * 32 + rg * 4 + j)] = c;
+            if (tc == 0)
+                a.by_row.scales[scale_offset(row0 + j, col_tile, blocks)] = (char)byte;
+        }
+    }
+    if (COLUMN) {
+        const int64_t blocks = blocks_of(a.rows);
+        char *to = (char *)(image + (ROW ? 1024 : 0));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t byte = scale_byte(col_most[i]);
+            const uint32_t w = byte == 255u ? kNanCodes : codes4(v[0][i], v[1][i], v[2][i], v[3][i], scale_factor(byte));
+            const int c = tc * 16 + i, r = wave * 32 + rg * 4;       // row c of the transpose, values r..r + 3 of its 128
+            const int slot = ((c >> 5) * 2 + (r >> 6)) * 128 + ((r >> 4) & 1) * 64 + ((r >> 5) & 1) * 32 + (c & 31);
+            *(uint32_t *)(to + turn_column(slot) * 16 + (r & 15)) = w;
+            if (rg == 0 && wave == 0)
+                a.by_column.scales[scale_offset(col_tile * 128 + c, row_tile, blocks)] = (char)byte;
+        }
+    }
+    __syncthreads();
+    // 1024 slots of each, 128 a unit; units of rows that do not exist are not written
+    if (ROW) {
+        const int64_t blocks = blocks_of(a.width), units = row_units(a.rows);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int slot = i * 256 + threadIdx.x;
+            const int64_t unit = row_tile * 4 + (slot >> 8);
+            if (unit < units)
+                *(u32x4 *)(a.by_row.codes + (unit * blocks + col_tile) * 2 * kUnit + (slot & 255) * 16) = image[turn_row(slot)];
+        }
+    }
+    if (COLUMN) {
+        const int64_t blocks = blocks_of(a.rows), units = row_units(a.width);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int slot = i * 256 + threadIdx.x;
+            const int64_t unit = col_tile * 4 + (slot >> 8);
+            if (unit < units)
+                *(u32x4 *)(a.by_column.codes + (unit * blocks + row_tile) * 2 * kUnit + (slot & 255) * 16) =
+                    image[(ROW ? 1024 : 0) + turn_column(slot)];
+        }
+    }
+}
+
+// A thread reads 16 codes of a row.
+template <typename X>
+__global__ __launch_bounds__(256) void load_kernel(Matrix m, X *x, int64_t ldx) {
+    const int64_t blocks = blocks_of(m.width), chunks = blocks * 8;
+    const int64_t unit = blockIdx.x / ((chunks + 7) / 8), part = blockIdx.x % ((chunks + 7) / 8);   // 32 rows, eight chunks
+    const int64_t row = unit * 32 + (threadIdx.x & 31), k = (part * 8 + (threadIdx.x >> 5)) * 16;
+    if (row >= m.rows || k >= m.width)
+        return;
+    const u32x4 c = *(const u32x4 *)(m.codes + code_offset(row, k, blocks));
+    const uint32_t byte = (uint8_t)m.scales[scale_offset(row, k / kBlock, blocks)];
+    const float s = byte == 255u ? __builtin_nanf("") : byte == 0u ? 0x1p-127f : __builtin_bit_cast(float, byte << 23);
+    X *to = x + row * ldx + k;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(c[e], 0) * s, __builtin_amdgcn_cvt_f32_fp8(c[e], 1) * s,
+                            __builtin_amdgcn_cvt_f32_fp8(c[e], 2) * s, __builtin_amdgcn_cvt_f32_fp8(c[e], 3) * s};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + 4 * e + i < m.width)
+                store_value(to + 4 * e + i, v[i]);
+    }
+}
+
+template <typename X, bool ROW, bool COLUMN>
+void launch_form(const QuantizeArgs &a, uint32_t blocks, hipStream_t stream) {
+    if (a.y && a.sums)
+        quantize_kernel<X, ROW, COLUMN, true, true><<<blocks, 256, 0, stream>>>(a);
+    else if (a.y)
+        quantize_kernel<X, ROW, COLUMN, true, false><<<blocks, 256, 0, stream>>>(a);
+    else if (a.sums)
+        quantize_kernel<X, ROW, COLUMN, false, true><<<blocks, 256, 0, stream>>>(a);
+    else
+        quantize_kernel<X, ROW, COLUMN, false, false><<<blocks, 256, 0, stream>>>(a);
+}
+
+template <typename X>
+void launch_type(const QuantizeArgs &a, uint32_t blocks, hipStream_t stream) {
+    if (a.by_row.codes && a.by_column.codes)
+        launch_form<X, true, true>(a, blocks, stream);
+    else if (a.by_row.codes)
+        launch_form<X, true, false>(a, blocks, stream);
+    else if (a.by_column.codes)
+        launch_form<X, false, true>(a, blocks, stream);
+    else
+        launch_form<X, false, false>(a, blocks, stream);
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantizeArgs &a, int32_t dtype, hipStream_t stream) {
+    const int64_t blocks = blocks_of(a.rows) * blocks_of(a.width);
+    if (blocks == 0)
+        return hipSuccess;
+    if (blocks > INT32_MAX)
+        return hipErrorInvalidValue;
+    if (dtype == HPACML_F32)
+        launch_type<float>(a, (uint32_t)blocks, stream);
+    else
+        launch_type<uint16_t>(a, (uint32_t)blocks, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_load(const Matrix &m, void *x, int32_t dtype, int64_t ldx, hipStream_t stream) {
+    const int64_t blocks = row_units(m.rows) * blocks_of(m.width);
+    if (blocks == 0)
+        return hipSuccess;
+    if (blocks > INT32_MAX)
+        return hipErrorInvalidValue;
+    if (dtype == HPACML_F32)
+        load_kernel<<<(uint32_t)blocks, 256, 0, stream>>>(m, (float *)x, ldx);
+    else
+        load_kernel<<<(uint32_t)blocks, 256, 0, stream>>>(m, (uint16_t *)x, ldx);
+    return hipGetLastError();
+}
+
+}  // namespace f8
+}  // namespace hpacml
