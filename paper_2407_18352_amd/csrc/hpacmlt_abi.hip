@@ -8,6 +8,7 @@
 #include <new>
 #include <vector>
 
+#include "columns.hpp"
 #include "f8.hpp"
 #include "gradients.hpp"
 #include "group_norm.hpp"
@@ -61,7 +62,7 @@ struct LinearLayout : Layout {
 
 struct BackwardLayout : Layout {
     MatrixAt by_row{}, by_column{};
-    size_t sums = 0, partial = 0;
+    size_t sums = 0, room = 0, partial = 0;
     BackwardLayout(int64_t rows, int64_t n_in, int64_t n_out, bool dw, bool db, bool dx) {
         int64_t most = 0;
         if (dx) {
@@ -73,8 +74,10 @@ struct BackwardLayout : Layout {
             const int64_t b = f8::product_partial_bytes(n_out, n_in, rows);
             most = b > most ? b : most;
         }
-        if (db)
+        if (db) {
             sums = take(f8::blocks_of(rows) * n_out * 4);
+            room = take(column_sums_room(f8::blocks_of(rows), n_out) * 4);
+        }
         partial = take(most);
     }
 };
@@ -363,7 +366,7 @@ hpacml_status hpacmlt_backward(const hpacmlt_matrix *kept, const void *dy, const
         if (!accumulate && dw)
             e = f8::launch_join(nullptr, 0, n_out, n_in, 0, dw, lddw, 0, st);
         if (!accumulate && db && e == hipSuccess)
-            e = f8::launch_join(nullptr, 0, 1, n_out, 0, db, n_out, 0, st);
+            e = launch_column_sums(nullptr, 0, n_out, 0, db, 0, nullptr, st);
         return status_of(e);
     }
     char *at = (char *)scratch;
@@ -371,7 +374,7 @@ hpacml_status hpacmlt_backward(const hpacmlt_matrix *kept, const void *dy, const
     float *sums = db ? (float *)(at + l.sums) : nullptr, *partial = (float *)(at + l.partial);
     hipError_t e = f8::launch_quantize({dy, y, lddy, ldy, rows, n_out, by_row, by_column, sums, 0}, dtype, st);
     if (e == hipSuccess && db)
-        e = f8::launch_join(sums, f8::blocks_of(rows), 1, n_out, n_out, db, n_out, accumulate != 0, st);
+        e = launch_column_sums(sums, f8::blocks_of(rows), n_out, n_out, db, accumulate != 0, (float *)(at + l.room), st);
     if (e == hipSuccess && dx)
         e = f8::launch_product({by_row, matrix_of(*Wt), nullptr, dx, lddx, 0, 0, partial}, dtype, st);
     if (e == hipSuccess && dw)
