@@ -63,9 +63,13 @@ struct ProductArgs {
 int64_t product_partial_bytes(int64_t p_rows, int64_t q_rows, int64_t width);
 hipError_t launch_product(const ProductArgs &a, int32_t y_dtype, hipStream_t stream);
 
-// out[r][c] (+)= sum over parts of part[i][r][c], rows of `pitch` floats
-hipError_t launch_join(const float *part, int64_t parts, int64_t rows, int64_t width, int64_t pitch, float *out, int64_t ldo,
-                       int32_t accumulate, hipStream_t stream);
+// Whether a product of these sizes reads everything in one launch: few rows,
+// and outputs for a good part of the chip or a width that few blocks pass
+// quickly.
+inline bool few_rows(int64_t p_rows, int64_t q_rows, int64_t width) { return p_rows <= 64 && width > 0 && (q_rows >= 512 || width <= 4096); }
+hipError_t launch_product_few(const ProductArgs &a, int32_t y_dtype, hipStream_t stream);
+// the same for rows x, whose codes it forms (of a.p: the rows)
+hipError_t launch_linear_few(const ProductArgs &a, const void *x, int32_t x_dtype, int64_t ldx, int32_t y_dtype, hipStream_t stream);
 
 // ---- device arithmetic --------------------------------------------------------------
 

@@ -1,0 +1,200 @@
+// y = act(x W^T + b) of few rows, in one launch.
+//
+// A few rows are asked for one answer at a time: what counts is reading the
+// weights once, from as many CUs as there are, and the latency of what comes
+// before and after.  A block takes 16 outputs and all the rows; its eight waves
+// take blocks of the width in turn, straight from memory to registers, and join
+// their sums through LDS.  Codes of x are formed by every block anew (or read,
+// where the product is given them).  The products run on the bf16 matrix
+// instruction, to which codes times their scale are exact: there is time for it.
+#include <type_traits>
+
+#include "f8.hpp"
+
+namespace hpacml {
+namespace f8 {
+
+namespace {
+
+constexpr int kWaves = 8;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+struct FewArgs {
+    const void *x;           // rows, or NULL: p
+    int64_t ldx;
+    Matrix p, q;
+    int64_t rows;
+    const float *b;
+    void *y;
+    int64_t ldy;
+    int32_t relu, accumulate;
+};
+
+// 32 codes of a lane, as four operands of the matrix instruction
+struct Operand {
+    bf16x8 v[4];
+};
+__device__ __forceinline__ Operand to_bf16(const uint32_t (&codes)[8], uint32_t byte) {
+    const float s = __builtin_bit_cast(float, byte << 23);
+    Operand o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], s, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], s, true);
+        o.v[i / 2][i % 2 * 4] = lo[0];
+        o.v[i / 2][i % 2 * 4 + 1] = lo[1];
+        o.v[i / 2][i % 2 * 4 + 2] = hi[0];
+        o.v[i / 2][i % 2 * 4 + 3] = hi[1];
+    }
+    return o;
+}
+
+// Lane l holds row l % 16 and values 32 (l / 16).. of a block: codes
+struct Codes {
+    uint32_t c[8], byte;
+};
+__device__ __forceinline__ Codes read_codes(const Matrix &m, int64_t row, int group, int64_t kb, int64_t blocks) {
+    const int64_t r = min(row, m.rows - 1);
+    const char *at = m.codes + code_offset(r, kb * kBlock + group * 32, blocks);
+    Codes o;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const u32x4 w = *(const u32x4 *)(at + h * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            o.c[h * 4 + e] = w[e];
+    }
+    o.byte = (uint8_t)m.scales[scale_offset(r, kb, blocks)];
+    return o;
+}
+
+// (of the last row where there is none: what comes of it is not stored)
+template <typename X>
+__device__ __forceinline__ Codes form_codes(const X *x, int64_t ldx, int64_t rows, int64_t row, int64_t k, int64_t width) {
+    float v[2][16];
+    uint32_t most = 0;
+    row = min(row, rows - 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t left = width - k - h * 16;
+        load16(x + row * ldx + k + h * 16, left > 16 ? 16 : left < 0 ? 0 : (int)left, v[h]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            most = max(most, magnitude(v[h][e]));
+    }
+    most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+    Codes o;
+    o.byte = scale_byte(most);
+    const float f = scale_factor(o.byte);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float *u = &v[i / 4][i % 4 * 4];
+        o.c[i] = o.byte == 255u ? kNanCodes : codes4(u[0], u[1], u[2], u[3], f);
+    }
+    return o;
+}
+
+// X: the type of x, or void: codes are given.  NB: sixteens of rows.
+template <typename X, typename Y, int NB>
+__global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
+    __shared__ f32x4 of[kWaves][NB][64];
+    constexpr int kAtOnce = 4 / NB;       // blocks of the width whose loads go out together
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, group = lane >> 4;
+    const int64_t blocks = blocks_of(a.q.width), out0 = (int64_t)blockIdx.x * 16;
+    f32x4 acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int64_t first = wave; first < blocks; first += kWaves * kAtOnce) {
+        Codes w[kAtOnce], x[kAtOnce][NB];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t kb = min(first + u * kWaves, blocks - 1);
+            w[u] = read_codes(a.q, out0 + r, group, kb, blocks);
+            if (first + u * kWaves >= blocks)       // the last block again, times 0
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[u].c[i] = 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t kb = min(first + u * kWaves, blocks - 1);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                if constexpr (std::is_void<X>::value)
+                    x[u][b] = read_codes(a.p, b * 16 + r, group, kb, blocks);
+                else
+                    x[u][b] = form_codes((const X *)a.x, a.ldx, a.rows, b * 16 + r, kb * kBlock + group * 32, a.q.width);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const Operand wo = to_bf16(w[u].c, w[u].byte);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const Operand xo = to_bf16(x[u][b].c, x[u][b].byte);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wo.v[i], xo.v[i], acc[b], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        of[wave][b][lane] = acc[b];
+    __syncthreads();
+    for (int b = wave; b < NB; b += kWaves) {
+        f32x4 t = of[0][b][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w)
+            t += of[w][b][lane];
+        const int64_t row = b * 16 + r, out = out0 + group * 4;
+        if (row >= a.rows)
+            continue;
+        Y *to = (Y *)a.y + row * a.ldy + out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (out + e < a.q.rows) {
+                float v = t[e] + (a.b ? a.b[out + e] : 0.f);
+                if (a.relu)
+                    v = relu_keep_nan(v);
+                if constexpr (sizeof(Y) == 4)
+                    v += a.accumulate ? to[e] : 0.f;
+                store_value(to + e, v);
+            }
+    }
+}
+
+template <typename X, typename Y>
+void launch(const FewArgs &a, hipStream_t stream) {
+    const uint32_t grid = (uint32_t)((a.q.rows + 15) / 16);
+    if (a.rows <= 16)
+        few_kernel<X, Y, 1><<<grid, 64 * kWaves, 0, stream>>>(a);
+    else if (a.rows <= 32)
+        few_kernel<X, Y, 2><<<grid, 64 * kWaves, 0, stream>>>(a);
+    else
+        few_kernel<X, Y, 4><<<grid, 64 * kWaves, 0, stream>>>(a);
+}
+template <typename X>
+hipError_t launch_type(const FewArgs &a, int32_t y_dtype, hipStream_t stream) {
+    if (y_dtype == HPACML_F32)
+        launch<X, float>(a, stream);
+    else
+        launch<X, uint16_t>(a, stream);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_product_few(const ProductArgs &a, int32_t y_dtype, hipStream_t stream) {
+    return launch_type<void>({nullptr, 0, a.p, a.q, a.p.rows, a.b, a.y, a.ldy, a.relu, a.accumulate}, y_dtype, stream);
+}
+
+hipError_t launch_linear_few(const ProductArgs &a, const void *x, int32_t x_dtype, int64_t ldx, int32_t y_dtype, hipStream_t stream) {
+    const FewArgs f = {x, ldx, a.p, a.q, a.p.rows, a.b, a.y, a.ldy, a.relu, a.accumulate};
+    return x_dtype == HPACML_F32 ? launch_type<float>(f, y_dtype, stream) : launch_type<uint16_t>(f, y_dtype, stream);
+}
+
+}  // namespace f8
+}  // namespace hpacml

@@ -481,40 +481,60 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void product_kernel(Args<Y> g) {
     }
 }
 
-// Four sums of parts a thread.
-__global__ __launch_bounds__(256) void join_kernel(const float *part, int64_t parts, int64_t rows, int64_t width, int64_t pitch, float *out,
-                                                   int64_t ldo, int32_t accumulate) {
-    const int64_t four = (width + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x, r = at / four, c = at % four * 4;
-    if (r >= rows)
-        return;
-    const float *p = part + r * pitch + c;
-    f32x4 t = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t i = 0; i < parts; ++i)
-        t += *(const f32x4_any *)(p + i * rows * pitch);
-    float *to = out + r * ldo + c;
+// y = act(the sum of parts + b), four outputs of a row at a time; `lanes` threads
+// share an output's parts (235 parts of 50 x 201 outputs took 64 us with one).
+template <typename Y, int LANES>
+__global__ __launch_bounds__(256) void finish_kernel(const float *part, int64_t parts, int64_t rows, int64_t width, int64_t pitch, const float *b,
+                                                     int32_t relu, int32_t accumulate, Y *y, int64_t ldy) {
+    constexpr int kFours = 256 / LANES;
+    __shared__ f32x4 of[LANES > 1 ? LANES : 1][kFours];
+    const int64_t four = (width + 3) / 4, all = rows * four;
+    const int at = threadIdx.x % kFours, share = threadIdx.x / kFours;
+    for (int64_t first = (int64_t)blockIdx.x * kFours; first < all; first += (int64_t)gridDim.x * kFours) {
+        const int64_t i = first + at, r = i / four, c = i % four * 4;
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+        if (i < all) {
+            const float *p = part + r * pitch + c;
+#pragma unroll 4
+            for (int64_t k = share; k < parts; k += LANES)
+                t += *(const f32x4_any *)(p + k * rows * pitch);
+        }
+        if constexpr (LANES > 1) {
+            __syncthreads();
+            of[share][at] = t;
+            __syncthreads();
+            if (share > 0)
+                continue;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < width)
-            to[e] = accumulate ? to[e] + t[e] : t[e];
+            for (int k = 1; k < LANES; ++k)
+                t += of[k][at];
+        }
+        if (i >= all)
+            continue;
+        Y *to = y + r * ldy + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < width) {
+                float v = t[e] + (b ? b[c + e] : 0.f);
+                if (relu)
+                    v = relu_keep_nan(v);
+                if constexpr (sizeof(Y) == 4)
+                    v += accumulate ? to[e] : 0.f;
+                store_value(to + e, v);
+            }
+    }
 }
 
-// y = act(parts' sum + b) in its type
 template <typename Y>
-__global__ __launch_bounds__(256) void finish_kernel(const float *part, int64_t parts, int64_t rows, int64_t width, int64_t pitch, const float *b,
-                                                     int32_t relu, Y *y, int64_t ldy) {
-    const int64_t four = (width + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x, r = at / four, c = at % four * 4;
-    if (r >= rows)
-        return;
-    const float *p = part + r * pitch + c;
-    f32x4 t = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t i = 0; i < parts; ++i)
-        t += *(const f32x4_any *)(p + i * rows * pitch);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < width) {
-            const float v = t[e] + (b ? b[c + e] : 0.f);
-            store_value(y + r * ldy + c + e, relu ? relu_keep_nan(v) : v);
-        }
+hipError_t launch_finish(const float *part, int64_t parts, int64_t rows, int64_t width, int64_t pitch, const float *b, int32_t relu,
+                         int32_t accumulate, Y *y, int64_t ldy, hipStream_t stream) {
+    const int64_t four = rows * ((width + 3) / 4), lanes = parts > 8 ? 16 : 1, blocks = (four + 256 / lanes - 1) / (256 / lanes);
+    const uint32_t grid = (uint32_t)(blocks < 1 << 20 ? blocks : 1 << 20);
+    if (lanes > 1)
+        finish_kernel<Y, 16><<<grid, 256, 0, stream>>>(part, parts, rows, width, pitch, b, relu, accumulate, y, ldy);
+    else
+        finish_kernel<Y, 1><<<grid, 256, 0, stream>>>(part, parts, rows, width, pitch, b, relu, accumulate, y, ldy);
+    return hipGetLastError();
 }
 
 struct Plan {
@@ -558,26 +578,20 @@ hipError_t launch_tiles(const ProductArgs &a, const Plan &p, bool exact, Y *y, i
     return p.big ? launch_shape<Y, false, 2, 4, 4, 2>(g, stream) : launch_shape<Y, false, 2, 2, 2, 2>(g, stream);
 }
 
-uint32_t fours(int64_t rows, int64_t width) { return (uint32_t)((rows * ((width + 3) / 4) + 255) / 256); }
-
 }  // namespace
 
 int64_t product_partial_bytes(int64_t p_rows, int64_t q_rows, int64_t width) {
+    if (few_rows(p_rows, q_rows, width))
+        return 0;
     const Plan p = plan_of(p_rows, q_rows, width);
     return p.parts > 1 ? (int64_t)p.parts * p_rows * partial_pitch(q_rows) * 4 : 0;
-}
-
-hipError_t launch_join(const float *part, int64_t parts, int64_t rows, int64_t width, int64_t pitch, float *out, int64_t ldo,
-                       int32_t accumulate, hipStream_t stream) {
-    if (rows == 0 || width == 0)
-        return hipSuccess;
-    join_kernel<<<fours(rows, width), 256, 0, stream>>>(part, parts, rows, width, pitch, out, ldo, accumulate);
-    return hipGetLastError();
 }
 
 hipError_t launch_product(const ProductArgs &a, int32_t y_dtype, hipStream_t stream) {
     if (a.p.rows == 0 || a.q.rows == 0)
         return hipSuccess;
+    if (few_rows(a.p.rows, a.q.rows, a.p.width))
+        return launch_product_few(a, y_dtype, stream);
     const Plan p = plan_of(a.p.rows, a.q.rows, a.p.width);
     const int64_t pitch = partial_pitch(a.q.rows);
     const bool empty = a.p.width == 0;
@@ -589,13 +603,9 @@ hipError_t launch_product(const ProductArgs &a, int32_t y_dtype, hipStream_t str
             return e;
     }
     const int64_t parts = empty ? 0 : p.parts;
-    if (a.accumulate)
-        return launch_join(a.partial, parts, a.p.rows, a.q.rows, pitch, (float *)a.y, a.ldy, 1, stream);
     if (y_dtype == HPACML_F32)
-        finish_kernel<<<fours(a.p.rows, a.q.rows), 256, 0, stream>>>(a.partial, parts, a.p.rows, a.q.rows, pitch, a.b, a.relu, (float *)a.y, a.ldy);
-    else
-        finish_kernel<<<fours(a.p.rows, a.q.rows), 256, 0, stream>>>(a.partial, parts, a.p.rows, a.q.rows, pitch, a.b, a.relu, (uint16_t *)a.y, a.ldy);
-    return hipGetLastError();
+        return launch_finish(a.partial, parts, a.p.rows, a.q.rows, pitch, a.b, a.relu, a.accumulate, (float *)a.y, a.ldy, stream);
+    return launch_finish(a.partial, parts, a.p.rows, a.q.rows, pitch, a.b, a.relu, 0, (uint16_t *)a.y, a.ldy, stream);
 }
 
 }  // namespace f8

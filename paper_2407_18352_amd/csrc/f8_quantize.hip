@@ -181,26 +181,44 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a) {
     }
 }
 
-// A thread reads 16 codes of a row.
+// A thread reads 16 codes of a row; eight neighbours a block of 128.
 template <typename X>
 __global__ __launch_bounds__(256) void load_kernel(Matrix m, X *x, int64_t ldx) {
     const int64_t blocks = blocks_of(m.width), chunks = blocks * 8;
     const int64_t unit = blockIdx.x / ((chunks + 7) / 8), part = blockIdx.x % ((chunks + 7) / 8);   // 32 rows, eight chunks
-    const int64_t row = unit * 32 + (threadIdx.x & 31), k = (part * 8 + (threadIdx.x >> 5)) * 16;
+    const int64_t row = unit * 32 + (threadIdx.x >> 3), k = (part * 8 + (threadIdx.x & 7)) * 16;
     if (row >= m.rows || k >= m.width)
         return;
     const u32x4 c = *(const u32x4 *)(m.codes + code_offset(row, k, blocks));
     const uint32_t byte = (uint8_t)m.scales[scale_offset(row, k / kBlock, blocks)];
     const float s = byte == 255u ? __builtin_nanf("") : byte == 0u ? 0x1p-127f : __builtin_bit_cast(float, byte << 23);
-    X *to = x + row * ldx + k;
+    float v[16];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(c[e], 0) * s, __builtin_amdgcn_cvt_f32_fp8(c[e], 1) * s,
-                            __builtin_amdgcn_cvt_f32_fp8(c[e], 2) * s, __builtin_amdgcn_cvt_f32_fp8(c[e], 3) * s};
+        v[4 * e] = __builtin_amdgcn_cvt_f32_fp8(c[e], 0) * s;
+        v[4 * e + 1] = __builtin_amdgcn_cvt_f32_fp8(c[e], 1) * s;
+        v[4 * e + 2] = __builtin_amdgcn_cvt_f32_fp8(c[e], 2) * s;
+        v[4 * e + 3] = __builtin_amdgcn_cvt_f32_fp8(c[e], 3) * s;
+    }
+    X *to = x + row * ldx + k;
+    if (k + 16 <= m.width) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (k + 4 * e + i < m.width)
-                store_value(to + 4 * e + i, v[i]);
+        for (int e = 0; e < (int)sizeof(X); ++e) {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(X) == 4)
+                    w[i] = __builtin_bit_cast(uint32_t, v[4 * e + i]);
+                else
+                    w[i] = pack_bf16(v[8 * e + 2 * i], v[8 * e + 2 * i + 1]);
+            }
+            *(u32x4_any *)(to + e * (16 / sizeof(X))) = w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (k + i < m.width)
+                store_value(to + i, v[i]);
     }
 }
 

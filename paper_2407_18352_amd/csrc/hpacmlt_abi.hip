@@ -52,9 +52,11 @@ MatrixAt take_matrix(Layout *l, int64_t rows, int64_t width) {
 }
 
 struct LinearLayout : Layout {
-    MatrixAt x;
-    size_t partial;
+    MatrixAt x{};
+    size_t partial = 0;
     LinearLayout(int64_t rows, int64_t n_in, int64_t n_out) {
+        if (f8::few_rows(rows, n_out, n_in))
+            return;
         x = take_matrix(this, rows, n_in);
         partial = take(f8::product_partial_bytes(rows, n_out, n_in));
     }
@@ -303,16 +305,20 @@ hpacml_status hpacmlt_linear_run(const hpacmlt_matrix *W, const float *b, const 
     o.add(y, rows, W->rows, ldy, size_of(y_dtype), size_of(y_dtype), true);
     if (keep)
         add_matrix(&o, *keep, true);
-    o.add(scratch, 1, (int64_t)l.bytes, (int64_t)l.bytes, 1, 16, true);
+    o.add(scratch, l.bytes > 0, (int64_t)l.bytes, (int64_t)l.bytes, 1, 16, true);
     if (o.check() != HPACML_OK)
         return o.status;
-    const Matrix q = l.x.in((char *)scratch, rows, W->width);
-    hipError_t e = f8::launch_quantize({x, nullptr, ldx, 0, rows, W->width, q, keep ? matrix_of(*keep) : Matrix{}, nullptr, 0}, x_dtype,
-                                       (hipStream_t)stream);
-    if (e == hipSuccess)
-        e = f8::launch_product({q, matrix_of(*W), b, y, ldy, act == HPACML_ACT_RELU, 0, (float *)((char *)scratch + l.partial)}, y_dtype,
-                               (hipStream_t)stream);
-    return status_of(e);
+    hipStream_t st = (hipStream_t)stream;
+    const Matrix kept = keep ? matrix_of(*keep) : Matrix{};
+    f8::ProductArgs product = {{nullptr, nullptr, rows, W->width}, matrix_of(*W), b, y, ldy, act == HPACML_ACT_RELU, 0, nullptr};
+    if (f8::few_rows(rows, W->rows, W->width)) {
+        hipError_t e = keep ? f8::launch_quantize({x, nullptr, ldx, 0, rows, W->width, Matrix{}, kept, nullptr, 0}, x_dtype, st) : hipSuccess;
+        return status_of(e == hipSuccess ? f8::launch_linear_few(product, x, x_dtype, ldx, y_dtype, st) : e);
+    }
+    product.p = l.x.in((char *)scratch, rows, W->width);
+    product.partial = (float *)((char *)scratch + l.partial);
+    hipError_t e = f8::launch_quantize({x, nullptr, ldx, 0, rows, W->width, product.p, kept, nullptr, 0}, x_dtype, st);
+    return status_of(e == hipSuccess ? f8::launch_product(product, y_dtype, st) : e);
 }
 
 hpacml_status hpacmlt_backward_scratch(int64_t rows, int64_t n_in, int32_t n_out, int32_t want_dw, int32_t want_db, int32_t want_dx,
@@ -364,7 +370,7 @@ hpacml_status hpacmlt_backward(const hpacmlt_matrix *kept, const void *dy, const
     if (rows == 0) {
         hipError_t e = hipSuccess;
         if (!accumulate && dw)
-            e = f8::launch_join(nullptr, 0, n_out, n_in, 0, dw, lddw, 0, st);
+            e = f8::launch_product({{nullptr, nullptr, n_out, 0}, {nullptr, nullptr, n_in, 0}, nullptr, dw, lddw, 0, 0, nullptr}, HPACML_F32, st);
         if (!accumulate && db && e == hipSuccess)
             e = launch_column_sums(nullptr, 0, n_out, 0, db, 0, nullptr, st);
         return status_of(e);
