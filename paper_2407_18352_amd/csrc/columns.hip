@@ -17,22 +17,28 @@ int64_t runs_of(int64_t rows) {
     return runs < 2 ? 1 : runs > kMostRuns ? kMostRuns : runs;
 }
 
-__global__ __launch_bounds__(256) void sums_kernel(const float *part, int64_t rows, int64_t width, int64_t pitch, int64_t run, float *out,
-                                                   int64_t ldo, int32_t accumulate) {
+// a.room: where the sums of the runs go, NULL: the run is all there is
+__global__ __launch_bounds__(256) void sums_kernel(ColumnSums a, int64_t run) {
     __shared__ double of[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane, first = (int64_t)blockIdx.y * run, last = min(first + run, rows);
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane, first = (int64_t)blockIdx.y * run, last = min(first + run, a.rows);
     double t = 0;
-    if (c < width)
+    if (c < a.width)
 #pragma unroll 8
         for (int64_t r = first + wave; r < last; r += 4)
-            t += part[r * pitch + c];
+            t += a.part[r * a.pitch + c];
     of[wave][lane] = t;
     __syncthreads();
-    if (wave == 0 && c < width) {
+    if (wave == 0 && c < a.width) {
         const float s = (float)((of[0][lane] + of[1][lane]) + (of[2][lane] + of[3][lane]));
-        float *to = out + blockIdx.y * ldo + c;
-        *to = accumulate ? *to + s : s;
+        if (a.room) {
+            a.room[blockIdx.y * a.width + c] = s;
+            return;
+        }
+        float *to = c < a.split ? a.out : a.more;
+        const int64_t at = c < a.split ? c : c - a.split;
+        if (to)
+            to[at] = a.accumulate ? to[at] + s : s;
     }
 }
 
@@ -40,18 +46,21 @@ __global__ __launch_bounds__(256) void sums_kernel(const float *part, int64_t ro
 
 int64_t column_sums_room(int64_t rows, int64_t width) { return runs_of(rows) > 1 ? runs_of(rows) * width : 0; }
 
-hipError_t launch_column_sums(const float *part, int64_t rows, int64_t width, int64_t pitch, float *out, int32_t accumulate, float *room,
-                              hipStream_t stream) {
-    if (width == 0)
+hipError_t launch_column_sums(const ColumnSums &a, hipStream_t stream) {
+    if (a.width == 0)
         return hipSuccess;
-    const int64_t runs = runs_of(rows);
-    const uint32_t across = (uint32_t)((width + 63) / 64);
+    const int64_t runs = runs_of(a.rows);
+    const uint32_t across = (uint32_t)((a.width + 63) / 64);
+    ColumnSums last = a;
     if (runs > 1) {
-        const int64_t run = (rows + runs - 1) / runs;
-        sums_kernel<<<dim3(across, (uint32_t)runs), 256, 0, stream>>>(part, rows, width, pitch, run, room, width, 0);
-        sums_kernel<<<across, 256, 0, stream>>>(room, runs, width, width, runs, out, 0, accumulate);
-    } else
-        sums_kernel<<<across, 256, 0, stream>>>(part, rows, width, pitch, rows, out, 0, accumulate);
+        const int64_t run = (a.rows + runs - 1) / runs;
+        sums_kernel<<<dim3(across, (uint32_t)runs), 256, 0, stream>>>(a, run);
+        last.part = a.room;
+        last.rows = runs;
+        last.pitch = a.width;
+    }
+    last.room = nullptr;
+    sums_kernel<<<across, 256, 0, stream>>>(last, last.rows);
     return hipGetLastError();
 }
 

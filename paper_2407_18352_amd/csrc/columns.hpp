@@ -6,10 +6,19 @@
 
 namespace hpacml {
 
-// out[c] (+)= sum over `rows` rows of part[r * pitch + c].  Many rows are joined
-// in two launches, through `room`: column_sums_room floats.
+// Of `rows` rows of `width` columns, `pitch` floats apart, the sums of the first
+// `split` columns (+)= to `out`, those of the others to `more` (either may be
+// NULL: not wanted).  Many rows are joined in two launches, through `room`:
+// column_sums_room floats.
+struct ColumnSums {
+    const float *part;
+    int64_t rows, width, pitch;
+    float *out, *more;
+    int64_t split;
+    int32_t accumulate;
+    float *room;
+};
 int64_t column_sums_room(int64_t rows, int64_t width);
-hipError_t launch_column_sums(const float *part, int64_t rows, int64_t width, int64_t pitch, float *out, int32_t accumulate, float *room,
-                              hipStream_t stream);
+hipError_t launch_column_sums(const ColumnSums &a, hipStream_t stream);
 
 }  // namespace hpacml

@@ -1,8 +1,9 @@
 // Group norm with an activation, channels last, and its backward pass.
 //
-// Two forms.  Where an image is one point (a hidden layer's activations), a few
+// Three forms.  Where an image is one point (a hidden layer's activations), a few
 // lanes of a wave hold a group of it in registers: one reading, one launch
-// (rows_*).  Otherwise three launches (parts_*): sums of every channel over runs
+// (rows_*).  Where a group of an image fits the registers of a block, the same
+// with a block (held_*).  Otherwise three launches (parts_*): sums of every channel over runs
 // of an image's points, which a second launch joins to the groups' statistics,
 // and the results, from a second reading (of what the first left in the
 // Infinity Cache, up to 256 MB).  A thread has the same few neighbouring
@@ -12,6 +13,8 @@
 // Statistics: the mean of a few values in registers, the squares about it, and
 // pairs of (mean, squares) joined as such, so that no difference of large sums
 // occurs; joins of many in 64 bits.
+#include <type_traits>
+
 #include "columns.hpp"
 #include "dense8.hpp"
 #include "group_norm.hpp"
@@ -21,7 +24,12 @@ namespace hpacml {
 
 namespace {
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+// By the exponential's and the reciprocal's own instructions: z log2(e) is
+// rounded to 2^-24 of itself, which moves the result by |z| 2^-24 (1 - result) of
+// it, less than the roundings around it, and the square of a SiLU's slope takes
+// five instructions a value where expf and a division take thirty: the backward
+// pass of 134 million values is bound by memory so, not by its arithmetic.
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896f)); }
 
 __device__ __forceinline__ float activation(float z, int32_t act) {
     if (act == HPACML_ACT_RELU)
@@ -62,6 +70,20 @@ struct Values {
             } else
                 v[e] = __builtin_bit_cast(float, e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
         }
+    }
+    // as they lie in memory
+    typedef typename std::conditional<V == 1, T, Word>::type Held;
+    static __device__ __forceinline__ Held hold(const T *p) {
+        if constexpr (V == 1)
+            return *p;
+        else
+            return *(const Any *)p;
+    }
+    static __device__ __forceinline__ void values(Held w, float (&v)[V]) {
+        if constexpr (V == 1)
+            v[0] = load_value(&w);
+        else
+            unpack(w, v);
     }
     static __device__ __forceinline__ void store(T *p, const float (&v)[V]) {
         if constexpr (V == 1)
@@ -200,19 +222,28 @@ __global__ __launch_bounds__(256) void parts_moments_kernel(GroupNorm a, Parts p
     }
 }
 
-__device__ __forceinline__ double join_wave(double t) {
+__device__ __forceinline__ double join_block(double t, double (&of_wave)[4]) {
 #pragma unroll
     for (int s = 1; s < 64; s *= 2)
         t += __shfl_xor(t, s);
-    return t;
-}
-__device__ __forceinline__ double join_block(double t, double (&of_wave)[4]) {
-    t = join_wave(t);
     __syncthreads();
     if ((threadIdx.x & 63) == 0)
         of_wave[threadIdx.x >> 6] = t;
     __syncthreads();
     return (of_wave[0] + of_wave[1]) + (of_wave[2] + of_wave[3]);
+}
+
+// The partial results of an image's group, `per` channels of each run: a thread
+// takes every so many runs of one channel (with one index over all of them, and
+// its divisions, 2049 runs of 4 channels took 23 us).
+template <typename F>
+__device__ __forceinline__ void over_runs(int per, uint32_t runs, F f) {
+    const int across = min(per, 256), high = 256 / across, c0 = threadIdx.x % across, r0 = threadIdx.x / across;
+    if (r0 < high)
+        for (int c = c0; c < per; c += across)
+#pragma unroll 4
+            for (uint32_t r = r0; r < runs; r += high)
+                f(c, r);
 }
 
 // A block per image and group: mean and rstd.
@@ -222,17 +253,15 @@ __global__ __launch_bounds__(256) void parts_join_kernel(GroupNorm a, Parts p, c
         const int64_t image = unit / a.groups;
         const int per = a.channels / a.groups, c0 = (int)(unit % a.groups) * per;
         const float2 *at = part + image * p.runs * a.channels + c0;
-        const int64_t entries = (int64_t)p.runs * per;
-        auto values = [&](int64_t i) { return (double)min(p.run, a.points - i / per * p.run); };
+        auto values = [&](uint32_t r) { return (double)min(p.run, a.points - r * p.run); };
         double t = 0;
-        for (int64_t i = threadIdx.x; i < entries; i += 256)
-            t += values(i) * at[i / per * a.channels + i % per].x;
+        over_runs(per, p.runs, [&](int c, uint32_t r) { t += values(r) * at[(int64_t)r * a.channels + c].x; });
         const double n = (double)a.points * per, mean = join_block(t, of_wave) / n;
         t = 0;
-        for (int64_t i = threadIdx.x; i < entries; i += 256) {
-            const float2 o = at[i / per * a.channels + i % per];
-            t += (double)o.y + values(i) * (o.x - mean) * (o.x - mean);
-        }
+        over_runs(per, p.runs, [&](int c, uint32_t r) {
+            const float2 o = at[(int64_t)r * a.channels + c];
+            t += (double)o.y + values(r) * (o.x - mean) * (o.x - mean);
+        });
         t = join_block(t, of_wave);
         if (threadIdx.x == 0) {
             mean_to[unit] = (float)mean;
@@ -344,13 +373,12 @@ __global__ __launch_bounds__(256) void parts_means_kernel(GroupNorm a, Parts p, 
         const int per = a.channels / a.groups, c0 = (int)(unit % a.groups) * per;
         const float *at = part + image * p.runs * 2 * a.channels + c0;
         double t = 0, u = 0;
-        for (int64_t i = threadIdx.x; i < (int64_t)p.runs * per; i += 256) {
-            const int c = (int)(i % per);
-            const float *o = at + i / per * 2 * a.channels + c;
+        over_runs(per, p.runs, [&](int c, uint32_t r) {
+            const float *o = at + (int64_t)r * 2 * a.channels + c;
             const double gamma = a.gamma ? a.gamma[c0 + c] : 1.f;
             t += gamma * o[0];
             u += gamma * o[a.channels];
-        }
+        });
         const double n = (double)a.points * per;
         t = join_block(t, of_wave) / n;
         u = join_block(u, of_wave) / n;
@@ -389,6 +417,13 @@ __global__ __launch_bounds__(256) void parts_dx_kernel(GroupNorm a, Parts p, con
             Values<T, V>::store((T *)a.y + row * a.ldy + q.c, v);
         }
     }
+}
+
+// dbeta and dgamma from rows of partial sums, [2][channels] each
+hipError_t launch_parameters(const GroupNorm &a, const float *part, int64_t rows, float *room, hipStream_t stream) {
+    if (!a.dgamma && !a.dbeta)
+        return hipSuccess;
+    return launch_column_sums({part, rows, 2 * a.channels, 2 * a.channels, a.dbeta, a.dgamma, a.channels, a.accumulate, room}, stream);
 }
 
 // ---- images of one point ------------------------------------------------------------
@@ -450,34 +485,45 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_forward_kernel(GroupNorm 
     const int column_block = blockIdx.x % p.column_blocks, wave = threadIdx.x >> 6;
     const RowLane<T, V, I> k(a, p, column_block);
     const float share = 1.f / (float)(a.channels / a.groups);
-    for (int64_t row = (int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave; row < a.images; row += (int64_t)p.strides * kRowWaves) {
-        float v[I][V], t = 0, s = 0;
-        k.load((const T *)a.x + row * a.ldx, v);
+    constexpr int kAtOnce = V * I <= 8 ? 4 : V * I <= 16 ? 2 : 1;     // rows whose loads go out together
+    const int64_t step = (int64_t)p.strides * kRowWaves;
+    for (int64_t first = (int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave; first < a.images; first += step * kAtOnce) {
+        float v[kAtOnce][I][V];
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int u = 0; u < kAtOnce; ++u)
+            k.load((const T *)a.x + min(first + u * step, a.images - 1) * a.ldx, v[u]);
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                t += v[i][e];
-        const float mean = join_lanes<64>(t, p.lanes) * share;
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t row = first + u * step;
+            float t = 0, s = 0;
 #pragma unroll
-        for (int i = 0; i < I; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                v[i][e] -= mean;
-                s = k.here[i] ? __builtin_fmaf(v[i][e], v[i][e], s) : s;
-            }
-        const float rstd = 1.f / sqrtf(join_lanes<64>(s, p.lanes) * share + a.eps);
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-            if (k.here[i]) {
+            for (int i = 0; i < I; ++i)
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    v[i][e] = activation(__builtin_fmaf(v[i][e], rstd * k.gamma[i][e], k.beta[i][e]), a.act);
-                Values<T, V>::store((T *)a.y + row * a.ldy + k.c[i], v[i]);
+                    t += v[u][i][e];
+            const float mean = join_lanes<64>(t, p.lanes) * share;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    v[u][i][e] -= mean;
+                    s = k.here[i] ? __builtin_fmaf(v[u][i][e], v[u][i][e], s) : s;
+                }
+            const float rstd = 1.f / sqrtf(join_lanes<64>(s, p.lanes) * share + a.eps);
+            if (row >= a.images)
+                continue;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                if (k.here[i]) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        v[u][i][e] = activation(__builtin_fmaf(v[u][i][e], rstd * k.gamma[i][e], k.beta[i][e]), a.act);
+                    Values<T, V>::store((T *)a.y + row * a.ldy + k.c[i], v[u][i]);
+                }
+            if (a.mean && k.lane == 0 && k.here[0]) {
+                a.mean[row * a.groups + k.group] = mean;
+                a.rstd[row * a.groups + k.group] = rstd;
             }
-        if (a.mean && k.lane == 0 && k.here[0]) {
-            a.mean[row * a.groups + k.group] = mean;
-            a.rstd[row * a.groups + k.group] = rstd;
         }
     }
 }
@@ -588,11 +634,7 @@ hipError_t launch_rows(const GroupNorm &a, const RowsPlan &o, bool backward, hip
     float *part = (float *)a.scratch, *room = part + (int64_t)o.p.strides * 2 * a.channels;
     rows_backward_kernel<T, V, I><<<o.grid, 64 * kRowWaves, 0, stream>>>(a, o.p, part);
     hipError_t e = hipGetLastError();
-    if (a.dbeta && e == hipSuccess)
-        e = launch_column_sums(part, o.p.strides, a.channels, 2 * a.channels, a.dbeta, a.accumulate, room, stream);
-    if (a.dgamma && e == hipSuccess)
-        e = launch_column_sums(part + a.channels, o.p.strides, a.channels, 2 * a.channels, a.dgamma, a.accumulate, room, stream);
-    return e;
+    return e == hipSuccess ? launch_parameters(a, part, o.p.strides, room, stream) : e;
 }
 template <typename T, int V>
 hipError_t launch_rows(const GroupNorm &a, const RowsPlan &o, bool backward, hipStream_t stream) {
@@ -610,6 +652,285 @@ hipError_t launch_rows(const GroupNorm &a, const RowsPlan &o, int32_t dtype, boo
         return o.v == 4 ? launch_rows<float, 4>(a, o, backward, stream) : launch_rows<float, 1>(a, o, backward, stream);
     return o.v == 8 ? launch_rows<uint16_t, 8>(a, o, backward, stream)
            : o.v == 4 ? launch_rows<uint16_t, 4>(a, o, backward, stream) : launch_rows<uint16_t, 1>(a, o, backward, stream);
+}
+
+// ---- images whose groups fit a block's registers -----------------------------------------
+
+// A block holds a run of neighbouring groups of one image: `across` vectors of
+// each point, `high` points at a time, up to I of them a thread.  It goes from
+// image to image with the same channels.
+struct Held {
+    int32_t groups, across, high;      // of a run; vectors of a run; points at a time
+    int32_t runs, strides;             // of a row; blocks of the same run
+};
+
+// Sums of `t` over the threads of each of the run's groups.  Thread t has
+// vector t % across of the run; a group is `each` vectors.  of: a pair per
+// thread, then one per group.  Groups' sums are taken by 32 threads each.
+__device__ __forceinline__ float2 join_groups(float2 t, const Held &h, int each, int group, bool here, float2 *of, float2 *of_group) {
+    __syncthreads();
+    of[threadIdx.x] = t;
+    __syncthreads();
+    const int entries = h.high * each;
+    for (int g = threadIdx.x >> 5; g < h.groups; g += blockDim.x >> 5) {
+        float2 s = {0.f, 0.f};
+        for (int i = threadIdx.x & 31; i < entries; i += 32) {
+            const float2 o = of[i / each * h.across + g * each + i % each];
+            s.x += o.x;
+            s.y += o.y;
+        }
+#pragma unroll
+        for (int x = 1; x < 32; x *= 2) {
+            s.x += __shfl_xor(s.x, x);
+            s.y += __shfl_xor(s.y, x);
+        }
+        if ((threadIdx.x & 31) == 0)
+            of_group[g] = s;
+    }
+    __syncthreads();
+    return here ? of_group[group] : float2{0.f, 0.f};
+}
+
+// Neighbouring runs of one image go to the same XCD at the same time: they share
+// cache lines.
+struct HeldPlace {
+    int run, stride;
+    __device__ __forceinline__ HeldPlace(const Held &h) {
+        const uint32_t per = gridDim.x >> 3, more = gridDim.x & 7, xcd = blockIdx.x & 7;
+        const uint32_t at = xcd * per + min(xcd, more) + (blockIdx.x >> 3);
+        run = at % h.runs;
+        stride = at / h.runs;
+    }
+};
+
+constexpr int kHeldThreads = 512;
+
+template <typename T, int V, int I>
+__global__ __launch_bounds__(kHeldThreads) void held_forward_kernel(GroupNorm a, Held h) {
+    extern __shared__ float2 of[];
+    float2 *of_group = of + blockDim.x;
+    const HeldPlace at(h);
+    const int per = a.channels / a.groups, each = per / V, v = threadIdx.x % h.across, r = threadIdx.x / h.across;
+    const int group = v / each, c = at.run * h.groups * per + v * V;
+    const bool here = r < h.high;
+    const float share = 1.f / ((float)a.points * per);
+    float gamma[V], beta[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
+        beta[e] = a.beta ? a.beta[c + e] : 0.f;
+    }
+    for (int64_t image = at.stride; image < a.images; image += h.strides) {
+        const T *x = (const T *)a.x + image * a.points * a.ldx + c;
+        float w[I][V], t = 0, s = 0;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points)
+                Values<T, V>::load(x + point * a.ldx, w[i]);
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    w[i][e] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                t += w[i][e];
+        const float mean = join_groups({t, 0.f}, h, each, group, here, of, of_group).x * share;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (here && r + (int64_t)i * h.high < a.points)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    w[i][e] -= mean;
+                    s = __builtin_fmaf(w[i][e], w[i][e], s);
+                }
+        const float rstd = 1.f / sqrtf(join_groups({s, 0.f}, h, each, group, here, of, of_group).x * share + a.eps);
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points) {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    w[i][e] = activation(__builtin_fmaf(w[i][e], rstd * gamma[e], beta[e]), a.act);
+                Values<T, V>::store((T *)a.y + (image * a.points + point) * a.ldy + c, w[i]);
+            }
+        }
+        if (a.mean && here && r == 0 && v % each == 0) {
+            a.mean[image * a.groups + at.run * h.groups + group] = mean;
+            a.rstd[image * a.groups + at.run * h.groups + group] = rstd;
+        }
+    }
+}
+
+// part: [stride][2][channel]
+template <typename T, int V, int I>
+__global__ __launch_bounds__(kHeldThreads) void held_backward_kernel(GroupNorm a, Held h, float *part) {
+    extern __shared__ float2 of[];
+    float2 *of_group = of + blockDim.x;
+    const HeldPlace at(h);
+    const int per = a.channels / a.groups, each = per / V, v = threadIdx.x % h.across, r = threadIdx.x / h.across;
+    const int group = v / each, c = at.run * h.groups * per + v * V;
+    const bool here = r < h.high;
+    const float share = 1.f / ((float)a.points * per);
+    float gamma[V], beta[V], s1[V], s2[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
+        beta[e] = a.beta ? a.beta[c + e] : 0.f;
+        s1[e] = s2[e] = 0;
+    }
+    for (int64_t image = at.stride; image < a.images; image += h.strides) {
+        const int64_t row0 = image * a.points, unit = image * a.groups + at.run * h.groups + group;
+        const float mean = a.mean[unit], rstd = a.rstd[unit];
+        // x's and dy's words stay as they are between the two uses
+        typename Values<T, V>::Held x[I], dy[I];
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points) {
+                x[i] = Values<T, V>::hold((const T *)a.x + (row0 + point) * a.ldx + c);
+                dy[i] = Values<T, V>::hold((const T *)a.dy + (row0 + point) * a.lddy + c);
+            }
+        }
+        auto value = [&](int i, int e, const float (&xs)[V], const float (&gs)[V], float &g, float &d) {
+            d = xs[e] - mean;
+            g = activation_gradient(gs[e], __builtin_fmaf(d, rstd * gamma[e], beta[e]), a.act);
+        };
+        float t = 0, u = 0;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (here && r + (int64_t)i * h.high < a.points) {
+                float xs[V], gs[V];
+                Values<T, V>::values(x[i], xs);
+                Values<T, V>::values(dy[i], gs);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float g, d;
+                    value(i, e, xs, gs, g, d);
+                    d *= rstd;
+                    s1[e] += g;
+                    s2[e] = __builtin_fmaf(g, d, s2[e]);
+                    g *= gamma[e];
+                    t += g;
+                    u = __builtin_fmaf(g, d, u);
+                }
+            }
+        if (!a.y)
+            continue;
+        const float2 m = join_groups({t, u}, h, each, group, here, of, of_group);
+        const float m1 = m.x * share, m2 = m.y * share;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points) {
+                float xs[V], gs[V];
+                Values<T, V>::values(x[i], xs);
+                Values<T, V>::values(dy[i], gs);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float g, d;
+                    value(i, e, xs, gs, g, d);
+                    xs[e] = rstd * ((g * gamma[e] - m1) - d * rstd * m2);
+                }
+                Values<T, V>::store((T *)a.y + (row0 + point) * a.ldy + c, xs);
+            }
+        }
+    }
+    if (!a.dgamma && !a.dbeta)
+        return;
+    float *to = part + (int64_t)at.stride * 2 * a.channels;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        float2 t = {s1[e], s2[e]};
+        __syncthreads();
+        of[threadIdx.x] = t;
+        for (int n = h.high, half; n > 1; n = half) {
+            half = (n + 1) / 2;
+            __syncthreads();
+            if (r < n - half) {
+                const float2 o = of[threadIdx.x + half * h.across];
+                t.x += o.x;
+                t.y += o.y;
+                of[threadIdx.x] = t;
+            }
+        }
+        if (r == 0) {
+            to[c + e] = t.x;
+            to[a.channels + c + e] = t.y;
+        }
+    }
+}
+
+struct HeldPlan {
+    Held h;
+    int v, each;             // channels of a vector; points of a thread
+    int threads;
+    uint32_t grid;
+};
+// Whether a group of an image fits: neighbouring groups until a point's part is
+// kLine bytes, at most eight points a thread.
+bool held_plan(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, HeldPlan *o) {
+    constexpr int kLine = 64;
+    const int per = channels / groups, size = dtype == HPACML_BF16 ? 2 : 4;
+    o->v = size == 2 && per % 8 == 0 ? 8 : per % 4 == 0 ? 4 : 1;
+    const int64_t most = (int64_t)kHeldThreads * 8;
+    if (points > most || points * (per / o->v) > most)
+        return false;
+    int run = 1;
+    for (int k = 1; k <= groups && points * k * (per / o->v) <= most && k * (per / o->v) <= kHeldThreads; ++k)
+        if (groups % k == 0) {
+            run = k;
+            if (k * per * size >= kLine)
+                break;
+        }
+    o->h.groups = run;
+    o->h.across = run * (per / o->v);
+    if (o->h.across > kHeldThreads)
+        return false;
+    // the fewest threads of 256, 512 with at most eight points each
+    for (o->threads = 256; o->threads <= kHeldThreads; o->threads *= 2) {
+        o->h.high = o->threads / o->h.across;
+        if (o->h.high > 0 && (points + o->h.high - 1) / o->h.high <= 8)
+            break;
+    }
+    if (o->threads > kHeldThreads)
+        return false;
+    if (o->h.high > points)
+        o->h.high = (int32_t)points;
+    const int64_t each = (points + o->h.high - 1) / o->h.high;
+    o->each = each <= 2 ? 2 : each <= 4 ? 4 : 8;
+    o->h.runs = groups / run;
+    const int64_t want = 256 * 2048 / o->threads / o->h.runs + 1;
+    o->h.strides = (int32_t)(images < want ? images : want);
+    o->grid = (uint32_t)(o->h.strides * o->h.runs);
+    return true;
+}
+
+template <typename T, int V, int I>
+hipError_t launch_held(const GroupNorm &a, const HeldPlan &o, bool backward, hipStream_t stream) {
+    const size_t lds = (size_t)(o.threads + o.h.groups) * sizeof(float2);
+    if (!backward) {
+        held_forward_kernel<T, V, I><<<o.grid, o.threads, lds, stream>>>(a, o.h);
+        return hipGetLastError();
+    }
+    float *part = (float *)a.scratch, *room = part + (int64_t)o.h.strides * 2 * a.channels;
+    held_backward_kernel<T, V, I><<<o.grid, o.threads, lds, stream>>>(a, o.h, part);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? launch_parameters(a, part, o.h.strides, room, stream) : e;
+}
+template <typename T, int V>
+hipError_t launch_held(const GroupNorm &a, const HeldPlan &o, bool backward, hipStream_t stream) {
+    return o.each == 2 ? launch_held<T, V, 2>(a, o, backward, stream)
+           : o.each == 4 ? launch_held<T, V, 4>(a, o, backward, stream) : launch_held<T, V, 8>(a, o, backward, stream);
+}
+hipError_t launch_held(const GroupNorm &a, const HeldPlan &o, int32_t dtype, bool backward, hipStream_t stream) {
+    if (dtype == HPACML_F32)
+        return o.v == 4 ? launch_held<float, 4>(a, o, backward, stream) : launch_held<float, 1>(a, o, backward, stream);
+    return o.v == 8 ? launch_held<uint16_t, 8>(a, o, backward, stream)
+           : o.v == 4 ? launch_held<uint16_t, 4>(a, o, backward, stream) : launch_held<uint16_t, 1>(a, o, backward, stream);
 }
 
 // Vectors that all of a row's channels fill: 16 bytes, or one value.
@@ -663,10 +984,8 @@ hipError_t backward_parts(const GroupNorm &a, const Parts &p, hipStream_t stream
     float *room = (float *)((char *)means + rounded((size_t)a.images * a.groups * 8));
     parts_sums_kernel<T, V><<<blocks, 256, 0, stream>>>(a, p, part);
     hipError_t e = hipGetLastError();
-    if (a.dbeta && e == hipSuccess)
-        e = launch_column_sums(part, rows, a.channels, 2 * a.channels, a.dbeta, a.accumulate, room, stream);
-    if (a.dgamma && e == hipSuccess)
-        e = launch_column_sums(part + a.channels, rows, a.channels, 2 * a.channels, a.dgamma, a.accumulate, room, stream);
+    if (e == hipSuccess)
+        e = launch_parameters(a, part, rows, room, stream);
     if (a.y && e == hipSuccess) {
         parts_means_kernel<<<grid_of(a.images * a.groups), 256, 0, stream>>>(a, p, part, means);
         parts_dx_kernel<T, V><<<blocks, 256, 0, stream>>>(a, p, means);
@@ -682,11 +1001,14 @@ int64_t group_norm_scratch(int32_t dtype, int64_t images, int64_t points, int32_
     if (images == 0)
         return 0;
     if (rows_plan(dtype, images, points, channels, groups, &o))
-        return backward ? (o.p.strides * 2 * channels + column_sums_room(o.p.strides, channels)) * 4 : 0;
+        return backward ? (o.p.strides * 2 * channels + column_sums_room(o.p.strides, 2 * channels)) * 4 : 0;
+    HeldPlan d;
+    if (held_plan(dtype, images, points, channels, groups, &d))
+        return backward ? (d.h.strides * 2 * channels + column_sums_room(d.h.strides, 2 * channels)) * 4 : 0;
     const Parts p = parts_of(dtype, images, points, channels);
     const int64_t rows = images * p.runs;
     return (int64_t)(rounded((size_t)rows * channels * 8) + rounded((size_t)images * groups * 8) +
-                     (backward ? rounded((size_t)column_sums_room(rows, channels) * 4) : 0));
+                     (backward ? rounded((size_t)column_sums_room(rows, 2 * channels) * 4) : 0));
 }
 
 hipError_t launch_group_norm(const GroupNorm &a, int32_t dtype, hipStream_t stream) {
@@ -695,6 +1017,9 @@ hipError_t launch_group_norm(const GroupNorm &a, int32_t dtype, hipStream_t stre
         return hipSuccess;
     if (rows_plan(dtype, a.images, a.points, a.channels, a.groups, &o))
         return launch_rows(a, o, dtype, false, stream);
+    HeldPlan d;
+    if (held_plan(dtype, a.images, a.points, a.channels, a.groups, &d))
+        return launch_held(a, d, dtype, false, stream);
     const Parts p = parts_of(dtype, a.images, a.points, a.channels);
     const int v = whole_vector(dtype, a.channels);
     if (dtype == HPACML_F32)
@@ -704,16 +1029,14 @@ hipError_t launch_group_norm(const GroupNorm &a, int32_t dtype, hipStream_t stre
 
 hipError_t launch_group_norm_backward(const GroupNorm &a, int32_t dtype, hipStream_t stream) {
     if (a.images == 0) {
-        hipError_t e = hipSuccess;
-        if (a.dbeta && !a.accumulate)
-            e = launch_column_sums(nullptr, 0, a.channels, 0, a.dbeta, 0, nullptr, stream);
-        if (a.dgamma && !a.accumulate && e == hipSuccess)
-            e = launch_column_sums(nullptr, 0, a.channels, 0, a.dgamma, 0, nullptr, stream);
-        return e;
+        return a.accumulate ? hipSuccess : launch_parameters(a, nullptr, 0, nullptr, stream);
     }
     RowsPlan o;
     if (rows_plan(dtype, a.images, a.points, a.channels, a.groups, &o))
         return launch_rows(a, o, dtype, true, stream);
+    HeldPlan d;
+    if (held_plan(dtype, a.images, a.points, a.channels, a.groups, &d))
+        return launch_held(a, d, dtype, true, stream);
     const Parts p = parts_of(dtype, a.images, a.points, a.channels);
     const int v = whole_vector(dtype, a.channels);
     if (dtype == HPACML_F32)

@@ -372,7 +372,7 @@ hpacml_status hpacmlt_backward(const hpacmlt_matrix *kept, const void *dy, const
         if (!accumulate && dw)
             e = f8::launch_product({{nullptr, nullptr, n_out, 0}, {nullptr, nullptr, n_in, 0}, nullptr, dw, lddw, 0, 0, nullptr}, HPACML_F32, st);
         if (!accumulate && db && e == hipSuccess)
-            e = launch_column_sums(nullptr, 0, n_out, 0, db, 0, nullptr, st);
+            e = launch_column_sums({nullptr, 0, n_out, 0, db, nullptr, n_out, 0, nullptr}, st);
         return status_of(e);
     }
     char *at = (char *)scratch;
@@ -380,7 +380,7 @@ hpacml_status hpacmlt_backward(const hpacmlt_matrix *kept, const void *dy, const
     float *sums = db ? (float *)(at + l.sums) : nullptr, *partial = (float *)(at + l.partial);
     hipError_t e = f8::launch_quantize({dy, y, lddy, ldy, rows, n_out, by_row, by_column, sums, 0}, dtype, st);
     if (e == hipSuccess && db)
-        e = launch_column_sums(sums, f8::blocks_of(rows), n_out, n_out, db, accumulate != 0, (float *)(at + l.room), st);
+        e = launch_column_sums({sums, f8::blocks_of(rows), n_out, n_out, db, nullptr, n_out, accumulate != 0, (float *)(at + l.room)}, st);
     if (e == hipSuccess && dx)
         e = f8::launch_product({by_row, matrix_of(*Wt), nullptr, dx, lddx, 0, 0, partial}, dtype, st);
     if (e == hipSuccess && dw)
