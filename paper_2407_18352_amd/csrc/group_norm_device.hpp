@@ -1,0 +1,141 @@
+// What the forms of group norm share: values and activations, sums of lanes, the
+// parameters' gradients; their plans and launchers.
+#pragma once
+
+#include <type_traits>
+
+#include "columns.hpp"
+#include "dense8.hpp"
+#include "group_norm.hpp"
+#include "hpacmlt.h"
+
+namespace hpacml {
+
+// By the exponential's and the reciprocal's own instructions: z log2(e) is
+// rounded to 2^-24 of itself, which moves the result by |z| 2^-24 (1 - result) of
+// it, less than the roundings around it, and the square of a SiLU's slope takes
+// five instructions a value where expf and a division take thirty: the backward
+// pass of 134 million values is bound by memory so, not by its arithmetic.
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896f)); }
+
+// A kernel has one activation: asked at every value, it kept the compiler from
+// putting a value's instructions between another's (norm_hidden 51 us).
+template <int ACT>
+__device__ __forceinline__ float activation(float z) {
+    if (ACT == HPACML_ACT_RELU)
+        return relu_keep_nan(z);
+    return ACT == HPACMLT_ACT_SILU ? z * sigmoid(z) : z;
+}
+// g = dy act'(z)
+template <int ACT>
+__device__ __forceinline__ float activation_gradient(float dy, float z) {
+    if (ACT == HPACML_ACT_RELU)
+        return z <= 0.f ? 0.f : dy;
+    if (ACT == HPACMLT_ACT_SILU) {
+        const float s = sigmoid(z);
+        return dy * (s * __builtin_fmaf(z, 1.f - s, 1.f));
+    }
+    return dy;
+}
+
+// f(an integral constant of act)
+template <typename F>
+inline hipError_t with_activation(int32_t act, F f) {
+    return act == HPACML_ACT_RELU     ? f(std::integral_constant<int, HPACML_ACT_RELU>())
+           : act == HPACMLT_ACT_SILU ? f(std::integral_constant<int, HPACMLT_ACT_SILU>())
+                                      : f(std::integral_constant<int, HPACML_ACT_IDENTITY>());
+}
+
+// Sums over `lanes` (a power of two) neighbouring lanes.  Up to 16 of them by
+// operand permutations of the vector unit, which leave LDS alone; the mirrored
+// orders serve, as what they exchange is the same in all lanes of a part.
+__device__ __forceinline__ float join_lanes(float t, int lanes) {
+    auto permuted = [](float v, auto control) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 15, 15, true));
+    };
+    if (lanes > 1)
+        t += permuted(t, std::integral_constant<int, 0xB1>());        // 1 0 3 2
+    if (lanes > 2)
+        t += permuted(t, std::integral_constant<int, 0x4E>());        // 2 3 0 1
+    if (lanes > 4)
+        t += permuted(t, std::integral_constant<int, 0x141>());       // eight mirrored
+    if (lanes > 8)
+        t += permuted(t, std::integral_constant<int, 0x140>());       // sixteen mirrored
+    if (lanes > 16)
+        t += __shfl_xor(t, 16);
+    if (lanes > 32)
+        t += __shfl_xor(t, 32);
+    return t;
+}
+
+// V neighbouring values: 16 or 8 bytes in one access, or one value.
+template <typename T, int V>
+struct Values {
+    static constexpr int kBytes = V * (int)sizeof(T);
+    typedef uint32_t Word __attribute__((ext_vector_type(kBytes >= 8 ? kBytes / 4 : 2)));
+    typedef Word __attribute__((aligned(sizeof(T)))) Any;
+    static __device__ __forceinline__ void load(const T *p, float (&v)[V]) {
+        if constexpr (V == 1)
+            v[0] = load_value(p);
+        else {
+            const Word w = *(const Any *)p;
+            unpack(w, v);
+        }
+    }
+    static __device__ __forceinline__ void unpack(Word w, float (&v)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if constexpr (sizeof(T) == 4) {
+                const uint32_t u = w[e];
+                v[e] = __builtin_bit_cast(float, u);
+            } else
+                v[e] = __builtin_bit_cast(float, e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+        }
+    }
+    // as they lie in memory
+    typedef typename std::conditional<V == 1, T, Word>::type Held;
+    static __device__ __forceinline__ Held hold(const T *p) {
+        if constexpr (V == 1)
+            return *p;
+        else
+            return *(const Any *)p;
+    }
+    static __device__ __forceinline__ void values(Held w, float (&v)[V]) {
+        if constexpr (V == 1)
+            v[0] = load_value(&w);
+        else
+            unpack(w, v);
+    }
+    static __device__ __forceinline__ void store(T *p, const float (&v)[V]) {
+        if constexpr (V == 1)
+            store_value(p, v[0]);
+        else {
+            Word w;
+#pragma unroll
+            for (int e = 0; e < kBytes / 4; ++e) {
+                if constexpr (sizeof(T) == 4)
+                    w[e] = __builtin_bit_cast(uint32_t, v[e]);
+                else
+                    w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+            }
+            *(Any *)p = w;
+        }
+    }
+};
+
+// dbeta and dgamma from rows of partial sums, [2][channels] each
+inline hipError_t launch_parameters(const GroupNorm &a, const float *part, int64_t rows, float *room, hipStream_t stream) {
+    if (!a.dgamma && !a.dbeta)
+        return hipSuccess;
+    return launch_column_sums({part, rows, 2 * a.channels, 2 * a.channels, a.dbeta, a.dgamma, a.channels, a.accumulate, room}, stream);
+}
+
+// The forms.  *_scratch: bytes, or -1 where the sizes do not have the form.
+int64_t norm_rows_scratch(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, bool backward);
+hipError_t launch_norm_rows(const GroupNorm &a, int32_t dtype, bool backward, hipStream_t stream);
+int64_t norm_held_scratch(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, bool backward);
+hipError_t launch_norm_held(const GroupNorm &a, int32_t dtype, bool backward, hipStream_t stream);
+int64_t norm_parts_scratch(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, bool backward);
+hipError_t launch_norm_parts(const GroupNorm &a, int32_t dtype, bool backward, hipStream_t stream);
+
+}  // namespace hpacml

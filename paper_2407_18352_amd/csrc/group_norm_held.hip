@@ -1,0 +1,291 @@
+// Group norm of images whose groups fit a block's registers: one reading, one launch.
+#include "group_norm_device.hpp"
+
+namespace hpacml {
+
+namespace {
+
+// ---- images whose groups fit a block's registers -----------------------------------------
+
+// A block holds a run of neighbouring groups of one image: `across` vectors of
+// each point, `high` points at a time, up to I of them a thread.  It goes from
+// image to image with the same channels.
+struct Held {
+    int32_t groups, across, high;      // of a run; vectors of a run; points at a time
+    int32_t runs, strides;             // of a row; blocks of the same run
+};
+
+// Sums of `t` over the threads of each of the run's groups.  Thread t has
+// vector t % across of the run; a group is `each` vectors.  of: a pair per
+// thread, then one per group.  Groups' sums are taken by 32 threads each.
+__device__ __forceinline__ float2 join_groups(float2 t, const Held &h, int each, int group, bool here, float2 *of, float2 *of_group) {
+    __syncthreads();
+    of[threadIdx.x] = t;
+    __syncthreads();
+    const int entries = h.high * each;
+    for (int g = threadIdx.x >> 5; g < h.groups; g += blockDim.x >> 5) {
+        float2 s = {0.f, 0.f};
+        for (int i = threadIdx.x & 31; i < entries; i += 32) {
+            const float2 o = of[i / each * h.across + g * each + i % each];
+            s.x += o.x;
+            s.y += o.y;
+        }
+        s.x = join_lanes(s.x, 32);
+        s.y = join_lanes(s.y, 32);
+        if ((threadIdx.x & 31) == 0)
+            of_group[g] = s;
+    }
+    __syncthreads();
+    return here ? of_group[group] : float2{0.f, 0.f};
+}
+
+// Neighbouring runs of one image go to the same XCD at the same time: they share
+// cache lines.
+struct HeldPlace {
+    int run, stride;
+    __device__ __forceinline__ HeldPlace(const Held &h) {
+        const uint32_t per = gridDim.x >> 3, more = gridDim.x & 7, xcd = blockIdx.x & 7;
+        const uint32_t at = xcd * per + min(xcd, more) + (blockIdx.x >> 3);
+        run = at % h.runs;
+        stride = at / h.runs;
+    }
+};
+
+constexpr int kHeldThreads = 512;
+
+template <typename T, int V, int I, int ACT>
+__global__ __launch_bounds__(kHeldThreads) void held_forward_kernel(GroupNorm a, Held h) {
+    extern __shared__ float2 of[];
+    float2 *of_group = of + blockDim.x;
+    const HeldPlace at(h);
+    const int per = a.channels / a.groups, each = per / V, v = threadIdx.x % h.across, r = threadIdx.x / h.across;
+    const int group = v / each, c = at.run * h.groups * per + v * V;
+    const bool here = r < h.high;
+    const float share = 1.f / ((float)a.points * per);
+    float gamma[V], beta[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
+        beta[e] = a.beta ? a.beta[c + e] : 0.f;
+    }
+    for (int64_t image = at.stride; image < a.images; image += h.strides) {
+        const T *x = (const T *)a.x + image * a.points * a.ldx + c;
+        float w[I][V], t = 0, s = 0;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points)
+                Values<T, V>::load(x + point * a.ldx, w[i]);
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    w[i][e] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                t += w[i][e];
+        const float mean = join_groups({t, 0.f}, h, each, group, here, of, of_group).x * share;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (here && r + (int64_t)i * h.high < a.points)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    w[i][e] -= mean;
+                    s = __builtin_fmaf(w[i][e], w[i][e], s);
+                }
+        const float rstd = __builtin_amdgcn_rsqf(join_groups({s, 0.f}, h, each, group, here, of, of_group).x * share + a.eps);      // 1 ulp
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points) {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    w[i][e] = activation<ACT>(__builtin_fmaf(w[i][e], rstd * gamma[e], beta[e]));
+                Values<T, V>::store((T *)a.y + (image * a.points + point) * a.ldy + c, w[i]);
+            }
+        }
+        if (a.mean && here && r == 0 && v % each == 0) {
+            a.mean[image * a.groups + at.run * h.groups + group] = mean;
+            a.rstd[image * a.groups + at.run * h.groups + group] = rstd;
+        }
+    }
+}
+
+// part: [stride][2][channel]
+template <typename T, int V, int I, int ACT>
+__global__ __launch_bounds__(kHeldThreads) void held_backward_kernel(GroupNorm a, Held h, float *part) {
+    extern __shared__ float2 of[];
+    float2 *of_group = of + blockDim.x;
+    const HeldPlace at(h);
+    const int per = a.channels / a.groups, each = per / V, v = threadIdx.x % h.across, r = threadIdx.x / h.across;
+    const int group = v / each, c = at.run * h.groups * per + v * V;
+    const bool here = r < h.high;
+    const float share = 1.f / ((float)a.points * per);
+    float gamma[V], beta[V], s1[V], s2[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
+        beta[e] = a.beta ? a.beta[c + e] : 0.f;
+        s1[e] = s2[e] = 0;
+    }
+    for (int64_t image = at.stride; image < a.images; image += h.strides) {
+        const int64_t row0 = image * a.points, unit = image * a.groups + at.run * h.groups + group;
+        const float mean = a.mean[unit], rstd = a.rstd[unit];
+        // x's words stay as they are until the second use, with g gamma beside them
+        typename Values<T, V>::Held x[I];
+        float gg[I][V], t = 0, u = 0;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points) {
+                x[i] = Values<T, V>::hold((const T *)a.x + (row0 + point) * a.ldx + c);
+                Values<T, V>::load((const T *)a.dy + (row0 + point) * a.lddy + c, gg[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (here && r + (int64_t)i * h.high < a.points) {
+                float xs[V];
+                Values<T, V>::values(x[i], xs);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float d = xs[e] - mean;
+                    const float g = activation_gradient<ACT>(gg[i][e], __builtin_fmaf(d, rstd * gamma[e], beta[e]));
+                    d *= rstd;
+                    s1[e] += g;
+                    s2[e] = __builtin_fmaf(g, d, s2[e]);
+                    gg[i][e] = g * gamma[e];
+                    t += gg[i][e];
+                    u = __builtin_fmaf(gg[i][e], d, u);
+                }
+            }
+        if (!a.y)
+            continue;
+        const float2 m = join_groups({t, u}, h, each, group, here, of, of_group);
+        const float m1 = m.x * share, m2 = m.y * share * rstd;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t point = r + (int64_t)i * h.high;
+            if (here && point < a.points) {
+                float xs[V];
+                Values<T, V>::values(x[i], xs);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    xs[e] = rstd * __builtin_fmaf(mean - xs[e], m2, gg[i][e] - m1);
+                Values<T, V>::store((T *)a.y + (row0 + point) * a.ldy + c, xs);
+            }
+        }
+    }
+    if (!a.dgamma && !a.dbeta)
+        return;
+    float *to = part + (int64_t)at.stride * 2 * a.channels;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        float2 t = {s1[e], s2[e]};
+        __syncthreads();
+        of[threadIdx.x] = t;
+        for (int n = h.high, half; n > 1; n = half) {
+            half = (n + 1) / 2;
+            __syncthreads();
+            if (r < n - half) {
+                const float2 o = of[threadIdx.x + half * h.across];
+                t.x += o.x;
+                t.y += o.y;
+                of[threadIdx.x] = t;
+            }
+        }
+        if (r == 0) {
+            to[c + e] = t.x;
+            to[a.channels + c + e] = t.y;
+        }
+    }
+}
+
+struct HeldPlan {
+    Held h;
+    int v, each;             // channels of a vector; points of a thread
+    int threads;
+    uint32_t grid;
+};
+// Whether a group of an image fits: neighbouring groups until a point's part is
+// kLine bytes, at most eight points a thread.
+bool held_plan(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, HeldPlan *o) {
+    constexpr int kLine = 64;
+    const int per = channels / groups, size = dtype == HPACML_BF16 ? 2 : 4;
+    o->v = size == 2 && per % 8 == 0 ? 8 : per % 4 == 0 ? 4 : 1;
+    const int64_t most = (int64_t)kHeldThreads * 8;
+    if (points > most || points * (per / o->v) > most)
+        return false;
+    int run = 1;
+    for (int k = 1; k <= groups && points * k * (per / o->v) <= most && k * (per / o->v) <= kHeldThreads; ++k)
+        if (groups % k == 0) {
+            run = k;
+            if (k * per * size >= kLine)
+                break;
+        }
+    o->h.groups = run;
+    o->h.across = run * (per / o->v);
+    if (o->h.across > kHeldThreads)
+        return false;
+    // the fewest threads of 256, 512 with at most eight points each
+    for (o->threads = 256; o->threads <= kHeldThreads; o->threads *= 2) {
+        o->h.high = o->threads / o->h.across;
+        if (o->h.high > 0 && (points + o->h.high - 1) / o->h.high <= 8)
+            break;
+    }
+    if (o->threads > kHeldThreads)
+        return false;
+    if (o->h.high > points)
+        o->h.high = (int32_t)points;
+    const int64_t each = (points + o->h.high - 1) / o->h.high;
+    o->each = each <= 2 ? 2 : each <= 4 ? 4 : 8;
+    o->h.runs = groups / run;
+    const int64_t want = 256 * 2048 / o->threads / o->h.runs + 1;
+    o->h.strides = (int32_t)(images < want ? images : want);
+    o->grid = (uint32_t)(o->h.strides * o->h.runs);
+    return true;
+}
+
+template <typename T, int V, int I>
+hipError_t launch_held(const GroupNorm &a, const HeldPlan &o, bool backward, hipStream_t stream) {
+    const size_t lds = (size_t)(o.threads + o.h.groups) * sizeof(float2);
+    if (!backward)
+        return with_activation(a.act, [&](auto act) {
+            held_forward_kernel<T, V, I, decltype(act)::value><<<o.grid, o.threads, lds, stream>>>(a, o.h);
+            return hipGetLastError();
+        });
+    float *part = (float *)a.scratch, *room = part + (int64_t)o.h.strides * 2 * a.channels;
+    const hipError_t e = with_activation(a.act, [&](auto act) {
+        held_backward_kernel<T, V, I, decltype(act)::value><<<o.grid, o.threads, lds, stream>>>(a, o.h, part);
+        return hipGetLastError();
+    });
+    return e == hipSuccess ? launch_parameters(a, part, o.h.strides, room, stream) : e;
+}
+template <typename T, int V>
+hipError_t launch_held(const GroupNorm &a, const HeldPlan &o, bool backward, hipStream_t stream) {
+    return o.each == 2 ? launch_held<T, V, 2>(a, o, backward, stream)
+           : o.each == 4 ? launch_held<T, V, 4>(a, o, backward, stream) : launch_held<T, V, 8>(a, o, backward, stream);
+}
+
+}  // namespace
+
+int64_t norm_held_scratch(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, bool backward) {
+    HeldPlan o;
+    if (!held_plan(dtype, images, points, channels, groups, &o))
+        return -1;
+    return backward ? ((int64_t)o.h.strides * 2 * channels + column_sums_room(o.h.strides, 2 * channels)) * 4 : 0;
+}
+
+hipError_t launch_norm_held(const GroupNorm &a, int32_t dtype, bool backward, hipStream_t stream) {
+    HeldPlan o;
+    held_plan(dtype, a.images, a.points, a.channels, a.groups, &o);
+    if (dtype == HPACML_F32)
+        return o.v == 4 ? launch_held<float, 4>(a, o, backward, stream) : launch_held<float, 1>(a, o, backward, stream);
+    return o.v == 8   ? launch_held<uint16_t, 8>(a, o, backward, stream)
+           : o.v == 4 ? launch_held<uint16_t, 4>(a, o, backward, stream)
+                      : launch_held<uint16_t, 1>(a, o, backward, stream);
+}
+
+}  // namespace hpacml

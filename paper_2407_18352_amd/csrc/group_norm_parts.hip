@@ -1,0 +1,414 @@
+// Group norm of large images: sums of runs of points, their join, and the results from a second reading.
+#include "group_norm_device.hpp"
+
+namespace hpacml {
+
+namespace {
+
+// ---- parts of an image ------------------------------------------------------------
+
+// A block takes `run` points of an image and up to 256 vectors of V channels,
+// `high` (a power of two) points at a time.
+struct Parts {
+    int32_t vectors, across, high;       // of a row; of a block; points at a time
+    uint32_t column_tiles, runs;         // of a row, of an image
+    int64_t run, blocks;                 // points; of all images
+};
+
+struct Place {
+    int64_t image, first, last;          // points of the record
+    int c, r;                            // the thread's first channel, its point
+    bool here;
+};
+template <int V>
+__device__ __forceinline__ Place place_of(const GroupNorm &a, const Parts &p, int64_t block) {
+    Place q;
+    const int64_t i = block / p.column_tiles;
+    const int tile = (int)(block % p.column_tiles);
+    q.image = i / p.runs;
+    const int64_t at = (int64_t)(i % p.runs) * p.run;
+    q.first = q.image * a.points + at;
+    q.last = q.image * a.points + min(at + p.run, a.points);
+    q.r = threadIdx.x / p.across;
+    const int v = tile * p.across + threadIdx.x % p.across;
+    q.c = v * V;
+    q.here = q.r < p.high && v < p.vectors;
+    return q;
+}
+
+// (mean, squares about it) of n values and of m: of both
+__device__ __forceinline__ void join_moments(float &mean, float &squares, float n, float mean2, float squares2, float m) {
+    const float d = mean2 - mean, share = m / (n + m);
+    mean += d * share;
+    squares += squares2 + d * d * (n * share);
+}
+
+// [image][run][channel] (mean, squares)
+template <typename T, int V>
+__global__ __launch_bounds__(256) void parts_moments_kernel(GroupNorm a, Parts p, float2 *part) {
+    constexpr int kBatch = 8;
+    __shared__ float2 of[256][V];
+    for (int64_t block = blockIdx.x; block < p.blocks; block += gridDim.x) {
+        const Place q = place_of<V>(a, p, block);
+        float mean[V], squares[V], n = 0;
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            mean[e] = squares[e] = 0;
+        if (q.here) {
+            const T *x = (const T *)a.x + q.c;
+            int64_t row = q.first + q.r;
+            for (; row + (kBatch - 1) * p.high < q.last; row += kBatch * p.high) {
+                float v[kBatch][V];
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+                    Values<T, V>::load(x + (row + b * p.high) * a.ldx, v[b]);
+                const float share = kBatch / (n + kBatch), weight = n * share;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float t = 0, s = 0;
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+                        t += v[b][e];
+                    t *= 1.f / kBatch;
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+                        s = __builtin_fmaf(v[b][e] - t, v[b][e] - t, s);
+                    const float d = t - mean[e];
+                    mean[e] += d * share;
+                    squares[e] += s + d * d * weight;
+                }
+                n += kBatch;
+            }
+            for (; row < q.last; row += p.high) {
+                float v[V];
+                Values<T, V>::load(x + row * a.ldx, v);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    join_moments(mean[e], squares[e], n, v[e], 0.f, 1.f);
+                n += 1;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            of[threadIdx.x][e] = {mean[e], squares[e]};
+        // threads' points: every `high`-th from r on; joined in halves
+        for (int h = p.high / 2; h > 0; h /= 2) {
+            __syncthreads();
+            const int rows = (int)(q.last - q.first);
+            auto count = [&](int r) {         // values of the threads r, r + 2 h, ... that r has joined
+                const int step = 2 * h;
+                int t = 0;
+                if (rows > r)
+                    t = (rows - r + step - 1) / step;
+                return (float)t;
+            };
+            if (q.here && q.r < h) {
+                const float m = count(q.r + h);
+                n = count(q.r);
+                if (m > 0)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float2 o = of[threadIdx.x + h * p.across][e];
+                        join_moments(mean[e], squares[e], n, o.x, o.y, m);
+                        of[threadIdx.x][e] = {mean[e], squares[e]};
+                    }
+            }
+        }
+        if (q.here && q.r == 0) {
+            float2 *to = part + (block / p.column_tiles) * (int64_t)a.channels + q.c;
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (q.c + e < a.channels)
+                    to[e] = {mean[e], squares[e]};
+        }
+        __syncthreads();
+    }
+}
+
+__device__ __forceinline__ double join_block(double t, double (&of_wave)[4]) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+        t += __shfl_xor(t, s);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+        of_wave[threadIdx.x >> 6] = t;
+    __syncthreads();
+    return (of_wave[0] + of_wave[1]) + (of_wave[2] + of_wave[3]);
+}
+
+// The partial results of an image's group, `per` channels of each run: a thread
+// takes every so many runs of one channel (with one index over all of them, and
+// its divisions, 2049 runs of 4 channels took 23 us).
+template <typename F>
+__device__ __forceinline__ void over_runs(int per, uint32_t runs, F f) {
+    const int across = min(per, 256), high = 256 / across, c0 = threadIdx.x % across, r0 = threadIdx.x / across;
+    if (r0 < high)
+        for (int c = c0; c < per; c += across)
+#pragma unroll 4
+            for (uint32_t r = r0; r < runs; r += high)
+                f(c, r);
+}
+
+// A block per image and group: mean and rstd.
+__global__ __launch_bounds__(256) void parts_join_kernel(GroupNorm a, Parts p, const float2 *part, float *mean_to, float *rstd_to) {
+    __shared__ double of_wave[4];
+    for (int64_t unit = blockIdx.x; unit < a.images * a.groups; unit += gridDim.x) {
+        const int64_t image = unit / a.groups;
+        const int per = a.channels / a.groups, c0 = (int)(unit % a.groups) * per;
+        const float2 *at = part + image * p.runs * a.channels + c0;
+        auto values = [&](uint32_t r) { return (double)min(p.run, a.points - r * p.run); };
+        double t = 0;
+        over_runs(per, p.runs, [&](int c, uint32_t r) { t += values(r) * at[(int64_t)r * a.channels + c].x; });
+        const double n = (double)a.points * per, mean = join_block(t, of_wave) / n;
+        t = 0;
+        over_runs(per, p.runs, [&](int c, uint32_t r) {
+            const float2 o = at[(int64_t)r * a.channels + c];
+            t += (double)o.y + values(r) * (o.x - mean) * (o.x - mean);
+        });
+        t = join_block(t, of_wave);
+        if (threadIdx.x == 0) {
+            mean_to[unit] = (float)mean;
+            rstd_to[unit] = (float)(1.0 / sqrt(t / n + (double)a.eps));
+        }
+    }
+}
+
+// The parameters of a thread's channels.
+template <int V>
+struct Channels {
+    float mean[V], rstd[V], gamma[V], beta[V];
+    __device__ __forceinline__ void load(const GroupNorm &a, int64_t image, int c, const float *means, const float *rstds) {
+        const int per = a.channels / a.groups;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int ce = min(c + e, a.channels - 1);
+            const int64_t at = image * a.groups + ce / per;
+            mean[e] = means[at];
+            rstd[e] = rstds[at];
+            gamma[e] = a.gamma ? a.gamma[ce] : 1.f;
+            beta[e] = a.beta ? a.beta[ce] : 0.f;
+        }
+    }
+};
+
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(256) void parts_apply_kernel(GroupNorm a, Parts p, const float *means, const float *rstds) {
+    for (int64_t block = blockIdx.x; block < p.blocks; block += gridDim.x) {
+        const Place q = place_of<V>(a, p, block);
+        if (!q.here)
+            continue;
+        Channels<V> k;
+        k.load(a, q.image, q.c, means, rstds);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            k.gamma[e] *= k.rstd[e];
+#pragma unroll 4
+        for (int64_t row = q.first + q.r; row < q.last; row += p.high) {
+            float v[V];
+            Values<T, V>::load((const T *)a.x + row * a.ldx + q.c, v);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                v[e] = activation<ACT>(__builtin_fmaf(v[e] - k.mean[e], k.gamma[e], k.beta[e]));
+            Values<T, V>::store((T *)a.y + row * a.ldy + q.c, v);
+        }
+    }
+}
+
+// sums of g and of g (x - mean) rstd: [image][run][2][channel]
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, float *part) {
+    __shared__ float2 of[256][V];
+    for (int64_t block = blockIdx.x; block < p.blocks; block += gridDim.x) {
+        const Place q = place_of<V>(a, p, block);
+        float s1[V], s2[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            s1[e] = s2[e] = 0;
+        Channels<V> k;
+        if (q.here) {
+            k.load(a, q.image, q.c, a.mean, a.rstd);
+#pragma unroll 4
+            for (int64_t row = q.first + q.r; row < q.last; row += p.high) {
+                float v[V], g[V];
+                Values<T, V>::load((const T *)a.x + row * a.ldx + q.c, v);
+                Values<T, V>::load((const T *)a.dy + row * a.lddy + q.c, g);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float d = v[e] - k.mean[e];
+                    const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.rstd[e] * k.gamma[e], k.beta[e]));
+                    s1[e] += t;
+                    s2[e] = __builtin_fmaf(t, d, s2[e]);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            of[threadIdx.x][e] = {s1[e], s2[e]};
+        for (int h = p.high / 2; h > 0; h /= 2) {
+            __syncthreads();
+            if (q.here && q.r < h)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float2 o = of[threadIdx.x + h * p.across][e];
+                    s1[e] += o.x;
+                    s2[e] += o.y;
+                    of[threadIdx.x][e] = {s1[e], s2[e]};
+                }
+        }
+        if (q.here && q.r == 0) {
+            float *to = part + (block / p.column_tiles) * (int64_t)(2 * a.channels) + q.c;
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (q.c + e < a.channels) {
+                    to[e] = s1[e];
+                    to[a.channels + e] = s2[e] * k.rstd[e];
+                }
+        }
+        __syncthreads();
+    }
+}
+
+// A block per image and group: the means of g gamma and g gamma (x - mean) rstd.
+__global__ __launch_bounds__(256) void parts_means_kernel(GroupNorm a, Parts p, const float *part, float2 *means) {
+    __shared__ double of_wave[4];
+    for (int64_t unit = blockIdx.x; unit < a.images * a.groups; unit += gridDim.x) {
+        const int64_t image = unit / a.groups;
+        const int per = a.channels / a.groups, c0 = (int)(unit % a.groups) * per;
+        const float *at = part + image * p.runs * 2 * a.channels + c0;
+        double t = 0, u = 0;
+        over_runs(per, p.runs, [&](int c, uint32_t r) {
+            const float *o = at + (int64_t)r * 2 * a.channels + c;
+            const double gamma = a.gamma ? a.gamma[c0 + c] : 1.f;
+            t += gamma * o[0];
+            u += gamma * o[a.channels];
+        });
+        const double n = (double)a.points * per;
+        t = join_block(t, of_wave) / n;
+        u = join_block(u, of_wave) / n;
+        if (threadIdx.x == 0)
+            means[unit] = {(float)t, (float)u};
+    }
+}
+
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(256) void parts_dx_kernel(GroupNorm a, Parts p, const float2 *means) {
+    for (int64_t block = blockIdx.x; block < p.blocks; block += gridDim.x) {
+        const Place q = place_of<V>(a, p, block);
+        if (!q.here)
+            continue;
+        Channels<V> k;
+        k.load(a, q.image, q.c, a.mean, a.rstd);
+        float m1[V], m2[V];
+        const int per = a.channels / a.groups;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float2 m = means[q.image * a.groups + min(q.c + e, a.channels - 1) / per];
+            m1[e] = m.x;
+            m2[e] = m.y;
+        }
+#pragma unroll 4
+        for (int64_t row = q.first + q.r; row < q.last; row += p.high) {
+            float v[V], g[V];
+            Values<T, V>::load((const T *)a.x + row * a.ldx + q.c, v);
+            Values<T, V>::load((const T *)a.dy + row * a.lddy + q.c, g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = v[e] - k.mean[e];
+                const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.rstd[e] * k.gamma[e], k.beta[e])) * k.gamma[e];
+                v[e] = k.rstd[e] * ((t - m1[e]) - d * k.rstd[e] * m2[e]);
+            }
+            Values<T, V>::store((T *)a.y + row * a.ldy + q.c, v);
+        }
+    }
+}
+
+// Vectors that all of a row's channels fill: 16 bytes, or one value.
+int whole_vector(int32_t dtype, int32_t channels) {
+    const int v = dtype == HPACML_F32 ? 4 : 8;
+    return channels % v == 0 ? v : 1;
+}
+
+Parts parts_of(int32_t dtype, int64_t images, int64_t points, int32_t channels) {
+    Parts p;
+    const int v = whole_vector(dtype, channels);
+    p.vectors = channels / v;
+    p.across = p.vectors < 256 ? p.vectors : 256;
+    p.column_tiles = (uint32_t)((p.vectors + p.across - 1) / p.across);
+    p.high = 1;
+    while (p.high * 2 * p.across <= 256)
+        p.high *= 2;
+    // about eight blocks for each of 256 CUs, runs of no less than eight values a thread
+    const int64_t want = 2048 / images / p.column_tiles + 1, least = 8 * p.high;
+    int64_t run = (points + want - 1) / want;
+    run = (run + least - 1) / least * least;
+    p.run = run;
+    p.runs = (uint32_t)((points + run - 1) / run);
+    p.blocks = images * p.runs * p.column_tiles;
+    return p;
+}
+
+// A grid's blocks of 256 threads: a launch has fewer than 2^32 threads.
+uint32_t grid_of(int64_t blocks) { return (uint32_t)(blocks < 1 << 20 ? blocks : 1 << 20); }
+
+size_t rounded(size_t n) { return (n + 255) / 256 * 256; }
+
+template <typename T, int V>
+hipError_t forward_parts(const GroupNorm &a, const Parts &p, hipStream_t stream) {
+    const uint32_t blocks = grid_of(p.blocks);
+    float2 *part = (float2 *)a.scratch;
+    float *moments = (float *)(a.scratch + rounded((size_t)a.images * p.runs * a.channels * 8));
+    float *mean = a.mean ? a.mean : moments, *rstd = a.mean ? a.rstd : moments + a.images * a.groups;
+    parts_moments_kernel<T, V><<<blocks, 256, 0, stream>>>(a, p, part);
+    parts_join_kernel<<<grid_of(a.images * a.groups), 256, 0, stream>>>(a, p, part, mean, rstd);
+    return with_activation(a.act, [&](auto act) {
+        parts_apply_kernel<T, V, decltype(act)::value><<<blocks, 256, 0, stream>>>(a, p, mean, rstd);
+        return hipGetLastError();
+    });
+}
+
+template <typename T, int V>
+hipError_t backward_parts(const GroupNorm &a, const Parts &p, hipStream_t stream) {
+    const int64_t rows = a.images * p.runs;
+    const uint32_t blocks = grid_of(p.blocks);
+    float *part = (float *)a.scratch;
+    float2 *means = (float2 *)(a.scratch + rounded((size_t)rows * a.channels * 8));
+    float *room = (float *)((char *)means + rounded((size_t)a.images * a.groups * 8));
+    hipError_t e = with_activation(a.act, [&](auto act) {
+        parts_sums_kernel<T, V, decltype(act)::value><<<blocks, 256, 0, stream>>>(a, p, part);
+        return hipGetLastError();
+    });
+    if (e == hipSuccess)
+        e = launch_parameters(a, part, rows, room, stream);
+    if (a.y && e == hipSuccess) {
+        parts_means_kernel<<<grid_of(a.images * a.groups), 256, 0, stream>>>(a, p, part, means);
+        e = with_activation(a.act, [&](auto act) {
+            parts_dx_kernel<T, V, decltype(act)::value><<<blocks, 256, 0, stream>>>(a, p, means);
+            return hipGetLastError();
+        });
+    }
+    return e;
+}
+
+}  // namespace
+
+int64_t norm_parts_scratch(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, bool backward) {
+    const Parts p = parts_of(dtype, images, points, channels);
+    const int64_t rows = images * p.runs;
+    return (int64_t)(rounded((size_t)rows * channels * 8) + rounded((size_t)images * groups * 8) +
+                     (backward ? rounded((size_t)column_sums_room(rows, 2 * channels) * 4) : 0));
+}
+
+hipError_t launch_norm_parts(const GroupNorm &a, int32_t dtype, bool backward, hipStream_t stream) {
+    const Parts p = parts_of(dtype, a.images, a.points, a.channels);
+    const int v = whole_vector(dtype, a.channels);
+    if (dtype == HPACML_F32) {
+        if (v == 4)
+            return backward ? backward_parts<float, 4>(a, p, stream) : forward_parts<float, 4>(a, p, stream);
+        return backward ? backward_parts<float, 1>(a, p, stream) : forward_parts<float, 1>(a, p, stream);
+    }
+    if (v == 8)
+        return backward ? backward_parts<uint16_t, 8>(a, p, stream) : forward_parts<uint16_t, 8>(a, p, stream);
+    return backward ? backward_parts<uint16_t, 1>(a, p, stream) : forward_parts<uint16_t, 1>(a, p, stream);
+}
+
+}  // namespace hpacml

@@ -1,0 +1,249 @@
+// Group norm of images of one point: in one launch, in registers.
+#include "group_norm_device.hpp"
+
+namespace hpacml {
+
+namespace {
+
+// ---- images of one point ------------------------------------------------------------
+
+// L lanes (a power of two) hold a group of a row, I vectors of V channels each;
+// a wave has 64 / L neighbouring groups and goes from row to row, so that a
+// lane's channels stay the same.
+constexpr int kRowWaves = 8;
+struct Rows {
+    int32_t lanes, vectors, column_blocks;     // L; of a group; waves that a row takes
+    int32_t strides;                           // blocks of the same groups
+};
+
+template <typename T, int V, int I>
+struct RowLane {
+    int group, lane;
+    bool here[I];
+    int c[I];
+    float gamma[I][V], beta[I][V];
+    __device__ __forceinline__ RowLane(const GroupNorm &a, const Rows &p, int column_block) {
+        const int per = a.channels / a.groups, l = threadIdx.x & 63;
+        group = column_block * (64 / p.lanes) + l / p.lanes;
+        lane = l % p.lanes;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int v = lane + i * p.lanes;
+            here[i] = group < a.groups && v < p.vectors;
+            c[i] = here[i] ? group * per + v * V : 0;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                gamma[i][e] = a.gamma ? a.gamma[c[i] + e] : 1.f;
+                beta[i][e] = a.beta ? a.beta[c[i] + e] : 0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const T *row, float (&v)[I][V]) const {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            Values<T, V>::load(row + c[i], v[i]);      // of channel 0 where there is none: left out of the sums
+        }
+    }
+};
+
+template <typename T, int V, int I, int ACT>
+__global__ __launch_bounds__(64 * kRowWaves) void rows_forward_kernel(GroupNorm a, Rows p) {
+    const int column_block = blockIdx.x % p.column_blocks, wave = threadIdx.x >> 6;
+    const RowLane<T, V, I> k(a, p, column_block);
+    const float share = 1.f / (float)(a.channels / a.groups);
+    constexpr int kAtOnce = V * I <= 16 ? 2 : 1;     // rows whose loads go out together
+    const int64_t step = (int64_t)p.strides * kRowWaves;
+    for (int64_t first = (int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave; first < a.images; first += step * kAtOnce) {
+        float v[kAtOnce][I][V];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            k.load((const T *)a.x + min(first + u * step, a.images - 1) * a.ldx, v[u]);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t row = first + u * step;
+            float t = 0, s = 0;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                float o = 0;
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    o += v[u][i][e];
+                t += k.here[i] ? o : 0.f;
+            }
+            const float mean = join_lanes(t, p.lanes) * share;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                float o = 0;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    v[u][i][e] -= mean;
+                    o = __builtin_fmaf(v[u][i][e], v[u][i][e], o);
+                }
+                s += k.here[i] ? o : 0.f;
+            }
+            const float rstd = __builtin_amdgcn_rsqf(join_lanes(s, p.lanes) * share + a.eps);      // 1 ulp
+            if (row >= a.images)
+                continue;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                if (k.here[i]) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        v[u][i][e] = activation<ACT>(__builtin_fmaf(v[u][i][e], rstd * k.gamma[i][e], k.beta[i][e]));
+                    Values<T, V>::store((T *)a.y + row * a.ldy + k.c[i], v[u][i]);
+                }
+            if (a.mean && k.lane == 0 && k.here[0]) {
+                a.mean[row * a.groups + k.group] = mean;
+                a.rstd[row * a.groups + k.group] = rstd;
+            }
+        }
+    }
+}
+
+// part: [block of the same groups][2][channel]
+template <typename T, int V, int I, int ACT>
+__global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm a, Rows p, float *part) {
+    __shared__ float2 of[kRowWaves][64][V];
+    const int column_block = blockIdx.x % p.column_blocks, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const RowLane<T, V, I> k(a, p, column_block);
+    const float share = 1.f / (float)(a.channels / a.groups);
+    float s1[I][V], s2[I][V];
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            s1[i][e] = s2[i][e] = 0;
+    for (int64_t row = (int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave; row < a.images; row += (int64_t)p.strides * kRowWaves) {
+        float v[I][V], g[I][V], t = 0, u = 0;
+        k.load((const T *)a.x + row * a.ldx, v);
+        k.load((const T *)a.dy + row * a.lddy, g);
+        const int64_t at = row * a.groups + min(k.group, a.groups - 1);
+        const float mean = a.mean[at], rstd = a.rstd[at];
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            float to = 0, uo = 0;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = v[i][e] - mean;
+                const float o = activation_gradient<ACT>(g[i][e], __builtin_fmaf(d, rstd * k.gamma[i][e], k.beta[i][e]));
+                v[i][e] = d * rstd;
+                s1[i][e] += o;
+                s2[i][e] = __builtin_fmaf(o, v[i][e], s2[i][e]);
+                g[i][e] = o * k.gamma[i][e];
+                to += g[i][e];
+                uo = __builtin_fmaf(g[i][e], v[i][e], uo);
+            }
+            t += k.here[i] ? to : 0.f;
+            u += k.here[i] ? uo : 0.f;
+        }
+        if (a.y) {
+            const float m1 = join_lanes(t, p.lanes) * share, m2 = join_lanes(u, p.lanes) * share;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                if (k.here[i]) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        v[i][e] = rstd * ((g[i][e] - m1) - v[i][e] * m2);
+                    Values<T, V>::store((T *)a.y + row * a.ldy + k.c[i], v[i]);
+                }
+        }
+    }
+    if (!a.dgamma && !a.dbeta)
+        return;
+    float *to = part + (int64_t)(blockIdx.x / p.column_blocks) * 2 * a.channels;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            of[wave][lane][e] = {s1[i][e], s2[i][e]};
+        __syncthreads();
+        if (wave == 0 && k.here[i])
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float2 t = of[0][lane][e];
+#pragma unroll
+                for (int w = 1; w < kRowWaves; ++w) {
+                    t.x += of[w][lane][e].x;
+                    t.y += of[w][lane][e].y;
+                }
+                to[k.c[i] + e] = t.x;
+                to[a.channels + k.c[i] + e] = t.y;
+            }
+        __syncthreads();
+    }
+}
+
+struct RowsPlan {
+    Rows p;
+    int v, each;             // channels of a vector; vectors of a lane
+    uint32_t grid;
+};
+// Whether images of one point have that form.
+bool rows_plan(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, RowsPlan *o) {
+    const int per = channels / groups;
+    if (points != 1)
+        return false;
+    o->v = dtype == HPACML_BF16 && per % 8 == 0 ? 8 : per % 4 == 0 ? 4 : 1;
+    o->p.vectors = per / o->v;
+    o->p.lanes = 1;
+    while (o->p.lanes < 64 && o->p.lanes < o->p.vectors)
+        o->p.lanes *= 2;
+    o->each = 1;
+    while (o->each * o->p.lanes < o->p.vectors)
+        o->each *= 2;
+    if (o->each > 8 || o->each * o->v > 32)         // a lane's values in registers
+        return false;
+    const int at_a_time = 64 / o->p.lanes;
+    o->p.column_blocks = (groups + at_a_time - 1) / at_a_time;
+    const int64_t most = (images + kRowWaves - 1) / kRowWaves, want = 1024 / o->p.column_blocks + 1;
+    o->p.strides = (int32_t)(most < want ? most : want);
+    o->grid = (uint32_t)(o->p.strides * o->p.column_blocks);
+    return true;
+}
+
+template <typename T, int V, int I>
+hipError_t launch_rows(const GroupNorm &a, const RowsPlan &o, bool backward, hipStream_t stream) {
+    if (!backward)
+        return with_activation(a.act, [&](auto act) {
+            rows_forward_kernel<T, V, I, decltype(act)::value><<<o.grid, 64 * kRowWaves, 0, stream>>>(a, o.p);
+            return hipGetLastError();
+        });
+    float *part = (float *)a.scratch, *room = part + (int64_t)o.p.strides * 2 * a.channels;
+    const hipError_t e = with_activation(a.act, [&](auto act) {
+        rows_backward_kernel<T, V, I, decltype(act)::value><<<o.grid, 64 * kRowWaves, 0, stream>>>(a, o.p, part);
+        return hipGetLastError();
+    });
+    return e == hipSuccess ? launch_parameters(a, part, o.p.strides, room, stream) : e;
+}
+template <typename T, int V>
+hipError_t launch_rows(const GroupNorm &a, const RowsPlan &o, bool backward, hipStream_t stream) {
+    if (o.each == 1)
+        return launch_rows<T, V, 1>(a, o, backward, stream);
+    if (o.each == 2)
+        return launch_rows<T, V, 2>(a, o, backward, stream);
+    if constexpr (V < 8)
+        if (o.each > 4)
+            return launch_rows<T, V, 8>(a, o, backward, stream);
+    return launch_rows<T, V, 4>(a, o, backward, stream);
+}
+
+}  // namespace
+
+int64_t norm_rows_scratch(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, bool backward) {
+    RowsPlan o;
+    if (!rows_plan(dtype, images, points, channels, groups, &o))
+        return -1;
+    return backward ? ((int64_t)o.p.strides * 2 * channels + column_sums_room(o.p.strides, 2 * channels)) * 4 : 0;
+}
+
+hipError_t launch_norm_rows(const GroupNorm &a, int32_t dtype, bool backward, hipStream_t stream) {
+    RowsPlan o;
+    rows_plan(dtype, a.images, a.points, a.channels, a.groups, &o);
+    if (dtype == HPACML_F32)
+        return o.v == 4 ? launch_rows<float, 4>(a, o, backward, stream) : launch_rows<float, 1>(a, o, backward, stream);
+    return o.v == 8   ? launch_rows<uint16_t, 8>(a, o, backward, stream)
+           : o.v == 4 ? launch_rows<uint16_t, 4>(a, o, backward, stream)
+                      : launch_rows<uint16_t, 1>(a, o, backward, stream);
+}
+
+}  // namespace hpacml
