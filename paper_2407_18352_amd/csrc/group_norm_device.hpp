@@ -13,9 +13,9 @@ namespace hpacml {
 
 // By the exponential's and the reciprocal's own instructions: z log2(e) is
 // rounded to 2^-24 of itself, which moves the result by |z| 2^-24 (1 - result) of
-// it, less than the roundings around it, and the square of a SiLU's slope takes
-// five instructions a value where expf and a division take thirty: the backward
-// pass of 134 million values is bound by memory so, not by its arithmetic.
+// it, less than the roundings around it.  expf and a division take some thirty
+// instructions a value, and the backward pass of 134 million values is bound by
+// its arithmetic as much as by memory (unnorm_frames 409 us with them).
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896f)); }
 
 // A kernel has one activation: asked at every value, it kept the compiler from
@@ -26,14 +26,18 @@ __device__ __forceinline__ float activation(float z) {
         return relu_keep_nan(z);
     return ACT == HPACMLT_ACT_SILU ? z * sigmoid(z) : z;
 }
-// g = dy act'(z)
+// z is asked for in units that save an instruction: of kUnit<ACT> * z
+template <int ACT>
+constexpr float kUnit = ACT == HPACMLT_ACT_SILU ? 1.44269504088896f : 1.f;
+// g = dy act'(z); a SiLU's slope is s (1 + z (1 - s)), s the sigmoid
 template <int ACT>
 __device__ __forceinline__ float activation_gradient(float dy, float z) {
     if (ACT == HPACML_ACT_RELU)
         return z <= 0.f ? 0.f : dy;
     if (ACT == HPACMLT_ACT_SILU) {
-        const float s = sigmoid(z);
-        return dy * (s * __builtin_fmaf(z, 1.f - s, 1.f));
+        constexpr float kLn2 = 0.693147180559945f;
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-z));
+        return dy * s * __builtin_fmaf(z, __builtin_fmaf(-s, kLn2, kLn2), 1.f);
     }
     return dy;
 }
@@ -122,6 +126,21 @@ struct Values {
         }
     }
 };
+
+// The V values at p, or `none` each.  (One branch around all loads: with one for
+// each, every load waited for the one before.)
+template <int V>
+__device__ __forceinline__ void load_parameters(const float *p, float none, float (&v)[V]) {
+    if (p) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            v[e] = p[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            v[e] = none;
+    }
+}
 
 // dbeta and dgamma from rows of partial sums, [2][channels] each
 inline hipError_t launch_parameters(const GroupNorm &a, const float *part, int64_t rows, float *room, hipStream_t stream) {

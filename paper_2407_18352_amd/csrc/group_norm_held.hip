@@ -61,45 +61,44 @@ __global__ __launch_bounds__(kHeldThreads) void held_forward_kernel(GroupNorm a,
     const int per = a.channels / a.groups, each = per / V, v = threadIdx.x % h.across, r = threadIdx.x / h.across;
     const int group = v / each, c = at.run * h.groups * per + v * V;
     const bool here = r < h.high;
+    const int last = (int)a.points - 1;
     const float share = 1.f / ((float)a.points * per);
     float gamma[V], beta[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
-        beta[e] = a.beta ? a.beta[c + e] : 0.f;
-    }
+    load_parameters<V>(a.gamma ? a.gamma + c : nullptr, 1.f, gamma);
+    load_parameters<V>(a.beta ? a.beta + c : nullptr, 0.f, beta);
     for (int64_t image = at.stride; image < a.images; image += h.strides) {
         const T *x = (const T *)a.x + image * a.points * a.ldx + c;
         float w[I][V], t = 0, s = 0;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t point = r + (int64_t)i * h.high;
-            if (here && point < a.points)
-                Values<T, V>::load(x + point * a.ldx, w[i]);
-            else
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    w[i][e] = 0.f;
+            // (the last point again where there is none: left out of the sums)
+            const int point = min(r + i * h.high, last);
+            Values<T, V>::load(x + (int64_t)point * a.ldx, w[i]);
         }
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int i = 0; i < I; ++i) {
+            float o = 0;
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                t += w[i][e];
+                o += w[i][e];
+            t += here && r + i * h.high <= last ? o : 0.f;
+        }
         const float mean = join_groups({t, 0.f}, h, each, group, here, of, of_group).x * share;
 #pragma unroll
-        for (int i = 0; i < I; ++i)
-            if (here && r + (int64_t)i * h.high < a.points)
+        for (int i = 0; i < I; ++i) {
+            float o = 0;
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    w[i][e] -= mean;
-                    s = __builtin_fmaf(w[i][e], w[i][e], s);
-                }
+            for (int e = 0; e < V; ++e) {
+                w[i][e] -= mean;
+                o = __builtin_fmaf(w[i][e], w[i][e], o);
+            }
+            s += here && r + i * h.high <= last ? o : 0.f;
+        }
         const float rstd = __builtin_amdgcn_rsqf(join_groups({s, 0.f}, h, each, group, here, of, of_group).x * share + a.eps);      // 1 ulp
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t point = r + (int64_t)i * h.high;
-            if (here && point < a.points) {
+            const int point = r + i * h.high;
+            if (here && point <= last) {
 #pragma unroll
                 for (int e = 0; e < V; ++e)
                     w[i][e] = activation<ACT>(__builtin_fmaf(w[i][e], rstd * gamma[e], beta[e]));
@@ -122,58 +121,69 @@ __global__ __launch_bounds__(kHeldThreads) void held_backward_kernel(GroupNorm a
     const int per = a.channels / a.groups, each = per / V, v = threadIdx.x % h.across, r = threadIdx.x / h.across;
     const int group = v / each, c = at.run * h.groups * per + v * V;
     const bool here = r < h.high;
+    const int last = (int)a.points - 1;
     const float share = 1.f / ((float)a.points * per);
     float gamma[V], beta[V], s1[V], s2[V];
+    load_parameters<V>(a.gamma ? a.gamma + c : nullptr, 1.f, gamma);
+    load_parameters<V>(a.beta ? a.beta + c : nullptr, 0.f, beta);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
-        beta[e] = a.beta ? a.beta[c + e] : 0.f;
+        beta[e] *= kUnit<ACT>;
         s1[e] = s2[e] = 0;
     }
     for (int64_t image = at.stride; image < a.images; image += h.strides) {
         const int64_t row0 = image * a.points, unit = image * a.groups + at.run * h.groups + group;
         const float mean = a.mean[unit], rstd = a.rstd[unit];
-        // x's words stay as they are until the second use, with g gamma beside them
+        // x's words stay as they are until the second use, with g beside them
         typename Values<T, V>::Held x[I];
-        float gg[I][V], t = 0, u = 0;
+        float gg[I][V], t = 0, u = 0, b1[V], b2[V], slope[V];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t point = r + (int64_t)i * h.high;
-            if (here && point < a.points) {
-                x[i] = Values<T, V>::hold((const T *)a.x + (row0 + point) * a.ldx + c);
-                Values<T, V>::load((const T *)a.dy + (row0 + point) * a.lddy + c, gg[i]);
-            }
+            // (the last point again where there is none: left out of the sums)
+            const int point = min(r + i * h.high, last);
+            x[i] = Values<T, V>::hold((const T *)a.x + (row0 + point) * a.ldx + c);
+            Values<T, V>::load((const T *)a.dy + (row0 + point) * a.lddy + c, gg[i]);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            b1[e] = b2[e] = 0;
+            slope[e] = rstd * gamma[e] * kUnit<ACT>;
         }
 #pragma unroll
         for (int i = 0; i < I; ++i)
-            if (here && r + (int64_t)i * h.high < a.points) {
+            if (here && r + i * h.high <= last) {
                 float xs[V];
                 Values<T, V>::values(x[i], xs);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    float d = xs[e] - mean;
-                    const float g = activation_gradient<ACT>(gg[i][e], __builtin_fmaf(d, rstd * gamma[e], beta[e]));
-                    d *= rstd;
-                    s1[e] += g;
-                    s2[e] = __builtin_fmaf(g, d, s2[e]);
-                    gg[i][e] = g * gamma[e];
-                    t += gg[i][e];
-                    u = __builtin_fmaf(gg[i][e], d, u);
+                    const float d = xs[e] - mean;
+                    gg[i][e] = activation_gradient<ACT>(gg[i][e], __builtin_fmaf(d, slope[e], beta[e]));
+                    b1[e] += gg[i][e];
+                    b2[e] = __builtin_fmaf(gg[i][e], d, b2[e]);
                 }
             }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            b2[e] *= rstd;
+            s1[e] += b1[e];
+            s2[e] += b2[e];
+            t = __builtin_fmaf(gamma[e], b1[e], t);
+            u = __builtin_fmaf(gamma[e], b2[e], u);
+        }
         if (!a.y)
             continue;
+        // dx = g gamma rstd - (x - mean) rstd^2 m2 - rstd m1
         const float2 m = join_groups({t, u}, h, each, group, here, of, of_group);
-        const float m1 = m.x * share, m2 = m.y * share * rstd;
+        const float m1 = -rstd * (m.x * share), m2 = -rstd * (rstd * (m.y * share));
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t point = r + (int64_t)i * h.high;
-            if (here && point < a.points) {
+            const int point = r + i * h.high;
+            if (here && point <= last) {
                 float xs[V];
                 Values<T, V>::values(x[i], xs);
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    xs[e] = rstd * __builtin_fmaf(mean - xs[e], m2, gg[i][e] - m1);
+                    xs[e] = __builtin_fmaf(gg[i][e], rstd * gamma[e], __builtin_fmaf(xs[e] - mean, m2, m1));
                 Values<T, V>::store((T *)a.y + (row0 + point) * a.ldy + c, xs);
             }
         }
@@ -212,7 +222,7 @@ struct HeldPlan {
 // Whether a group of an image fits: neighbouring groups until a point's part is
 // kLine bytes, at most eight points a thread.
 bool held_plan(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, HeldPlan *o) {
-    constexpr int kLine = 64;
+    constexpr int kLine = 32;
     const int per = channels / groups, size = dtype == HPACML_BF16 ? 2 : 4;
     o->v = size == 2 && per % 8 == 0 ? 8 : per % 4 == 0 ? 4 : 1;
     const int64_t most = (int64_t)kHeldThreads * 8;

@@ -36,6 +36,23 @@ __device__ __forceinline__ Place place_of(const GroupNorm &a, const Parts &p, in
     return q;
 }
 
+// f(points, how many of them exist) for the thread's points, kAtOnce at a time,
+// so that their loads go out together (the last again where there is none).
+constexpr int kAtOnce = 4;
+template <int V, typename F>
+__device__ __forceinline__ void over_points(const Place &q, const Parts &p, F f) {
+    for (int64_t row = q.first + q.r; row < q.last; row += kAtOnce * p.high) {
+        int64_t rows[kAtOnce];
+        int n = 0;
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) {
+            rows[b] = min(row + b * p.high, q.last - 1);
+            n += row + b * p.high < q.last;
+        }
+        f(rows, n);
+    }
+}
+
 // (mean, squares about it) of n values and of m: of both
 __device__ __forceinline__ void join_moments(float &mean, float &squares, float n, float mean2, float squares2, float m) {
     const float d = mean2 - mean, share = m / (n + m);
@@ -178,15 +195,15 @@ template <int V>
 struct Channels {
     float mean[V], rstd[V], gamma[V], beta[V];
     __device__ __forceinline__ void load(const GroupNorm &a, int64_t image, int c, const float *means, const float *rstds) {
+        // (whole vectors: channels c .. c + V - 1 exist)
         const int per = a.channels / a.groups;
+        load_parameters<V>(a.gamma ? a.gamma + c : nullptr, 1.f, gamma);
+        load_parameters<V>(a.beta ? a.beta + c : nullptr, 0.f, beta);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const int ce = min(c + e, a.channels - 1);
-            const int64_t at = image * a.groups + ce / per;
+            const int64_t at = image * a.groups + (c + e) / per;
             mean[e] = means[at];
             rstd[e] = rstds[at];
-            gamma[e] = a.gamma ? a.gamma[ce] : 1.f;
-            beta[e] = a.beta ? a.beta[ce] : 0.f;
         }
     }
 };
@@ -202,15 +219,22 @@ __global__ __launch_bounds__(256) void parts_apply_kernel(GroupNorm a, Parts p, 
 #pragma unroll
         for (int e = 0; e < V; ++e)
             k.gamma[e] *= k.rstd[e];
-#pragma unroll 4
-        for (int64_t row = q.first + q.r; row < q.last; row += p.high) {
-            float v[V];
-            Values<T, V>::load((const T *)a.x + row * a.ldx + q.c, v);
+        over_points<V>(q, p, [&](const int64_t (&rows)[kAtOnce], int n) {
+            typename Values<T, V>::Held w[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                v[e] = activation<ACT>(__builtin_fmaf(v[e] - k.mean[e], k.gamma[e], k.beta[e]));
-            Values<T, V>::store((T *)a.y + row * a.ldy + q.c, v);
-        }
+            for (int b = 0; b < kAtOnce; ++b)
+                w[b] = Values<T, V>::hold((const T *)a.x + rows[b] * a.ldx + q.c);
+#pragma unroll
+            for (int b = 0; b < kAtOnce; ++b)
+                if (b < n) {
+                    float v[V];
+                    Values<T, V>::values(w[b], v);
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        v[e] = activation<ACT>(__builtin_fmaf(v[e] - k.mean[e], k.gamma[e], k.beta[e]));
+                    Values<T, V>::store((T *)a.y + rows[b] * a.ldy + q.c, v);
+                }
+        });
     }
 }
 
@@ -227,19 +251,34 @@ __global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, f
         Channels<V> k;
         if (q.here) {
             k.load(a, q.image, q.c, a.mean, a.rstd);
-#pragma unroll 4
-            for (int64_t row = q.first + q.r; row < q.last; row += p.high) {
-                float v[V], g[V];
-                Values<T, V>::load((const T *)a.x + row * a.ldx + q.c, v);
-                Values<T, V>::load((const T *)a.dy + row * a.lddy + q.c, g);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float d = v[e] - k.mean[e];
-                    const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.rstd[e] * k.gamma[e], k.beta[e]));
-                    s1[e] += t;
-                    s2[e] = __builtin_fmaf(t, d, s2[e]);
-                }
+            for (int e = 0; e < V; ++e) {
+                k.gamma[e] *= k.rstd[e];
+                k.gamma[e] *= kUnit<ACT>;
+                k.beta[e] *= kUnit<ACT>;
             }
+            over_points<V>(q, p, [&](const int64_t (&rows)[kAtOnce], int n) {
+                typename Values<T, V>::Held w[kAtOnce], o[kAtOnce];
+#pragma unroll
+                for (int b = 0; b < kAtOnce; ++b) {
+                    w[b] = Values<T, V>::hold((const T *)a.x + rows[b] * a.ldx + q.c);
+                    o[b] = Values<T, V>::hold((const T *)a.dy + rows[b] * a.lddy + q.c);
+                }
+#pragma unroll
+                for (int b = 0; b < kAtOnce; ++b)
+                    if (b < n) {
+                        float v[V], g[V];
+                        Values<T, V>::values(w[b], v);
+                        Values<T, V>::values(o[b], g);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const float d = v[e] - k.mean[e];
+                            const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.gamma[e], k.beta[e]));
+                            s1[e] += t;
+                            s2[e] = __builtin_fmaf(t, d, s2[e]);
+                        }
+                    }
+            });
         }
 #pragma unroll
         for (int e = 0; e < V; ++e)
@@ -298,27 +337,40 @@ __global__ __launch_bounds__(256) void parts_dx_kernel(GroupNorm a, Parts p, con
             continue;
         Channels<V> k;
         k.load(a, q.image, q.c, a.mean, a.rstd);
-        float m1[V], m2[V];
+        // dx = g gamma rstd - (x - mean) rstd^2 m2 - rstd m1
+        float slope[V], shift[V], scale[V];
         const int per = a.channels / a.groups;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float2 m = means[q.image * a.groups + min(q.c + e, a.channels - 1) / per];
-            m1[e] = m.x;
-            m2[e] = m.y;
+            shift[e] = -k.rstd[e] * m.x;
+            slope[e] = -k.rstd[e] * (k.rstd[e] * m.y);
+            scale[e] = k.gamma[e] * k.rstd[e];
+            k.gamma[e] = scale[e] * kUnit<ACT>;
+            k.beta[e] *= kUnit<ACT>;
         }
-#pragma unroll 4
-        for (int64_t row = q.first + q.r; row < q.last; row += p.high) {
-            float v[V], g[V];
-            Values<T, V>::load((const T *)a.x + row * a.ldx + q.c, v);
-            Values<T, V>::load((const T *)a.dy + row * a.lddy + q.c, g);
+        over_points<V>(q, p, [&](const int64_t (&rows)[kAtOnce], int n) {
+            typename Values<T, V>::Held w[kAtOnce], o[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float d = v[e] - k.mean[e];
-                const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.rstd[e] * k.gamma[e], k.beta[e])) * k.gamma[e];
-                v[e] = k.rstd[e] * ((t - m1[e]) - d * k.rstd[e] * m2[e]);
+            for (int b = 0; b < kAtOnce; ++b) {
+                w[b] = Values<T, V>::hold((const T *)a.x + rows[b] * a.ldx + q.c);
+                o[b] = Values<T, V>::hold((const T *)a.dy + rows[b] * a.lddy + q.c);
             }
-            Values<T, V>::store((T *)a.y + row * a.ldy + q.c, v);
-        }
+#pragma unroll
+            for (int b = 0; b < kAtOnce; ++b)
+                if (b < n) {
+                    float v[V], g[V];
+                    Values<T, V>::values(w[b], v);
+                    Values<T, V>::values(o[b], g);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float d = v[e] - k.mean[e];
+                        const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.gamma[e], k.beta[e]));
+                        v[e] = __builtin_fmaf(t, scale[e], __builtin_fmaf(d, slope[e], shift[e]));
+                    }
+                    Values<T, V>::store((T *)a.y + rows[b] * a.ldy + q.c, v);
+                }
+        });
     }
 }
 

@@ -31,12 +31,23 @@ struct RowLane {
             const int v = lane + i * p.lanes;
             here[i] = group < a.groups && v < p.vectors;
             c[i] = here[i] ? group * per + v * V : 0;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                gamma[i][e] = a.gamma ? a.gamma[c[i] + e] : 1.f;
-                beta[i][e] = a.beta ? a.beta[c[i] + e] : 0.f;
-            }
         }
+        if (a.gamma)
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                load_parameters<V>(a.gamma + c[i], 1.f, gamma[i]);
+        else
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                load_parameters<V>(nullptr, 1.f, gamma[i]);
+        if (a.beta)
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                load_parameters<V>(a.beta + c[i], 0.f, beta[i]);
+        else
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                load_parameters<V>(nullptr, 0.f, beta[i]);
     }
     __device__ __forceinline__ void load(const T *row, float (&v)[I][V]) const {
 #pragma unroll
@@ -125,7 +136,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float d = v[i][e] - mean;
-                const float o = activation_gradient<ACT>(g[i][e], __builtin_fmaf(d, rstd * k.gamma[i][e], k.beta[i][e]));
+                const float o = activation_gradient<ACT>(g[i][e], __builtin_fmaf(d, rstd * k.gamma[i][e] * kUnit<ACT>, k.beta[i][e] * kUnit<ACT>));
                 v[i][e] = d * rstd;
                 s1[i][e] += o;
                 s2[i][e] = __builtin_fmaf(o, v[i][e], s2[i][e]);
