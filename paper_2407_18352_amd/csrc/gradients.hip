@@ -57,30 +57,57 @@ __device__ __forceinline__ void values_of(u32x4 u, float (&v)[per_load<T>]) {
     }
 }
 
-template <bool MAX, typename T>
-__device__ __forceinline__ uint64_t chunk_norm(const T *p, int32_t count, uint64_t t) {
-    constexpr int kPer = per_load<T>;
+// f(index of the load's first value, its words) for the thread's whole loads of a
+// run, eight under way together, and g(index) for a value of its end.
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void over_chunk(const T *p, int32_t count, F f, G g) {
+    constexpr int kPer = per_load<T>, kAtOnce = 8;
     const int32_t whole = count / kPer;
-#pragma unroll 4
-    for (int32_t i = threadIdx.x; i < whole; i += 256) {
-        float v[kPer];
-        values_of<T>(*(const u32x4_any *)(p + i * kPer), v);
+    int32_t i = threadIdx.x;
+    for (; i + (kAtOnce - 1) * 256 < whole; i += kAtOnce * 256) {
+        u32x4 w[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            t = Partial<MAX>::with(t, v[e]);
+        for (int b = 0; b < kAtOnce; ++b)
+            w[b] = *(const u32x4_any *)(p + (i + b * 256) * kPer);
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b)
+            f((i + b * 256) * kPer, w[b]);
     }
-    const int32_t i = whole * kPer + threadIdx.x;
-    return i < count ? Partial<MAX>::with(t, load_value(p + i)) : t;
+    for (; i < whole; i += 256)
+        f(i * kPer, *(const u32x4_any *)(p + i * kPer));
+    const int32_t end = whole * kPer + (int32_t)threadIdx.x;
+    if (end < count)
+        g(end);
+}
+
+// into four sums: one would wait for itself at every value
+template <bool MAX, typename T>
+__device__ __forceinline__ void chunk_norm(const T *p, int32_t count, uint64_t (&t)[4]) {
+    over_chunk(p, count,
+               [&](int32_t, u32x4 w) {
+                   float v[per_load<T>];
+                   values_of<T>(w, v);
+#pragma unroll
+                   for (int e = 0; e < per_load<T>; ++e)
+                       t[e % 4] = Partial<MAX>::with(t[e % 4], v[e]);
+               },
+               [&](int32_t i) { t[0] = Partial<MAX>::with(t[0], load_value(p + i)); });
 }
 
 template <bool MAX>
 __global__ __launch_bounds__(256) void norm_kernel(const GradChunk *chunks, int64_t n, uint64_t *partial) {
     __shared__ uint64_t of_wave[4];
-    uint64_t t = 0;
+    uint64_t sums[4] = {0, 0, 0, 0};
+    GradChunk next = chunks[blockIdx.x];
     for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
-        const GradChunk g = chunks[c];
-        t = g.types & 1 ? chunk_norm<MAX>((const uint16_t *)g.from, g.count, t) : chunk_norm<MAX>((const float *)g.from, g.count, t);
+        const GradChunk g = next;
+        next = chunks[min(c + gridDim.x, n - 1)];
+        if (g.types & 1)
+            chunk_norm<MAX>((const uint16_t *)g.from, g.count, sums);
+        else
+            chunk_norm<MAX>((const float *)g.from, g.count, sums);
     }
+    uint64_t t = Partial<MAX>::join(Partial<MAX>::join(sums[0], sums[1]), Partial<MAX>::join(sums[2], sums[3]));
     t = join_block<MAX>(t, of_wave);
     if (threadIdx.x == 0)
         partial[blockIdx.x] = t;
@@ -107,44 +134,47 @@ __global__ __launch_bounds__(256) void join_norm_kernel(const uint64_t *partial,
 template <typename T, typename U>
 __device__ __forceinline__ void chunk_scale(const T *p, U *to, int32_t count, float f) {
     constexpr int kPer = per_load<T>;
-    const int32_t whole = count / kPer;
-#pragma unroll 4
-    for (int32_t i = threadIdx.x; i < whole; i += 256) {
-        float v[kPer];
-        values_of<T>(*(const u32x4_any *)(p + i * kPer), v);
-        u32x4 out[kPer * sizeof(U) / 16 ? kPer * sizeof(U) / 16 : 1];
-        if constexpr (sizeof(U) == 4) {
+    over_chunk(p, count,
+               [&](int32_t i, u32x4 w) {
+                   float v[kPer];
+                   values_of<T>(w, v);
+                   if constexpr (sizeof(U) == 4) {
 #pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                out[e / 4][e % 4] = __builtin_bit_cast(uint32_t, v[e] * f);
+                       for (int q = 0; q < kPer / 4; ++q) {
+                           f32x4 out;
 #pragma unroll
-            for (int e = 0; e < kPer / 4; ++e)
-                *(u32x4_any *)(to + i * kPer + e * 4) = out[e];
-        } else if constexpr (kPer == 8) {
+                           for (int e = 0; e < 4; ++e)
+                               out[e] = v[q * 4 + e] * f;
+                           *(f32x4_any *)(to + i + q * 4) = out;
+                       }
+                   } else if constexpr (kPer == 8) {
+                       u32x4 out;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                out[0][e] = pack_bf16(v[2 * e] * f, v[2 * e + 1] * f);
-            *(u32x4_any *)(to + i * kPer) = out[0];
-        } else {
-#pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                store_value(to + i * kPer + e, v[e] * f);
-        }
-    }
-    const int32_t i = whole * kPer + threadIdx.x;
-    if (i < count)
-        store_value(to + i, load_value(p + i) * f);
+                       for (int e = 0; e < 4; ++e)
+                           out[e] = pack_bf16(v[2 * e] * f, v[2 * e + 1] * f);
+                       *(u32x4_any *)(to + i) = out;
+                   } else {
+                       typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                       typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+                       *(u32x2_any *)(to + i) = u32x2{pack_bf16(v[0] * f, v[1] * f), pack_bf16(v[2] * f, v[3] * f)};
+                   }
+               },
+               [&](int32_t i) { store_value(to + i, load_value(p + i) * f); });
 }
 
 template <bool MAX>
 __global__ __launch_bounds__(256) void clip_kernel(const GradChunk *chunks, int64_t n, const uint64_t *partial, int blocks, double most, float *norm) {
     __shared__ uint64_t of_wave[4];
+    GradChunk next{};
+    if (n > 0)
+        next = chunks[blockIdx.x];
     const double d = joined<MAX>(partial, blocks, of_wave), q = most / (d + 1e-6);
     const float f = (float)(q > 1.0 ? 1.0 : q);         // a NaN stays one
     if (blockIdx.x == 0 && threadIdx.x == 0)
         *norm = (float)d;
     for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
-        const GradChunk g = chunks[c];
+        const GradChunk g = next;
+        next = chunks[min(c + gridDim.x, n - 1)];
         if (f == 1.f && g.from == g.to)
             continue;
         if (g.types == 0)

@@ -20,7 +20,7 @@ constexpr size_t kGradScratch = kGradBlocks * 8;
 // Values of a chunk in a set of `total`: enough chunks for the chip, and not
 // more than a block's work is worth.
 inline int64_t grad_chunk(int64_t total) {
-    const int64_t per = total / 4096 / 1024 * 1024;
+    const int64_t per = total / 8192 / 1024 * 1024;
     return per < 2048 ? 2048 : per > 32768 ? 32768 : per;
 }
 

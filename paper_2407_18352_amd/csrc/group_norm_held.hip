@@ -222,7 +222,7 @@ struct HeldPlan {
 // Whether a group of an image fits: neighbouring groups until a point's part is
 // kLine bytes, at most eight points a thread.
 bool held_plan(int32_t dtype, int64_t images, int64_t points, int32_t channels, int32_t groups, HeldPlan *o) {
-    constexpr int kLine = 32;
+    constexpr int kLine = 64;
     const int per = channels / groups, size = dtype == HPACML_BF16 ? 2 : 4;
     o->v = size == 2 && per % 8 == 0 ? 8 : per % 4 == 0 ? 4 : 1;
     const int64_t most = (int64_t)kHeldThreads * 8;

@@ -142,7 +142,8 @@ __global__ __launch_bounds__(256) void parts_moments_kernel(GroupNorm a, Parts p
     }
 }
 
-__device__ __forceinline__ double join_block(double t, double (&of_wave)[4]) {
+template <int THREADS>
+__device__ __forceinline__ double join_block(double t, double (&of_wave)[THREADS / 64]) {
 #pragma unroll
     for (int s = 1; s < 64; s *= 2)
         t += __shfl_xor(t, s);
@@ -150,39 +151,44 @@ __device__ __forceinline__ double join_block(double t, double (&of_wave)[4]) {
     if ((threadIdx.x & 63) == 0)
         of_wave[threadIdx.x >> 6] = t;
     __syncthreads();
-    return (of_wave[0] + of_wave[1]) + (of_wave[2] + of_wave[3]);
+    t = of_wave[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w)
+        t += of_wave[w];
+    return t;
 }
 
 // The partial results of an image's group, `per` channels of each run: a thread
 // takes every so many runs of one channel (with one index over all of them, and
 // its divisions, 2049 runs of 4 channels took 23 us).
-template <typename F>
+template <int THREADS, typename F>
 __device__ __forceinline__ void over_runs(int per, uint32_t runs, F f) {
-    const int across = min(per, 256), high = 256 / across, c0 = threadIdx.x % across, r0 = threadIdx.x / across;
+    const int across = min(per, THREADS), high = THREADS / across, c0 = threadIdx.x % across, r0 = threadIdx.x / across;
     if (r0 < high)
         for (int c = c0; c < per; c += across)
-#pragma unroll 4
+#pragma unroll 8
             for (uint32_t r = r0; r < runs; r += high)
                 f(c, r);
 }
 
 // A block per image and group: mean and rstd.
-__global__ __launch_bounds__(256) void parts_join_kernel(GroupNorm a, Parts p, const float2 *part, float *mean_to, float *rstd_to) {
-    __shared__ double of_wave[4];
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void parts_join_kernel(GroupNorm a, Parts p, const float2 *part, float *mean_to, float *rstd_to) {
+    __shared__ double of_wave[THREADS / 64];
     for (int64_t unit = blockIdx.x; unit < a.images * a.groups; unit += gridDim.x) {
         const int64_t image = unit / a.groups;
         const int per = a.channels / a.groups, c0 = (int)(unit % a.groups) * per;
         const float2 *at = part + image * p.runs * a.channels + c0;
         auto values = [&](uint32_t r) { return (double)min(p.run, a.points - r * p.run); };
         double t = 0;
-        over_runs(per, p.runs, [&](int c, uint32_t r) { t += values(r) * at[(int64_t)r * a.channels + c].x; });
-        const double n = (double)a.points * per, mean = join_block(t, of_wave) / n;
+        over_runs<THREADS>(per, p.runs, [&](int c, uint32_t r) { t += values(r) * at[(int64_t)r * a.channels + c].x; });
+        const double n = (double)a.points * per, mean = join_block<THREADS>(t, of_wave) / n;
         t = 0;
-        over_runs(per, p.runs, [&](int c, uint32_t r) {
+        over_runs<THREADS>(per, p.runs, [&](int c, uint32_t r) {
             const float2 o = at[(int64_t)r * a.channels + c];
             t += (double)o.y + values(r) * (o.x - mean) * (o.x - mean);
         });
-        t = join_block(t, of_wave);
+        t = join_block<THREADS>(t, of_wave);
         if (threadIdx.x == 0) {
             mean_to[unit] = (float)mean;
             rstd_to[unit] = (float)(1.0 / sqrt(t / n + (double)a.eps));
@@ -308,22 +314,23 @@ __global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, f
 }
 
 // A block per image and group: the means of g gamma and g gamma (x - mean) rstd.
-__global__ __launch_bounds__(256) void parts_means_kernel(GroupNorm a, Parts p, const float *part, float2 *means) {
-    __shared__ double of_wave[4];
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void parts_means_kernel(GroupNorm a, Parts p, const float *part, float2 *means) {
+    __shared__ double of_wave[THREADS / 64];
     for (int64_t unit = blockIdx.x; unit < a.images * a.groups; unit += gridDim.x) {
         const int64_t image = unit / a.groups;
         const int per = a.channels / a.groups, c0 = (int)(unit % a.groups) * per;
         const float *at = part + image * p.runs * 2 * a.channels + c0;
         double t = 0, u = 0;
-        over_runs(per, p.runs, [&](int c, uint32_t r) {
+        over_runs<THREADS>(per, p.runs, [&](int c, uint32_t r) {
             const float *o = at + (int64_t)r * 2 * a.channels + c;
             const double gamma = a.gamma ? a.gamma[c0 + c] : 1.f;
             t += gamma * o[0];
             u += gamma * o[a.channels];
         });
         const double n = (double)a.points * per;
-        t = join_block(t, of_wave) / n;
-        u = join_block(u, of_wave) / n;
+        t = join_block<THREADS>(t, of_wave) / n;
+        u = join_block<THREADS>(u, of_wave) / n;
         if (threadIdx.x == 0)
             means[unit] = {(float)t, (float)u};
     }
@@ -389,8 +396,9 @@ Parts parts_of(int32_t dtype, int64_t images, int64_t points, int32_t channels) 
     p.high = 1;
     while (p.high * 2 * p.across <= 256)
         p.high *= 2;
-    // about eight blocks for each of 256 CUs, runs of no less than eight values a thread
-    const int64_t want = 2048 / images / p.column_tiles + 1, least = 8 * p.high;
+    // two blocks for each of 256 CUs, runs of no less than eight values a thread
+    // (norm_grid: 93 us with eight blocks, 89 us with two, whose runs are fewer to join)
+    const int64_t want = 512 / images / p.column_tiles + 1, least = 8 * p.high;
     int64_t run = (points + want - 1) / want;
     run = (run + least - 1) / least * least;
     p.run = run;
@@ -402,6 +410,9 @@ Parts parts_of(int32_t dtype, int64_t images, int64_t points, int32_t channels) 
 // A grid's blocks of 256 threads: a launch has fewer than 2^32 threads.
 uint32_t grid_of(int64_t blocks) { return (uint32_t)(blocks < 1 << 20 ? blocks : 1 << 20); }
 
+// Whether larger blocks join the parts of a group: there are fewer groups than CUs.
+bool few_units(const GroupNorm &a) { return a.images * a.groups < 256; }
+
 size_t rounded(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T, int V>
@@ -411,7 +422,10 @@ hipError_t forward_parts(const GroupNorm &a, const Parts &p, hipStream_t stream)
     float *moments = (float *)(a.scratch + rounded((size_t)a.images * p.runs * a.channels * 8));
     float *mean = a.mean ? a.mean : moments, *rstd = a.mean ? a.rstd : moments + a.images * a.groups;
     parts_moments_kernel<T, V><<<blocks, 256, 0, stream>>>(a, p, part);
-    parts_join_kernel<<<grid_of(a.images * a.groups), 256, 0, stream>>>(a, p, part, mean, rstd);
+    if (few_units(a))
+        parts_join_kernel<1024><<<grid_of(a.images * a.groups), 1024, 0, stream>>>(a, p, part, mean, rstd);
+    else
+        parts_join_kernel<256><<<grid_of(a.images * a.groups), 256, 0, stream>>>(a, p, part, mean, rstd);
     return with_activation(a.act, [&](auto act) {
         parts_apply_kernel<T, V, decltype(act)::value><<<blocks, 256, 0, stream>>>(a, p, mean, rstd);
         return hipGetLastError();
@@ -432,7 +446,10 @@ hipError_t backward_parts(const GroupNorm &a, const Parts &p, hipStream_t stream
     if (e == hipSuccess)
         e = launch_parameters(a, part, rows, room, stream);
     if (a.y && e == hipSuccess) {
-        parts_means_kernel<<<grid_of(a.images * a.groups), 256, 0, stream>>>(a, p, part, means);
+        if (few_units(a))
+            parts_means_kernel<1024><<<grid_of(a.images * a.groups), 1024, 0, stream>>>(a, p, part, means);
+        else
+            parts_means_kernel<256><<<grid_of(a.images * a.groups), 256, 0, stream>>>(a, p, part, means);
         e = with_activation(a.act, [&](auto act) {
             parts_dx_kernel<T, V, decltype(act)::value><<<blocks, 256, 0, stream>>>(a, p, means);
             return hipGetLastError();
