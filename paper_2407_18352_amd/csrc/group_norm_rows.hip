@@ -8,28 +8,31 @@ namespace {
 // ---- images of one point ------------------------------------------------------------
 
 // L lanes (a power of two) hold a group of a row, I vectors of V channels each;
-// a wave has 64 / L neighbouring groups and goes from row to row, so that a
-// lane's channels stay the same.
+// a wave has 64 / L neighbouring groups, or all groups of as many rows as it has
+// room for, and goes from row to row, so that a lane's channels stay the same.
 constexpr int kRowWaves = 8;
 struct Rows {
     int32_t lanes, vectors, column_blocks;     // L; of a group; waves that a row takes
+    int32_t rows;                              // of a wave at a time
     int32_t strides;                           // blocks of the same groups
 };
 
 template <typename T, int V, int I>
 struct RowLane {
-    int group, lane;
+    int group, lane, sub;                      // sub: its row among the wave's
     bool here[I];
     int c[I];
     float gamma[I][V], beta[I][V];
     __device__ __forceinline__ RowLane(const GroupNorm &a, const Rows &p, int column_block) {
         const int per = a.channels / a.groups, l = threadIdx.x & 63;
-        group = column_block * (64 / p.lanes) + l / p.lanes;
+        const int slot = l / p.lanes;
+        sub = p.column_blocks > 1 ? 0 : slot / a.groups;
+        group = p.column_blocks > 1 ? column_block * (64 / p.lanes) + slot : slot % a.groups;
         lane = l % p.lanes;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * p.lanes;
-            here[i] = group < a.groups && v < p.vectors;
+            here[i] = sub < p.rows && group < a.groups && v < p.vectors;
             c[i] = here[i] ? group * per + v * V : 0;
         }
         if (a.gamma)
@@ -63,15 +66,15 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_forward_kernel(GroupNorm 
     const RowLane<T, V, I> k(a, p, column_block);
     const float share = 1.f / (float)(a.channels / a.groups);
     constexpr int kAtOnce = V * I <= 16 ? 2 : 1;     // rows whose loads go out together
-    const int64_t step = (int64_t)p.strides * kRowWaves;
-    for (int64_t first = (int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave; first < a.images; first += step * kAtOnce) {
+    const int64_t step = (int64_t)p.strides * kRowWaves * p.rows;
+    for (int64_t first = ((int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave) * p.rows; first < a.images; first += step * kAtOnce) {
         float v[kAtOnce][I][V];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u)
-            k.load((const T *)a.x + min(first + u * step, a.images - 1) * a.ldx, v[u]);
+            k.load((const T *)a.x + min(first + u * step + k.sub, a.images - 1) * a.ldx, v[u]);
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            const int64_t row = first + u * step;
+            const int64_t row = first + u * step + k.sub;
             float t = 0, s = 0;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
@@ -93,17 +96,16 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_forward_kernel(GroupNorm 
                 s += k.here[i] ? o : 0.f;
             }
             const float rstd = __builtin_amdgcn_rsqf(join_lanes(s, p.lanes) * share + a.eps);      // 1 ulp
-            if (row >= a.images)
-                continue;
+            const bool live = row < a.images;
 #pragma unroll
             for (int i = 0; i < I; ++i)
-                if (k.here[i]) {
+                if (live && k.here[i]) {
 #pragma unroll
                     for (int e = 0; e < V; ++e)
                         v[u][i][e] = activation<ACT>(__builtin_fmaf(v[u][i][e], rstd * k.gamma[i][e], k.beta[i][e]));
                     Values<T, V>::store((T *)a.y + row * a.ldy + k.c[i], v[u][i]);
                 }
-            if (a.mean && k.lane == 0 && k.here[0]) {
+            if (a.mean && live && k.lane == 0 && k.here[0]) {
                 a.mean[row * a.groups + k.group] = mean;
                 a.rstd[row * a.groups + k.group] = rstd;
             }
@@ -124,7 +126,11 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm
 #pragma unroll
         for (int e = 0; e < V; ++e)
             s1[i][e] = s2[i][e] = 0;
-    for (int64_t row = (int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave; row < a.images; row += (int64_t)p.strides * kRowWaves) {
+    for (int64_t first = ((int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave) * p.rows; first < a.images;
+         first += (int64_t)p.strides * kRowWaves * p.rows) {
+        // (a lane without a row has the last one again, and leaves it out)
+        const bool live = first + k.sub < a.images;
+        const int64_t row = min(first + k.sub, a.images - 1);
         float v[I][V], g[I][V], t = 0, u = 0;
         k.load((const T *)a.x + row * a.ldx, v);
         k.load((const T *)a.dy + row * a.lddy, g);
@@ -138,8 +144,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm
                 const float d = v[i][e] - mean;
                 const float o = activation_gradient<ACT>(g[i][e], __builtin_fmaf(d, rstd * k.gamma[i][e] * kUnit<ACT>, k.beta[i][e] * kUnit<ACT>));
                 v[i][e] = d * rstd;
-                s1[i][e] += o;
-                s2[i][e] = __builtin_fmaf(o, v[i][e], s2[i][e]);
+                s1[i][e] += live ? o : 0.f;
+                s2[i][e] += live ? o * v[i][e] : 0.f;
                 g[i][e] = o * k.gamma[i][e];
                 to += g[i][e];
                 uo = __builtin_fmaf(g[i][e], v[i][e], uo);
@@ -151,7 +157,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm
             const float m1 = join_lanes(t, p.lanes) * share, m2 = join_lanes(u, p.lanes) * share;
 #pragma unroll
             for (int i = 0; i < I; ++i)
-                if (k.here[i]) {
+                if (live && k.here[i]) {
 #pragma unroll
                     for (int e = 0; e < V; ++e)
                         v[i][e] = rstd * ((g[i][e] - m1) - v[i][e] * m2);
@@ -168,15 +174,17 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm
         for (int e = 0; e < V; ++e)
             of[wave][lane][e] = {s1[i][e], s2[i][e]};
         __syncthreads();
-        if (wave == 0 && k.here[i])
+        if (wave == 0 && k.here[i] && k.sub == 0)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                float2 t = of[0][lane][e];
+                float2 t = {0.f, 0.f};
+                for (int r = 0; r < p.rows; ++r)
 #pragma unroll
-                for (int w = 1; w < kRowWaves; ++w) {
-                    t.x += of[w][lane][e].x;
-                    t.y += of[w][lane][e].y;
-                }
+                    for (int w = 0; w < kRowWaves; ++w) {
+                        const float2 o = of[w][lane + r * a.groups * p.lanes][e];
+                        t.x += o.x;
+                        t.y += o.y;
+                    }
                 to[k.c[i] + e] = t.x;
                 to[a.channels + k.c[i] + e] = t.y;
             }
@@ -206,7 +214,8 @@ bool rows_plan(int32_t dtype, int64_t images, int64_t points, int32_t channels, 
         return false;
     const int at_a_time = 64 / o->p.lanes;
     o->p.column_blocks = (groups + at_a_time - 1) / at_a_time;
-    const int64_t most = (images + kRowWaves - 1) / kRowWaves, want = 1024 / o->p.column_blocks + 1;
+    o->p.rows = at_a_time / groups < 1 ? 1 : at_a_time / groups;
+    const int64_t at_once = (int64_t)kRowWaves * o->p.rows, most = (images + at_once - 1) / at_once, want = 1024 / o->p.column_blocks + 1;
     o->p.strides = (int32_t)(most < want ? most : want);
     o->grid = (uint32_t)(o->p.strides * o->p.column_blocks);
     return true;

@@ -1,0 +1,174 @@
+"""A surrogate learned with its layers in 8-bit floating point, group norm
+between them and its gradients clipped by their common norm, and answering
+with the same layers.
+
+    python -m paper_2407_18352_amd.surrogatef8 [--points N] [--dims 5,256,256,1] [--groups G] [--steps K]
+
+The command learns what ``surrogate8``'s does (European calls, recorded through
+the region's tensor maps).  The class holds what a training loop and a server
+need: ``update`` lays the weights out after an optimizer's step, ``forward``
+keeps what ``backward`` reads, ``clip`` scales the gradients, ``answer`` is
+``forward`` without keeping anything.
+"""
+from __future__ import annotations
+
+import argparse
+import math
+
+import torch
+
+from . import _abi, api
+from .surrogate8 import _rows, collect
+
+
+class SurrogateF8:
+    """A perceptron of the widths ``dims`` with group norm and ``act`` (ACT_SILU
+    or ACT_RELU) behind every hidden layer: a_l = act(norm(a_{l-1} W_l^T + b_l)).
+    fp32 parameters with gradients in ``.grad``; activations between layers in
+    bf16, products of 8-bit floats with a scale for each 128 values.  ``backward``
+    is that of the last ``forward`` and with the weights of the last ``update``.
+    Calls may come on one stream after another, each works after the one before;
+    from several threads at a time they may not."""
+
+    def __init__(self, dims, groups: int = 8, act: int = _abi.ACT_SILU, eps: float = 1e-5, seed: int = 0):
+        g = torch.Generator().manual_seed(seed)
+        self.dims, self.groups, self.act, self.eps = [int(d) for d in dims], int(groups), int(act), float(eps)
+        for d in self.dims[1:-1]:
+            if d % self.groups:
+                raise ValueError("a hidden width of %d is no multiple of %d groups" % (d, self.groups))
+        self.W = [(torch.randn((o, i), generator=g) * math.sqrt(2 / i)).cuda().requires_grad_()
+                  for i, o in zip(self.dims, self.dims[1:])]
+        self.b = [torch.zeros(o, device="cuda").requires_grad_() for o in self.dims[1:]]
+        self.gamma = [torch.ones(d, device="cuda").requires_grad_() for d in self.dims[1:-1]]
+        self.beta = [torch.zeros(d, device="cuda").requires_grad_() for d in self.dims[1:-1]]
+        for p in self.parameters():
+            p.grad = torch.zeros_like(p)
+        with torch.no_grad():
+            self.layers = [api.LinearF8(w, b, learn=True) for w, b in zip(self.W, self.b)]
+        self.rows, self.kept, self.stats, self.z, self.set, self.stream = -1, [], [], [], None, torch.cuda.current_stream()
+
+    def parameters(self):
+        return self.W + self.b + self.gamma + self.beta
+
+    def _buffers(self):
+        layers = [t for a in self.layers for t in (a.W.codes, a.W.scales, a.Wt.codes, a.Wt.scales, a.b)]
+        return layers + [t for k in self.kept for t in (k.codes, k.scales)] + [t for s in self.stats for t in s] + self.z
+
+    def _in_order(self):
+        """What a call keeps is used again by the next: one on another stream
+        than the last waits for it.  (A capture into a graph begins after a
+        synchronization, and a stream in it may not wait for one outside.)"""
+        now = torch.cuda.current_stream()
+        if now != self.stream and not torch.cuda.is_current_stream_capturing():
+            now.wait_stream(self.stream)
+            for t in self._buffers():
+                t.record_stream(now)
+        self.stream = now
+
+    @torch.no_grad()
+    def update(self):
+        """Lays the weights and biases out as they are now."""
+        self._in_order()
+        for layer, w, b in zip(self.layers, self.W, self.b):
+            layer.update(w, b)
+
+    def _run(self, x, keep):
+        n, a, last = x.shape[0], _rows(x if x.dtype in (torch.float32, torch.bfloat16) else x.float()), len(self.layers) - 1
+        for l, layer in enumerate(self.layers):
+            z = torch.empty((n, layer.n_out), dtype=torch.float32 if l == last else torch.bfloat16, device="cuda")
+            api.linearf8(layer, a, z, kept=self.kept[l] if keep else None)
+            if l == last:
+                return z
+            a = torch.empty_like(z)
+            mean, rstd = self.stats[l] if keep else (None, None)
+            api.group_norm(z, a, 1, self.groups, self.gamma[l], self.beta[l], self.eps, self.act, mean, rstd)
+            if keep:
+                self.z.append(z)
+
+    @torch.no_grad()
+    def forward(self, x):
+        """Outputs [n][dims[-1]] (fp32) of inputs [n][dims[0]]; keeps what
+        ``backward`` reads."""
+        self._in_order()
+        n = x.shape[0]
+        if self.rows != n:
+            self.rows, self.kept = n, [api.MatrixF8(d, n) for d in self.dims[:-1]]
+            self.stats = [tuple(torch.empty((n, self.groups), device="cuda") for _ in range(2)) for _ in self.dims[1:-1]]
+        self.z = []
+        return self._run(x, True)
+
+    @torch.no_grad()
+    def answer(self, x):
+        """Outputs (fp32) of inputs [n][dims[0]], with nothing kept."""
+        self._in_order()
+        return self._run(x, False)
+
+    @torch.no_grad()
+    def backward(self, dy, accumulate: bool = False):
+        """Gradients of the loss in ``.grad`` (made where an optimizer has taken
+        them away) from that of the outputs."""
+        self._in_order()
+        for p in self.parameters():
+            if p.grad is None:
+                p.grad = torch.zeros_like(p)
+        dy = _rows(dy.float())
+        for l in range(len(self.layers) - 1, -1, -1):
+            if l < len(self.layers) - 1:
+                dz = torch.empty_like(self.z[l])
+                api.group_norm_backward(self.z[l], dy, 1, self.groups, *self.stats[l], dz, self.gamma[l].grad, self.beta[l].grad,
+                                        self.gamma[l], self.beta[l], self.act, accumulate)
+                dy = dz
+            dx = torch.empty((dy.shape[0], self.dims[l]), dtype=dy.dtype, device="cuda") if l else None
+            api.backwardf8(self.kept[l], dy, self.W[l].grad, self.b[l].grad, layer=self.layers[l] if l else None, dx=dx,
+                           accumulate=accumulate)
+            dy = None if dx is None else dx.to(torch.bfloat16)
+
+    @torch.no_grad()
+    def clip(self, most: float):
+        """Scales the gradients so that their common norm is at most ``most``;
+        the norm before ([1], fp32, on the device)."""
+        self._in_order()
+        grads = [p.grad for p in self.parameters()]
+        if any(g is None for g in grads):
+            raise ValueError("there are no gradients to clip")
+        if self.set is None or any(a is not b for a, b in zip(self.set.gradients, grads)):
+            self.set = api.GradientSet(grads)
+        norm = torch.empty(1, device="cuda")
+        api.clip_gradients(self.set, most, norm)
+        return norm
+
+
+# ---- the command ------------------------------------------------------------
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--points", type=int, default=65536)
+    ap.add_argument("--dims", default="5,256,256,1")
+    ap.add_argument("--groups", type=int, default=8)
+    ap.add_argument("--steps", type=int, default=300)
+    a = ap.parse_args(argv)
+    x, y = collect(a.points, 1)
+    mean, std = x.mean(0), x.std(0)
+    unit = y.std()
+    model = SurrogateF8([int(d) for d in a.dims.split(",")], a.groups)
+    opt = torch.optim.Adam(model.parameters(), lr=2e-3)
+    xn, yn = (x - mean) / std, y / unit
+    loss = None
+    for step in range(a.steps):
+        off = model.forward(xn) - yn
+        loss = off.square().mean()
+        model.backward(off * (2 / off.numel()))
+        norm = model.clip(1.0)
+        if step % 50 == 0:
+            print("step %4d: rms error %.4f of the prices' spread, gradients' norm %.3f" % (step, loss.sqrt().item(), norm.item()), flush=True)
+        opt.step()
+        model.update()
+    xs, ys = collect(a.points, 2)
+    rms = ((model.answer((xs - mean) / std) * unit - ys).square().mean().sqrt() / unit).item()
+    print("step %4d: rms error %.4f; answering new points: %.4f" % (a.steps, loss.sqrt().item(), rms))
+    return loss.sqrt().item(), rms
+
+
+if __name__ == "__main__":
+    main()

@@ -193,3 +193,27 @@ def test_no_images():
     assert (dgamma == 1).all() and (dbeta == 1).all()
     api.group_norm_backward(x, x, 3, 2, m, m, x, dgamma, dbeta)
     assert (dgamma == 0).all() and (dbeta == 0).all()
+
+
+@pytest.mark.parametrize("images, channels, groups", [(1, 64, 8), (777, 64, 8), (9001, 256, 8), (1000, 24, 3), (1000, 8, 8), (513, 40, 5), (20000, 4, 1), (77, 1024, 2)])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_few_groups_of_one_point(images, channels, groups, kind):
+    """Several rows share a wave where a row has few groups."""
+    g = torch.Generator().manual_seed(images + channels)
+    x, dy = data(g, images, 1, channels, kind, 0)
+    gamma, beta = 1 + torch.randn(channels, generator=g).cuda() * 0.3, torch.randn(channels, generator=g).cuda()
+    y, dx, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty((images, groups), device="cuda"), torch.empty((images, groups), device="cuda")
+    dgamma, dbeta = torch.empty(channels, device="cuda"), torch.empty(channels, device="cuda")
+    api.group_norm(x, y, 1, groups, gamma, beta, EPS, NONE, mean, rstd)
+    api.group_norm_backward(x, dy, 1, groups, mean, rstd, dx, dgamma, dbeta, gamma, beta)
+    want, wm, wr, h, _ = forward(x, 1, groups, gamma, beta, NONE)
+    assert ((y.double() - want).abs() <= HALF[kind] * want.abs() + 2.0 ** -20 * (1 + wr.max()) * (8 + h.abs())).all()
+    assert ((mean.double() - wm).abs() <= 2.0 ** -21 * 10).all() and ((rstd.double() - wr).abs() <= 2.0 ** -19 * wr * (1 + wr)).all()
+    h = forward(x, 1, groups, gamma, beta, NONE, moments=(mean, rstd))[3]
+    for got, each in ((dgamma, dy.double() * h), (dbeta, dy.double())):
+        assert ((got.double() - each.sum(0)).abs() <= 2.0 ** -19 * (each.abs() + 2.0 ** -20).sum(0)).all()
+    gg = (dy.double() * gamma.double()).view(images, groups, -1)
+    hh = h.view(images, groups, -1)
+    want = (rstd.double()[:, :, None] * (gg - gg.mean(2, keepdim=True) - hh * (gg * hh).mean(2, keepdim=True))).view(x.shape)
+    terms = (rstd.double()[:, :, None] * (gg.abs() + gg.abs().mean(2, keepdim=True) + hh.abs() * (gg * hh).abs().mean(2, keepdim=True))).view(x.shape)
+    assert ((dx.double() - want).abs() <= HALF[kind] * want.abs() + 2.0 ** -20 * terms + 2.0 ** -130).all()
