@@ -1,36 +1,39 @@
-// Sums of columns.  A block takes 64 columns and a run of rows, four rows at a
+// Sums of columns.  A block takes 64 columns and a run of rows, sixteen rows at a
 // time; sums are in 64 bits, so that a thousand partial results add no error.
 // One thread per column and all the rows took 58 us for 235 rows of 201 and 408
-// us for 1024 rows of 2048: latency.  Runs of 32 rows in a first launch bring
-// that to a few microseconds.
+// us for 1024 rows of 2048: latency.  Sixteen threads a column, and for more than
+// 512 rows runs of them in a first launch, bring that to a few microseconds.
 #include "columns.hpp"
 
 namespace hpacml {
 
 namespace {
 
-constexpr int64_t kRun = 32;              // rows of a run, at least
+constexpr int64_t kOneRun = 512, kRun = 128;     // rows that one launch takes; of a run otherwise, at least
 constexpr int64_t kMostRuns = 256;
 
 int64_t runs_of(int64_t rows) {
     const int64_t runs = (rows + kRun - 1) / kRun;
-    return runs < 2 ? 1 : runs > kMostRuns ? kMostRuns : runs;
+    return rows <= kOneRun ? 1 : runs > kMostRuns ? kMostRuns : runs;
 }
 
 // a.room: where the sums of the runs go, NULL: the run is all there is
-__global__ __launch_bounds__(256) void sums_kernel(ColumnSums a, int64_t run) {
-    __shared__ double of[4][64];
+__global__ __launch_bounds__(1024) void sums_kernel(ColumnSums a, int64_t run) {
+    __shared__ double of[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane, first = (int64_t)blockIdx.y * run, last = min(first + run, a.rows);
     double t = 0;
     if (c < a.width)
 #pragma unroll 8
-        for (int64_t r = first + wave; r < last; r += 4)
+        for (int64_t r = first + wave; r < last; r += 16)
             t += a.part[r * a.pitch + c];
     of[wave][lane] = t;
     __syncthreads();
     if (wave == 0 && c < a.width) {
-        const float s = (float)((of[0][lane] + of[1][lane]) + (of[2][lane] + of[3][lane]));
+#pragma unroll
+        for (int w = 1; w < 16; ++w)
+            t += of[w][lane];
+        const float s = (float)t;
         if (a.room) {
             a.room[blockIdx.y * a.width + c] = s;
             return;
@@ -54,13 +57,13 @@ hipError_t launch_column_sums(const ColumnSums &a, hipStream_t stream) {
     ColumnSums last = a;
     if (runs > 1) {
         const int64_t run = (a.rows + runs - 1) / runs;
-        sums_kernel<<<dim3(across, (uint32_t)runs), 256, 0, stream>>>(a, run);
+        sums_kernel<<<dim3(across, (uint32_t)runs), 1024, 0, stream>>>(a, run);
         last.part = a.room;
         last.rows = runs;
         last.pitch = a.width;
     }
     last.room = nullptr;
-    sums_kernel<<<across, 256, 0, stream>>>(last, last.rows);
+    sums_kernel<<<across, 1024, 0, stream>>>(last, last.rows);
     return hipGetLastError();
 }
 

@@ -95,38 +95,35 @@ constexpr uint32_t kNanCodes = 0x7F7F7F7Fu;      // of a block whose scale's byt
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
 
-// 16 neighbouring values at p, those from `have` on as 0
-__device__ __forceinline__ void load16(const float *p, int have, float (&v)[16]) {
-    if (have >= 16) {
+// 16 neighbouring values, as they lie in memory
+template <typename X>
+struct Sixteen {
+    static constexpr int kWords = (int)sizeof(X);
+    u32x4 w[kWords];
+    __device__ __forceinline__ void load(const X *p) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 t = *(const f32x4_any *)(p + 4 * i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[4 * i + e] = t[e];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            v[i] = i < have ? p[i] : 0.f;
+        for (int i = 0; i < kWords; ++i)
+            w[i] = *(const u32x4_any *)(p + i * (16 / kWords));
     }
-}
-__device__ __forceinline__ void load16(const uint16_t *p, int have, float (&v)[16]) {
-    if (have >= 16) {
+    __device__ __forceinline__ void values(float (&v)[16]) const {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const u32x4 t = *(const u32x4_any *)(p + 8 * i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[8 * i + 2 * e] = __builtin_bit_cast(float, t[e] << 16);
-                v[8 * i + 2 * e + 1] = __builtin_bit_cast(float, t[e] & 0xFFFF0000u);
+        for (int i = 0; i < 16; ++i) {
+            if constexpr (kWords == 4) {
+                const uint32_t u = w[i / 4][i % 4];
+                v[i] = __builtin_bit_cast(float, u);
+            } else {
+                const uint32_t u = w[i / 8][i / 2 % 4];
+                v[i] = __builtin_bit_cast(float, i & 1 ? u & 0xFFFF0000u : u << 16);
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            v[i] = i < have ? bf16_bits_value(p[i]) : 0.f;
     }
+};
+// the first `have` of them, 0 behind (the end of a row)
+template <typename X>
+__device__ __forceinline__ void load_some(const X *p, int have, float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        v[i] = i < have ? load_value(p + i) : 0.f;
 }
 
 // The products of 32 rows of each operand over 64 values, e4m3 with a scale

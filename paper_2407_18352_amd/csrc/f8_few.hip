@@ -2,10 +2,11 @@
 //
 // A few rows are asked for one answer at a time: what counts is reading the
 // weights once, from as many CUs as there are, and the latency of what comes
-// before and after.  A block takes 16 outputs and all the rows; its sixteen waves
+// before and after.  A block takes 16 outputs and all the rows; its waves
 // take blocks of the width in turn, straight from memory to registers, and join
 // their sums through LDS (4096 -> 4096, one row: 11.6, 9.1 and 8.4 us with 4, 8
-// and 16 waves; reading the weights alone takes 3.5).  Codes of x are formed by every block anew (or read,
+// and 16 waves, 7.7 with x's loads ahead of its codes; reading the weights alone
+// takes 3.5).  Codes of x are formed by every block anew (or read,
 // where the product is given them).  The products run on the bf16 matrix
 // instruction, to which codes times their scale are exact: there is time for it.
 #include <type_traits>
@@ -17,7 +18,9 @@ namespace f8 {
 
 namespace {
 
-constexpr int kWaves = 16;
+// Sixteen waves where their registers hold what one of them loads at a time.
+template <int NB>
+constexpr int kWavesOf = NB == 1 ? 16 : 8;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -69,20 +72,17 @@ __device__ __forceinline__ Codes read_codes(const Matrix &m, int64_t row, int gr
     return o;
 }
 
-// (of the last row where there is none: what comes of it is not stored)
+// Of 32 values of a row (the last row where there is none: what comes of it is
+// not stored).
 template <typename X>
-__device__ __forceinline__ Codes form_codes(const X *x, int64_t ldx, int64_t rows, int64_t row, int64_t k, int64_t width) {
-    float v[2][16];
+struct Row {
+    Sixteen<X> half[2];
+};
+__device__ __forceinline__ Codes form_codes(const float (&v)[2][16]) {
     uint32_t most = 0;
-    row = min(row, rows - 1);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t left = width - k - h * 16;
-        load16(x + row * ldx + k + h * 16, left > 16 ? 16 : left < 0 ? 0 : (int)left, v[h]);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            most = max(most, magnitude(v[h][e]));
-    }
+    for (int i = 0; i < 32; ++i)
+        most = max(most, magnitude(v[i / 16][i % 16]));
     most = max(most, (uint32_t)__shfl_xor((int)most, 16));
     most = max(most, (uint32_t)__shfl_xor((int)most, 32));
     Codes o;
@@ -98,7 +98,8 @@ __device__ __forceinline__ Codes form_codes(const X *x, int64_t ldx, int64_t row
 
 // X: the type of x, or void: codes are given.  NB: sixteens of rows.
 template <typename X, typename Y, int NB>
-__global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
+__global__ __launch_bounds__(64 * kWavesOf<NB>) void few_kernel(FewArgs a) {
+    constexpr int kWaves = kWavesOf<NB>;
     __shared__ f32x4 of[kWaves][NB][64];
     constexpr int kAtOnce = NB < 4 ? 2 : 1;       // blocks of the width whose loads go out together
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, group = lane >> 4;
@@ -118,15 +119,47 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
                 for (int i = 0; i < 8; ++i)
                     w[u].c[i] = 0;
         }
+        if constexpr (std::is_void<X>::value) {
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            const int64_t kb = min(first + u * kWaves, blocks - 1);
+            for (int u = 0; u < kAtOnce; ++u)
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                if constexpr (std::is_void<X>::value)
-                    x[u][b] = read_codes(a.p, b * 16 + r, group, kb, blocks);
-                else
-                    x[u][b] = form_codes((const X *)a.x, a.ldx, a.rows, b * 16 + r, kb * kBlock + group * 32, a.q.width);
+                for (int b = 0; b < NB; ++b)
+                    x[u][b] = read_codes(a.p, b * 16 + r, group, min(first + u * kWaves, blocks - 1), blocks);
+        } else {
+            auto at = [&](int u, int b) {
+                return (const X *)a.x + min((int64_t)(b * 16 + r), a.rows - 1) * a.ldx + min(first + u * kWaves, blocks - 1) * kBlock + group * 32;
+            };
+            if ((min(first + (kAtOnce - 1) * kWaves, blocks - 1) + 1) * kBlock <= a.q.width) {
+                Row<X> row[kAtOnce][NB];         // all loads before the first value
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            row[u][b].half[h].load(at(u, b) + h * 16);
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        float v[2][16];
+                        row[u][b].half[0].values(v[0]);
+                        row[u][b].half[1].values(v[1]);
+                        x[u][b] = form_codes(v);
+                    }
+            } else {
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        float v[2][16];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int64_t left = a.q.width - min(first + u * kWaves, blocks - 1) * kBlock - group * 32 - h * 16;
+                            load_some(at(u, b) + h * 16, left > 16 ? 16 : left < 0 ? 0 : (int)left, v[h]);
+                        }
+                        x[u][b] = form_codes(v);
+                    }
             }
         }
 #pragma unroll
@@ -171,11 +204,11 @@ template <typename X, typename Y>
 void launch(const FewArgs &a, hipStream_t stream) {
     const uint32_t grid = (uint32_t)((a.q.rows + 15) / 16);
     if (a.rows <= 16)
-        few_kernel<X, Y, 1><<<grid, 64 * kWaves, 0, stream>>>(a);
+        few_kernel<X, Y, 1><<<grid, 64 * kWavesOf<1>, 0, stream>>>(a);
     else if (a.rows <= 32)
-        few_kernel<X, Y, 2><<<grid, 64 * kWaves, 0, stream>>>(a);
+        few_kernel<X, Y, 2><<<grid, 64 * kWavesOf<2>, 0, stream>>>(a);
     else
-        few_kernel<X, Y, 4><<<grid, 64 * kWaves, 0, stream>>>(a);
+        few_kernel<X, Y, 4><<<grid, 64 * kWavesOf<4>, 0, stream>>>(a);
 }
 template <typename X>
 hipError_t launch_type(const FewArgs &a, int32_t y_dtype, hipStream_t stream) {
