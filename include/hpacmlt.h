@@ -46,7 +46,7 @@ extern "C" {
 typedef struct {
     void *codes;          /* DEVICE, 16-byte aligned, of hpacmlt_matrix_bytes */
     void *scales;         /* DEVICE, 16-byte aligned, of hpacmlt_matrix_bytes */
-    int64_t rows, width;  /* rows >= 0, width >= 0; each up to INT32_MAX */
+    int64_t rows, width;  /* rows >= 0, width >= 0; each up to INT32_MAX, fewer than 2^24 blocks of 128 x 128 */
 } hpacmlt_matrix;
 
 /* Bytes of a matrix's buffers. */
@@ -123,7 +123,7 @@ hpacml_status hpacmlt_backward_scratch(int64_t rows, int64_t n_in, int32_t n_out
  *     z = (x - mean) * (rstd * gamma) + beta     y = act(z)
  * in fp32, y rounded once to its type, which is x's.
  *   dtype: HPACML_F32 or HPACML_BF16; gamma, beta: fp32 [channels] or NULL (1
- *   and 0); eps > 0, finite; act: HPACML_ACT_* or HPACMLT_ACT_SILU (z / (1 +
+ *   and 0); eps >= 2^-126, finite; act: HPACML_ACT_* or HPACMLT_ACT_SILU (z / (1 +
  *   exp(-z))); mean, rstd: fp32 [images][groups], for the backward pass, or
  *   both NULL.  channels: 1..HPACMLT_MAX_CHANNELS, a multiple of groups.
  * An image with an infinity or a NaN in a group has NaNs there.  points is at

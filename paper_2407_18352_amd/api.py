@@ -775,12 +775,15 @@ class GradientSet:
     float32 or bfloat16 device tensors whose values are one after another in
     memory; ``into``: as many tensors of the same shapes and strides that
     clipping writes to (None: in place).  The set holds the tensors: gradients
-    that an optimizer replaces need a new set."""
+    that an optimizer replaces need a new set.  It synchronises the device, so it
+    is made before a capture into a graph, and outlives the graphs that use it."""
 
     def __init__(self, gradients, into=None):
+        import torch
         if not _kinds8:
-            import torch
             _kinds8.update({torch.float32: _abi.F32, torch.bfloat16: _abi.BF16})
+        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a set of gradients is made before the capture, not in it")
         gradients = list(gradients)
         into = gradients if into is None else list(into)
         if len(into) != len(gradients):

@@ -21,27 +21,29 @@ int64_t runs_of(int64_t rows) {
 __global__ __launch_bounds__(1024) void sums_kernel(ColumnSums a, int64_t run) {
     __shared__ double of[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane, first = (int64_t)blockIdx.y * run, last = min(first + run, a.rows);
-    double t = 0;
-    if (c < a.width)
+    const int64_t first = (int64_t)blockIdx.y * run, last = min(first + run, a.rows);
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < a.width; c0 += (int64_t)gridDim.x * 64) {
+        const int64_t c = c0 + lane;
+        double t = 0;
+        if (c < a.width)
 #pragma unroll 8
-        for (int64_t r = first + wave; r < last; r += 16)
-            t += a.part[r * a.pitch + c];
-    of[wave][lane] = t;
-    __syncthreads();
-    if (wave == 0 && c < a.width) {
+            for (int64_t r = first + wave; r < last; r += 16)
+                t += a.part[r * a.pitch + c];
+        of[wave][lane] = t;
+        __syncthreads();
+        if (wave == 0 && c < a.width) {
 #pragma unroll
-        for (int w = 1; w < 16; ++w)
-            t += of[w][lane];
-        const float s = (float)t;
-        if (a.room) {
-            a.room[blockIdx.y * a.width + c] = s;
-            return;
+            for (int w = 1; w < 16; ++w)
+                t += of[w][lane];
+            const float s = (float)t;
+            if (a.room)
+                a.room[blockIdx.y * a.width + c] = s;
+            else if (float *to = c < a.split ? a.out : a.more) {
+                const int64_t at = c < a.split ? c : c - a.split;
+                to[at] = a.accumulate ? to[at] + s : s;
+            }
         }
-        float *to = c < a.split ? a.out : a.more;
-        const int64_t at = c < a.split ? c : c - a.split;
-        if (to)
-            to[at] = a.accumulate ? to[at] + s : s;
+        __syncthreads();
     }
 }
 
@@ -53,7 +55,8 @@ hipError_t launch_column_sums(const ColumnSums &a, hipStream_t stream) {
     if (a.width == 0)
         return hipSuccess;
     const int64_t runs = runs_of(a.rows);
-    const uint32_t across = (uint32_t)((a.width + 63) / 64);
+    const int64_t tiles = (a.width + 63) / 64;
+    const uint32_t across = (uint32_t)(tiles < 1 << 16 ? tiles : 1 << 16);      // a launch has fewer than 2^32 threads
     ColumnSums last = a;
     if (runs > 1) {
         const int64_t run = (a.rows + runs - 1) / runs;

@@ -223,11 +223,9 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a) {
     }
 }
 
-// A thread reads 16 codes of a row; eight neighbours a block of 128.
+// A block takes 32 rows by 128 values, a thread 16 codes of a row.
 template <typename X>
-__global__ __launch_bounds__(256) void load_kernel(Matrix m, X *x, int64_t ldx) {
-    const int64_t blocks = blocks_of(m.width), chunks = blocks * 8;
-    const int64_t unit = blockIdx.x / ((chunks + 7) / 8), part = blockIdx.x % ((chunks + 7) / 8);   // 32 rows, eight chunks
+__device__ __forceinline__ void load_block(const Matrix &m, X *x, int64_t ldx, int64_t unit, int64_t part, int64_t blocks) {
     const int64_t row = unit * 32 + (threadIdx.x >> 3), k = (part * 8 + (threadIdx.x & 7)) * 16;
     if (row >= m.rows || k >= m.width)
         return;
@@ -263,17 +261,26 @@ __global__ __launch_bounds__(256) void load_kernel(Matrix m, X *x, int64_t ldx) 
                 store_value(to + i, v[i]);
     }
 }
+template <typename X>
+__global__ __launch_bounds__(256) void load_kernel(Matrix m, X *x, int64_t ldx) {
+    const int64_t blocks = blocks_of(m.width), all = row_units(m.rows) * blocks;
+    for (int64_t at = blockIdx.x; at < all; at += gridDim.x)
+        load_block(m, x, ldx, at / blocks, at % blocks, blocks);
+}
 
 template <typename X, bool ROW, bool COLUMN>
 void launch_form(const QuantizeArgs &a, uint32_t blocks, hipStream_t stream) {
-    if (a.y && a.sums)
-        quantize_kernel<X, ROW, COLUMN, true, true><<<blocks, 256, 0, stream>>>(a);
-    else if (a.y)
-        quantize_kernel<X, ROW, COLUMN, true, false><<<blocks, 256, 0, stream>>>(a);
-    else if (a.sums)
-        quantize_kernel<X, ROW, COLUMN, false, true><<<blocks, 256, 0, stream>>>(a);
-    else
-        quantize_kernel<X, ROW, COLUMN, false, false><<<blocks, 256, 0, stream>>>(a);
+    if (a.sums) {
+        if (a.y)
+            quantize_kernel<X, ROW, COLUMN, true, true><<<blocks, 256, 0, stream>>>(a);
+        else
+            quantize_kernel<X, ROW, COLUMN, false, true><<<blocks, 256, 0, stream>>>(a);
+    } else if constexpr (ROW || COLUMN) {
+        if (a.y)
+            quantize_kernel<X, ROW, COLUMN, true, false><<<blocks, 256, 0, stream>>>(a);
+        else
+            quantize_kernel<X, ROW, COLUMN, false, false><<<blocks, 256, 0, stream>>>(a);
+    }
 }
 
 template <typename X>
@@ -294,7 +301,7 @@ hipError_t launch_quantize(const QuantizeArgs &a, int32_t dtype, hipStream_t str
     const int64_t blocks = blocks_of(a.rows) * blocks_of(a.width);
     if (blocks == 0)
         return hipSuccess;
-    if (blocks > INT32_MAX)
+    if (too_many_blocks(a.rows, a.width))
         return hipErrorInvalidValue;
     if (dtype == HPACML_F32)
         launch_type<float>(a, (uint32_t)blocks, stream);
@@ -307,12 +314,11 @@ hipError_t launch_load(const Matrix &m, void *x, int32_t dtype, int64_t ldx, hip
     const int64_t blocks = row_units(m.rows) * blocks_of(m.width);
     if (blocks == 0)
         return hipSuccess;
-    if (blocks > INT32_MAX)
-        return hipErrorInvalidValue;
+    const uint32_t grid = (uint32_t)(blocks < 1 << 20 ? blocks : 1 << 20);
     if (dtype == HPACML_F32)
-        load_kernel<<<(uint32_t)blocks, 256, 0, stream>>>(m, (float *)x, ldx);
+        load_kernel<<<grid, 256, 0, stream>>>(m, (float *)x, ldx);
     else
-        load_kernel<<<(uint32_t)blocks, 256, 0, stream>>>(m, (uint16_t *)x, ldx);
+        load_kernel<<<grid, 256, 0, stream>>>(m, (uint16_t *)x, ldx);
     return hipGetLastError();
 }
 

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -22,7 +23,7 @@ namespace {
 hpacml_status matrix_status(const hpacmlt_matrix *m) {
     if (!m || m->rows < 0 || m->width < 0)
         return HPACML_E_INVAL;
-    return m->rows > kMaxRows || m->width > kMaxRows ? HPACML_E_UNSUPPORTED : HPACML_OK;
+    return m->rows > kMaxRows || m->width > kMaxRows || f8::too_many_blocks(m->rows, m->width) ? HPACML_E_UNSUPPORTED : HPACML_OK;
 }
 Matrix matrix_of(const hpacmlt_matrix &m) { return {(char *)m.codes, (char *)m.scales, m.rows, m.width}; }
 void add_matrix(Operands *o, const hpacmlt_matrix &m, bool written) {
@@ -182,7 +183,7 @@ hpacml_status hpacmlt_quantize(const void *x, int32_t dtype, int64_t ldx, int64_
                                const hpacmlt_matrix *by_column, int32_t square, void *stream) {
     if (!is_type(dtype) || rows < 0 || width < 0 || (!by_row && !by_column) || !pitch_ok(ldx, width))
         return HPACML_E_INVAL;
-    if (rows > kMaxRows || width > kMaxRows)
+    if (rows > kMaxRows || width > kMaxRows || f8::too_many_blocks(rows, width))
         return HPACML_E_UNSUPPORTED;
     for (const hpacmlt_matrix *m : {by_row, by_column})
         if (m) {
@@ -271,7 +272,7 @@ hpacml_status hpacmlt_linear_scratch(const hpacmlt_matrix *W, int64_t rows, size
         return s;
     if (!bytes || rows < 0 || W->rows < 1 || W->width < 1)
         return HPACML_E_INVAL;
-    if (rows > kMaxRows)
+    if (rows > kMaxRows || f8::too_many_blocks(rows, W->width))
         return HPACML_E_UNSUPPORTED;
     *bytes = rows ? LinearLayout(rows, W->width, W->rows).bytes : 0;
     return HPACML_OK;
@@ -288,7 +289,7 @@ hpacml_status hpacmlt_linear_run(const hpacmlt_matrix *W, const float *b, const 
     if (W->rows < 1 || W->width < 1 || !is_type(x_dtype) || !is_type(y_dtype) || !is_act(act) || rows < 0 || !pitch_ok(ldx, W->width) ||
         !pitch_ok(ldy, W->rows))
         return HPACML_E_INVAL;
-    if (rows > kMaxRows)
+    if (rows > kMaxRows || f8::too_many_blocks(rows, W->width))
         return HPACML_E_UNSUPPORTED;
     if (keep && (keep->rows != W->width || keep->width != rows))
         return HPACML_E_SHAPE;
@@ -325,7 +326,7 @@ hpacml_status hpacmlt_backward_scratch(int64_t rows, int64_t n_in, int32_t n_out
                                        size_t *bytes) {
     if (!bytes || rows < 0 || n_in < 1 || n_out < 1)
         return HPACML_E_INVAL;
-    if (rows > kMaxRows || n_in > kMaxRows)
+    if (rows > kMaxRows || n_in > kMaxRows || f8::too_many_blocks(rows, n_out) || f8::too_many_blocks(rows, n_in))
         return HPACML_E_UNSUPPORTED;
     *bytes = rows ? BackwardLayout(rows, n_in, n_out, want_dw != 0, want_db != 0, want_dx != 0).bytes : 0;
     return HPACML_OK;
@@ -343,6 +344,8 @@ hpacml_status hpacmlt_backward(const hpacmlt_matrix *kept, const void *dy, const
     if (!is_type(dtype) || n_out < 1 || n_in < 1 || !pitch_ok(lddy, n_out) || (y && !pitch_ok(ldy, n_out)) || (!dw && !db && !dx) ||
         (dw && !pitch_ok(lddw, n_in)) || (dx && !pitch_ok(lddx, n_in)))
         return HPACML_E_INVAL;
+    if (f8::too_many_blocks(rows, n_out))
+        return HPACML_E_UNSUPPORTED;
     if (dx && (Wt->rows != n_in || Wt->width != n_out))
         return HPACML_E_SHAPE;
     const BackwardLayout l(rows, n_in, n_out, dw, db, dx);
@@ -405,7 +408,7 @@ hpacml_status hpacmlt_group_norm(const void *x, int32_t dtype, int64_t ldx, int6
     const hpacml_status s = norm_status(dtype, images, points, channels, groups);
     if (s != HPACML_OK)
         return s;
-    if (!pitch_ok(ldx, channels) || !pitch_ok(ldy, channels) || !(eps > 0.f) || std::isinf(eps) || !is_norm_act(act) || !mean != !rstd)
+    if (!pitch_ok(ldx, channels) || !pitch_ok(ldy, channels) || !(eps >= FLT_MIN) || std::isinf(eps) || !is_norm_act(act) || !mean != !rstd)
         return HPACML_E_INVAL;
     if (images == 0)
         return HPACML_OK;

@@ -28,7 +28,10 @@ class SurrogateF8:
     bf16, products of 8-bit floats with a scale for each 128 values.  ``backward``
     is that of the last ``forward`` and with the weights of the last ``update``.
     Calls may come on one stream after another, each works after the one before;
-    from several threads at a time they may not."""
+    from several threads at a time they may not.  Calls captured into a graph read
+    the weights as ``update`` lays them out and write the gradients where they
+    are then; a forward pass captured keeps what it does for the graph's own
+    backward pass."""
 
     def __init__(self, dims, groups: int = 8, act: int = _abi.ACT_SILU, eps: float = 1e-5, seed: int = 0):
         g = torch.Generator().manual_seed(seed)
@@ -46,6 +49,7 @@ class SurrogateF8:
         with torch.no_grad():
             self.layers = [api.LinearF8(w, b, learn=True) for w, b in zip(self.W, self.b)]
         self.rows, self.kept, self.stats, self.z, self.set, self.stream = -1, [], [], [], None, torch.cuda.current_stream()
+        self.captured = []              # what graphs read
 
     def parameters(self):
         return self.W + self.b + self.gamma + self.beta
@@ -91,9 +95,11 @@ class SurrogateF8:
         ``backward`` reads."""
         self._in_order()
         n = x.shape[0]
-        if self.rows != n:
+        if self.rows != n or torch.cuda.is_current_stream_capturing():
             self.rows, self.kept = n, [api.MatrixF8(d, n) for d in self.dims[:-1]]
             self.stats = [tuple(torch.empty((n, self.groups), device="cuda") for _ in range(2)) for _ in self.dims[1:-1]]
+            if torch.cuda.is_current_stream_capturing():
+                self.rows = -1          # the next eager pass has its own
         self.z = []
         return self._run(x, True)
 
@@ -107,6 +113,8 @@ class SurrogateF8:
     def backward(self, dy, accumulate: bool = False):
         """Gradients of the loss in ``.grad`` (made where an optimizer has taken
         them away) from that of the outputs."""
+        if len(self.z) != len(self.dims) - 2 or not self.kept:
+            raise ValueError("there is no forward pass to go back from")
         self._in_order()
         for p in self.parameters():
             if p.grad is None:
@@ -133,6 +141,8 @@ class SurrogateF8:
             raise ValueError("there are no gradients to clip")
         if self.set is None or any(a is not b for a, b in zip(self.set.gradients, grads)):
             self.set = api.GradientSet(grads)
+        if torch.cuda.is_current_stream_capturing() and self.set not in self.captured:
+            self.captured.append(self.set)
         norm = torch.empty(1, device="cuda")
         api.clip_gradients(self.set, most, norm)
         return norm

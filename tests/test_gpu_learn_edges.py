@@ -243,6 +243,23 @@ def test_offsets_beyond_32_bits():
     assert ((z[n - 1100 :].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2e-5).all()
 
 
+def test_more_blocks_than_a_grid():
+    """Integers up to 8, which codes hold exactly: what comes of them is exact."""
+    wide = torch.empty((33, (1 << 26) + 1000), dtype=BF16, device="cuda").random_(-8, 9)
+    back = torch.full_like(wide, 99)
+    api.loadf8(quantized(wide), back)                          # 2^20 blocks of 32 rows x 128 values, and more
+    assert all(torch.equal(a, b) for a, b in zip(wide, back))
+    del wide, back
+    n_out = (1 << 22) + 777                                    # 2^16 sums of 64 columns, and more
+    dy, db = torch.empty((3, n_out), dtype=BF16, device="cuda").random_(-8, 9), torch.empty(n_out, device="cuda")
+    api.backwardf8(api.MatrixF8(1, 3), dy, db=db)
+    assert torch.equal(db, dy.float().sum(0))
+    n_out = (1 << 24) + 33                                     # of one row: more outputs than one launch for few rows has threads for
+    W, x, y = torch.empty((n_out, 5), dtype=BF16, device="cuda").random_(-8, 9), torch.empty((1, 5), device="cuda").random_(-8, 9), torch.empty((1, n_out), device="cuda")
+    api.productf8(quantized(x), quantized(W), y)
+    assert torch.equal(y[0], (W.float() * x).sum(1))
+
+
 def test_a_product_of_few_and_many_rows_agree():
     """The forms for few rows and for many, on the same whole numbers."""
     g = torch.Generator().manual_seed(4)
@@ -329,6 +346,65 @@ def test_surrogate_batches_streams_and_updates():
     assert not torch.equal(model.forward(x), same.forward(x))
     with pytest.raises(ValueError):
         surrogatef8.SurrogateF8([4, 30, 2], groups=4)
+
+
+def test_surrogate_captured_into_a_graph():
+    """A step's passes and its clipping replayed between eager ones of another size, whose buffers replace those of the passes before the capture."""
+    g = torch.Generator().manual_seed(9)
+    model, same = surrogatef8.SurrogateF8([4, 32, 2], groups=4, seed=3), surrogatef8.SurrogateF8([4, 32, 2], groups=4, seed=3)
+    x, dy = torch.randn((150, 4), generator=g).cuda(), torch.randn((150, 2), generator=g).cuda()
+    for _ in range(2):
+        model.forward(x)
+        model.backward(dy)
+        model.clip(0.5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = model.forward(x)
+        model.backward(dy)
+        norm = model.clip(0.5)
+    other = torch.randn((40, 4), generator=g).cuda()
+    for k in range(3):
+        model.forward(other)
+        model.backward(dy[:40])
+        taken = [torch.full((4096,), 255, dtype=torch.uint8, device="cuda") for _ in range(64)]     # what the first passes' buffers left
+        x.copy_(torch.randn((150, 4), generator=g))
+        graph.replay()
+        want = same.forward(x)
+        same.backward(dy)
+        total = same.clip(0.5)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(norm, total)
+        assert all(torch.equal(p.grad, q.grad) for p, q in zip(model.parameters(), same.parameters()))
+        assert all(bool((t == 255).all()) for t in taken)
+        with torch.no_grad():
+            for m in (model, same):
+                m.W[0].mul_(1.5)
+                m.update()
+    held = model.set
+    for p in model.parameters():                     # other gradients: a set of their own, and the graph's stays
+        p.grad = None
+    model.backward(dy[:40])
+    model.clip(0.5)
+    assert model.set is not held and held.handle
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, model.answer(x)) and torch.isfinite(norm).all()
+
+
+def test_surrogate_calls_out_of_order():
+    model = surrogatef8.SurrogateF8([4, 32, 2], groups=4)
+    with pytest.raises(ValueError):
+        model.backward(torch.zeros((3, 2), device="cuda"))
+    graph = torch.cuda.CUDAGraph()
+    t = torch.zeros(3, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        t.add_(1)
+        with pytest.raises(RuntimeError):
+            api.GradientSet([t])                     # synchronises: not in a capture
+    graph.replay()
+    assert t.tolist() == [1, 1, 1]
 
 
 def test_surrogate_command_runs():

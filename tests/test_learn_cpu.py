@@ -53,6 +53,18 @@ def test_matrix_descriptions():
     assert L.hpacmlt_matrix_bytes(5, 5, None, s) == _abi.E_INVAL
 
 
+@pytest.mark.parametrize("rows, width, status", [(1 << 31, 1, _abi.E_UNSUPPORTED), ((1 << 31) - 1, 1, _abi.E_UNSUPPORTED), ((1 << 31) - 128, 128, _abi.OK),
+                                                 ((1 << 30) + 1, 129, _abi.E_UNSUPPORTED), (1 << 24, 1 << 14, _abi.E_UNSUPPORTED), (1 << 24, (1 << 14) - 128, _abi.OK)])
+def test_fewer_blocks_than_a_launch_has(rows, width, status):
+    c, s = C.c_size_t(), C.c_size_t()
+    assert L.hpacmlt_matrix_bytes(rows, width, c, s) == status and L.hpacmlt_matrix_bytes(width, rows, c, s) == status
+    assert L.hpacmlt_backward_scratch(rows, 5, width, 0, 1, 0, c) == status
+    assert L.hpacmlt_linear_scratch(matrix(9, width), rows, c) == status
+    if status != _abi.OK:
+        assert L.hpacmlt_quantize(FAKE, _abi.F32, width, rows, width, matrix(rows, width), None, 0, None) == status
+        assert L.hpacmlt_load(matrix(rows, width), FAKE, _abi.F32, width, None) == status
+
+
 def matrix(rows, width):
     return _abi.Matrix(FAKE, FAKE + (1 << 20), rows, width)
 
@@ -105,7 +117,7 @@ NORM = dict(dtype=_abi.F32, ld=24, images=3, points=50, channels=24, groups=4, e
 @pytest.mark.parametrize("more, status", [
     (dict(dtype=7), _abi.E_INVAL), (dict(images=-1), _abi.E_INVAL), (dict(points=0), _abi.E_INVAL), (dict(channels=0), _abi.E_INVAL), (dict(groups=0), _abi.E_INVAL),
     (dict(groups=5), _abi.E_INVAL), (dict(ld=23), _abi.E_INVAL), (dict(act=3), _abi.E_INVAL), (dict(eps=0.0), _abi.E_INVAL), (dict(eps=-1.0), _abi.E_INVAL),
-    (dict(eps=math.nan), _abi.E_INVAL), (dict(eps=math.inf), _abi.E_INVAL), (dict(mean=None), _abi.E_INVAL),
+    (dict(eps=math.nan), _abi.E_INVAL), (dict(eps=2.0 ** -127), _abi.E_INVAL), (dict(eps=math.inf), _abi.E_INVAL), (dict(mean=None), _abi.E_INVAL),
     (dict(channels=32768, ld=32768), _abi.E_UNSUPPORTED), (dict(images=1 << 20, points=1 << 20), _abi.E_UNSUPPORTED),
     (dict(points=100000, bytes=0), _abi.E_RANGE), (dict(images=0), _abi.OK)])
 def test_group_norm_refusals(more, status):
