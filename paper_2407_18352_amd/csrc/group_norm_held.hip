@@ -123,7 +123,8 @@ __global__ __launch_bounds__(kHeldThreads) void held_backward_kernel(GroupNorm a
     const bool here = r < h.high;
     const int last = (int)a.points - 1;
     const float share = 1.f / ((float)a.points * per);
-    float gamma[V], beta[V], s1[V], s2[V];
+    float gamma[V], beta[V];
+    Total<V> s1[V], s2[V];
     load_parameters<V>(a.gamma ? a.gamma + c : nullptr, 1.f, gamma);
     load_parameters<V>(a.beta ? a.beta + c : nullptr, 0.f, beta);
 #pragma unroll
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(kHeldThreads) void held_backward_kernel(GroupNorm a
     float *to = part + (int64_t)at.stride * 2 * a.channels;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        float2 t = {s1[e], s2[e]};
+        float2 t = {(float)s1[e], (float)s2[e]};
         __syncthreads();
         of[threadIdx.x] = t;
         for (int n = h.high, half; n > 1; n = half) {

@@ -36,11 +36,13 @@ __device__ __forceinline__ Place place_of(const GroupNorm &a, const Parts &p, in
     return q;
 }
 
-// f(points, how many of them exist) for the thread's points, kAtOnce at a time,
+// f(points, how many of them exist) for the thread's points, points_at_once<V> at a time,
 // so that their loads go out together (the last again where there is none).
-constexpr int kAtOnce = 4;
+template <int V>
+constexpr int points_at_once = V == 1 ? 8 : 4;
 template <int V, typename F>
 __device__ __forceinline__ void over_points(const Place &q, const Parts &p, F f) {
+    constexpr int kAtOnce = points_at_once<V>;
     for (int64_t row = q.first + q.r; row < q.last; row += kAtOnce * p.high) {
         int64_t rows[kAtOnce];
         int n = 0;
@@ -225,13 +227,13 @@ __global__ __launch_bounds__(256) void parts_apply_kernel(GroupNorm a, Parts p, 
 #pragma unroll
         for (int e = 0; e < V; ++e)
             k.gamma[e] *= k.rstd[e];
-        over_points<V>(q, p, [&](const int64_t (&rows)[kAtOnce], int n) {
-            typename Values<T, V>::Held w[kAtOnce];
+        over_points<V>(q, p, [&](const int64_t (&rows)[points_at_once<V>], int n) {
+            typename Values<T, V>::Held w[points_at_once<V>];
 #pragma unroll
-            for (int b = 0; b < kAtOnce; ++b)
+            for (int b = 0; b < points_at_once<V>; ++b)
                 w[b] = Values<T, V>::hold((const T *)a.x + rows[b] * a.ldx + q.c);
 #pragma unroll
-            for (int b = 0; b < kAtOnce; ++b)
+            for (int b = 0; b < points_at_once<V>; ++b)
                 if (b < n) {
                     float v[V];
                     Values<T, V>::values(w[b], v);
@@ -250,7 +252,7 @@ __global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, f
     __shared__ float2 of[256][V];
     for (int64_t block = blockIdx.x; block < p.blocks; block += gridDim.x) {
         const Place q = place_of<V>(a, p, block);
-        float s1[V], s2[V];
+        Total<V> s1[V], s2[V];
 #pragma unroll
         for (int e = 0; e < V; ++e)
             s1[e] = s2[e] = 0;
@@ -263,15 +265,19 @@ __global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, f
                 k.gamma[e] *= kUnit<ACT>;
                 k.beta[e] *= kUnit<ACT>;
             }
-            over_points<V>(q, p, [&](const int64_t (&rows)[kAtOnce], int n) {
-                typename Values<T, V>::Held w[kAtOnce], o[kAtOnce];
+            over_points<V>(q, p, [&](const int64_t (&rows)[points_at_once<V>], int n) {
+                typename Values<T, V>::Held w[points_at_once<V>], o[points_at_once<V>];
 #pragma unroll
-                for (int b = 0; b < kAtOnce; ++b) {
+                for (int b = 0; b < points_at_once<V>; ++b) {
                     w[b] = Values<T, V>::hold((const T *)a.x + rows[b] * a.ldx + q.c);
                     o[b] = Values<T, V>::hold((const T *)a.dy + rows[b] * a.lddy + q.c);
                 }
+                float t1[V], t2[V];
 #pragma unroll
-                for (int b = 0; b < kAtOnce; ++b)
+                for (int e = 0; e < V; ++e)
+                    t1[e] = t2[e] = 0;
+#pragma unroll
+                for (int b = 0; b < points_at_once<V>; ++b)
                     if (b < n) {
                         float v[V], g[V];
                         Values<T, V>::values(w[b], v);
@@ -280,15 +286,20 @@ __global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, f
                         for (int e = 0; e < V; ++e) {
                             const float d = v[e] - k.mean[e];
                             const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.gamma[e], k.beta[e]));
-                            s1[e] += t;
-                            s2[e] = __builtin_fmaf(t, d, s2[e]);
+                            t1[e] += t;
+                            t2[e] = __builtin_fmaf(t, d, t2[e]);
                         }
                     }
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    s1[e] += t1[e];
+                    s2[e] += t2[e];
+                }
             });
         }
 #pragma unroll
         for (int e = 0; e < V; ++e)
-            of[threadIdx.x][e] = {s1[e], s2[e]};
+            of[threadIdx.x][e] = {(float)s1[e], (float)s2[e]};
         for (int h = p.high / 2; h > 0; h /= 2) {
             __syncthreads();
             if (q.here && q.r < h)
@@ -297,7 +308,7 @@ __global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, f
                     const float2 o = of[threadIdx.x + h * p.across][e];
                     s1[e] += o.x;
                     s2[e] += o.y;
-                    of[threadIdx.x][e] = {s1[e], s2[e]};
+                    of[threadIdx.x][e] = {(float)s1[e], (float)s2[e]};
                 }
         }
         if (q.here && q.r == 0) {
@@ -305,8 +316,8 @@ __global__ __launch_bounds__(256) void parts_sums_kernel(GroupNorm a, Parts p, f
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 if (q.c + e < a.channels) {
-                    to[e] = s1[e];
-                    to[a.channels + e] = s2[e] * k.rstd[e];
+                    to[e] = (float)s1[e];
+                    to[a.channels + e] = (float)(s2[e] * k.rstd[e]);
                 }
         }
         __syncthreads();
@@ -356,15 +367,15 @@ __global__ __launch_bounds__(256) void parts_dx_kernel(GroupNorm a, Parts p, con
             k.gamma[e] = scale[e] * kUnit<ACT>;
             k.beta[e] *= kUnit<ACT>;
         }
-        over_points<V>(q, p, [&](const int64_t (&rows)[kAtOnce], int n) {
-            typename Values<T, V>::Held w[kAtOnce], o[kAtOnce];
+        over_points<V>(q, p, [&](const int64_t (&rows)[points_at_once<V>], int n) {
+            typename Values<T, V>::Held w[points_at_once<V>], o[points_at_once<V>];
 #pragma unroll
-            for (int b = 0; b < kAtOnce; ++b) {
+            for (int b = 0; b < points_at_once<V>; ++b) {
                 w[b] = Values<T, V>::hold((const T *)a.x + rows[b] * a.ldx + q.c);
                 o[b] = Values<T, V>::hold((const T *)a.dy + rows[b] * a.lddy + q.c);
             }
 #pragma unroll
-            for (int b = 0; b < kAtOnce; ++b)
+            for (int b = 0; b < points_at_once<V>; ++b)
                 if (b < n) {
                     float v[V], g[V];
                     Values<T, V>::values(w[b], v);

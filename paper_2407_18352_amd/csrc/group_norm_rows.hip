@@ -120,7 +120,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm
     const int column_block = blockIdx.x % p.column_blocks, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const RowLane<T, V, I> k(a, p, column_block);
     const float share = 1.f / (float)(a.channels / a.groups);
-    float s1[I][V], s2[I][V];
+    Total<I * V> s1[I][V], s2[I][V];
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_backward_kernel(GroupNorm
     for (int i = 0; i < I; ++i) {
 #pragma unroll
         for (int e = 0; e < V; ++e)
-            of[wave][lane][e] = {s1[i][e], s2[i][e]};
+            of[wave][lane][e] = {(float)s1[i][e], (float)s2[i][e]};
         __syncthreads();
         if (wave == 0 && k.here[i] && k.sub == 0)
 #pragma unroll
