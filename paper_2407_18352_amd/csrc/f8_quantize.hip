@@ -10,8 +10,8 @@
 // they fall on different banks.  Reading and writing is what it has to do:
 // 131,072 x 4096 in bf16 by row takes 0.30 ms (1.6 GB at 5.4 TB/s), 131,072 x 2048
 // by row and column behind a ReLU 0.33 ms (4.9 TB/s), 65,536 x 512 by row and
-// column 36 us (3.7 TB/s: two blocks a CU, which wait for their loads together);
-// one block alone takes 6 us.
+// column 36 us (3.7 TB/s; limits on the registers, for more waves, change nothing
+// there or cost spills); one block alone takes 6 us.
 #include <type_traits>
 
 #include "f8.hpp"

@@ -276,6 +276,25 @@ def test_a_product_of_few_and_many_rows_agree():
             assert torch.equal(few, y[:n])
 
 
+@pytest.mark.parametrize("n, n_in, n_out", [(16, 12200, 100), (16, 12300, 100), (17, 6100, 130), (17, 6200, 130), (32, 6100, 33), (33, 3000, 70), (33, 3100, 70),
+                                            (64, 3000, 5), (64, 3100, 5), (65, 300, 40), (1, 4096, 4096), (1, 4097, 4097), (2, 130, 12288), (2, 130, 12289),
+                                            (40, 1024, 4097), (40, 1025, 4097)])
+def test_sizes_beside_the_rule_for_few_rows(n, n_in, n_out):
+    """Whole numbers, whose sums fp32 holds."""
+    g = torch.Generator().manual_seed(n + n_in)
+    W, x = torch.randint(-8, 9, (n_out, n_in), generator=g).float().cuda(), torch.randint(-8, 9, (n, n_in), generator=g).float().cuda()
+    b = torch.randint(-8, 9, (n_out,), generator=g).float().cuda()
+    want = (x.double() @ W.double().t() + b).relu()
+    layer = api.LinearF8(W, b)
+    for kind in (F32, BF16):
+        y = torch.empty((n, n_out), dtype=kind, device="cuda")
+        api.linearf8(layer, x.to(kind), y, act=_abi.ACT_RELU)
+        assert torch.equal(y, want.to(kind))
+        y = torch.empty((n, n_out), dtype=kind, device="cuda")
+        api.productf8(quantized(x), layer.W, y, b, act=_abi.ACT_RELU)
+        assert torch.equal(y, want.to(kind))
+
+
 # ---- the class that trains with them ---------------------------------------------
 
 
