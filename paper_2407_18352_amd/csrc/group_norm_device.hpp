@@ -120,20 +120,29 @@ struct Values {
         else
             unpack(w, v);
     }
+    static __device__ __forceinline__ Word words(const float (&v)[V]) {
+        Word w;
+#pragma unroll
+        for (int e = 0; e < kBytes / 4; ++e) {
+            if constexpr (sizeof(T) == 4)
+                w[e] = __builtin_bit_cast(uint32_t, v[e]);
+            else
+                w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+        }
+        return w;
+    }
     static __device__ __forceinline__ void store(T *p, const float (&v)[V]) {
         if constexpr (V == 1)
             store_value(p, v[0]);
-        else {
-            Word w;
-#pragma unroll
-            for (int e = 0; e < kBytes / 4; ++e) {
-                if constexpr (sizeof(T) == 4)
-                    w[e] = __builtin_bit_cast(uint32_t, v[e]);
-                else
-                    w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-            }
-            *(Any *)p = w;
-        }
+        else
+            *(Any *)p = words(v);
+    }
+    // past the caches
+    static __device__ __forceinline__ void store_past(T *p, const float (&v)[V]) {
+        if constexpr (V == 1)
+            store_value(p, v[0]);
+        else
+            __builtin_nontemporal_store(words(v), (Any *)p);
     }
 };
 

@@ -1,7 +1,9 @@
 // Group norm of large images: sums of runs of points, their join, and the results
 // from a second reading.  An image of 2048^2 points x 8 channels in fp32 takes 89
-// us: 41 for the first reading (3.3 TB/s, beside the write-back of what was computed
-// before), 6 for the join, 43 for the results (6.2 TB/s, out of the Infinity Cache).
+// us with results through the caches (41 for the first reading, which meets the
+// write-back of what was computed before, 6 for the join, 43 for the results), 75 with
+// results past them (its gradients 145 and 121), and with a call behind it that reads
+// them 132 and 126.
 #include "group_norm_device.hpp"
 
 namespace hpacml {
@@ -243,7 +245,7 @@ __global__ __launch_bounds__(256) void parts_apply_kernel(GroupNorm a, Parts p, 
 #pragma unroll
                     for (int e = 0; e < V; ++e)
                         v[e] = activation<ACT>(__builtin_fmaf(v[e] - k.mean[e], k.gamma[e], k.beta[e]));
-                    Values<T, V>::store((T *)a.y + rows[b] * a.ldy + q.c, v);
+                    Values<T, V>::store_past((T *)a.y + rows[b] * a.ldy + q.c, v);
                 }
         });
     }
@@ -389,7 +391,7 @@ __global__ __launch_bounds__(256) void parts_dx_kernel(GroupNorm a, Parts p, con
                         const float t = activation_gradient<ACT>(g[e], __builtin_fmaf(d, k.gamma[e], k.beta[e]));
                         v[e] = __builtin_fmaf(t, scale[e], __builtin_fmaf(d, slope[e], shift[e]));
                     }
-                    Values<T, V>::store((T *)a.y + rows[b] * a.ldy + q.c, v);
+                    Values<T, V>::store_past((T *)a.y + rows[b] * a.ldy + q.c, v);
                 }
         });
     }

@@ -1,5 +1,7 @@
 // Group norm of images of one point: in one launch, in registers.  Memory bounds
-// it: 65,536 x 512 in bf16, 16 groups, takes 32 us (4.1 TB/s).
+// it: 65,536 x 512 in bf16, 16 groups, takes 32 us (4.1 TB/s).  Results go through the
+// caches: past them it takes 24 us, but the next call finds nothing there, and the two
+// together take 57 us instead of 52.
 #include "group_norm_device.hpp"
 
 namespace hpacml {
