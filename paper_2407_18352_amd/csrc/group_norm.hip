@@ -10,9 +10,10 @@
 // channels throughout, so that their parameters are in registers, and the sums
 // that the parameters' gradients are made of stay apart until the end.
 //
-// Statistics: the mean of a few values in registers, the squares about it, and
-// pairs of (mean, squares) joined as such, so that no difference of large sums
-// occurs; joins of many in 64 bits.
+// Statistics: in registers sums in 64 bits of what the values are more than one
+// of them, and of its squares (Moments); in parts pairs of (mean, squares about
+// it) joined as such, so that no difference of large sums occurs; joins of many
+// in 64 bits.
 #include "group_norm_device.hpp"
 
 namespace hpacml {

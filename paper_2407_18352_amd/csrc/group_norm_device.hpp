@@ -54,24 +54,63 @@ inline hipError_t with_activation(int32_t act, F f) {
 // Sums over `lanes` (a power of two) neighbouring lanes.  Up to 16 of them by
 // operand permutations of the vector unit, which leave LDS alone; the mirrored
 // orders serve, as what they exchange is the same in all lanes of a part.
-__device__ __forceinline__ float join_lanes(float t, int lanes) {
-    auto permuted = [](float v, auto control) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 15, 15, true));
-    };
+template <int CONTROL>
+__device__ __forceinline__ float permuted(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, 15, 15, true));
+}
+template <int CONTROL>
+__device__ __forceinline__ double permuted(double v) {
+    typedef int Words __attribute__((ext_vector_type(2)));
+    Words w = __builtin_bit_cast(Words, v);
+    w[0] = __builtin_amdgcn_update_dpp(0, w[0], CONTROL, 15, 15, true);
+    w[1] = __builtin_amdgcn_update_dpp(0, w[1], CONTROL, 15, 15, true);
+    return __builtin_bit_cast(double, w);
+}
+template <typename N>
+__device__ __forceinline__ N join_lanes(N t, int lanes) {
     if (lanes > 1)
-        t += permuted(t, std::integral_constant<int, 0xB1>());        // 1 0 3 2
+        t += permuted<0xB1>(t);        // 1 0 3 2
     if (lanes > 2)
-        t += permuted(t, std::integral_constant<int, 0x4E>());        // 2 3 0 1
+        t += permuted<0x4E>(t);        // 2 3 0 1
     if (lanes > 4)
-        t += permuted(t, std::integral_constant<int, 0x141>());       // eight mirrored
+        t += permuted<0x141>(t);       // eight mirrored
     if (lanes > 8)
-        t += permuted(t, std::integral_constant<int, 0x140>());       // sixteen mirrored
+        t += permuted<0x140>(t);       // sixteen mirrored
     if (lanes > 16)
         t += __shfl_xor(t, 16);
     if (lanes > 32)
         t += __shfl_xor(t, 32);
     return t;
 }
+
+// 1 / sqrt(v) of v >= 2^-126, from a rounding to fp32 (2^-24 of v) and its
+// reciprocal root (1 ulp): the power of two is taken out, as v may be beyond fp32.
+__device__ __forceinline__ float reciprocal_root(double v) {
+    const int half = __builtin_amdgcn_frexp_exp(v) >> 1;        // (0 of an infinity and a NaN)
+    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_rsqf((float)__builtin_amdgcn_ldexp(v, -2 * half)), -half);
+}
+
+// A group's statistics from one reading: sums of v - pivot and of its square in
+// 64 bits, where the difference and, but for one rounding, the square are exact.
+// pivot, one of the group's values, is at most sqrt(n) standard deviations
+// from the mean, so that squares / n less the square of sum / n loses no more
+// than n of 2^53, however far from zero the values lie; of equal values both
+// sums are 0.  (In 32 bits the mean's rounding was taken for a spread: a group
+// of 1e5 had a deviation of 8e-3, and squares passed the range from 1.8e19 on.)
+struct Moments {
+    double sum = 0, squares = 0;
+    __device__ __forceinline__ void add(float v, double pivot) {
+        const double d = (double)v - pivot;
+        sum += d;
+        squares = __builtin_fma(d, d, squares);
+        asm volatile("" : "+v"(sum), "+v"(squares));        // one after another: side by side, all the differences took registers
+    }
+    // share: 1 / n
+    __device__ __forceinline__ double variance(double share) const {
+        const double m = sum * share, v = __builtin_fma(squares, share, -m * m);
+        return v < 0 ? 0 : v;                                    // (a NaN stays one)
+    }
+};
 
 // What a thread sums a channel's gradients in, a few points' sum at a time.  It
 // may have a thousand points, whose sum in 32 bits is off by 5e-7 of the values'

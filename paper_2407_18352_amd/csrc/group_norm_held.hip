@@ -1,5 +1,6 @@
 // Group norm of images whose groups fit a block's registers: one reading, one
-// launch.  The gradients of 1024 images of 1024 points x 128 channels in bf16, SiLU,
+// launch.  1024 images of 1024 points x 128 channels in bf16, SiLU, take 136 us (3.9
+// TB/s; 163 with two joins, of sums in 32 bits).  The gradients of 1024 images of 1024 points x 128 channels in bf16, SiLU,
 // take 229 us (3.5 TB/s): the activation's gradient takes as many cycles as the
 // loads, and there is room for the registers of two blocks a CU.  Three launches, each
 // value read twice, took 379 us.  Results go past the caches (4096 images of 64 points x
@@ -24,15 +25,16 @@ struct Held {
 // Sums of `t` over the threads of each of the run's groups.  Thread t has
 // vector t % across of the run; a group is `each` vectors.  of: a pair per
 // thread, then one per group.  Groups' sums are taken by 32 threads each.
-__device__ __forceinline__ float2 join_groups(float2 t, const Held &h, int each, int group, bool here, float2 *of, float2 *of_group) {
+template <typename Pair>
+__device__ __forceinline__ Pair join_groups(Pair t, const Held &h, int each, int group, bool here, Pair *of, Pair *of_group) {
     __syncthreads();
     of[threadIdx.x] = t;
     __syncthreads();
     const int entries = h.high * each;
     for (int g = threadIdx.x >> 5; g < h.groups; g += blockDim.x >> 5) {
-        float2 s = {0.f, 0.f};
+        Pair s = {0, 0};
         for (int i = threadIdx.x & 31; i < entries; i += 32) {
-            const float2 o = of[i / each * h.across + g * each + i % each];
+            const Pair o = of[i / each * h.across + g * each + i % each];
             s.x += o.x;
             s.y += o.y;
         }
@@ -42,7 +44,7 @@ __device__ __forceinline__ float2 join_groups(float2 t, const Held &h, int each,
             of_group[g] = s;
     }
     __syncthreads();
-    return here ? of_group[group] : float2{0.f, 0.f};
+    return here ? of_group[group] : Pair{0, 0};
 }
 
 // Neighbouring runs of one image go to the same XCD at the same time: they share
@@ -61,54 +63,56 @@ constexpr int kHeldThreads = 512;
 
 template <typename T, int V, int I, int ACT>
 __global__ __launch_bounds__(kHeldThreads) void held_forward_kernel(GroupNorm a, Held h) {
-    extern __shared__ float2 of[];
-    float2 *of_group = of + blockDim.x;
+    extern __shared__ double2 sums[];
+    double2 *sums_of_group = sums + blockDim.x;
     const HeldPlace at(h);
     const int per = a.channels / a.groups, each = per / V, v = threadIdx.x % h.across, r = threadIdx.x / h.across;
     const int group = v / each, c = at.run * h.groups * per + v * V;
     const bool here = r < h.high;
     const int last = (int)a.points - 1;
-    const float share = 1.f / ((float)a.points * per);
+    const double share = 1.0 / ((double)a.points * per);
     float gamma[V], beta[V];
     load_parameters<V>(a.gamma ? a.gamma + c : nullptr, 1.f, gamma);
     load_parameters<V>(a.beta ? a.beta + c : nullptr, 0.f, beta);
     for (int64_t image = at.stride; image < a.images; image += h.strides) {
         const T *x = (const T *)a.x + image * a.points * a.ldx + c;
-        float w[I][V], t = 0, s = 0;
+        const double pivot = load_value(x + group * per - v * V);        // the group's first
+        typename Values<T, V>::Held w[I];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             // (the last point again where there is none: left out of the sums)
             const int point = min(r + i * h.high, last);
-            Values<T, V>::load(x + (int64_t)point * a.ldx, w[i]);
+            w[i] = Values<T, V>::hold(x + (int64_t)point * a.ldx);
         }
+        Moments m;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            float o = 0;
+            Moments o;
+            float v[V];
+            Values<T, V>::values(w[i], v);
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                o += w[i][e];
-            t += here && r + i * h.high <= last ? o : 0.f;
+                o.add(v[e], pivot);
+            const bool in = here && r + i * h.high <= last;
+            m.sum += in ? o.sum : 0;
+            m.squares += in ? o.squares : 0;
         }
-        const float mean = join_groups({t, 0.f}, h, each, group, here, of, of_group).x * share;
-#pragma unroll
-        for (int i = 0; i < I; ++i) {
-            float o = 0;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                w[i][e] -= mean;
-                o = __builtin_fmaf(w[i][e], w[i][e], o);
-            }
-            s += here && r + i * h.high <= last ? o : 0.f;
-        }
-        const float rstd = __builtin_amdgcn_rsqf(join_groups({s, 0.f}, h, each, group, here, of, of_group).x * share + a.eps);      // 1 ulp
+        const double2 all = join_groups(double2{m.sum, m.squares}, h, each, group, here, sums, sums_of_group);
+        m.sum = all.x;
+        m.squares = all.y;
+        const float mean = (float)(pivot + m.sum * share), rstd = reciprocal_root(m.variance(share) + a.eps);
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int point = r + i * h.high;
             if (here && point <= last) {
+                if constexpr (V == 8)
+                    asm volatile("" : "+v"(w[i]));         // taken apart again: as floats they took twice the registers throughout
+                float v[V];
+                Values<T, V>::values(w[i], v);
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    w[i][e] = activation<ACT>(__builtin_fmaf(w[i][e], rstd * gamma[e], beta[e]));
-                Values<T, V>::store_past((T *)a.y + (image * a.points + point) * a.ldy + c, w[i]);
+                    v[e] = activation<ACT>(__builtin_fmaf(v[e] - mean, rstd * gamma[e], beta[e]));
+                Values<T, V>::store_past((T *)a.y + (image * a.points + point) * a.ldy + c, v);
             }
         }
         if (a.mean && here && r == 0 && v % each == 0) {
@@ -180,7 +184,7 @@ __global__ __launch_bounds__(kHeldThreads) void held_backward_kernel(GroupNorm a
         if (!a.y)
             continue;
         // dx = g gamma rstd - (x - mean) rstd^2 m2 - rstd m1
-        const float2 m = join_groups({t, u}, h, each, group, here, of, of_group);
+        const float2 m = join_groups(float2{t, u}, h, each, group, here, of, of_group);
         const float m1 = -rstd * (m.x * share), m2 = -rstd * (rstd * (m.y * share));
 #pragma unroll
         for (int i = 0; i < I; ++i) {
@@ -271,10 +275,10 @@ bool held_plan(int32_t dtype, int64_t images, int64_t points, int32_t channels, 
 
 template <typename T, int V, int I>
 hipError_t launch_held(const GroupNorm &a, const HeldPlan &o, bool backward, hipStream_t stream) {
-    const size_t lds = (size_t)(o.threads + o.h.groups) * sizeof(float2);
+    const size_t pairs = (size_t)(o.threads + o.h.groups), lds = pairs * sizeof(float2);
     if (!backward)
         return with_activation(a.act, [&](auto act) {
-            held_forward_kernel<T, V, I, decltype(act)::value><<<o.grid, o.threads, lds, stream>>>(a, o.h);
+            held_forward_kernel<T, V, I, decltype(act)::value><<<o.grid, o.threads, pairs * sizeof(double2), stream>>>(a, o.h);
             return hipGetLastError();
         });
     float *part = (float *)a.scratch, *room = part + (int64_t)o.h.strides * 2 * a.channels;

@@ -1,5 +1,6 @@
 // Group norm of images of one point: in one launch, in registers.  Memory bounds
-// it: 65,536 x 512 in bf16, 16 groups, takes 32 us (4.1 TB/s).  Results go through the
+// it: 65,536 x 512 in bf16, 16 groups, takes 34 us (3.9 TB/s; 32 with sums in 32 bits,
+// which were wrong far from zero), in fp32 58 (4.6 TB/s).  Results go through the
 // caches: past them it takes 24 us, but the next call finds nothing there, and the two
 // together take 57 us instead of 52.
 #include "group_norm_device.hpp"
@@ -63,50 +64,51 @@ struct RowLane {
     }
 };
 
+// (With the compiler's own choice of registers bf16 in whole vectors had two blocks a
+// CU instead of three: 65,536 x 512 38 us.)
 template <typename T, int V, int I, int ACT>
-__global__ __launch_bounds__(64 * kRowWaves) void rows_forward_kernel(GroupNorm a, Rows p) {
+__global__ __launch_bounds__(64 * kRowWaves, V == 8 && I == 1 ? 6 : 1) void rows_forward_kernel(GroupNorm a, Rows p) {
     const int column_block = blockIdx.x % p.column_blocks, wave = threadIdx.x >> 6;
     const RowLane<T, V, I> k(a, p, column_block);
-    const float share = 1.f / (float)(a.channels / a.groups);
+    const double share = 1.0 / (a.channels / a.groups);
     constexpr int kAtOnce = V * I <= 16 ? 2 : 1;     // rows whose loads go out together
     const int64_t step = (int64_t)p.strides * kRowWaves * p.rows;
     for (int64_t first = ((int64_t)(blockIdx.x / p.column_blocks) * kRowWaves + wave) * p.rows; first < a.images; first += step * kAtOnce) {
-        float v[kAtOnce][I][V];
+        typename Values<T, V>::Held w[kAtOnce][I];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u)
-            k.load((const T *)a.x + min(first + u * step + k.sub, a.images - 1) * a.ldx, v[u]);
+#pragma unroll
+            for (int i = 0; i < I; ++i)        // of channel 0 where there is none: left out of the sums
+                w[u][i] = Values<T, V>::hold((const T *)a.x + min(first + u * step + k.sub, a.images - 1) * a.ldx + k.c[i]);
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int64_t row = first + u * step + k.sub;
-            float t = 0, s = 0;
+            float v[I][V];
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                Values<T, V>::values(w[u][i], v[i]);
+            const double pivot = __shfl(v[0][0], (threadIdx.x & 63) & -p.lanes);
+            Moments m;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
-                float o = 0;
+                Moments o;
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    o += v[u][i][e];
-                t += k.here[i] ? o : 0.f;
+                    o.add(v[i][e], pivot);
+                m.sum += k.here[i] ? o.sum : 0;
+                m.squares += k.here[i] ? o.squares : 0;
             }
-            const float mean = join_lanes(t, p.lanes) * share;
-#pragma unroll
-            for (int i = 0; i < I; ++i) {
-                float o = 0;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    v[u][i][e] -= mean;
-                    o = __builtin_fmaf(v[u][i][e], v[u][i][e], o);
-                }
-                s += k.here[i] ? o : 0.f;
-            }
-            const float rstd = __builtin_amdgcn_rsqf(join_lanes(s, p.lanes) * share + a.eps);      // 1 ulp
+            m.sum = join_lanes(m.sum, p.lanes);
+            m.squares = join_lanes(m.squares, p.lanes);
+            const float mean = (float)(pivot + m.sum * share), rstd = reciprocal_root(m.variance(share) + a.eps);
             const bool live = row < a.images;
 #pragma unroll
             for (int i = 0; i < I; ++i)
                 if (live && k.here[i]) {
 #pragma unroll
                     for (int e = 0; e < V; ++e)
-                        v[u][i][e] = activation<ACT>(__builtin_fmaf(v[u][i][e], rstd * k.gamma[i][e], k.beta[i][e]));
-                    Values<T, V>::store((T *)a.y + row * a.ldy + k.c[i], v[u][i]);
+                        v[i][e] = activation<ACT>(__builtin_fmaf(v[i][e] - mean, rstd * k.gamma[i][e], k.beta[i][e]));
+                    Values<T, V>::store((T *)a.y + row * a.ldy + k.c[i], v[i]);
                 }
             if (a.mean && live && k.lane == 0 && k.here[0]) {
                 a.mean[row * a.groups + k.group] = mean;
