@@ -121,7 +121,8 @@ hpacml_status hpacmlt_backward_scratch(int64_t rows, int64_t n_in, int32_t n_out
  * channels.  Over an image's points and a group's channels together (n values)
  *     mean = sum x / n    rstd = 1 / sqrt(sum (x - mean)^2 / n + eps)
  *     z = (x - mean) * (rstd * gamma) + beta     y = act(z)
- * in fp32, y rounded once to its type, which is x's.
+ * Sums are in 64 bits, mean and rstd are rounded to fp32, what follows is in
+ * fp32 (which x - mean has to fit), y rounded once to its type, which is x's.
  *   dtype: HPACML_F32 or HPACML_BF16; gamma, beta: fp32 [channels] or NULL (1
  *   and 0); eps >= 2^-126, finite; act: HPACML_ACT_* or HPACMLT_ACT_SILU (z / (1 +
  *   exp(-z))); mean, rstd: fp32 [images][groups], for the backward pass, or
@@ -140,7 +141,8 @@ hpacml_status hpacmlt_group_norm(const void *x, int32_t dtype, int64_t ldx, int6
  *     dgamma_c (+)= sum g (x - mean) rstd     dbeta_c (+)= sum g
  *     dx = rstd (g gamma - m1 - (x - mean) rstd m2)
  * with m1 and m2 the means of g gamma and g gamma (x - mean) rstd over image
- * and group.  A ReLU's act' is 0 where z <= 0 and 1 elsewhere.
+ * and group, in fp32, whose range sums of g (x - mean) have to keep.  A ReLU's
+ * act' is 0 where z <= 0 and 1 elsewhere.
  *   dy, dx: x's type; dx, dgamma, dbeta may be NULL (not wanted); gamma, beta,
  *   act as given to hpacmlt_group_norm, mean and rstd as it wrote them.
  * accumulate: nonzero adds to dgamma and dbeta, zero sets them (no images: to

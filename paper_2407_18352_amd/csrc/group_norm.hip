@@ -10,10 +10,9 @@
 // channels throughout, so that their parameters are in registers, and the sums
 // that the parameters' gradients are made of stay apart until the end.
 //
-// Statistics: in registers sums in 64 bits of what the values are more than one
-// of them, and of its squares (Moments); in parts pairs of (mean, squares about
-// it) joined as such, so that no difference of large sums occurs; joins of many
-// in 64 bits.
+// Statistics: sums in 64 bits of what the values are more than one of them, and
+// of its squares (Moments); in parts those of every channel and run, which are
+// joined as (mean, deviation), so that no difference of large sums occurs.
 #include "group_norm_device.hpp"
 
 namespace hpacml {
