@@ -582,9 +582,9 @@ template <typename Y, bool EXACT, int WA, int WB, int NA, int NB>
 hipError_t launch_shape(const Args<Y> &g, hipStream_t stream) {
     typedef Shape<WA, WB, NA, NB> S;
     auto kernel = product_kernel<Y, EXACT, WA, WB, NA, NB>;
-    static const hipError_t ready = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-    if (ready != hipSuccess)
-        return ready;
+    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);     // of this device
+    if (e != hipSuccess)
+        return e;
     const uint32_t grid = nt::blocks_for_tiles((int64_t)g.out_tiles * g.point_tiles * g.parts, S::kPerCu);
     kernel<<<grid, S::kThreads, S::kLds, stream>>>(g);
     return hipGetLastError();
