@@ -31,7 +31,9 @@ class SurrogateF8:
     from several threads at a time they may not.  Calls captured into a graph read
     the weights as ``update`` lays them out and write the gradients where they
     are then; a forward pass captured keeps what it does for the graph's own
-    backward pass."""
+    backward pass.  ``captured`` keeps that memory (parameters and gradients
+    exchanged for others since then included) for the graphs' replays; it may be
+    cleared once they are gone."""
 
     def __init__(self, dims, groups: int = 8, act: int = _abi.ACT_SILU, eps: float = 1e-5, seed: int = 0):
         g = torch.Generator().manual_seed(seed)
@@ -49,7 +51,7 @@ class SurrogateF8:
         with torch.no_grad():
             self.layers = [api.LinearF8(w, b, learn=True) for w, b in zip(self.W, self.b)]
         self.rows, self.kept, self.stats, self.z, self.set, self.stream = -1, [], [], [], None, torch.cuda.current_stream()
-        self.captured = []              # what graphs read
+        self.captured = {}              # what graphs read and write, by its address
 
     def parameters(self):
         return self.W + self.b + self.gamma + self.beta
@@ -69,14 +71,22 @@ class SurrogateF8:
                 t.record_stream(now)
         self.stream = now
 
+    def _hold(self, tensors):
+        """A graph reads and writes where the tensors are now: their memory stays, whatever becomes of them."""
+        if torch.cuda.is_current_stream_capturing():
+            for t in tensors:
+                self.captured.setdefault((t.data_ptr(), t.numel()), t.detach())
+
     @torch.no_grad()
     def update(self):
         """Lays the weights and biases out as they are now."""
         self._in_order()
+        self._hold(self._buffers() + self.W + self.b)
         for layer, w, b in zip(self.layers, self.W, self.b):
             layer.update(w, b)
 
     def _run(self, x, keep):
+        self._hold(self._buffers() + self.gamma + self.beta)
         n, a, last = x.shape[0], _rows(x if x.dtype in (torch.float32, torch.bfloat16) else x.float()), len(self.layers) - 1
         for l, layer in enumerate(self.layers):
             z = torch.empty((n, layer.n_out), dtype=torch.float32 if l == last else torch.bfloat16, device="cuda")
@@ -119,6 +129,7 @@ class SurrogateF8:
         for p in self.parameters():
             if p.grad is None:
                 p.grad = torch.zeros_like(p)
+        self._hold(self._buffers() + self.gamma + self.beta + [p.grad for p in self.parameters()])
         dy = _rows(dy.float())
         for l in range(len(self.layers) - 1, -1, -1):
             if l < len(self.layers) - 1:
@@ -141,8 +152,8 @@ class SurrogateF8:
             raise ValueError("there are no gradients to clip")
         if self.set is None or any(a is not b for a, b in zip(self.set.gradients, grads)):
             self.set = api.GradientSet(grads)
-        if torch.cuda.is_current_stream_capturing() and self.set not in self.captured:
-            self.captured.append(self.set)
+        if torch.cuda.is_current_stream_capturing():
+            self.captured[id(self.set)] = self.set
         norm = torch.empty(1, device="cuda")
         api.clip_gradients(self.set, most, norm)
         return norm
