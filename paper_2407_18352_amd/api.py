@@ -774,8 +774,9 @@ class GradientSet:
     """Gradients whose norm is taken together (``hpacmlt_gradients_create``):
     float32 or bfloat16 device tensors whose values are one after another in
     memory; ``into``: as many tensors of the same shapes and strides that
-    clipping writes to (None: in place).  The set holds the tensors: gradients
-    that an optimizer replaces need a new set.  It synchronises the device, so it
+    clipping writes to (None: in place).  The set holds the memory where the
+    tensors are now: gradients that an optimizer replaces, or whose storage is
+    exchanged, need a new set (``holds`` tells).  It synchronises the device, so it
     is made before a capture into a graph, and outlives the graphs that use it."""
 
     def __init__(self, gradients, into=None):
@@ -803,7 +804,15 @@ class GradientSet:
             e.from_dtype, e.to_dtype = _kinds8[g.dtype], _kinds8[t.dtype]
         h = C.c_void_p()
         check(lib().hpacmlt_gradients_create(table, len(gradients), C.byref(h)), "hpacmlt_gradients_create")
-        self.handle, self.gradients, self.into = h, gradients, into
+        # (aliases: an exchanged storage stays theirs)
+        self.handle, self.gradients, self.into = h, [g.detach() for g in gradients], [t.detach() for t in into]
+
+    def holds(self, gradients) -> bool:
+        """Whether the set is of these gradients, in place, where they are now."""
+        gradients = list(gradients)
+        return len(gradients) == len(self.gradients) and all(
+            v.data_ptr() == g.data_ptr() and v.dtype == g.dtype and v.shape == g.shape and v.stride() == g.stride()
+            for own in (self.gradients, self.into) for v, g in zip(own, gradients))
 
     def scratch_bytes(self) -> int:
         n = C.c_size_t()

@@ -145,12 +145,15 @@ class SurrogateF8:
     @torch.no_grad()
     def clip(self, most: float):
         """Scales the gradients so that their common norm is at most ``most``;
-        the norm before ([1], fp32, on the device)."""
+        the norm before ([1], fp32, on the device).  Gradients that are not where
+        they were at the last call (``zero_grad`` drops them) make it lay out a
+        new set of them, which synchronises the device: ``backward`` sets them
+        anew, and nothing need drop them."""
         self._in_order()
         grads = [p.grad for p in self.parameters()]
         if any(g is None for g in grads):
             raise ValueError("there are no gradients to clip")
-        if self.set is None or any(a is not b for a, b in zip(self.set.gradients, grads)):
+        if self.set is None or not self.set.holds(grads):
             self.set = api.GradientSet(grads)
         if torch.cuda.is_current_stream_capturing():
             self.captured[id(self.set)] = self.set

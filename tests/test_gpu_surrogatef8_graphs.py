@@ -3,7 +3,7 @@ stays the graph's, whatever an optimizer or a loader exchanges afterwards."""
 import torch
 import pytest
 
-from paper_2407_18352_amd import surrogatef8
+from paper_2407_18352_amd import api, surrogatef8
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +96,45 @@ def test_a_backward_pass_alone_in_a_graph():
     torch.cuda.synchronize()
     assert all(torch.equal(p.grad, w) for p, w in zip(model.parameters(), want))
     assert all(bool((t == 255).all()) for t in taken)
+
+
+def test_gradients_of_another_storage_are_clipped_where_they_are():
+    model, x, dy = model_and_batch()
+    model.forward(x)
+    model.backward(dy)
+    model.clip(1e9)
+    held = model.set
+    model.clip(1e9)
+    assert model.set is held                         # where they were: the same set
+    old = [p.grad.detach() for p in model.parameters()]
+    before = [t.clone() for t in old]
+    for i, p in enumerate(model.parameters()):       # the same tensor objects
+        if i % 2:
+            p.grad.data = p.grad.detach() * 2
+        else:
+            p.grad.set_(p.grad.detach() * 2)
+    total = torch.stack([t.double().norm() for t in before]).norm().item()
+    norm = model.clip(total)
+    torch.cuda.synchronize()
+    assert abs(norm.item() - 2 * total) <= 1e-6 * total
+    for p, t, b in zip(model.parameters(), old, before):
+        assert torch.equal(t, b) and torch.allclose(p.grad, b, rtol=1e-6)
+    assert model.set is not held
+
+
+def test_a_set_holds_the_memory_it_was_made_of():
+    a, b, into = (torch.full((1000,), v, device="cuda") for v in (3.0, 4.0, 0.0))
+    grads, norm = api.GradientSet([a, b]), torch.empty(1, device="cuda")
+    other = api.GradientSet([a], into=[into])
+    assert grads.holds([a, b]) and not grads.holds([a]) and not grads.holds([b, a]) and not grads.holds([a, into])
+    assert not other.holds([a])                      # not in place
+    was = b.detach()
+    b.data = torch.full((1000,), 7.0, device="cuda")
+    assert not grads.holds([a, b]) and grads.holds([a, was])
+    del was
+    taken = others([4000])
+    api.clip_gradients(grads, 1e9, norm)
+    assert abs(norm.item() - 5 * 1000 ** 0.5) <= 1e-4 and all(bool((t == 255).all()) for t in taken)
+    c = torch.ones((4, 6), device="cuda")
+    grads = api.GradientSet([c])
+    assert not grads.holds([c.t()]) and not grads.holds([c.view(-1)]) and grads.holds([c])
