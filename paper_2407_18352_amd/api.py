@@ -592,48 +592,56 @@ def productf8(p: MatrixF8, q: MatrixF8, y, b=None, act: int = _abi.ACT_IDENTITY,
 
 class LinearF8:
     """A dense layer's weights in 8-bit floating point, a scale for each 128 x
-    128 of them: ``W`` [out][in] and ``b`` [out] or None (float32 or bfloat16
-    W, on the CPU or the device), on the current stream; ``learn``: the weights
-    by column as well, as ``backwardf8`` reads them for dx."""
+    128 of them: ``W`` [out][in] and ``b`` [out] or None (numpy, or torch on the
+    CPU or the device; other types than float32 and bfloat16 are taken as
+    float32), on the current stream; ``learn``: the weights by column as well, as
+    ``backwardf8`` reads them for dx."""
 
     def __init__(self, W, b=None, learn: bool = False):
-        import numpy as np
         import torch
-        W = torch.as_tensor(np.asarray(W) if not isinstance(W, torch.Tensor) else W)
+        W, b = self._tensor(W), self._tensor(b)
         if W.dim() != 2 or W.numel() == 0:
             raise ValueError("W: shape %s, expected out x in" % (tuple(W.shape),))
         self.n_out, self.n_in = int(W.shape[0]), int(W.shape[1])
         self.W = MatrixF8(self.n_out, self.n_in)
         self.Wt = MatrixF8(self.n_in, self.n_out) if learn else None
         self.b = None if b is None else torch.empty(self.n_out, device="cuda")
-        if b is not None and not isinstance(b, torch.Tensor):
-            b = torch.as_tensor(np.asarray(b))
-        if W.dtype not in (torch.float32, torch.bfloat16):
-            W = W.to(torch.float32)
-        self.update(W.detach().cuda(), b)
+        self.update(W, b)
+
+    @staticmethod
+    def _tensor(t):
+        import numpy as np
+        import torch
+        if t is None:
+            return None
+        return t.detach() if isinstance(t, torch.Tensor) else torch.as_tensor(np.asarray(t))
 
     def update(self, W, b=None, stream=None) -> None:
         """Other weights (and biases, which a layer made without has none of)
-        in the same buffers: ``hpacmlt_quantize`` on ``stream``."""
+        in the same buffers, given as to the constructor: ``hpacmlt_quantize`` on
+        ``stream``, where W has to be a float32 or bfloat16 device tensor whose
+        rows are contiguous."""
         import torch
+        W, b = self._tensor(W), self._tensor(b)
         if tuple(W.shape) != (self.n_out, self.n_in):
             raise ValueError("W: shape %s, expected %s" % (tuple(W.shape), (self.n_out, self.n_in)))
         if (b is None) != (self.b is None):
             raise ValueError("b: a layer keeps its biases, or has none")
         if b is not None and tuple(b.shape) != (self.n_out,):
             raise ValueError("b: shape %s, expected %d" % (tuple(b.shape), self.n_out))
-        W = W.detach()
-        if (W.stride(1) != 1 and W.shape[1] > 1) or (W.shape[0] > 1 and W.stride(0) < W.shape[1]):
+        kind = W.dtype if W.dtype == torch.bfloat16 else torch.float32
+        rows = (W.stride(1) == 1 or W.shape[1] == 1) and (W.shape[0] == 1 or W.stride(0) >= W.shape[1])
+        if not (rows and W.is_cuda and W.dtype == kind):
             if stream is not None:
-                raise ValueError("W: the values of a row must be contiguous in a call on a stream of its own")
-            W = W.contiguous()
+                raise ValueError("W: a call on a stream of its own takes a float32 or bfloat16 device tensor with contiguous rows")
+            W = W.to(device="cuda", dtype=kind).contiguous()
         quantizef8(W, self.W, self.Wt, square=True, stream=stream)
         if b is not None:
             if stream is None:
-                self.b.copy_(b.detach(), non_blocking=True)
+                self.b.copy_(b, non_blocking=True)
             else:
                 with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
-                    self.b.copy_(b.detach(), non_blocking=True)
+                    self.b.copy_(b, non_blocking=True)
 
     def scratch_bytes(self, n_rows: int) -> int:
         n = C.c_size_t()
