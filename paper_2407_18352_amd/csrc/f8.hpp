@@ -6,7 +6,7 @@
 #include <stdint.h>
 
 #include "dense8.hpp"
-#include "hpacmlt.h"
+#include "f8_rules.hpp"
 
 namespace hpacml {
 namespace f8 {
@@ -20,8 +20,7 @@ namespace f8 {
 // r's in byte r / 32 of word r % 32, so that one word serves the four matrix
 // instructions of 128 rows (they select a byte of it).  What pads the last rows
 // and blocks has codes 0 and some finite scale.
-constexpr int kBlock = HPACMLT_BLOCK, kUnit = 2048;
-constexpr int64_t blocks_of(int64_t width) { return (width + kBlock - 1) / kBlock; }
+constexpr int kUnit = 2048;
 // a launch has fewer than 2^32 threads, and quantizing has 256 for each 128 x 128
 constexpr bool too_many_blocks(int64_t rows, int64_t width) { return blocks_of(rows) * blocks_of(width) >= 1 << 24; }
 constexpr int64_t row_units(int64_t rows) { return (rows + 31) / 32; }
@@ -65,19 +64,7 @@ struct ProductArgs {
 int64_t product_partial_bytes(int64_t p_rows, int64_t q_rows, int64_t width);
 hipError_t launch_product(const ProductArgs &a, int32_t y_dtype, hipStream_t stream);
 
-// Whether a product of few rows is computed in one launch, whose blocks take 16
-// outputs and pass over the width 32, 16 or 8 blocks of it at a time (for up to
-// 16, 32 and 64 rows).  It is the faster one while that is short: up to three
-// passes, counted once for every 4096 outputs (a block on each CU).  In
-// microseconds, so and with codes of x and tiles, bf16: one row, 4096 -> 4096
-// (one pass) 7.6 and 13.6, 8192 -> 4096 (two) 10.9 and 16.6, 4096 -> 8192 (two)
-// 13.3 and 16.7, 16,384 -> 512 (four) 15.7 and 13.2, 1024 -> 65,536 (sixteen) 59
-// and 19; 32 rows, 6144 -> 4096 (three) 17.6 and 18.7, 8192 -> 4096 (four) 21.4 and
-// 19.0; 64 rows, 2048 -> 4096 (two) 12.1 and 15.6, 4096 -> 64 (four) 19.4 and 13.5.
-inline bool few_rows(int64_t p_rows, int64_t q_rows, int64_t width) {
-    const int64_t at_once = p_rows <= 16 ? 32 : p_rows <= 32 ? 16 : 8;
-    return p_rows <= 64 && width > 0 && q_rows <= 3 * 4096 && (blocks_of(width) + at_once - 1) / at_once * ((q_rows + 4095) / 4096) <= 3;
-}
+// of few_rows
 hipError_t launch_product_few(const ProductArgs &a, int32_t y_dtype, hipStream_t stream);
 // the same for rows x, whose codes it forms (of a.p: the rows)
 hipError_t launch_linear_few(const ProductArgs &a, const void *x, int32_t x_dtype, int64_t ldx, int32_t y_dtype, hipStream_t stream);

@@ -542,40 +542,6 @@ hipError_t launch_finish(const float *part, int64_t parts, int64_t rows, int64_t
     return hipGetLastError();
 }
 
-// Tiles of 256 x 256 read less LDS for a product, tiles of 128 x 128 fill the
-// chip with less and are shorter to begin and end.  Measured, large against small:
-// 4096^3 56 and 65 us, 65,536 x 512 x 512 27 and 29 us; 2048^3, where the large
-// ones have to split the width, 37 and 13 us; 20,000 x 1000 x 300 22 and 18 us;
-// 2048 x 2048 x 131,072 in fp32, split in four, 780 and 1134 us; 256 x 256 x
-// 262,144 56 and 46 us (the parts' join).  So large tiles where there is one for
-// each CU and a width of four blocks, or parts of 64 blocks and more.
-// A part has four blocks of the width at least: 128 x 4096 x 4096 25 us without
-// that, 19 us with it.
-struct Plan {
-    bool big;
-    uint32_t out_tiles, point_tiles;
-    int32_t parts;
-};
-Plan plan_for(int64_t p_rows, int64_t q_rows, int64_t width, bool big) {
-    Plan p;
-    p.big = big;
-    const int64_t side = big ? 256 : 128;
-    p.out_tiles = (uint32_t)((q_rows + side - 1) / side);
-    p.point_tiles = (uint32_t)((p_rows + side - 1) / side);
-    const int64_t tiles = (int64_t)p.out_tiles * p.point_tiles, blocks = blocks_of(width), chip = big ? 256 : 512;
-    const int64_t parts = tiles >= chip / 2 || tiles == 0 ? 1 : chip / tiles, most = blocks < 8 ? 1 : blocks / 4;
-    p.parts = (int32_t)(parts > most ? most : parts);
-    return p;
-}
-Plan plan_of(int64_t p_rows, int64_t q_rows, int64_t width) {
-    const int64_t blocks = blocks_of(width);
-    if (p_rows > 128 && q_rows > 128) {
-        const Plan p = plan_for(p_rows, q_rows, width, true);
-        if (((int64_t)p.out_tiles * p.point_tiles >= 256 && blocks >= 4) || blocks / p.parts >= 64)
-            return p;
-    }
-    return plan_for(p_rows, q_rows, width, false);
-}
 int64_t partial_pitch(int64_t q_rows) { return (q_rows + 3) / 4 * 4; }
 
 template <typename Y, bool EXACT, int WA, int WB, int NA, int NB>
