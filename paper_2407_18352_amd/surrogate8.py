@@ -26,12 +26,21 @@ def _rows(t):
     return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
 
 
+def _hold(captured, tensors):
+    """A graph reads and writes where the tensors are now: their memory stays, whatever becomes of them."""
+    if torch.cuda.is_current_stream_capturing():
+        for t in tensors:
+            captured.setdefault((t.data_ptr(), t.numel()), t.detach())
+
+
 class Surrogate8:
     """A ReLU perceptron of the widths ``dims``: fp32 weights ``W[l]``
     [out][in] and biases ``b[l]`` with gradients in ``.grad``; products in
     bf16.  ``backward`` is that of the last ``forward``: another one in between
     replaces what was kept.  Calls may come on one stream after another, each
-    works after the one before; from several threads at a time they may not."""
+    works after the one before; from several threads at a time they may not.
+    What calls captured into a graph read and write ``captured`` keeps for the
+    graph's replays; it may be cleared once the graph is gone."""
 
     def __init__(self, dims, seed: int = 0):
         g = torch.Generator().manual_seed(seed)
@@ -42,9 +51,13 @@ class Surrogate8:
         for p in self.parameters():
             p.grad = torch.zeros_like(p)
         self.kept, self.scratch, self.Wh, self.stream = [], None, [], torch.cuda.current_stream()
+        self.captured = {}              # by its address
 
     def parameters(self):
         return self.W + self.b
+
+    def _buffers(self):
+        return [t for k in self.kept for t in (k.codes, k.exps)] + self.Wh + ([] if self.scratch is None else [self.scratch])
 
     def _in_order(self):
         """Kept values, weights in bf16 and scratch memory are used again by
@@ -54,9 +67,8 @@ class Surrogate8:
         now = torch.cuda.current_stream()
         if now != self.stream and not torch.cuda.is_current_stream_capturing():
             now.wait_stream(self.stream)
-            for t in [t for k in self.kept for t in (k.codes, k.exps)] + self.Wh + [self.scratch]:
-                if t is not None:
-                    t.record_stream(now)
+            for t in self._buffers():
+                t.record_stream(now)
         self.stream = now
 
     @torch.no_grad()
@@ -68,6 +80,7 @@ class Surrogate8:
         if not self.kept or self.kept[0].rows != n:
             self.kept = [api.Checkpoint8(n, d, _abi.ACT_RELU if l else _abi.ACT_IDENTITY) for l, d in enumerate(self.dims[:-1])]
         self.Wh = [w.to(torch.bfloat16) for w in self.W]
+        _hold(self.captured, self._buffers() + self.parameters())
         api.checkpoint8_save(self.kept[0], a)
         for l in range(1, len(self.dims) - 1):
             a = torch.nn.functional.linear(a, self.Wh[l - 1], self.b[l - 1].to(torch.bfloat16))
@@ -89,6 +102,7 @@ class Surrogate8:
             need = api.backward8_scratch_bytes(self.kept[l], dy, W)
             if self.scratch is None or self.scratch.numel() < need:
                 self.scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+            _hold(self.captured, self._buffers() + [self.W[l].grad, self.b[l].grad])
             api.backward8(self.kept[l], dy, self.W[l].grad, self.b[l].grad, W=W, dx=dx, accumulate=accumulate,
                           scratch=self.scratch)
             dy = dx

@@ -18,7 +18,7 @@ import math
 import torch
 
 from . import _abi, api
-from .surrogate8 import _rows, collect
+from .surrogate8 import _hold, _rows, collect
 
 
 class SurrogateF8:
@@ -71,22 +71,16 @@ class SurrogateF8:
                 t.record_stream(now)
         self.stream = now
 
-    def _hold(self, tensors):
-        """A graph reads and writes where the tensors are now: their memory stays, whatever becomes of them."""
-        if torch.cuda.is_current_stream_capturing():
-            for t in tensors:
-                self.captured.setdefault((t.data_ptr(), t.numel()), t.detach())
-
     @torch.no_grad()
     def update(self):
         """Lays the weights and biases out as they are now."""
         self._in_order()
-        self._hold(self._buffers() + self.W + self.b)
+        _hold(self.captured, self._buffers() + self.W + self.b)
         for layer, w, b in zip(self.layers, self.W, self.b):
             layer.update(w, b)
 
     def _run(self, x, keep):
-        self._hold(self._buffers() + self.gamma + self.beta)
+        _hold(self.captured, self._buffers() + self.gamma + self.beta)
         n, a, last = x.shape[0], _rows(x if x.dtype in (torch.float32, torch.bfloat16) else x.float()), len(self.layers) - 1
         for l, layer in enumerate(self.layers):
             z = torch.empty((n, layer.n_out), dtype=torch.float32 if l == last else torch.bfloat16, device="cuda")
@@ -129,7 +123,7 @@ class SurrogateF8:
         for p in self.parameters():
             if p.grad is None:
                 p.grad = torch.zeros_like(p)
-        self._hold(self._buffers() + self.gamma + self.beta + [p.grad for p in self.parameters()])
+        _hold(self.captured, self._buffers() + self.gamma + self.beta + [p.grad for p in self.parameters()])
         dy = _rows(dy.float())
         for l in range(len(self.layers) - 1, -1, -1):
             if l < len(self.layers) - 1:
