@@ -71,7 +71,8 @@ hpacml_status hpacmlt_load(const hpacmlt_matrix *m, void *x, int32_t dtype, int6
  * products exact, sums in fp32, rounded once to y's type.  (Where y is bf16 the
  * 8-bit matrix instruction may drop of each product what is below 2^-13 of the
  * largest of its eight neighbours: less than 2^-10 of the sum of magnitudes, for
- * values without a common sign about 2^-16 of the result.)
+ * values without a common sign about 2^-16 of the result.  Where y is fp32 nothing
+ * is dropped.)
  *   y_dtype: HPACML_F32 or HPACML_BF16; b: fp32 [q->rows] or NULL;
  *   act: HPACML_ACT_* (a ReLU keeps a NaN);
  *   accumulate: nonzero adds to y, which is fp32 then, without b and act.

@@ -1,11 +1,11 @@
 // Group norm of images whose groups fit a block's registers: one reading, one
 // launch.  1024 images of 1024 points x 128 channels in bf16, SiLU, take 136 us (3.9
-// TB/s; 163 with two joins, of sums in 32 bits).  The gradients of 1024 images of 1024 points x 128 channels in bf16, SiLU,
-// take 229 us (3.5 TB/s): the activation's gradient takes as many cycles as the
-// loads, and there is room for the registers of two blocks a CU.  Three launches, each
-// value read twice, took 379 us.  Results go past the caches (4096 images of 64 points x
-// 256 channels in bf16 60 us, 62 through them), those of the gradients do not (229 us,
-// 234 past them).
+// TB/s; 163 with two joins, of sums in 32 bits).  Their gradients take 229 us (3.5
+// TB/s): the activation's gradient takes as many cycles as the loads, and there is
+// room for the registers of two blocks a CU.  Three launches, each value read twice,
+// took 379 us.  Results go past the caches (4096 images of 64 points x 256 channels in
+// bf16 57 us, 59.5 through them, with a reader behind 96 either way; of 2 MB 8.5 and
+// 13.8 either way), those of the gradients do not (229 us, 234 past them).
 #include "group_norm_device.hpp"
 
 namespace hpacml {

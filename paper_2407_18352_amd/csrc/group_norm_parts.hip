@@ -1,11 +1,10 @@
 // Group norm of large images: sums of runs of points, their join, and the results
 // from a second reading.  A run's values count from its first one on (Moments): with
-// pairs of mean and squares in 32 bits, joined a few values at a time, 100,000 +- 0.1 had an rstd
-// 0.1-10% off.  An image of 2048^2 points x 8 channels in fp32 takes 89
-// us with results through the caches (41 for the first reading, which meets the
-// write-back of what was computed before, 6 for the join, 43 for the results), 75 with
-// results past them (its gradients 145 and 121), and with a call behind it that reads
-// them 132 and 126.
+// pairs of mean and squares in 32 bits, joined a few values at a time, 100,000 +- 0.02
+// had an rstd up to 10% off.  An image of 2048^2 points x 8 channels in fp32 takes 75 us
+// (27 for the first reading, 7 for the join, 43 for the results), 89 with results
+// through the caches, whose write-back the next first reading meets (its gradients 121
+// and 145).
 #include "group_norm_device.hpp"
 
 namespace hpacml {

@@ -1,8 +1,8 @@
 // Group norm of images of one point: in one launch, in registers.  Memory bounds
 // it: 65,536 x 512 in bf16, 16 groups, takes 34 us (3.9 TB/s; 32 with sums in 32 bits,
 // which were wrong far from zero), in fp32 58 (4.6 TB/s).  Results go through the
-// caches: past them it takes 24 us, but the next call finds nothing there, and the two
-// together take 57 us instead of 52.
+// caches: past them it took 24 us, but the next call finds nothing there, and the two
+// together took 57 us instead of 52.  Its gradients with SiLU take 54-56 us, in fp32 89.
 #include "group_norm_device.hpp"
 
 namespace hpacml {
